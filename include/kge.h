@@ -445,6 +445,90 @@ int kge_encode_bwd(const kge_encoder_t *enc, const int32_t *h, const int32_t *t,
 size_t kge_encode_workspace_bytes(int op, const kge_encoder_t *enc, int64_t B, int64_t N);
 
 /*
+ * The text side of an entity's features (Section 3.1 "Encoder": e_F comes from a text encoder): token embeddings, dropout, and
+ * projections in 8 bits.  The matrices of these calls are row-major with a row stride (ld, in elements) of at least the width; rows may start at any
+ * element (no alignment beyond the element's own, except where codes and scales say so).  Types are kge_dtype_t.  The calls only
+ * launch kernels and may be captured into a HIP graph.
+ *
+ * kge_dropout_t: element (row, column) of a matrix is kept iff its 16 random bits are >= thr = round(p * 2^16), and is then
+ * multiplied by 2^16 / (2^16 - thr).  The bits: Philox4x32-10, key = seed, counter (row, column / 8, step, tag), word (column % 8) / 2, low
+ * half for even columns.  The mask is stored nowhere: the backward pass makes it again from the same values.  0 <= p < 1, step < 2^32; with
+ * step_counter set (a DEVICE counter, see kge_step_counter_add) the step is step + *step_counter, read when the kernels run.
+ */
+typedef struct {
+    float p;
+    uint32_t tag;                     /* stream tag: another one for every layer */
+    uint64_t seed, step;
+    const uint64_t *step_counter;
+} kge_dropout_t;
+
+/*
+ * kge_dropout: out = residual + D o x (residual may be NULL: out = D o x), [rows, cols], all three of one dtype, computed in fp32 and rounded
+ * once.  out may be x or residual, with the same row stride; otherwise it must not overlap them.  Its backward pass is the same call
+ * on the gradient without the residual (whose own gradient passes unchanged).  What is dropped is 0 whatever x holds.
+ * cols <= 65,536, rows < 2^31.
+ */
+int kge_dropout(const void *x, int64_t x_ld, const void *residual, int64_t residual_ld, void *out, int64_t out_ld, int32_t dtype,
+                int64_t rows, int32_t cols, const kge_dropout_t *drop, void *hip_stream);
+
+/*
+ * kge_embed: out[i, :] = D_i o (scale * table[ids[i], :]), i < M, in fp32, rounded once to out_dtype; D from `drop` with row i (NULL: no
+ * dropout).  ids: device int32[M]; an id outside [0, n_rows) - a padded position - gives a row of zeros.  dim <= 65,536.
+ * kge_embed_bwd: g_table[r, :] = scale * sum over i with ids[i] = r of D_i o g[i, :], rows without a position zeros; with accumulate = 1 it is added
+ * to g_table, and rows without a position are neither read nor written.  The positions of a row are added in a fixed order, in fp32, and
+ * rounded once to table_dtype: results do not depend on scheduling.  g: [M, dim]; workspace from kge_embed_bwd_workspace_bytes (0 for invalid
+ * arguments).  g and g_table must not overlap.  n_rows < 2^31 - 1.
+ * A table that is trained with kge_sparse_adam needs no dense gradient: that call takes the rows of g and the ids themselves.
+ */
+int kge_embed(const void *table, int32_t table_dtype, int64_t n_rows, int32_t dim, int64_t ld, const int32_t *ids, int64_t M,
+              float scale, const kge_dropout_t *drop, void *out, int32_t out_dtype, int64_t out_ld, void *hip_stream);
+int kge_embed_bwd(const void *g, int32_t g_dtype, int64_t g_ld, const int32_t *ids, int64_t M, float scale, const kge_dropout_t *drop,
+                  void *g_table, int32_t table_dtype, int64_t n_rows, int32_t dim, int64_t ld, int32_t accumulate, void *ws,
+                  size_t ws_bytes, void *hip_stream);
+size_t kge_embed_bwd_workspace_bytes(int64_t M, int64_t n_rows, int32_t dim);
+
+/*
+ * A matrix [rows, cols] in 8-bit floating point with a scale for each block of 128 consecutive elements of a row:
+ *     element (i, k) = code(i, k) * 2^(scales[i * scales_ld + k / 128] - 127)
+ * codes: OCP e4m3 (largest value 448, no infinity) or e5m2 (57,344), a row's codes padded with zeros to a multiple of 128 (ld a multiple of 16
+ * and at least that; codes 16-byte aligned); scales: exponent bytes 0..254, a row's padded with zeros to a multiple of 4 (scales_ld a multiple
+ * of 4 and at least that; 4-byte aligned).  90M text features of 768 take 74 GB in this form, 138 GB in bf16.
+ */
+typedef enum { KGE_E4M3 = 0, KGE_E5M2 = 1 } kge_float_code_t;
+typedef struct {
+    int32_t format;                   /* kge_float_code_t */
+    int32_t reserved;                 /* 0 */
+    int64_t rows, cols;
+    uint8_t *codes; int64_t ld;
+    uint8_t *scales; int64_t scales_ld;
+} kge_quantized_t;
+
+/*
+ * kge_quantize: writes x [rows, cols] quantised by rows (by_row: [rows, cols], blocks of 128 columns) and / or the transposed matrix (by_col:
+ * [cols, rows], blocks of 128 rows), padding included; x is read once.  Of a block's finite elements the largest magnitude decides
+ * the scale, the smallest power of two that no finite element outgrows the format with; codes are rounded to nearest even.  NaN stays NaN; an
+ * infinity stays one in e5m2 and becomes NaN in e4m3.  A block of zeros has scale byte 0.  Both layouts have the same format.
+ */
+int kge_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, const kge_quantized_t *by_row,
+                 const kge_quantized_t *by_col, void *hip_stream);
+
+/*
+ * kge_matmul_quantized: out[i, j] = sum over k of a[rows[i], k] * b[j, k], i < m, j < b->rows; rows NULL: row i itself (m = a->rows); a row
+ * number outside [0, a->rows) gives a row of zeros.  With accumulate = 1 the product is added to out.  A layer y = x W^t is (x by row, W by
+ * row), its dx = dy W (dy by row, W by column), dW = dy^t x (dy by column, x by column).
+ * Arithmetic: out_dtype KGE_F32: the codes widened exactly to bf16, fp32 sums on the bf16 matrix cores.  KGE_BF16: the 8-bit
+ * matrix cores, twice as fast, which align every eight products to the largest of them and drop what lies 2^-13 below it (1.4e-5 of the
+ * result on normal values); sums of these groups in fp32, one rounding at the end.  A value that needs more than fp32's range (a block that holds numbers next to the largest
+ * fp32 one) overflows.
+ * Few rows over many blocks are split along k into partial sums in the workspace, which are added in order: the size to give is
+ * kge_matmul_quantized_workspace_bytes (k = a->cols); with less (NULL too) the call takes fewer splits, and sums are associated accordingly.
+ * out must not overlap the operands.
+ */
+int kge_matmul_quantized(const kge_quantized_t *a, const int32_t *rows, int64_t m, const kge_quantized_t *b, int32_t accumulate, void *out,
+                         int32_t out_dtype, int64_t out_ld, void *ws, size_t ws_bytes, void *hip_stream);
+size_t kge_matmul_quantized_workspace_bytes(int64_t m, int64_t n, int64_t k);
+
+/*
  * Workspace size in bytes for one call (pure function; host only).  Meaning of (B, N, K):
  *   KGE_OP_SCORE, KGE_OP_LOSS_BWD  B triples, N shared negatives, K unused
  *   KGE_OP_SPARSE_ADAM             B = M gradient rows, N = dim, K unused; model may be NULL

@@ -23,7 +23,8 @@ EXPORTS = ["kge_sample_negatives", "kge_score", "kge_loss_bwd", "kge_sparse_adam
            "kge_workspace_bytes", "kge_status_string", "kge_profile_enable", "kge_profile_collect",
            "kge_calibrate_mfma", "kge_calibrate_mfma_varied", "kge_calibrate_copy", "kge_step_counter_add", "kge_sample_negatives_dev",
            "kge_sparse_adam_apply_tables", "kge_sparse_adam_plan_tables", "kge_loss_bwd_sampled",
-           "kge_loss_bwd_sampled_planned"]
+           "kge_loss_bwd_sampled_planned", "kge_dropout", "kge_embed", "kge_embed_bwd", "kge_embed_bwd_workspace_bytes",
+           "kge_quantize", "kge_matmul_quantized", "kge_matmul_quantized_workspace_bytes"]
 PROF_SLOTS = {"block_score": 0, "block_fwd": 1, "block_gradt": 2, "adam": 3, "sort": 4, "topk_scan": 5,
               "enc_fwd": 6, "enc_bwd": 7, "gather": 8, "finish": 9}
 
@@ -66,6 +67,15 @@ class KgeAdamTableT(C.Structure):
     _fields_ = [("param_f32", C.c_void_p), ("param_bf16", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
                 ("n_rows", C.c_int64), ("dim", C.c_int32), ("ld", C.c_int64), ("grads", C.c_void_p), ("M", C.c_int64),
                 ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
+class KgeDropoutT(C.Structure):
+    _fields_ = [("p", C.c_float), ("tag", C.c_uint32), ("seed", C.c_uint64), ("step", C.c_uint64), ("step_counter", C.c_void_p)]
+
+
+class KgeQuantizedT(C.Structure):
+    _fields_ = [("format", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("codes", C.c_void_p),
+                ("ld", C.c_int64), ("scales", C.c_void_p), ("scales_ld", C.c_int64)]
 
 
 class KgeError(RuntimeError):
@@ -137,6 +147,19 @@ def load():
                                            C.c_int32, C.c_int64] + [C.c_void_p] * 11
         lib.kge_sample_negatives_sharded.argtypes = [C.c_uint64, C.c_uint64, C.c_uint32, C.c_int64, C.c_int64,
                                                      C.c_int32, C.c_int64, C.c_void_p, C.c_void_p]
+        lib.kge_dropout.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int64, C.c_int32,
+                                    C.c_void_p, C.c_void_p]
+        lib.kge_embed.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_int64, C.c_float, C.c_void_p,
+                                  C.c_void_p, C.c_int32, C.c_int64, C.c_void_p]
+        lib.kge_embed_bwd.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p, C.c_int32,
+                                      C.c_int64, C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.kge_embed_bwd_workspace_bytes.restype = C.c_size_t
+        lib.kge_embed_bwd_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int32]
+        lib.kge_quantize.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]
+        lib.kge_matmul_quantized.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int64,
+                                             C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.kge_matmul_quantized_workspace_bytes.restype = C.c_size_t
+        lib.kge_matmul_quantized_workspace_bytes.argtypes = [C.c_int64] * 3
         _lib = lib
     return _lib
 
@@ -556,3 +579,155 @@ class Encoder:
                                      _ptr(proj), _ptr(de), _ptr(g_es), _ptr(g_mh), _ptr(g_mt), _ptr(buf), buf.numel(),
                                      _stream()), "kge_encode_bwd")
         return g_es, g_mh, g_mt
+
+
+# ---------------------------------------------------------------------------------------------
+# Text side: token embeddings, dropout, 8-bit projections
+# ---------------------------------------------------------------------------------------------
+_DTYPE = {torch.float32: 0, torch.bfloat16: 1}
+_CODES = {"e4m3": 0, "e5m2": 1}
+
+
+def _here(*tensors):
+    """Every given tensor lies on the current device, whose stream the call takes."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise KgeError(f"tensors have to be on the current device cuda:{dev}, got one on {t.device}")
+
+
+def _matrix(t, what: str):
+    """(pointer, dtype, row stride) of a 2-D fp32 or bf16 tensor with contiguous rows that do not overlap."""
+    if t.dim() != 2 or t.dtype not in _DTYPE or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise KgeError(f"{what}: a 2-D fp32 or bf16 tensor with contiguous rows is wanted, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr(), _DTYPE[t.dtype], (t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1))
+
+
+def _rows_of(t, n: int, what: str):
+    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise KgeError(f"{what}: a contiguous int32 tensor of {n} entries is wanted, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _out(out, shape, dtype, device, what: str):
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(out.shape) != tuple(shape):
+        raise KgeError(f"{what}: out is {tuple(out.shape)}, {tuple(shape)} is wanted")
+    return out
+
+
+class Dropout:
+    """kge_dropout_t: probability, generator key and counter words of one layer's dropout.  step_counter: a device counter
+    (step_counter_add) that is added to `step` when the kernels run, for steps replayed from a HIP graph."""
+
+    def __init__(self, p: float, seed: int, step: int = 0, tag: int = 0, step_counter=None):
+        _here(step_counter)
+        self.counter = step_counter                        # (kept alive with the struct that points to it)
+        self.struct = KgeDropoutT(p, tag, seed, step, _counter(step_counter))
+        self.ref = C.byref(self.struct)
+
+
+def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
+    """kge_dropout: residual + D o x; on a gradient, without the residual, the backward pass.  out may be x or residual."""
+    _here(x, residual, out)
+    px, dt, ld = _matrix(x, "x")
+    out = _out(out, x.shape, x.dtype, x.device, "kge_dropout")
+    po, dto, ldo = _matrix(out, "out")
+    pr, ldr = None, 0
+    if residual is not None:
+        pr, dtr, ldr = _matrix(residual, "residual")
+        if residual.shape != x.shape or dtr != dt:
+            raise KgeError("residual has another shape or type than x")
+    if dto != dt:
+        raise KgeError("out has another type than x")
+    _check(load().kge_dropout(px, ld, pr, ldr, po, ldo, dt, x.shape[0], x.shape[1], drop.ref, _stream(stream)), "kge_dropout")
+    return out
+
+
+def embed(table, ids, scale: float = 1.0, dropout: Dropout | None = None, dtype=None, out=None, stream=None):
+    """kge_embed: rows `ids` of the table times scale, with dropout; dtype of the result: the table's, unless given."""
+    _here(table, ids, out)
+    pt, dt, ld = _matrix(table, "table")
+    M, dim = ids.numel(), table.shape[1]
+    out = _out(out, (M, dim), dtype or table.dtype, table.device, "kge_embed")
+    po, dto, ldo = _matrix(out, "out")
+    _check(load().kge_embed(pt, dt, table.shape[0], dim, ld, _rows_of(ids, M, "ids"), M, scale, dropout.ref if dropout else None, po, dto, ldo,
+                            _stream(stream)), "kge_embed")
+    return out
+
+
+def embed_bwd(g, ids, n_rows: int, scale: float = 1.0, dropout: Dropout | None = None, dtype=torch.float32, out=None,
+              accumulate: bool = False, ws: Workspace | None = None, stream=None):
+    """kge_embed_bwd: the table's gradient [n_rows, dim] from the gradient rows of the positions; accumulate: added to `out`."""
+    _here(g, ids, out)
+    pg, dg, ldg = _matrix(g, "g")
+    M, dim = g.shape
+    if accumulate and out is None:
+        raise KgeError("accumulate needs the gradient to add to")
+    out = _out(out, (n_rows, dim), dtype, g.device, "kge_embed_bwd")
+    po, do, ldo = _matrix(out, "out")
+    buf = (ws or _default_ws).get(int(load().kge_embed_bwd_workspace_bytes(M, n_rows, dim)))
+    _check(load().kge_embed_bwd(pg, dg, ldg, _rows_of(ids, M, "ids"), M, scale, dropout.ref if dropout else None, po, do, n_rows, dim, ldo,
+                                1 if accumulate else 0, _ptr(buf), buf.numel(), _stream(stream)), "kge_embed_bwd")
+    return out
+
+
+class Quantized:
+    """kge_quantized_t: a matrix [rows, cols] in 8-bit codes (uint8 [rows, 128 ceil(cols / 128)]) with an exponent byte per 128 columns
+    (uint8 [rows, ceil(cols / 128) to a multiple of four])."""
+
+    def __init__(self, codes, scales, cols: int, fmt: str = "e4m3"):
+        _here(codes, scales)
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2 or scales.dim() != 2 or codes.shape[0] != scales.shape[0]:
+            raise KgeError("codes and scales: uint8 tensors [rows, ...]")
+        nb = -(-cols // 128)
+        if codes.shape[1] < 128 * nb or scales.shape[1] < -(-nb // 4) * 4 or (codes.numel() and codes.stride(1) != 1) or (scales.numel() and scales.stride(1) != 1):
+            raise KgeError("codes: contiguous rows padded to a multiple of 128; scales: one byte per 128, padded to a multiple of four")
+        self.codes, self.scales, self.cols, self.fmt, self.rows = codes, scales, cols, fmt, codes.shape[0]
+        many = self.rows > 1 and cols > 0                      # (torch gives a stride of its own choice where there is nothing to stride over)
+        ld = codes.stride(0) if many else 128 * nb
+        self.struct = KgeQuantizedT(_CODES[fmt], 0, self.rows, cols, codes.data_ptr(), ld, scales.data_ptr(),
+                                    scales.stride(0) if many else -(-nb // 4) * 4)
+        self.ref = C.byref(self.struct)
+
+    @staticmethod
+    def empty(rows: int, cols: int, fmt: str = "e4m3", device="cuda"):
+        nb = -(-cols // 128)
+        return Quantized(torch.empty((rows, 128 * nb), dtype=torch.uint8, device=device),
+                         torch.empty((rows, -(-nb // 4) * 4), dtype=torch.uint8, device=device), cols, fmt)
+
+
+def quantize(x, fmt: str = "e4m3", by: str = "row", out=None, stream=None):
+    """kge_quantize: x by rows (by="row"), the transposed matrix (by="col"), or the pair of both (by="both") from one read of x.  out: a
+    Quantized, or a pair of them, to write to."""
+    _here(x)
+    px, dt, ld = _matrix(x, "x")
+    rows, cols = x.shape
+    if by not in ("row", "col", "both"):
+        raise KgeError(f"by: row, col or both, got {by!r}")
+    if out is None:
+        qr = Quantized.empty(rows, cols, fmt) if by != "col" else None
+        qc = Quantized.empty(cols, rows, fmt) if by != "row" else None
+    else:
+        qr, qc = out if by == "both" else (out, None) if by == "row" else (None, out)
+        for q in (qr, qc):
+            if q is not None:
+                _here(q.codes)
+    _check(load().kge_quantize(px, dt, rows, cols, ld, qr.ref if qr else None, qc.ref if qc else None, _stream(stream)), "kge_quantize")
+    return (qr, qc) if by == "both" else qr or qc
+
+
+def matmul_quantized(a: Quantized, b: Quantized, rows=None, dtype=torch.bfloat16, out=None, accumulate: bool = False,
+                     ws: Workspace | None = None, stream=None):
+    """kge_matmul_quantized: a[rows] b^t in fp32 or bf16; accumulate: added to `out`."""
+    _here(a.codes, b.codes, rows, out)
+    m = a.rows if rows is None else rows.numel()
+    if accumulate and out is None:
+        raise KgeError("accumulate needs a matrix to add to")
+    out = _out(out, (m, b.rows), dtype, b.codes.device, "kge_matmul_quantized")
+    po, do, ldo = _matrix(out, "out")
+    buf = (ws or _default_ws).get(int(load().kge_matmul_quantized_workspace_bytes(m, b.rows, a.cols)))
+    _check(load().kge_matmul_quantized(a.ref, None if rows is None else _rows_of(rows, m, "rows"), m, b.ref, 1 if accumulate else 0, po, do, ldo,
+                                       _ptr(buf), buf.numel(), _stream(stream)), "kge_matmul_quantized")
+    return out

@@ -1,0 +1,93 @@
+// Shared by the kernels of the text side (embed.hip, quantize.hip, matmul_quantized.hip): groups of eight elements of a row, and the dropout
+// generator.
+#pragma once
+#include "kge_internal.h"
+
+typedef uint32_t kge_u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t kge_u32x4 __attribute__((ext_vector_type(4)));
+typedef float kge_f32x4 __attribute__((ext_vector_type(4)));
+
+// A thread's share of a row is a group of eight consecutive columns.  Rows may start anywhere (odd widths, odd strides): vector memory
+// instructions of gfx950 take any byte address, so the types below only promise the element's own alignment and there is one
+// path for all rows; a group that the row's end cuts goes element by element.
+typedef uint32_t kge_u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t kge_u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef float kge_f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+
+template <bool BF16> __device__ __forceinline__ void kge_load8(const void *row, int64_t col, int n, float (&v)[8]) {
+    if (n >= 8) {
+        if constexpr (BF16) {
+            const kge_u32x4 r = *(const kge_u32x4_a2 *)((const uint16_t *)row + col);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { v[2 * u] = __uint_as_float(r[u] << 16); v[2 * u + 1] = __uint_as_float(r[u] & 0xffff0000u); }
+        } else {
+            const kge_f32x4 a = *(const kge_f32x4_a4 *)((const float *)row + col), b = *(const kge_f32x4_a4 *)((const float *)row + col + 4);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { v[u] = a[u]; v[4 + u] = b[u]; }
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            v[u] = 0.f;
+            if (u < n) v[u] = BF16 ? __uint_as_float((uint32_t)((const uint16_t *)row)[col + u] << 16) : ((const float *)row)[col + u];
+        }
+    }
+}
+
+template <bool BF16> __device__ __forceinline__ void kge_store8(void *row, int64_t col, int n, const float (&v)[8]) {
+    if (n >= 8) {
+        if constexpr (BF16) {
+            typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf2;
+            kge_u32x4 r;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) r[u] = __builtin_bit_cast(uint32_t, bf2{(__bf16)v[2 * u], (__bf16)v[2 * u + 1]});
+            *(kge_u32x4_a2 *)((uint16_t *)row + col) = r;
+        } else {
+            *(kge_f32x4_a4 *)((float *)row + col) = kge_f32x4{v[0], v[1], v[2], v[3]};
+            *(kge_f32x4_a4 *)((float *)row + col + 4) = kge_f32x4{v[4], v[5], v[6], v[7]};
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (u < n) {
+                if constexpr (BF16) ((__bf16 *)row)[col + u] = (__bf16)v[u];
+                else ((float *)row)[col + u] = v[u];
+            }
+    }
+}
+
+// Dropout: element (row, column) is kept iff its 16 bits of Philox4x32-10 (key = seed, counter (row, column / 8, step, tag); word
+// (column % 8) / 2, the low half for even columns) are >= thr, and is then scaled by 2^16 / (2^16 - thr).  The mask is a function of these
+// alone, so the backward pass makes it again and nothing is stored.  Sixteen bits an element and not a word: a block costs ten
+// rounds of two wide products, which at four elements a block is as much time as a bf16 element takes to copy.
+struct KgeDropDev {
+    uint32_t k0, k1, step, tag, thr; float scale; const uint64_t *step_counter;
+};
+
+__device__ __forceinline__ uint32_t kge_drop_step(const KgeDropDev &d) { return d.step + (d.step_counter ? (uint32_t)*d.step_counter : 0u); }
+
+__device__ __forceinline__ void kge_drop8(const KgeDropDev &d, uint32_t step, uint32_t row, uint32_t group, float (&v)[8]) {
+    uint32_t c0 = row, c1 = group, c2 = step, c3 = d.tag, k0 = d.k0, k1 = d.k1;
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
+        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0; c1 = (uint32_t)p1;
+        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1; c3 = (uint32_t)p0;
+        k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
+    }
+    const uint32_t w[4] = {c0, c1, c2, c3};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {                              // (a select, not a product: what is dropped may be infinite)
+        v[2 * u] = (w[u] & 0xffffu) >= d.thr ? v[2 * u] * d.scale : 0.f;
+        v[2 * u + 1] = (w[u] >> 16) >= d.thr ? v[2 * u + 1] * d.scale : 0.f;
+    }
+}
+
+// The kernels' form of a caller's dropout; nullptr and p that rounds to nothing drop nothing (thr = 0).  KGE_E_INVALID_ARG: p outside [0, 1) or
+// a step that is no 32-bit word.
+int kge_drop_dev(const kge_dropout_t *drop, KgeDropDev *out);
+
+// Item -> (row, group of the row) without a division: the quotient n / d of n, d < 2^16 from one product.
+struct KgeFastDiv { uint32_t d; uint64_t magic; };
+inline KgeFastDiv kge_fast_div(uint32_t d) { return KgeFastDiv{d, ((1ull << 32) + d - 1) / d}; }
+__device__ __forceinline__ uint32_t kge_div(uint32_t n, const KgeFastDiv &f) { return (uint32_t)((n * f.magic) >> 32); }
