@@ -477,7 +477,7 @@ int kge_dropout(const void *x, int64_t x_ld, const void *residual, int64_t resid
  * kge_embed_bwd: g_table[r, :] = scale * sum over i with ids[i] = r of D_i o g[i, :], rows without a position zeros; with accumulate = 1 it is added
  * to g_table, and rows without a position are neither read nor written.  The positions of a row are added in a fixed order, in fp32, and
  * rounded once to table_dtype: results do not depend on scheduling.  g: [M, dim]; workspace from kge_embed_bwd_workspace_bytes (0 for invalid
- * arguments).  g and g_table must not overlap.  n_rows < 2^31 - 1.
+ * arguments).  g and g_table must not overlap.
  * A table that is trained with kge_sparse_adam needs no dense gradient: that call takes the rows of g and the ids themselves.
  */
 int kge_embed(const void *table, int32_t table_dtype, int64_t n_rows, int32_t dim, int64_t ld, const int32_t *ids, int64_t M,

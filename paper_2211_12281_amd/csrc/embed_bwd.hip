@@ -1,0 +1,605 @@
+// Gradient of the token lookup:  G[r, :] (+)= scale sum over i with ids[i] = r of D_i o g[i, :]
+//
+//   1. the positions are sorted by row, stable; every row gets the place of its run in the sorted list
+//   2. sums_kernel: sums of the whole chunks of CHUNK positions inside one run, and the rows whose runs hold no whole chunk
+//   3. joins_kernel: the other rows: sums of their whole chunks, and the positions in front of and behind them
+// A gradient row is read once and a table row written once (rows without a position as zeros, or with accumulate not at all), every sum is
+// taken in an order that the sorted list alone decides, in fp32, without atomics.
+//
+// The sort.  Rows are cut into parts of consecutive rows, and one workgroup per part orders the part's list.  Long lists (2^rb rows a part, at
+// most 1,024 parts): one launch counts the ids of each part per block of ids, one deals them out stable.  Up to COLLECT_MAX ids the part's workgroup
+// (256 of them) reads all ids and collects its own, and these two launches fall away.  Up to WHOLE_MAX ids that workgroup goes on to the sums of its rows, and the call is
+// one launch.  Ids outside the table belong to no part and are gone from the list.
+#include "text_ops.hpp"
+
+namespace {
+
+constexpr int NT = 256;
+constexpr int SORT_NT = 1024, WAVES = SORT_NT / 64;
+constexpr int PARTS_BITS = 10;                                // parts of a long list
+static_assert(1 << PARTS_BITS <= SORT_NT, "one thread per part");
+constexpr int COLLECT_PARTS = 256;                            // parts of a list that every part reads: one workgroup per compute unit
+constexpr int DIGIT_BITS = 8;                                 // of a counting pass inside a part
+constexpr int64_t COLLECT_MAX = 32768, WHOLE_MAX = 4096;
+constexpr int MAX_BLOCKS = 256;                               // blocks of ids of a long list: every one adds up the others' counts
+constexpr int CHUNK = 32;
+constexpr int ROWS = 4;                                       // rows of a slot, whose runs are looked up together
+constexpr int JOIN_LP = 4;                                    // columns of a workgroup of joins_kernel: 2^4 groups, so that sixteen slots share a run
+constexpr int JOIN_CHUNKS = 16;                               // chunks that a workgroup of joins_kernel looks at
+constexpr uint32_t EMPTY = 0xffffffffu;
+
+struct SortArgs {
+    const int32_t *ids; int64_t M, n_rows;
+    uint32_t *ka, *pa, *kb, *pb;                              // (row, position) lists; what is sorted last stands in a or b
+    uint32_t *counts;                                         // [blocks][parts]
+    uint32_t *base;                                           // [parts + 1] first place of each part's list; the last one: ids in all
+    uint32_t *first, *last;                                   // [n_rows] run of each row: places [first, last), first = EMPTY for none
+    int64_t part_rows;                                        // of each part; 2^rb where ids are dealt out
+    int parts, rb, blocks; int64_t per_block;                 // rb: bits of the numbers below part_rows
+};
+
+__device__ __forceinline__ bool in_table(const SortArgs &a, int32_t id) { return (uint32_t)id < (uint64_t)a.n_rows; }
+
+__global__ __launch_bounds__(SORT_NT) void count_kernel(const SortArgs a) {
+    __shared__ uint32_t cnt[1 << PARTS_BITS];
+    if (threadIdx.x < 1 << PARTS_BITS) cnt[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t lo = (int64_t)blockIdx.x * a.per_block, hi = lo + a.per_block < a.M ? lo + a.per_block : a.M;
+    for (int64_t i = lo + threadIdx.x; i < hi; i += SORT_NT) {
+        const int32_t id = a.ids[i];
+        if (in_table(a, id)) atomicAdd(&cnt[(uint32_t)id >> a.rb], 1u);
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < a.parts) a.counts[(int64_t)blockIdx.x * a.parts + threadIdx.x] = cnt[threadIdx.x];
+}
+
+// exclusive scan of one value per thread over the workgroup, in thread order
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *sums, uint32_t &total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t s = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t t = (uint32_t)__shfl_up((int)s, o);
+        if (lane >= o) s += t;
+    }
+    if (lane == 63) sums[wave] = s;
+    __syncthreads();
+    uint32_t before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) { const uint32_t t = sums[w]; before += w < wave ? t : 0u; total += t; }
+    __syncthreads();
+    return before + s - v;
+}
+
+// Lanes whose digit equals this lane's (of the lanes with `valid`)
+__device__ __forceinline__ uint64_t peers_of(uint32_t digit, int bits, bool valid) {
+    uint64_t p = __ballot(valid);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t m = __ballot(valid && (digit >> b & 1u));
+        p &= digit >> b & 1u ? m : ~m;
+    }
+    return p;
+}
+
+// Deals a block's ids out to the parts' lists.  A wave owns a run of the block's ids: the waves' counts per part give every wave its places, in which
+// it then moves on by itself, 64 ids at a time.
+__global__ __launch_bounds__(SORT_NT) void deal_kernel(const SortArgs a) {
+    __shared__ uint32_t place[WAVES][1 << PARTS_BITS];
+    __shared__ uint32_t sums[WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, p = threadIdx.x;
+    uint32_t before = 0, all = 0, total;
+    if (p < a.parts) {
+        int b = 0;
+        for (; b + 8 <= a.blocks; b += 8) {
+            uint32_t c[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) c[u] = a.counts[(int64_t)(b + u) * a.parts + p];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) { before += b + u < (int)blockIdx.x ? c[u] : 0u; all += c[u]; }
+        }
+        for (; b < a.blocks; ++b) {
+            const uint32_t c = a.counts[(int64_t)b * a.parts + p];
+            before += b < (int)blockIdx.x ? c : 0u; all += c;
+        }
+    }
+    const uint32_t base = block_scan(all, sums, total);
+    if (blockIdx.x == 0) {
+        if (p < a.parts) a.base[p] = base;
+        if (p == 0) a.base[a.parts] = total;
+    }
+    const bool counter = p < 1 << PARTS_BITS;                 // threads that have a column of the table of places
+    if (counter)
+        for (int w = 0; w < WAVES; ++w) place[w][p] = 0;
+    __syncthreads();
+    const int64_t lo = (int64_t)blockIdx.x * a.per_block, hi = lo + a.per_block < a.M ? lo + a.per_block : a.M;
+    const int64_t each = (a.per_block / WAVES + 63) / 64 * 64, w0 = lo + wave * each, w1 = w0 + each < hi ? w0 + each : hi;
+    for (int64_t i = w0 + lane; i < w1; i += 64) {
+        const int32_t id = a.ids[i];
+        if (in_table(a, id)) atomicAdd(&place[wave][(uint32_t)id >> a.rb], 1u);
+    }
+    __syncthreads();
+    if (counter) {
+        uint32_t run = base + before;
+        for (int w = 0; w < WAVES; ++w) { const uint32_t c = place[w][p]; place[w][p] = run; run += c; }
+    }
+    __syncthreads();
+    volatile uint32_t *mine = place[wave];                    // (one wave's own: its accesses stay in order)
+    for (int64_t i0 = w0; i0 < w1; i0 += 64) {
+        const int64_t i = i0 + lane;
+        const int32_t id = i < w1 ? a.ids[i] : -1;
+        const bool valid = in_table(a, id);
+        const uint32_t d = (uint32_t)id >> a.rb;
+        const uint64_t peers = peers_of(d, PARTS_BITS, valid);
+        const int rank = __popcll(peers & ((1ull << lane) - 1ull));
+        const uint32_t at = valid ? mine[d] : 0u;
+        __builtin_amdgcn_wave_barrier();
+        if (valid) {
+            a.ka[at + rank] = (uint32_t)id; a.pa[at + rank] = (uint32_t)i;
+            if (rank == 0) mine[d] = at + (uint32_t)__popcll(peers);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Orders the list of the workgroup's part by row, eight bits at a time, and notes the rows' runs.
+struct PartLds { uint32_t place[WAVES][1 << DIGIT_BITS]; uint32_t sums[WAVES]; uint32_t found[COLLECT_MAX / (4 * SORT_NT)][WAVES]; };
+template <bool COLLECT>
+__device__ __forceinline__ void sort_part(const SortArgs &a, PartLds &l) {
+    auto &place = l.place;
+    uint32_t *sums = l.sums;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const uint32_t part = blockIdx.x;
+    const int64_t row0 = (int64_t)part * a.part_rows, rows = min(a.part_rows, a.n_rows - row0);
+    const uint32_t r0 = (uint32_t)row0;
+    uint32_t base, n;
+    if constexpr (COLLECT) {
+        // ids four at a time: element e of thread t in round r is position (r SORT_NT + t) 4 + e
+        uint32_t own = 0, lower = 0;                          // own: four bits a round
+        const int rounds = (int)((a.M + 4 * SORT_NT - 1) / (4 * SORT_NT));
+        for (int r = 0; r < rounds; ++r) {
+            const int64_t i = ((int64_t)r * SORT_NT + tid) * 4;
+            uint32_t c = 0;
+            int32_t four[4];
+            if (i + 4 <= a.M) __builtin_memcpy(four, a.ids + i, 16);
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e) four[e] = i + e < a.M ? a.ids[i + e] : -1;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t id = (uint32_t)four[e];        // (a negative id is one past every table)
+                const bool mine = id - r0 < (uint32_t)rows;
+                own |= (mine ? 1u : 0u) << (4 * r + e);
+                lower += id < r0 ? 1u : 0u;
+                c += (uint32_t)__popcll(__ballot(mine));
+            }
+            if (lane == 0) l.found[r][wave] = c;
+        }
+        uint32_t total;
+        block_scan(lower, sums, total);                       // (its barriers also publish found)
+        base = total;
+        uint32_t at = base;
+        n = 0;
+        for (int r = 0; r < rounds; ++r) {
+            uint32_t before = 0, here = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) { const uint32_t t = l.found[r][w]; before += w < wave ? t : 0u; here += t; }
+            uint32_t k = at + before;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k += (uint32_t)__popcll(__ballot(own >> (4 * r + e) & 1u) & ((1ull << lane) - 1ull));
+            const int64_t i = ((int64_t)r * SORT_NT + tid) * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (own >> (4 * r + e) & 1u) { a.ka[k] = (uint32_t)a.ids[i + e]; a.pa[k] = (uint32_t)(i + e); ++k; }
+            at += here; n += here;
+        }
+        if (tid == 0 && part == (uint32_t)a.parts - 1) a.base[a.parts] = base + n;
+        __syncthreads();
+    } else {
+        base = a.base[part];
+        n = a.base[part + 1] - base;
+    }
+    uint32_t *ki = a.ka + base, *pi = a.pa + base, *ko = a.kb + base, *po = a.pb + base;
+    const uint32_t each = ((n + WAVES - 1) / WAVES + 63) / 64 * 64, w0 = min(n, wave * each), w1 = min(n, w0 + each);
+    for (int shift = 0; shift < a.rb; shift += DIGIT_BITS) {
+        const int bits = min(DIGIT_BITS, a.rb - shift);
+        const uint32_t mask = (1u << bits) - 1u;
+        for (int k = tid; k < WAVES << DIGIT_BITS; k += SORT_NT) (&place[0][0])[k] = 0;
+        __syncthreads();
+#pragma unroll 8
+        for (uint32_t i = w0 + lane; i < w1; i += 64) atomicAdd(&place[wave][(ki[i] - r0) >> shift & mask], 1u);
+        __syncthreads();
+        uint32_t c = 0, total;
+        if (tid < 1 << DIGIT_BITS)
+            for (int w = 0; w < WAVES; ++w) c += place[w][tid];
+        uint32_t run = block_scan(c, sums, total);
+        if (tid < 1 << DIGIT_BITS) {
+            if (a.rb <= DIGIT_BITS && tid < rows) {           // one pass: its counts are the runs
+                a.first[row0 + tid] = c ? base + run : EMPTY;
+                a.last[row0 + tid] = base + run + c;
+            }
+            for (int w = 0; w < WAVES; ++w) { const uint32_t t = place[w][tid]; place[w][tid] = run; run += t; }
+        }
+        __syncthreads();
+        volatile uint32_t *mine = place[wave];
+        constexpr int AHEAD = 8;                              // rounds whose loads are in flight (a frequent row's part is one long list)
+        for (uint32_t i0 = w0; i0 < w1; i0 += 64 * AHEAD) {
+            uint32_t key[AHEAD], pos[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const uint32_t i = min(i0 + 64 * u + lane, w1 - 1);
+                key[u] = ki[i]; pos[u] = pi[i];
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (i0 + 64 * u >= w1) break;
+                const bool valid = i0 + 64 * u + lane < w1;
+                const uint32_t d = (key[u] - r0) >> shift & mask;
+                const uint64_t peers = peers_of(d, bits, valid);
+                const int rank = __popcll(peers & ((1ull << lane) - 1ull));
+                const uint32_t at = mine[d];
+                __builtin_amdgcn_wave_barrier();
+                if (valid) {
+                    ko[at + rank] = key[u]; po[at + rank] = pos[u];
+                    if (rank == 0) mine[d] = at + (uint32_t)__popcll(peers);
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+        __syncthreads();
+        uint32_t *t = ki; ki = ko; ko = t;
+        t = pi; pi = po; po = t;
+    }
+    if (a.rb > 0 && a.rb <= DIGIT_BITS) return;
+    if (a.rb == 0) {                                          // a part is a row
+        if (tid == 0) { a.first[row0] = n ? base : EMPTY; a.last[row0] = base + n; }
+        return;
+    }
+    for (int64_t r = tid; r < rows; r += SORT_NT) a.first[row0 + r] = EMPTY;
+    __syncthreads();
+    for (uint32_t i = tid; i < n; i += SORT_NT) {
+        const uint32_t key = ki[i];
+        if (i == 0 || ki[i - 1] != key) a.first[key] = base + i;
+        if (i == n - 1 || ki[i + 1] != key) a.last[key] = base + i + 1;
+    }
+}
+
+template <bool COLLECT>
+__global__ __launch_bounds__(SORT_NT) void parts_kernel(const SortArgs a) {
+    __shared__ PartLds l;
+    sort_part<COLLECT>(a, l);
+}
+
+// ---------------------------------------------------------------------------------------------
+struct SumArgs {
+    const uint32_t *sk, *sp, *count;         // sorted rows and positions, their number
+    const uint32_t *first, *last;
+    float *part;                             // [M / CHUNK][8 cg] sums of whole chunks
+    const void *g; int64_t g_ld; int64_t M;
+    void *out; int64_t out_ld; int64_t n_rows;
+    int dim, cg, accumulate; float scale; KgeDropDev drop;
+    int64_t chunk_items, row_items;          // workgroups of sums_kernel's two halves
+    int lp;                                  // 2^lp threads take the groups of a row
+};
+
+// s += D_i o g[i, group] of the positions sp[0 .. n), in order, 8 (fp32: 4) rows in flight
+template <bool G16> __device__ __forceinline__ void add_rows(const SumArgs &a, uint32_t step, const uint32_t *sp, int n, int grp, float (&s)[8]) {
+    constexpr int B = G16 ? 8 : 4;
+    const int cols = a.dim - 8 * grp;
+    const int64_t esz = G16 ? 2 : 4;
+    auto add = [&](float (&v)[8], uint32_t p) {
+        if (a.drop.thr) kge_drop8(a.drop, step, p, (uint32_t)grp, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] += v[e];
+    };
+    if (cols < 8) {                                            // the row's last columns
+        for (int k = 0; k < n; ++k) {
+            float v[8];
+            kge_load8<G16>((const char *)a.g + (int64_t)sp[k] * a.g_ld * esz, 8 * grp, cols, v);
+            add(v, sp[k]);
+        }
+        return;
+    }
+    for (int k = 0; k < n; k += B) {
+        uint32_t p[B];
+        KgeRaw8<G16> raw[B];
+#pragma unroll
+        for (int u = 0; u < B; ++u) p[u] = sp[min(k + u, n - 1)];          // (past the end: the last one again, from the cache, not added)
+#pragma unroll
+        for (int u = 0; u < B; ++u) raw[u] = kge_raw8<G16>((const char *)a.g + (int64_t)p[u] * a.g_ld * esz, 8 * grp);
+#pragma unroll
+        for (int u = 0; u < B; ++u)
+            if (k + u < n) {
+                float v[8];
+                kge_values8<G16>(raw[u], v);
+                add(v, p[u]);
+            }
+    }
+}
+
+template <bool OUT16> __device__ __forceinline__ void finish(const SumArgs &a, int64_t row, int grp, float (&s)[8]) {
+    char *orow = (char *)a.out + row * a.out_ld * (OUT16 ? 2 : 4);
+    const int n = a.dim - 8 * grp;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] *= a.scale;
+    if (a.accumulate) {
+        float o[8];
+        kge_load8<OUT16>(orow, 8 * grp, n, o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] += o[e];
+    }
+    kge_store8<OUT16>(orow, 8 * grp, n, s);
+}
+
+__device__ __forceinline__ bool holds_chunk(uint32_t k0, uint32_t k1) { return (k0 + CHUNK - 1) / CHUNK * CHUNK + CHUNK <= k1; }
+
+// The workgroup's slots (THREADS / 2^lp groups of threads, lp <= 6) add up their parts of a sum, through the LDS, in slot order; slot 0 has the sum.
+template <int THREADS> __device__ __forceinline__ void join_slots(float (*red)[8], int lp, float (&s)[8]) {
+    __syncthreads();
+    *(kge_f32x4 *)red[threadIdx.x] = kge_f32x4{s[0], s[1], s[2], s[3]};
+    *(kge_f32x4 *)(red[threadIdx.x] + 4) = kge_f32x4{s[4], s[5], s[6], s[7]};
+    __syncthreads();
+    if ((int)threadIdx.x < 1 << lp)
+        for (int t = threadIdx.x + (1 << lp); t < THREADS; t += 1 << lp)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] += red[t][e];
+}
+
+// Up to WHOLE_MAX ids: the part's workgroup sorts and adds up.  A slot takes the rows with a FEW positions, ROWS of them at a time; the others are
+// shared by all slots one after the other.
+constexpr int FEW = 16;
+template <bool G16, bool OUT16>
+__global__ __launch_bounds__(SORT_NT) void whole_kernel(const SortArgs so, const SumArgs a) {
+    __shared__ union { PartLds sort; float red[SORT_NT][8]; } l;
+    __shared__ uint32_t many[WHOLE_MAX / FEW][3], n_many;
+    if (threadIdx.x == 0) n_many = 0;
+    sort_part<true>(so, l.sort);
+    __syncthreads();
+    const uint32_t step = a.drop.thr ? kge_drop_step(a.drop) : 0u;
+    const int per = 1 << a.lp, sub = threadIdx.x >> a.lp, subs = SORT_NT >> a.lp, grp0 = threadIdx.x & (per - 1);
+    const int64_t first_row = (int64_t)blockIdx.x * so.part_rows, end = min(first_row + so.part_rows, a.n_rows);
+    for (int64_t row0 = first_row + sub * ROWS; row0 < end; row0 += subs * ROWS) {
+        uint32_t k0[ROWS], k1[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const bool in = row0 + r < end;
+            k0[r] = in ? a.first[row0 + r] : EMPTY; k1[r] = in ? a.last[row0 + r] : EMPTY;
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            if (row0 + r >= end) break;
+            const bool none = k0[r] == EMPTY;
+            if (none && a.accumulate) continue;
+            if (!none && k1[r] - k0[r] > FEW) {
+                if (grp0 == 0) {
+                    const uint32_t f = atomicAdd(&n_many, 1u);
+                    many[f][0] = (uint32_t)(row0 + r); many[f][1] = k0[r]; many[f][2] = k1[r];
+                }
+                continue;
+            }
+            for (int grp = grp0; grp < a.cg; grp += per) {
+                float s[8] = {};
+                if (!none) add_rows<G16>(a, step, a.sp + k0[r], (int)(k1[r] - k0[r]), grp, s);
+                finish<OUT16>(a, row0 + r, grp, s);
+            }
+        }
+    }
+    __syncthreads();
+    const uint32_t n = n_many;
+    for (uint32_t f = 0; f < n; ++f) {
+        const uint32_t row = many[f][0], b0 = many[f][1], len = many[f][2] - b0, each = (len + subs - 1) / subs, lo = min(len, sub * each),
+                       hi = min(len, lo + each);
+        for (int g0 = 0; g0 < a.cg; g0 += per) {
+            const int grp = g0 + grp0;
+            float s[8] = {};
+            if (grp < a.cg) add_rows<G16>(a, step, a.sp + b0 + lo, (int)(hi - lo), grp, s);
+            join_slots<SORT_NT>(l.red, a.lp, s);
+            if (sub == 0 && grp < a.cg) finish<OUT16>(a, row, grp, s);
+        }
+    }
+}
+
+template <bool G16, bool OUT16>
+__global__ __launch_bounds__(NT) void sums_kernel(const SumArgs a) {
+    __shared__ float red[NT][8];
+    const uint32_t step = a.drop.thr ? kge_drop_step(a.drop) : 0u;
+    const int per = 1 << a.lp, sub = threadIdx.x >> a.lp, subs = NT >> a.lp, grp0 = threadIdx.x & (per - 1);
+    for (int64_t w = blockIdx.x; w < a.chunk_items + a.row_items; w += gridDim.x) {
+        if (w < a.chunk_items) {                               // a chunk: the slots take its positions in turn
+            const int64_t c0 = w * CHUNK;
+            if (c0 + CHUNK > *a.count || a.sk[c0] != a.sk[c0 + CHUNK - 1]) continue;      // (equal ends, equal chunk)
+            const int each = CHUNK / min(subs, CHUNK);
+            for (int g0 = 0; g0 < a.cg; g0 += per) {
+                const int grp = g0 + grp0;
+                float s[8] = {};
+                if (grp < a.cg && sub * each < CHUNK) add_rows<G16>(a, step, a.sp + c0 + sub * each, each, grp, s);
+                join_slots<NT>(red, a.lp, s);
+                if (sub == 0 && grp < a.cg) {
+                    float *p = a.part + (w * a.cg + grp) * 8;
+                    *(kge_f32x4 *)p = kge_f32x4{s[0], s[1], s[2], s[3]};
+                    *(kge_f32x4 *)(p + 4) = kge_f32x4{s[4], s[5], s[6], s[7]};
+                }
+            }
+        } else {                                               // ROWS rows per slot
+            const int64_t row0 = ((w - a.chunk_items) * subs + sub) * ROWS;
+            uint32_t k0[ROWS], k1[ROWS];
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const bool in = row0 + r < a.n_rows && a.M;
+                k0[r] = in ? a.first[row0 + r] : EMPTY; k1[r] = in ? a.last[row0 + r] : EMPTY;
+            }
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                if (row0 + r >= a.n_rows) break;
+                if (k0[r] == EMPTY ? a.accumulate : holds_chunk(k0[r], k1[r])) continue;
+                for (int grp = grp0; grp < a.cg; grp += per) {
+                    float s[8] = {};
+                    if (k0[r] != EMPTY) add_rows<G16>(a, step, a.sp + k0[r], (int)(k1[r] - k0[r]), grp, s);
+                    finish<OUT16>(a, row0 + r, grp, s);
+                }
+            }
+        }
+    }
+}
+
+// One workgroup per JOIN_CHUNKS chunks and 2^lp groups of columns: of the chunks that are a run's first whole one, it adds up the run.
+template <bool G16, bool OUT16>
+__global__ __launch_bounds__(NT) void joins_kernel(const SumArgs a, int slices) {
+    __shared__ float red[NT][8];
+    __shared__ uint32_t found[JOIN_CHUNKS][3];
+    const uint32_t step = a.drop.thr ? kge_drop_step(a.drop) : 0u;
+    const int per = 1 << a.lp, sub = threadIdx.x >> a.lp, subs = NT >> a.lp;
+    const int64_t tiles = (a.chunk_items + JOIN_CHUNKS - 1) / JOIN_CHUNKS;
+    for (int64_t w = blockIdx.x; w < tiles * slices; w += gridDim.x) {
+        const int64_t tile = w / slices;
+        bool owner = false;
+        uint32_t row = 0, k0 = 0, k1 = 0;
+        if (threadIdx.x < JOIN_CHUNKS) {
+            const int64_t c = tile * JOIN_CHUNKS + threadIdx.x, c0 = c * CHUNK;
+            if (c < a.chunk_items && c0 + CHUNK <= *a.count) {
+                row = a.sk[c0];
+                if (row == a.sk[c0 + CHUNK - 1]) { k0 = a.first[row]; k1 = a.last[row]; owner = (k0 + CHUNK - 1) / CHUNK == c; }
+            }
+            found[threadIdx.x][0] = owner ? row : EMPTY; found[threadIdx.x][1] = k0; found[threadIdx.x][2] = k1;
+        }
+        if (!__syncthreads_or(owner)) continue;
+        const int grp = (int)(w - tile * slices) * per + (threadIdx.x & (per - 1));
+        for (int f = 0; f < JOIN_CHUNKS; ++f) {
+            const uint32_t r = found[f][0];
+            if (r == EMPTY) continue;
+            const uint32_t b0 = found[f][1], b1 = found[f][2], e0 = (b0 + CHUNK - 1) / CHUNK, e1 = b1 / CHUNK;
+            float s[8] = {};
+            if (grp < a.cg) {
+                // slot by slot: a share of the positions in front, of the chunks, of the positions behind
+                auto share = [&](uint32_t n, uint32_t &lo) { const uint32_t x = (n + subs - 1) / subs; lo = min(n, sub * x); return min(n, lo + x) - lo; };
+                uint32_t lo, n = share(e0 * CHUNK - b0, lo);
+                add_rows<G16>(a, step, a.sp + b0 + lo, (int)n, grp, s);
+                n = share(e1 - e0, lo);
+                const float *p = a.part + ((int64_t)(e0 + lo) * a.cg + grp) * 8;
+                for (uint32_t k = 0; k < n; k += 8) {
+                    kge_f32x4 x[8][2];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const float *q = p + (int64_t)min(k + u, n - 1) * a.cg * 8;
+                        x[u][0] = *(const kge_f32x4 *)q; x[u][1] = *(const kge_f32x4 *)(q + 4);
+                    }
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+                        if (k + u < n) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) { s[e] += x[u][0][e]; s[4 + e] += x[u][1][e]; }
+                        }
+                }
+                n = share(b1 - e1 * CHUNK, lo);
+                add_rows<G16>(a, step, a.sp + e1 * CHUNK + lo, (int)n, grp, s);
+            }
+            join_slots<NT>(red, a.lp, s);
+            if (sub == 0 && grp < a.cg) finish<OUT16>(a, r, grp, s);
+        }
+        __syncthreads();                                       // (found is written again)
+    }
+}
+
+struct Ws { SortArgs s; float *part; };
+int bits_of(int64_t n) {                     // of the numbers below n
+    int b = 0;
+    while ((1ll << b) < n) ++b;
+    return b;
+}
+size_t carve(int64_t M, int64_t n_rows, int dim, void *ws, Ws &w) {
+    char *p = (char *)ws;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { void *q = p ? p + off : nullptr; off += (bytes + 255) / 256 * 256; return (uint32_t *)q; };
+    SortArgs &s = w.s;
+    s.M = M; s.n_rows = n_rows;
+    if (M <= COLLECT_MAX) {
+        s.part_rows = (n_rows + COLLECT_PARTS - 1) / COLLECT_PARTS;
+        if (s.part_rows < 1) s.part_rows = 1;
+        s.rb = bits_of(s.part_rows);
+    } else {
+        const int bits = bits_of(n_rows);
+        s.rb = bits > PARTS_BITS ? bits - PARTS_BITS : 0;
+        s.part_rows = 1ll << s.rb;
+    }
+    s.parts = (int)((n_rows + s.part_rows - 1) / s.part_rows);
+    // blocks of 2,048 ids (32 rounds of a wave), larger ones beyond 256 of them
+    s.per_block = 2048;
+    while (s.per_block * MAX_BLOCKS < M) s.per_block *= 2;
+    s.blocks = (int)((M + s.per_block - 1) / s.per_block);
+    s.ka = take((size_t)M * 4); s.pa = take((size_t)M * 4); s.kb = take((size_t)M * 4); s.pb = take((size_t)M * 4);
+    s.counts = take((size_t)MAX_BLOCKS * (4u << PARTS_BITS));
+    s.base = take((4u << PARTS_BITS) + 4);
+    s.first = take((size_t)n_rows * 4); s.last = take((size_t)n_rows * 4);
+    w.part = (float *)take((size_t)(M / CHUNK) * ((dim + 7) / 8) * 32);
+    return off;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t kge_embed_bwd_workspace_bytes(int64_t M, int64_t n_rows, int32_t dim) {
+    if (M < 0 || M > KGE_MAX_ROWS || n_rows < 0 || n_rows > KGE_MAX_ROWS || dim < 1 || dim > KGE_MAX_DIM) return 0;
+    Ws w;
+    return carve(M, n_rows, dim, nullptr, w) + 256;
+}
+
+int kge_embed_bwd(const void *g, int32_t g_dtype, int64_t g_ld, const int32_t *ids, int64_t M, float scale, const kge_dropout_t *drop,
+                  void *g_table, int32_t table_dtype, int64_t n_rows, int32_t dim, int64_t ld, int32_t accumulate, void *ws, size_t ws_bytes,
+                  void *hip_stream) {
+    SumArgs a = {};
+    const int rc = kge_drop_dev(drop, &a.drop);
+    if (rc != KGE_OK) return rc;
+    if (kge_bad_type(g_dtype) || kge_bad_type(table_dtype) || dim < 1 || dim > KGE_MAX_DIM || n_rows < 0 || n_rows > KGE_MAX_ROWS || M < 0 ||
+        M > KGE_MAX_ROWS || g_ld >= KGE_MAX_LD || ld >= KGE_MAX_LD || (accumulate != 0 && accumulate != 1)) return KGE_E_INVALID_ARG;
+    if (n_rows == 0 || (M == 0 && accumulate)) return KGE_OK;
+    if (kge_bad_rows(g_table, table_dtype, ld, dim) || (M > 0 && (!ids || ((uintptr_t)ids & 3) != 0 || kge_bad_rows(g, g_dtype, g_ld, dim))))
+        return KGE_E_INVALID_ARG;
+    if (!ws) return KGE_E_WORKSPACE_TOO_SMALL;
+    const size_t lost = (256 - ((uintptr_t)ws & 255)) & 255;
+    Ws w = {};
+    if (carve(M, n_rows, dim, nullptr, w) + lost > ws_bytes) return KGE_E_WORKSPACE_TOO_SMALL;
+    carve(M, n_rows, dim, (char *)ws + lost, w);
+    hipStream_t st = (hipStream_t)hip_stream;
+    SortArgs &s = w.s;
+    s.ids = ids;
+    const bool odd = ((s.rb + DIGIT_BITS - 1) / DIGIT_BITS & 1) != 0;
+    a.sk = odd ? s.kb : s.ka; a.sp = odd ? s.pb : s.pa; a.count = s.base + s.parts; a.first = s.first; a.last = s.last; a.part = w.part;
+    a.g = g; a.g_ld = g_ld; a.M = M; a.out = g_table; a.out_ld = ld; a.n_rows = n_rows; a.dim = dim; a.cg = (dim + 7) / 8;
+    a.accumulate = accumulate; a.scale = scale;
+    a.lp = bits_of(a.cg);
+    if (a.lp > 6) a.lp = 6;
+    const bool g16 = g_dtype == KGE_BF16, o16 = table_dtype == KGE_BF16;
+    if (M > 0 && M <= WHOLE_MAX) {
+        const dim3 grid((unsigned)s.parts);
+        if (g16 && o16) hipLaunchKernelGGL((whole_kernel<true, true>), grid, dim3(SORT_NT), 0, st, s, a);
+        else if (g16) hipLaunchKernelGGL((whole_kernel<true, false>), grid, dim3(SORT_NT), 0, st, s, a);
+        else if (o16) hipLaunchKernelGGL((whole_kernel<false, true>), grid, dim3(SORT_NT), 0, st, s, a);
+        else hipLaunchKernelGGL((whole_kernel<false, false>), grid, dim3(SORT_NT), 0, st, s, a);
+        return kge_launch_status();
+    }
+    if (M > COLLECT_MAX) {
+        hipLaunchKernelGGL(count_kernel, dim3(s.blocks), dim3(SORT_NT), 0, st, s);
+        hipLaunchKernelGGL(deal_kernel, dim3(s.blocks), dim3(SORT_NT), 0, st, s);
+        hipLaunchKernelGGL(parts_kernel<false>, dim3(s.parts), dim3(SORT_NT), 0, st, s);
+    } else if (M > 0) hipLaunchKernelGGL(parts_kernel<true>, dim3(s.parts), dim3(SORT_NT), 0, st, s);
+    SumArgs j = a;                                             // long runs: many slots, few columns each
+    if (j.lp > JOIN_LP) j.lp = JOIN_LP;
+    const int slots = NT >> a.lp, slices = (a.cg + (1 << j.lp) - 1) >> j.lp;
+    a.chunk_items = j.chunk_items = M / CHUNK;
+    a.row_items = (n_rows + slots * ROWS - 1) / (slots * ROWS);
+    const dim3 grid = kge_grid_of(a.chunk_items + a.row_items, 1), grid2 = kge_grid_of((a.chunk_items + JOIN_CHUNKS - 1) / JOIN_CHUNKS * slices, 1);
+#define KGE_BWD(G, O)                                                                                           \
+    do {                                                                                                        \
+        hipLaunchKernelGGL((sums_kernel<G, O>), grid, dim3(NT), 0, st, a);                                      \
+        if (a.chunk_items > 0) hipLaunchKernelGGL((joins_kernel<G, O>), grid2, dim3(NT), 0, st, j, slices);     \
+    } while (0)
+    if (g16 && o16) KGE_BWD(true, true);
+    else if (g16) KGE_BWD(true, false);
+    else if (o16) KGE_BWD(false, true);
+    else KGE_BWD(false, false);
+#undef KGE_BWD
+    return kge_launch_status();
+}
+
+}  // extern "C"

@@ -11,6 +11,7 @@ typedef float kge_f32x4 __attribute__((ext_vector_type(4)));
 // instructions of gfx950 take any byte address, so the types below only promise the element's own alignment and there is one
 // path for all rows; a group that the row's end cuts goes element by element.
 typedef uint32_t kge_u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t kge_u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t kge_u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
 typedef float kge_f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -31,6 +32,25 @@ template <bool BF16> __device__ __forceinline__ void kge_load8(const void *row, 
             v[u] = 0.f;
             if (u < n) v[u] = BF16 ? __uint_as_float((uint32_t)((const uint16_t *)row)[col + u] << 16) : ((const float *)row)[col + u];
         }
+    }
+}
+
+// The same in two steps, for loads that stay in flight: a whole group's words, and its values.
+template <bool BF16> struct KgeRaw8 { kge_u32x4 w[BF16 ? 1 : 2]; };
+template <bool BF16> __device__ __forceinline__ KgeRaw8<BF16> kge_raw8(const void *row, int64_t col) {
+    KgeRaw8<BF16> r;
+    if constexpr (BF16) r.w[0] = *(const kge_u32x4_a2 *)((const uint16_t *)row + col);
+    else {
+        r.w[0] = *(const kge_u32x4_a4 *)((const uint32_t *)row + col);
+        r.w[1] = *(const kge_u32x4_a4 *)((const uint32_t *)row + col + 4);
+    }
+    return r;
+}
+template <bool BF16> __device__ __forceinline__ void kge_values8(const KgeRaw8<BF16> &r, float (&v)[8]) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        if constexpr (BF16) { v[2 * u] = __uint_as_float(r.w[0][u] << 16); v[2 * u + 1] = __uint_as_float(r.w[0][u] & 0xffff0000u); }
+        else { v[u] = __uint_as_float(r.w[0][u]); v[4 + u] = __uint_as_float(r.w[1][u]); }
     }
 }
 
@@ -91,3 +111,14 @@ int kge_drop_dev(const kge_dropout_t *drop, KgeDropDev *out);
 struct KgeFastDiv { uint32_t d; uint64_t magic; };
 inline KgeFastDiv kge_fast_div(uint32_t d) { return KgeFastDiv{d, ((1ull << 32) + d - 1) / d}; }
 __device__ __forceinline__ uint32_t kge_div(uint32_t n, const KgeFastDiv &f) { return (uint32_t)((n * f.magic) >> 32); }
+
+// Workgroups of a launch: a grid is limited to 2^32 threads, beyond 2^22 workgroups they take turns
+inline dim3 kge_grid_of(int64_t n, int64_t per) { const int64_t b = (n + per - 1) / per; return dim3((unsigned)(b < (1 << 22) ? b : 1 << 22)); }
+
+inline bool kge_bad_type(int32_t dtype) { return dtype != KGE_F32 && dtype != KGE_BF16; }
+// rows of a matrix: a stride below the width would make them overlap, and the addresses have to be whole elements
+inline bool kge_bad_rows(const void *p, int32_t dtype, int64_t ld, int64_t cols) {
+    return !p || ld < cols || ((uintptr_t)p & (dtype == KGE_BF16 ? 1 : 3)) != 0;
+}
+constexpr int64_t KGE_MAX_ROWS = (1ll << 31) - 1, KGE_MAX_LD = 1ll << 31;
+constexpr int KGE_MAX_DIM = 65536;

@@ -136,7 +136,8 @@ def test_embed_bwd(dt, odt, M, V, dim, pad, p, acc):
     _within(got, want, tol + (want.abs() + tol) * HALF[odt], "embed_bwd")
 
 
-@pytest.mark.parametrize("M,V,dim", [(32768, 700, 40), (32769, 700, 40), (70000, 90000, 24), (70000, 3, 72)])
+@pytest.mark.parametrize("M,V,dim", [(32768, 700, 40), (32769, 700, 40), (70000, 90000, 24), (70000, 3, 72), (32768, 3_000_000, 8), (40000, 3_000_000, 8),
+                                     (530_000, 5000, 8), (33000, 1, 16), (20000, 70_000, 600)])
 def test_embed_bwd_long(M, V, dim):
     """Both sorts, runs of thousands of positions, every chunk boundary."""
     g, ids, scale, want, tol = _bwd_case(M, V, dim, 0.0, BF16)
