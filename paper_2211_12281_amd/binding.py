@@ -6,6 +6,7 @@ stream.  There is no CPU fallback: if the library is missing or a call fails, an
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -592,15 +593,16 @@ def _here(*tensors):
     """Every given tensor lies on the current device, whose stream the call takes."""
     dev = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
+        if t is not None and t.get_device() != dev:
             raise KgeError(f"tensors have to be on the current device cuda:{dev}, got one on {t.device}")
 
 
 def _matrix(t, what: str):
     """(pointer, dtype, row stride) of a 2-D fp32 or bf16 tensor with contiguous rows that do not overlap."""
-    if t.dim() != 2 or t.dtype not in _DTYPE or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise KgeError(f"{what}: a 2-D fp32 or bf16 tensor with contiguous rows is wanted, got {t.dtype} {tuple(t.shape)}")
-    return t.data_ptr(), _DTYPE[t.dtype], (t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1))
+    dtype, shape = _DTYPE.get(t.dtype), t.shape
+    if dtype is None or len(shape) != 2 or (shape[1] > 1 and t.stride(1) != 1):
+        raise KgeError(f"{what}: a 2-D fp32 or bf16 tensor with contiguous rows is wanted, got {t.dtype} {tuple(shape)}")
+    return t.data_ptr(), dtype, (t.stride(0) if shape[0] > 1 else max(shape[1], 1))
 
 
 def _rows_of(t, n: int, what: str):
@@ -609,12 +611,26 @@ def _rows_of(t, n: int, what: str):
     return t.data_ptr()
 
 
-def _out(out, shape, dtype, device, what: str):
+def _new(out, rows: int, cols: int, dtype, what: str):
+    """(out, pointer, dtype, row stride): the given matrix, or a new one on the current device."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(out.shape) != tuple(shape):
-        raise KgeError(f"{what}: out is {tuple(out.shape)}, {tuple(shape)} is wanted")
-    return out
+        if dtype not in _DTYPE:
+            raise KgeError(f"{what}: fp32 or bf16, got {dtype}")
+        out = torch.empty((rows, cols), dtype=dtype, device="cuda")
+        return out, out.data_ptr(), _DTYPE[dtype], max(cols, 1)
+    if tuple(out.shape) != (rows, cols):
+        raise KgeError(f"{what}: out is {tuple(out.shape)}, {(rows, cols)} is wanted")
+    return (out, *_matrix(out, "out"))
+
+
+@functools.lru_cache(maxsize=1024)
+def _embed_bwd_bytes(M: int, n_rows: int, dim: int) -> int:
+    return int(load().kge_embed_bwd_workspace_bytes(M, n_rows, dim))
+
+
+@functools.lru_cache(maxsize=1024)
+def _matmul_bytes(m: int, n: int, k: int) -> int:
+    return int(load().kge_matmul_quantized_workspace_bytes(m, n, k))
 
 
 class Dropout:
@@ -632,8 +648,8 @@ def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
     """kge_dropout: residual + D o x; on a gradient, without the residual, the backward pass.  out may be x or residual."""
     _here(x, residual, out)
     px, dt, ld = _matrix(x, "x")
-    out = _out(out, x.shape, x.dtype, x.device, "kge_dropout")
-    po, dto, ldo = _matrix(out, "out")
+    rows, cols = x.shape
+    out, po, dto, ldo = _new(out, rows, cols, x.dtype, "kge_dropout")
     pr, ldr = None, 0
     if residual is not None:
         pr, dtr, ldr = _matrix(residual, "residual")
@@ -641,7 +657,7 @@ def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
             raise KgeError("residual has another shape or type than x")
     if dto != dt:
         raise KgeError("out has another type than x")
-    _check(load().kge_dropout(px, ld, pr, ldr, po, ldo, dt, x.shape[0], x.shape[1], drop.ref, _stream(stream)), "kge_dropout")
+    _check(load().kge_dropout(px, ld, pr, ldr, po, ldo, dt, rows, cols, drop.ref, _stream(stream)), "kge_dropout")
     return out
 
 
@@ -649,10 +665,9 @@ def embed(table, ids, scale: float = 1.0, dropout: Dropout | None = None, dtype=
     """kge_embed: rows `ids` of the table times scale, with dropout; dtype of the result: the table's, unless given."""
     _here(table, ids, out)
     pt, dt, ld = _matrix(table, "table")
-    M, dim = ids.numel(), table.shape[1]
-    out = _out(out, (M, dim), dtype or table.dtype, table.device, "kge_embed")
-    po, dto, ldo = _matrix(out, "out")
-    _check(load().kge_embed(pt, dt, table.shape[0], dim, ld, _rows_of(ids, M, "ids"), M, scale, dropout.ref if dropout else None, po, dto, ldo,
+    M, (n_rows, dim) = ids.numel(), table.shape
+    out, po, dto, ldo = _new(out, M, dim, dtype or table.dtype, "kge_embed")
+    _check(load().kge_embed(pt, dt, n_rows, dim, ld, _rows_of(ids, M, "ids"), M, scale, dropout.ref if dropout else None, po, dto, ldo,
                             _stream(stream)), "kge_embed")
     return out
 
@@ -665,11 +680,10 @@ def embed_bwd(g, ids, n_rows: int, scale: float = 1.0, dropout: Dropout | None =
     M, dim = g.shape
     if accumulate and out is None:
         raise KgeError("accumulate needs the gradient to add to")
-    out = _out(out, (n_rows, dim), dtype, g.device, "kge_embed_bwd")
-    po, do, ldo = _matrix(out, "out")
-    buf = (ws or _default_ws).get(int(load().kge_embed_bwd_workspace_bytes(M, n_rows, dim)))
+    out, po, do, ldo = _new(out, n_rows, dim, dtype, "kge_embed_bwd")
+    buf = (ws or _default_ws).get(_embed_bwd_bytes(M, n_rows, dim))
     _check(load().kge_embed_bwd(pg, dg, ldg, _rows_of(ids, M, "ids"), M, scale, dropout.ref if dropout else None, po, do, n_rows, dim, ldo,
-                                1 if accumulate else 0, _ptr(buf), buf.numel(), _stream(stream)), "kge_embed_bwd")
+                                1 if accumulate else 0, buf.data_ptr(), buf.numel(), _stream(stream)), "kge_embed_bwd")
     return out
 
 
@@ -678,17 +692,17 @@ class Quantized:
     (uint8 [rows, ceil(cols / 128) to a multiple of four])."""
 
     def __init__(self, codes, scales, cols: int, fmt: str = "e4m3"):
-        _here(codes, scales)
-        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2 or scales.dim() != 2 or codes.shape[0] != scales.shape[0]:
+        nb = (cols + 127) // 128
+        (rows, wide), (srows, swide) = codes.shape, scales.shape
+        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or rows != srows:
             raise KgeError("codes and scales: uint8 tensors [rows, ...]")
-        nb = -(-cols // 128)
-        if codes.shape[1] < 128 * nb or scales.shape[1] < -(-nb // 4) * 4 or (codes.numel() and codes.stride(1) != 1) or (scales.numel() and scales.stride(1) != 1):
+        ld, sld = 128 * nb, (nb + 3) // 4 * 4
+        if wide < ld or swide < sld or (cols > 0 and rows > 0 and (codes.stride(1) != 1 or scales.stride(1) != 1)):
             raise KgeError("codes: contiguous rows padded to a multiple of 128; scales: one byte per 128, padded to a multiple of four")
-        self.codes, self.scales, self.cols, self.fmt, self.rows = codes, scales, cols, fmt, codes.shape[0]
-        many = self.rows > 1 and cols > 0                      # (torch gives a stride of its own choice where there is nothing to stride over)
-        ld = codes.stride(0) if many else 128 * nb
-        self.struct = KgeQuantizedT(_CODES[fmt], 0, self.rows, cols, codes.data_ptr(), ld, scales.data_ptr(),
-                                    scales.stride(0) if many else -(-nb // 4) * 4)
+        if rows > 1 and cols > 0:                          # (else torch gives strides of its own choice)
+            ld, sld = codes.stride(0), scales.stride(0)
+        self.codes, self.scales, self.rows, self.cols, self.fmt = codes, scales, rows, cols, fmt
+        self.struct = KgeQuantizedT(_CODES[fmt], 0, rows, cols, codes.data_ptr(), ld, scales.data_ptr(), sld)
         self.ref = C.byref(self.struct)
 
     @staticmethod
@@ -713,7 +727,7 @@ def quantize(x, fmt: str = "e4m3", by: str = "row", out=None, stream=None):
         qr, qc = out if by == "both" else (out, None) if by == "row" else (None, out)
         for q in (qr, qc):
             if q is not None:
-                _here(q.codes)
+                _here(q.codes, q.scales)
     _check(load().kge_quantize(px, dt, rows, cols, ld, qr.ref if qr else None, qc.ref if qc else None, _stream(stream)), "kge_quantize")
     return (qr, qc) if by == "both" else qr or qc
 
@@ -721,13 +735,12 @@ def quantize(x, fmt: str = "e4m3", by: str = "row", out=None, stream=None):
 def matmul_quantized(a: Quantized, b: Quantized, rows=None, dtype=torch.bfloat16, out=None, accumulate: bool = False,
                      ws: Workspace | None = None, stream=None):
     """kge_matmul_quantized: a[rows] b^t in fp32 or bf16; accumulate: added to `out`."""
-    _here(a.codes, b.codes, rows, out)
+    _here(a.codes, a.scales, b.codes, b.scales, rows, out)
     m = a.rows if rows is None else rows.numel()
     if accumulate and out is None:
         raise KgeError("accumulate needs a matrix to add to")
-    out = _out(out, (m, b.rows), dtype, b.codes.device, "kge_matmul_quantized")
-    po, do, ldo = _matrix(out, "out")
-    buf = (ws or _default_ws).get(int(load().kge_matmul_quantized_workspace_bytes(m, b.rows, a.cols)))
+    out, po, do, ldo = _new(out, m, b.rows, dtype, "kge_matmul_quantized")
+    buf = (ws or _default_ws).get(_matmul_bytes(m, b.rows, a.cols))
     _check(load().kge_matmul_quantized(a.ref, None if rows is None else _rows_of(rows, m, "rows"), m, b.ref, 1 if accumulate else 0, po, do, ldo,
-                                       _ptr(buf), buf.numel(), _stream(stream)), "kge_matmul_quantized")
+                                       buf.data_ptr(), buf.numel(), _stream(stream)), "kge_matmul_quantized")
     return out

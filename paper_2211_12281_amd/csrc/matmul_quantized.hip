@@ -11,6 +11,7 @@
 //   fp32 output  the codes are widened to bf16 with their scale, which is exact, and multiplied with 32 x 32 x 16 bf16
 //                instructions and fp32 sums: 1e-7, at half the rate.
 #include "text_ops.hpp"
+#include <type_traits>
 
 typedef int mq_i32x8 __attribute__((ext_vector_type(8)));
 typedef float mq_f32x16 __attribute__((ext_vector_type(16)));
@@ -53,36 +54,58 @@ template <int FMT> __device__ __forceinline__ mq_bf16x8 mq_widen8(uint32_t lo, u
     return __builtin_bit_cast(mq_bf16x8, r);
 }
 
-// four consecutive columns of an output row
-__device__ __forceinline__ void mq_store4(const MatmulArgs &p, int64_t row, int64_t col, const float (&v)[4], bool valid) {
-    const int n = (int)(p.n - col < 4 ? p.n - col : 4);
+// eight (bf16 output) or four (fp32 output, and partial sums) consecutive columns of an output row
+template <bool OUT16> __device__ __forceinline__ void mq_store(const MatmulArgs &p, int64_t row, int64_t col, float (&v)[OUT16 ? 8 : 4], bool valid) {
+    constexpr int C = OUT16 ? 8 : 4;
+    const int n = (int)(p.n - col < C ? p.n - col : C);
     if (n <= 0) return;
-    float o[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = valid ? v[e] : 0.f;
-    if (p.out16) {
-        uint16_t *q = (uint16_t *)p.out + row * p.out_ld + col;
-        if (n == 4) {
-            if (p.accumulate) {
-                const kge_u32x2 r = *(const kge_u32x2_a2 *)q;
+    for (int e = 0; e < C; ++e) v[e] = valid ? v[e] : 0.f;
+    if constexpr (OUT16) {
+        uint16_t *q = (uint16_t *)p.out + row * p.out_ld;
+        if (p.accumulate) {
+            float o[8];
+            kge_load8<true>(q, col, n, o);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] += __uint_as_float(e & 1 ? r[e >> 1] & 0xffff0000u : r[e >> 1] << 16);
-            }
-            typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf2;
-            *(kge_u32x2_a2 *)q = kge_u32x2{__builtin_bit_cast(uint32_t, bf2{(__bf16)o[0], (__bf16)o[1]}), __builtin_bit_cast(uint32_t, bf2{(__bf16)o[2], (__bf16)o[3]})};
-        } else
-            for (int e = 0; e < n; ++e) {
-                if (p.accumulate) o[e] += __uint_as_float((uint32_t)q[e] << 16);
-                ((__bf16 *)q)[e] = (__bf16)o[e];
-            }
+            for (int e = 0; e < C; ++e) v[e] += o[e];
+        }
+        kge_store8<true>(q, col, n, v);
     } else {
         float *q = (float *)p.out + row * p.out_ld + col;
         if (n == 4) {
-            kge_f32x4 r = {o[0], o[1], o[2], o[3]};
-            if (p.accumulate) r = r + *(const kge_f32x4_a4 *)q;
+            kge_f32x4 r = {v[0], v[1], v[2], v[3]};
+            if (p.accumulate) {
+                const kge_f32x4 o = *(const kge_f32x4_a4 *)q;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e] += o[e];
+            }
             *(kge_f32x4_a4 *)q = r;
-        } else
-            for (int e = 0; e < n; ++e) q[e] = p.accumulate ? q[e] + o[e] : o[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (e < n) q[e] = p.accumulate ? q[e] + v[e] : v[e];
+        }
+    }
+}
+// four columns, whatever the output's type
+__device__ __forceinline__ void mq_store4(const MatmulArgs &p, int64_t row, int64_t col, kge_f32x4 s, bool valid) {
+    if (!p.out16) {
+        float v[4] = {s[0], s[1], s[2], s[3]};
+        mq_store<false>(p, row, col, v, valid);
+        return;
+    }
+    const int n = (int)(p.n - col < 4 ? p.n - col : 4);
+    uint16_t *q = (uint16_t *)p.out + row * p.out_ld + col;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (p.accumulate && e < n ? __uint_as_float((uint32_t)q[e] << 16) : 0.f) + (valid ? s[e] : 0.f);
+    if (n == 4) {
+        typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf2;
+        *(kge_u32x2_a2 *)q = kge_u32x2{__builtin_bit_cast(uint32_t, bf2{(__bf16)v[0], (__bf16)v[1]}), __builtin_bit_cast(uint32_t, bf2{(__bf16)v[2], (__bf16)v[3]})};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) ((__bf16 *)q)[e] = (__bf16)v[e];
     }
 }
 __device__ __forceinline__ bool mq_row_valid(const MatmulArgs &p, int64_t row) {
@@ -91,15 +114,21 @@ __device__ __forceinline__ bool mq_row_valid(const MatmulArgs &p, int64_t row) {
     return r >= 0 && r < p.a_rows;
 }
 
-// Workgroup = 4 waves = 64 NJ rows of A x 64 NI rows of B, wave = a quarter (NI x NJ blocks of 32 x 32).  Stages of 128 bytes of every row
-// and the word of every row's scales that holds the block's byte pass through an LDS ring, filled by asynchronous copies; a row's eight 16-byte pieces
-// lie XOR-swizzled by row % 8, so that the fragment reads of eight consecutive rows fall into different banks.  Rows beyond the matrices are read from row 0 and
-// not stored.  Which 32 bytes of a block a lane half contracts first does not matter as long as both operands agree.
-template <int NI, int NJ, int NST, bool WIDE, int FA, int FB>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NI * NJ > 4 ? 1 : 2, NI * NJ > 4 ? 1 : 2))) void matmul_tiles_kernel(const MatmulArgs p) {
-    constexpr int TN = 64 * NI, TM = 64 * NJ, CODES = (TN + TM) * BLOCK, STAGE = CODES + (TN + TM) * 4;
-    constexpr int SC = (NI + NJ) / 4, PER = 2 * NI + 2 * NJ + SC;                 // copies of a wave per stage
-    static_assert((NI + NJ) % 4 == 0 && (NST - 1) * PER < 64, "copies of a stage");
+// Workgroup = WM x WN waves = TM rows of A x TN rows of B, wave = NJ x NI blocks of 32 x 32.  Stages of 64 bytes of every row (half a
+// block; with the first half the word of every row's scales that holds the block's byte) pass through a ring of NST stages in the LDS, filled by asynchronous
+// copies.  A row's four 16-byte pieces lie XOR-swizzled by (row / 4) % 4: the fragment reads of sixteen consecutive rows then fall into
+// different ones of the 64 banks.  Rows beyond the matrices are read from row 0 and
+// not stored.  Which bytes of a stage a lane half contracts first does not matter as long as both operands agree.
+//
+// The fragments of the next step are read while this one's are multiplied, across the stages too: the only barrier of a stage stands in front of the
+// products of its last step, whose operands are in registers by then, and the stage that it frees is refilled behind it.
+template <int WM, int WN, int NJ, int NI, int NST, bool WIDE, int FA, int FB>
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(NI * NJ > 8 ? 1 : 2, NI * NJ > 8 ? 1 : 2)))
+void matmul_tiles_kernel(const MatmulArgs p) {
+    constexpr int NW = WM * WN, TM = 32 * NJ * WM, TN = 32 * NI * WN, ROWS = TM + TN, HALF = BLOCK / 2;
+    constexpr int CP = ROWS / 16 / NW, SC = (ROWS / 64 + NW - 1) / NW;                    // copies of a wave per stage: codes, scales (every other one)
+    constexpr int CODES = ROWS * HALF, STAGE = CODES + NW * SC * 256, STEPS = WIDE ? 2 : 1;
+    static_assert(ROWS % (16 * NW) == 0 && ROWS % 64 == 0 && TN % 64 == 0 && NST % 2 == 0 && NST * (CP + SC) < 64 && NST * STAGE <= 160 * 1024, "copies of a stage");
     __shared__ __attribute__((aligned(16))) char lds[NST * STAGE];
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, g = lane >> 5;
@@ -111,48 +140,48 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NI * NJ > 4
     w -= split * p.tiles_m * p.tiles_n;
     const int band = w / (8 * p.tiles_n), deep = min(8, p.tiles_m - 8 * band), in = w - band * 8 * p.tiles_n;
     const int64_t m0 = (int64_t)(8 * band + in % deep) * TM, n0 = (int64_t)(in / deep) * TN;
-    const int kb0 = split * p.kb_per, kb1 = min(p.kb, kb0 + p.kb_per);
+    const int kb0 = split * p.kb_per, kb1 = min(p.kb, kb0 + p.kb_per), halves = 2 * (kb1 - kb0);
 
-    const int srow = lane >> 3, piece = (lane & 7) ^ srow;
-    const uint8_t *gb[2 * NI], *ga[2 * NJ], *gs[SC];
-#pragma unroll
-    for (int j = 0; j < 2 * NI; ++j) {
-        const int64_t r = n0 + 16 * NI * wave + 8 * j + srow;
-        gb[j] = p.b + (r < p.n ? r : 0) * p.b_ld + piece * 16;
-    }
-    auto source = [&](int64_t r) -> int64_t {
-        if (r >= p.m) return 0;
-        if (!p.rows) return r;
-        const int64_t s = p.rows[r];
-        return s >= 0 && s < p.a_rows ? s : 0;
+    // Row r of the stage: B's tile first, then A's.  Copy j of this wave takes rows 16 (CP wave + j) .. + 15
+    auto b_row = [&](int r) { const int64_t s = n0 + r; return s < p.n ? s : 0; };
+    auto a_row = [&](int r) -> int64_t {
+        const int64_t s = m0 + r;
+        if (s >= p.m) return 0;
+        if (!p.rows) return s;
+        const int64_t t = p.rows[s];
+        return t >= 0 && t < p.a_rows ? t : 0;
     };
+    const int srow = lane >> 2, piece = (lane & 3) ^ (lane >> 4);
+    const uint8_t *gc[CP], *gs[SC];
 #pragma unroll
-    for (int j = 0; j < 2 * NJ; ++j) ga[j] = p.a + source(m0 + 16 * NJ * wave + 8 * j + srow) * p.a_ld + piece * 16;
+    for (int j = 0; j < CP; ++j) {
+        const int r = 16 * (CP * wave + j);                                       // (uniform: sixteen rows are of one operand)
+        gc[j] = (r < TN ? p.b + b_row(r + srow) * p.b_ld : p.a + a_row(r - TN + srow) * p.a_ld) + piece * 16 + (int64_t)kb0 * BLOCK;
+    }
 #pragma unroll
     for (int j = 0; j < SC; ++j) {
-        const int q = wave * SC + j;                                              // 64 rows of B's, then of A's tile
-        if (q < NI) {
-            const int64_t r = n0 + 64 * q + lane;
-            gs[j] = p.bs + (r < p.n ? r : 0) * p.bs_ld;
-        } else gs[j] = p.as + source(m0 + 64 * (q - NI) + lane) * p.as_ld;
+        const int r = 64 * (SC * wave + j);                                       // (past the last row: row 0 again, to a place that nothing reads)
+        gs[j] = r < TN ? p.bs + b_row(r + lane) * p.bs_ld : r < ROWS ? p.as + a_row(r - TN + lane) * p.as_ld : p.bs;
     }
     // (the gathered row numbers have to be there before the loop: a wait of the compiler's inside it would drain the ring)
 #pragma unroll
-    for (int j = 0; j < 2 * NJ; ++j) asm volatile("" : "+v"(ga[j]));
+    for (int j = 0; j < CP; ++j) asm volatile("" : "+v"(gc[j]));
 #pragma unroll
     for (int j = 0; j < SC; ++j) asm volatile("" : "+v"(gs[j]));
 
-    auto issue = [&](int t, int slot) {                                           // block min(t, kb1 - 1) -> stage slot
-        const int kb = min(t, kb1 - 1);
+    int next = 0;                                                                 // half that the next copies fetch, and their pointers'
+    auto copy = [&](int slot, int c) {
         const uint32_t sb = lds0 + (uint32_t)slot * STAGE;
-#pragma unroll
-        for (int j = 0; j < 2 * NI; ++j) mq_copy16(gb[j] + (int64_t)kb * BLOCK, sb + (uint32_t)(16 * NI * wave + 8 * j) * BLOCK);
-#pragma unroll
-        for (int j = 0; j < 2 * NJ; ++j) mq_copy16(ga[j] + (int64_t)kb * BLOCK, sb + (uint32_t)(TN + 16 * NJ * wave + 8 * j) * BLOCK);
-#pragma unroll
-        for (int j = 0; j < SC; ++j) mq_copy4(gs[j] + (kb >> 2) * 4, sb + CODES + (uint32_t)(wave * SC + j) * 256);
+        if (c < CP) mq_copy16(gc[c], sb + (uint32_t)(CP * wave + c) * (16 * HALF));
+        else mq_copy4(gs[c - CP] + ((kb0 + (next >> 1)) >> 2) * 4, sb + CODES + (uint32_t)(SC * wave + c - CP) * 256);
     };
-    const int wn = (wave & 1) * 32 * NI, wm = (wave >> 1) * 32 * NJ;
+    auto advance = [&] {                                                          // past the end: the last two halves again, harmless
+        const int d = next + 1 < halves ? 1 : -1;
+        next += d;
+#pragma unroll
+        for (int j = 0; j < CP; ++j) gc[j] += d * HALF;
+    };
+    const int wn = (wave % WN) * 32 * NI, wm = (wave / WN) * 32 * NJ;
     mq_f32x16 acc[NI][NJ];
 #pragma unroll
     for (int i = 0; i < NI; ++i)
@@ -161,88 +190,158 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(NI * NJ > 4
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-    auto compute = [&](int slot, int kb) {
-        const char *sb = lds + slot * STAGE, *sa = sb + TN * BLOCK;
-        const uint32_t *sc = (const uint32_t *)(sb + CODES);
-        uint32_t eb[NI], ea[NJ];
+    constexpr int Q = WIDE ? 1 : 2;                                               // 16-byte pieces of a row that a lane reads per step
+    struct Frags { kge_u32x4 b[NI][Q], a[NJ][Q]; };
+    struct Scales { uint32_t b[NI], a[NJ]; };
+    constexpr int READS = (NI + NJ) * Q, SLOTS = NI * NJ * (WIDE ? 2 : 1);        // per step: fragment reads, products
+    const int swz = (lr >> 2) & 3;
+    auto read = [&](Frags &f, int slot, int step, int r) {
+        const char *s = lds + slot * STAGE;
+        const int u = r % Q, k = r / Q, c = ((WIDE ? 2 * step + g : 2 * g + u) ^ swz) << 4;
+        if (k < NI) f.b[k][u] = *(const kge_u32x4 *)(s + (wn + 32 * k + lr) * HALF + c);
+        else f.a[k - NI][u] = *(const kge_u32x4 *)(s + (TN + wm + 32 * (k - NI) + lr) * HALF + c);
+    };
+    auto read_scales = [&](Scales &x, int slot) {                                 // the words; use_scales takes block kb's bytes from them
+        const uint32_t *s = (const uint32_t *)(lds + slot * STAGE + CODES);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) eb[i] = (sc[wn + 32 * i + lr] >> (8 * (kb & 3))) & 255u;
+        for (int i = 0; i < NI; ++i) x.b[i] = s[wn + 32 * i + lr];
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) ea[j] = (sc[TN + wm + 32 * j + lr] >> (8 * (kb & 3))) & 255u;
-        auto read = [&](const char *s, int row, int c) { return *(const kge_u32x4 *)(s + row * BLOCK + ((c ^ (lr & 7)) << 4)); };
+        for (int j = 0; j < NJ; ++j) x.a[j] = s[TN + wm + 32 * j + lr];
+    };
+    auto use_scales = [&](Scales &x, const Scales &words, int kb) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) x.b[i] = words.b[i] >> (8 * (kb & 3)) & 255u;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) x.a[j] = words.a[j] >> (8 * (kb & 3)) & 255u;
+    };
+    // The products of one step; between them, at most one of each at a time, whatever `between` does at its slot.  (Left to itself the compiler puts all reads
+    // in front of all products, and those behind the barrier: a wave that is alone on its SIMD then does either.)
+    auto multiply = [&](const Frags &f, const Scales &x, auto between) {
         if constexpr (!WIDE) {
+            auto full = [](const kge_u32x4 (&q)[Q]) {
+                return mq_i32x8{(int)q[0][0], (int)q[0][1], (int)q[0][2], (int)q[0][3], (int)q[Q - 1][0], (int)q[Q - 1][1], (int)q[Q - 1][2], (int)q[Q - 1][3]};
+            };
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                mq_i32x8 fb[NI], fa[NJ];
-#pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    const kge_u32x4 x = read(sb, wn + 32 * i + lr, 4 * ks + 2 * g), y = read(sb, wn + 32 * i + lr, 4 * ks + 2 * g + 1);
-                    fb[i] = mq_i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
-                }
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    const kge_u32x4 x = read(sa, wm + 32 * j + lr, 4 * ks + 2 * g), y = read(sa, wm + 32 * j + lr, 4 * ks + 2 * g + 1);
-                    fa[j] = mq_i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
-                }
-#pragma unroll
-                for (int i = 0; i < NI; ++i)
-#pragma unroll
-                    for (int j = 0; j < NJ; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[i], fa[j], acc[i][j], FB, FA, 0, (int)eb[i], 0, (int)ea[j]);
+            for (int t = 0; t < SLOTS; ++t) {
+                const int i = t / NJ, j = t % NJ;
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(full(f.b[i]), full(f.a[j]), acc[i][j], FB, FA, 0, (int)x.b[i], 0, (int)x.a[j]);
+                between(t);
+                __builtin_amdgcn_sched_barrier(0);
             }
         } else {
+            mq_bf16x8 fb[NI][2], fa[NJ][2];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                mq_bf16x8 fb[NI][2], fa[NJ][2];
+            for (int i = 0; i < NI; ++i) {
+                const float sc = __uint_as_float(x.b[i] << 23);
+                fb[i][0] = mq_widen8<FB>(f.b[i][0][0], f.b[i][0][1], sc); fb[i][1] = mq_widen8<FB>(f.b[i][0][2], f.b[i][0][3], sc);
+            }
 #pragma unroll
-                for (int i = 0; i < NI; ++i) {
-                    const kge_u32x4 x = read(sb, wn + 32 * i + lr, 2 * q + g);
-                    fb[i][0] = mq_widen8<FB>(x[0], x[1], __uint_as_float(eb[i] << 23)); fb[i][1] = mq_widen8<FB>(x[2], x[3], __uint_as_float(eb[i] << 23));
-                }
+            for (int j = 0; j < NJ; ++j) {
+                const float sc = __uint_as_float(x.a[j] << 23);
+                fa[j][0] = mq_widen8<FA>(f.a[j][0][0], f.a[j][0][1], sc); fa[j][1] = mq_widen8<FA>(f.a[j][0][2], f.a[j][0][3], sc);
+            }
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) {
-                    const kge_u32x4 x = read(sa, wm + 32 * j + lr, 2 * q + g);
-                    fa[j][0] = mq_widen8<FA>(x[0], x[1], __uint_as_float(ea[j] << 23)); fa[j][1] = mq_widen8<FA>(x[2], x[3], __uint_as_float(ea[j] << 23));
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < NI; ++i)
-#pragma unroll
-                        for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[i][h], fa[j][h], acc[i][j], 0, 0, 0);
+            for (int t = 0; t < SLOTS; ++t) {
+                const int h = t / (NI * NJ), i = t / NJ % NI, j = t % NJ;
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[i][h], fa[j][h], acc[i][j], 0, 0, 0);
+                between(t);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
     };
 
     if (kb0 < kb1) {
-        for (int s = 0; s < NST - 1; ++s) issue(kb0 + s, s);
+#pragma unroll
+        for (int s = 0; s < NST; ++s) {
+#pragma unroll
+            for (int c = 0; c < (s % 2 == 0 ? CP + SC : CP); ++c) copy(s, c);
+            advance();
+        }
+        mq_wait_vmcnt<(NST - 1) * CP + (NST / 2 - 1) * SC>();
+        __syncthreads();
+        Frags f[2];
+        Scales x, words;
+#pragma unroll
+        for (int r = 0; r < READS; ++r) read(f[0], 0, 0, r);
+        read_scales(words, 0);
+        use_scales(x, words, kb0);
+        // reads go with the first two thirds of a step's products, so that the last ones cover their way; copies with all of them
+        constexpr int SPAN = SLOTS * 2 / 3 > 0 ? SLOTS * 2 / 3 : 1;
         int slot = 0;
         for (int kb = kb0; kb < kb1; ++kb) {
-            mq_wait_vmcnt<(NST - 2) * PER>();                                     // block kb has landed ...
-            __syncthreads();                                                      // ... for everyone, and everyone is done with block kb - 1,
-            issue(kb + NST - 1, slot == 0 ? NST - 1 : slot - 1);                  // whose stage is refilled (past the end: a harmless repeat)
-            compute(slot, kb);
-            slot = slot == NST - 1 ? 0 : slot + 1;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int after = slot == NST - 1 ? 0 : slot + 1, copies = half == 0 ? CP + SC : CP;
+#pragma unroll
+                for (int st = 0; st < STEPS; ++st) {
+                    const bool last = st == STEPS - 1;
+                    if (last) {
+                        mq_wait_vmcnt<(NST - 2) * CP + (NST / 2 - 1) * SC>();     // the next stage has landed ...
+                        __syncthreads();                                          // ... for everyone, and everyone has read this one, which is refilled
+                    }
+                    const int now = STEPS == 2 ? st : half;                       // (which of the two sets of fragments)
+                    multiply(f[now], x, [&](int t) {
+#pragma unroll
+                        for (int r = 0; r < READS; ++r)
+                            if (r * SPAN / READS == t) read(f[now ^ 1], last ? after : slot, last ? 0 : st + 1, r);
+                        if (last) {
+                            if (half == 1 && t == SPAN - 1) read_scales(words, after);
+#pragma unroll
+                            for (int c = 0; c < copies; ++c)
+                                if (c * SLOTS / copies == t) copy(slot, c);
+                        }
+                    });
+                    if (last) advance();
+                }
+                slot = after;
+            }
+            use_scales(x, words, kb + 1);
         }
         mq_wait_vmcnt<0>();                                                       // no copy may be in flight when the LDS is released
     }
 
-    // accumulator layout: lane holds row lr of A's block; element e is B's row 8 (e / 4) + 4 g + e % 4
+    // Accumulator layout: lane holds row lr of A's block; element e is B's row 8 (e / 4) + 4 g + e % 4.  Stored from there a row gets sixteen bytes at a
+    // time, a quarter of the copy rate and up to a third of the call; so 32 rows of the wave at a time go through the LDS, and rows leave in whole lines.
+    // (Row stride one piece more than the row: writes and reads of sixteen lanes fall into different banks.)
+    constexpr int LD = 32 * NI + 4;
+    static_assert(NW * 32 * LD * 4 <= NST * STAGE, "the waves' rows fit the ring");
+    float *mine = (float *)lds + wave * (32 * LD);
+    __syncthreads();                                                              // everyone is done with the ring
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-        const int64_t row = m0 + wm + 32 * j + lr;
-        if (row >= p.m) continue;
-        const bool valid = mq_row_valid(p, row);
 #pragma unroll
         for (int i = 0; i < NI; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t col = n0 + wn + 32 * i + 8 * q + 4 * g;
-                const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                if (p.part) {
-                    if (col < p.part_ld) *(kge_f32x4 *)(p.part + ((int64_t)split * p.m + row) * p.part_ld + col) = kge_f32x4{v[0], v[1], v[2], v[3]};
-                } else mq_store4(p, row, col, v, valid);
+            for (int q = 0; q < 4; ++q)
+                *(kge_f32x4 *)(mine + lr * LD + 32 * i + 8 * q + 4 * g) = kge_f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        __builtin_amdgcn_wave_barrier();
+        const int64_t row0 = m0 + wm + 32 * j, col0 = n0 + wn;
+        auto rows = [&](auto wide) {                                              // wide: eight columns per lane, else four
+            constexpr int C = decltype(wide)::value ? 8 : 4, LPR = 32 * NI / C, RPI = 64 / LPR;     // lanes per row, rows at a time
+            const int c = C * (lane % LPR);
+#pragma unroll
+            for (int r0 = 0; r0 < 32; r0 += RPI) {
+                const int r = r0 + lane / LPR;
+                const int64_t row = row0 + r;
+                float v[C];
+#pragma unroll
+                for (int e = 0; e < C; e += 4) {
+                    const kge_f32x4 x = *(const kge_f32x4 *)(mine + r * LD + c + e);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) v[e + u] = x[u];
+                }
+                if (row >= p.m) continue;
+                if constexpr (C == 4)
+                    if (p.part) {
+                        if (col0 + c < p.part_ld) *(kge_f32x4 *)(p.part + ((int64_t)split * p.m + row) * p.part_ld + col0 + c) = kge_f32x4{v[0], v[1], v[2], v[3]};
+                        continue;
+                    }
+                mq_store<C == 8>(p, row, col0 + c, v, mq_row_valid(p, row));
             }
+        };
+        if (p.part || !p.out16) rows(std::false_type());
+        else rows(std::true_type());
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -257,8 +356,7 @@ __global__ __launch_bounds__(256) void matmul_join_kernel(const MatmulArgs p) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[e] += x[e];
         }
-        const float v[4] = {s[0], s[1], s[2], s[3]};
-        mq_store4(p, row, col, v, mq_row_valid(p, row));
+        mq_store4(p, row, col, s, mq_row_valid(p, row));
     }
 }
 
@@ -326,14 +424,19 @@ __global__ __launch_bounds__(64 * SKINNY_WAVES) void matmul_skinny_kernel(const 
         }
         const int64_t r = 16 * f + row;
         if (r >= p.m) continue;
-        const float v[4] = {s[0], s[1], s[2], s[3]};
-        mq_store4(p, r, n0 + c, v, mq_row_valid(p, r));
+        mq_store4(p, r, n0 + c, s, mq_row_valid(p, r));
     }
 }
 
 // ---------------------------------------------------------------------------------------------
 constexpr int SKINNY_ROWS = 64;
-constexpr int64_t WANTED = 512;                                // workgroups that a launch of 128 x 128 tiles aims at: two per compute unit
+constexpr int64_t WANTED = 512;                                // workgroups that a launch of the smaller tiles aims at
+
+// Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B, and stages
+struct Tile { int wm, wn, nj, ni, nst; };
+constexpr Tile BIG = {2, 4, 4, 2, 4}, MID = {2, 2, 2, 2, 4};
+constexpr int tile_m(const Tile &t) { return 32 * t.wm * t.nj; }
+constexpr int tile_n(const Tile &t) { return 32 * t.wn * t.ni; }
 
 struct Plan { int skinny, big, tiles_m, tiles_n, splits, kb_per; int64_t part_ld, part_bytes; };
 
@@ -342,11 +445,11 @@ Plan make_plan(int64_t m, int64_t n, int64_t k, size_t room) {
     const int64_t kb = (k + BLOCK - 1) / BLOCK;
     q.splits = 1; q.kb_per = (int)kb;
     if (m <= SKINNY_ROWS) { q.skinny = 1; return q; }
-    const int64_t big = ((m + 255) / 256) * ((n + 255) / 256);
-    q.big = big >= 256;
-    const int64_t tile = q.big ? 256 : 128;
-    q.tiles_m = (int)((m + tile - 1) / tile); q.tiles_n = (int)((n + tile - 1) / tile);
-    const int64_t tiles = (int64_t)q.tiles_m * q.tiles_n;
+    auto tiles_of = [&](const Tile &t, int64_t &tm, int64_t &tn) { tm = (m + tile_m(t) - 1) / tile_m(t); tn = (n + tile_n(t) - 1) / tile_n(t); return tm * tn; };
+    int64_t tm, tn, tiles = tiles_of(BIG, tm, tn);
+    q.big = tiles >= 256;
+    if (!q.big) tiles = tiles_of(MID, tm, tn);
+    q.tiles_m = (int)tm; q.tiles_n = (int)tn;
     q.part_ld = (n + 3) / 4 * 4;
     if (!q.big && tiles * 2 <= WANTED && kb >= 16) {
         int64_t s = WANTED / tiles;
@@ -371,8 +474,8 @@ template <bool WIDE, int FA, int FB> void launch(const MatmulArgs &p, const Plan
         return;
     }
     const dim3 grid((unsigned)((p.tiles_m * p.tiles_n * p.splits + 7) / 8 * 8));
-    if (q.big) hipLaunchKernelGGL((matmul_tiles_kernel<4, 4, 2, WIDE, FA, FB>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((matmul_tiles_kernel<2, 2, 2, WIDE, FA, FB>), grid, dim3(256), 0, st, p);
+    if (q.big) hipLaunchKernelGGL((matmul_tiles_kernel<BIG.wm, BIG.wn, BIG.nj, BIG.ni, BIG.nst, WIDE, FA, FB>), grid, dim3(64 * BIG.wm * BIG.wn), 0, st, p);
+    else hipLaunchKernelGGL((matmul_tiles_kernel<MID.wm, MID.wn, MID.nj, MID.ni, MID.nst, WIDE, FA, FB>), grid, dim3(64 * MID.wm * MID.wn), 0, st, p);
     if (p.part) {
         const int64_t blocks = (p.m * (p.part_ld / 4) + 255) / 256;
         hipLaunchKernelGGL(matmul_join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, p);
