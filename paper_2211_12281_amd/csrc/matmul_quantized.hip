@@ -23,6 +23,23 @@ namespace {
 
 constexpr int BLOCK = 128;                                    // elements of a scale's block, and bytes of a row that a stage holds
 
+// acc + u v^t with the scales in byte i of sb and byte j of sa; i and j are known when this is inlined into unrolled loops
+template <int FU, int FV, int I, int J> __device__ __forceinline__ mq_f32x16 mq_mma_ij(mq_i32x8 u, mq_i32x8 v, mq_f32x16 acc, int sb, int sa) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(u, v, acc, FU, FV, I, sb, J, sa);
+}
+template <int FU, int FV> __device__ __forceinline__ mq_f32x16 mq_mma(mq_i32x8 u, mq_i32x8 v, mq_f32x16 acc, int i, int j, int sb, int sa) {
+    switch (4 * i + j) {
+    case 0: return mq_mma_ij<FU, FV, 0, 0>(u, v, acc, sb, sa);
+    case 1: return mq_mma_ij<FU, FV, 0, 1>(u, v, acc, sb, sa);
+    case 2: return mq_mma_ij<FU, FV, 0, 2>(u, v, acc, sb, sa);
+    case 3: return mq_mma_ij<FU, FV, 0, 3>(u, v, acc, sb, sa);
+    case 4: return mq_mma_ij<FU, FV, 1, 0>(u, v, acc, sb, sa);
+    case 5: return mq_mma_ij<FU, FV, 1, 1>(u, v, acc, sb, sa);
+    case 6: return mq_mma_ij<FU, FV, 1, 2>(u, v, acc, sb, sa);
+    default: return mq_mma_ij<FU, FV, 1, 3>(u, v, acc, sb, sa);
+    }
+}
+
 struct MatmulArgs {
     const uint8_t *a, *as; int64_t a_ld, as_ld; const int32_t *rows; int64_t a_rows;
     const uint8_t *b, *bs; int64_t b_ld, bs_ld;
@@ -38,6 +55,13 @@ __device__ __forceinline__ void mq_copy16(const void *g, uint32_t lds) {
 }
 __device__ __forceinline__ void mq_copy4(const void *g, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(g) : "memory");
+}
+// the same from base + a 32-bit offset of each lane
+__device__ __forceinline__ void mq_copy16(const uint8_t *base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void mq_copy4(const uint8_t *base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }
 template <int N> __device__ __forceinline__ void mq_wait_vmcnt() {
     static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
@@ -114,22 +138,26 @@ __device__ __forceinline__ bool mq_row_valid(const MatmulArgs &p, int64_t row) {
     return r >= 0 && r < p.a_rows;
 }
 
-// Workgroup = WM x WN waves = TM rows of A x TN rows of B, wave = NJ x NI blocks of 32 x 32.  Stages of 64 bytes of every row (half a
-// block; with the first half the word of every row's scales that holds the block's byte) pass through a ring of NST stages in the LDS, filled by asynchronous
-// copies.  A row's four 16-byte pieces lie XOR-swizzled by (row / 4) % 4: the fragment reads of sixteen consecutive rows then fall into
-// different ones of the 64 banks.  Rows beyond the matrices are read from row 0 and
-// not stored.  Which bytes of a stage a lane half contracts first does not matter as long as both operands agree.
+// Workgroup = WM x WN waves = TM rows of A x TN rows of B, wave = NJ x NI blocks of 32 x 32.  Stages of a block of 128 bytes of every row pass through a
+// ring of NST stages in the LDS, filled by asynchronous copies (whole lines: with half of one per row and copy they ran at half the rate, 65 instead
+// of 136 GB/s per compute unit from the L2); the words with four blocks' scales of every row come with the first block that needs them, into one of two
+// places.  A row's 16-byte pieces lie XOR-swizzled by (row / 2) % 8, so that the fragment reads of sixteen consecutive rows fall into different ones of
+// the 64 banks.  Rows beyond the matrices are read from row 0 and
+// not stored.  Which bytes of a block a lane half contracts first does not matter as long as both operands agree.
 //
 // The fragments of the next step are read while this one's are multiplied, across the stages too: the only barrier of a stage stands in front of the
 // products of its last step, whose operands are in registers by then, and the stage that it frees is refilled behind it.
-template <int WM, int WN, int NJ, int NI, int NST, bool WIDE, int FA, int FB>
+//
+// FAR: a copy's lanes have 64-bit addresses; else (matrices of less than 4 GiB) a base and 32-bit offsets, which the larger wave tile needs for its registers.
+template <int WM, int WN, int NJ, int NI, int NST, bool FAR, bool WIDE, int FA, int FB>
 __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(NI * NJ > 8 ? 1 : 2, NI * NJ > 8 ? 1 : 2)))
 void matmul_tiles_kernel(const MatmulArgs p) {
-    constexpr int NW = WM * WN, TM = 32 * NJ * WM, TN = 32 * NI * WN, ROWS = TM + TN, HALF = BLOCK / 2;
-    constexpr int CP = ROWS / 16 / NW, SC = (ROWS / 64 + NW - 1) / NW;                    // copies of a wave per stage: codes, scales (every other one)
-    constexpr int CODES = ROWS * HALF, STAGE = CODES + NW * SC * 256, STEPS = WIDE ? 2 : 1;
-    static_assert(ROWS % (16 * NW) == 0 && ROWS % 64 == 0 && TN % 64 == 0 && NST % 2 == 0 && NST * (CP + SC) < 64 && NST * STAGE <= 160 * 1024, "copies of a stage");
-    __shared__ __attribute__((aligned(16))) char lds[NST * STAGE];
+    constexpr int NW = WM * WN, TM = 32 * NJ * WM, TN = 32 * NI * WN, ROWS = TM + TN;
+    constexpr int CP = ROWS / 8 / NW, SC = (ROWS / 64 + NW - 1) / NW, PER = CP + SC;      // copies of a wave per stage: codes, scales
+    constexpr int STAGE = ROWS * BLOCK, WORDS = NW * SC * 256, STEPS = WIDE ? 4 : 2;
+    static_assert(ROWS % (8 * NW) == 0 && ROWS % 64 == 0 && TN % 64 == 0 && NST >= 2, "tile");
+    static_assert((NST - 1) * PER < 64 && NST * STAGE + 3 * WORDS <= 160 * 1024, "copies in flight, LDS");
+    __shared__ __attribute__((aligned(16))) char lds[NST * STAGE + 3 * WORDS];           // (the third place of the words: nothing reads it)
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, g = lane >> 5;
     // ids go round-robin to the 8 dies: a die takes a run of tiles, eight tiles of A deep, so that both operands' rows meet in its L2
@@ -140,9 +168,9 @@ void matmul_tiles_kernel(const MatmulArgs p) {
     w -= split * p.tiles_m * p.tiles_n;
     const int band = w / (8 * p.tiles_n), deep = min(8, p.tiles_m - 8 * band), in = w - band * 8 * p.tiles_n;
     const int64_t m0 = (int64_t)(8 * band + in % deep) * TM, n0 = (int64_t)(in / deep) * TN;
-    const int kb0 = split * p.kb_per, kb1 = min(p.kb, kb0 + p.kb_per), halves = 2 * (kb1 - kb0);
+    const int kb0 = split * p.kb_per, kb1 = min(p.kb, kb0 + p.kb_per);
 
-    // Row r of the stage: B's tile first, then A's.  Copy j of this wave takes rows 16 (CP wave + j) .. + 15
+    // Row r of the stage: B's tile first, then A's.  Copy j of this wave takes rows 8 (CP wave + j) .. + 7
     auto b_row = [&](int r) { const int64_t s = n0 + r; return s < p.n ? s : 0; };
     auto a_row = [&](int r) -> int64_t {
         const int64_t s = m0 + r;
@@ -151,35 +179,63 @@ void matmul_tiles_kernel(const MatmulArgs p) {
         const int64_t t = p.rows[s];
         return t >= 0 && t < p.a_rows ? t : 0;
     };
-    const int srow = lane >> 2, piece = (lane & 3) ^ (lane >> 4);
-    const uint8_t *gc[CP], *gs[SC];
+    auto swizzle = [](int r) { return (r >> 1) & 7; };
+    static_assert(FAR || (TN % 64 == 0 && SC == 1 && CP == 8), "all rows that a wave copies are of one operand");
+    const bool of_b = 64 * wave < TN;                                              // (not FAR)
+    const uint8_t *base = of_b ? p.b : p.a, *sbase = of_b ? p.bs : p.as;
+    const uint8_t *gc[FAR ? CP : 1], *gs[FAR ? SC : 1];
+    uint32_t oc[FAR ? 1 : CP], os = 0;
 #pragma unroll
     for (int j = 0; j < CP; ++j) {
-        const int r = 16 * (CP * wave + j);                                       // (uniform: sixteen rows are of one operand)
-        gc[j] = (r < TN ? p.b + b_row(r + srow) * p.b_ld : p.a + a_row(r - TN + srow) * p.a_ld) + piece * 16 + (int64_t)kb0 * BLOCK;
+        const int r0 = 8 * (CP * wave + j), r = r0 + (lane >> 3), piece = ((lane & 7) ^ swizzle(r)) * 16;
+        if constexpr (FAR) gc[j] = (r0 < TN ? p.b + b_row(r) * p.b_ld : p.a + a_row(r - TN) * p.a_ld) + piece + (int64_t)kb0 * BLOCK;   // (a copy's rows are of one operand)
+        else oc[j] = (uint32_t)(of_b ? b_row(r) * p.b_ld : a_row(r - TN) * p.a_ld) + piece;
     }
+    if constexpr (!FAR) {
+        base += (int64_t)kb0 * BLOCK;
+        const int r = 64 * wave + lane;
+        os = (uint32_t)(of_b ? b_row(r) * p.bs_ld : a_row(r - TN) * p.as_ld);
+    } else {
 #pragma unroll
-    for (int j = 0; j < SC; ++j) {
-        const int r = 64 * (SC * wave + j);                                       // (past the last row: row 0 again, to a place that nothing reads)
-        gs[j] = r < TN ? p.bs + b_row(r + lane) * p.bs_ld : r < ROWS ? p.as + a_row(r - TN + lane) * p.as_ld : p.bs;
+        for (int j = 0; j < SC; ++j) {
+            const int r = 64 * (SC * wave + j);                                   // (past the last row: row 0 again, to a place that nothing reads)
+            gs[j] = r < TN ? p.bs + b_row(r + lane) * p.bs_ld : r < ROWS ? p.as + a_row(r - TN + lane) * p.as_ld : p.bs;
+        }
     }
     // (the gathered row numbers have to be there before the loop: a wait of the compiler's inside it would drain the ring)
 #pragma unroll
-    for (int j = 0; j < CP; ++j) asm volatile("" : "+v"(gc[j]));
+    for (int j = 0; j < CP; ++j) {
+        if constexpr (FAR) asm volatile("" : "+v"(gc[j]));
+        else asm volatile("" : "+v"(oc[j]));
+    }
+    if constexpr (FAR) {
 #pragma unroll
-    for (int j = 0; j < SC; ++j) asm volatile("" : "+v"(gs[j]));
+        for (int j = 0; j < SC; ++j) asm volatile("" : "+v"(gs[j]));
+    } else asm volatile("" : "+v"(os));
 
-    int next = 0;                                                                 // half that the next copies fetch, and their pointers'
+    int next = kb0;                                                               // block that the next copies fetch, and their addresses'
     auto copy = [&](int slot, int c) {
-        const uint32_t sb = lds0 + (uint32_t)slot * STAGE;
-        if (c < CP) mq_copy16(gc[c], sb + (uint32_t)(CP * wave + c) * (16 * HALF));
-        else mq_copy4(gs[c - CP] + ((kb0 + (next >> 1)) >> 2) * 4, sb + CODES + (uint32_t)(SC * wave + c - CP) * 256);
+        if (c >= SC) {
+            const uint32_t to = lds0 + (uint32_t)slot * STAGE + (uint32_t)(CP * wave + c - SC) * 1024;
+            if constexpr (FAR) mq_copy16(gc[c - SC], to);
+            else mq_copy16(base, oc[c - SC], to);
+        } else {
+            // scales first.  Where the word has been copied before, all lanes take one address and write to the third place: no branch, which would
+            // take the products of the step before behind the barrier, and no lines fetched again
+            const bool need = (next & 3) == 0 || next == kb0;
+            const uint32_t to = lds0 + NST * STAGE + (need ? (uint32_t)(next >> 2 & 1) : 2u) * WORDS + (uint32_t)(SC * wave + c) * 256;
+            const int off = (next >> 2) * 4;
+            if constexpr (FAR) mq_copy4((need ? gs[c] : p.bs) + off, to);
+            else mq_copy4(sbase + off, os & (need ? 0xffffffffu : 0u), to);
+        }
     };
-    auto advance = [&] {                                                          // past the end: the last two halves again, harmless
-        const int d = next + 1 < halves ? 1 : -1;
+    auto advance = [&] {                                                          // past the end: the last block again, harmless
+        const int d = next + 1 < kb1 ? 1 : 0;
         next += d;
+        if constexpr (FAR) {
 #pragma unroll
-        for (int j = 0; j < CP; ++j) gc[j] += d * HALF;
+            for (int j = 0; j < CP; ++j) gc[j] += d * BLOCK;
+        } else base += d * BLOCK;
     };
     const int wn = (wave % WN) * 32 * NI, wm = (wave / WN) * 32 * NJ;
     mq_f32x16 acc[NI][NJ];
@@ -190,63 +246,85 @@ void matmul_tiles_kernel(const MatmulArgs p) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
+    // Fragments of the operands.  Of the codes, the last block of A and all of B have two places each, for this step's and the next one's; the other blocks of A are
+    // read again as soon as their last product of the step has been issued.  Widened codes (WIDE) leave their place at once: every block has one; of the
+    // widened ones, B and the first block of A have two places (made behind the last products of the step before), the other blocks of A take turns in two.
     constexpr int Q = WIDE ? 1 : 2;                                               // 16-byte pieces of a row that a lane reads per step
-    struct Frags { kge_u32x4 b[NI][Q], a[NJ][Q]; };
-    struct Scales { uint32_t b[NI], a[NJ]; };
-    constexpr int READS = (NI + NJ) * Q, SLOTS = NI * NJ * (WIDE ? 2 : 1);        // per step: fragment reads, products
-    const int swz = (lr >> 2) & 3;
-    auto read = [&](Frags &f, int slot, int step, int r) {
-        const char *s = lds + slot * STAGE;
-        const int u = r % Q, k = r / Q, c = ((WIDE ? 2 * step + g : 2 * g + u) ^ swz) << 4;
-        if (k < NI) f.b[k][u] = *(const kge_u32x4 *)(s + (wn + 32 * k + lr) * HALF + c);
-        else f.a[k - NI][u] = *(const kge_u32x4 *)(s + (TN + wm + 32 * (k - NI) + lr) * HALF + c);
+    struct Codes { kge_u32x4 b[WIDE ? 1 : 2][NI][Q], a[NJ - 1][Q], l[WIDE ? 1 : 2][Q]; } f;
+    struct Wide { mq_bf16x8 b[2][NI][2], a0[2][2], a[2][2]; } v;
+    struct Words { uint32_t b[NI], a[NJ]; } words;                                // of the rows, as copied
+    uint32_t xb, xa;                                                              // the block's byte of each of the wave's blocks of rows
+    constexpr int SLOTS = NI * NJ * (WIDE ? 2 : 1);                               // products per step
+    const int swz = swizzle(lr);
+    auto read = [&](kge_u32x4 (&to)[Q], int slot, int step, int row) {
+        const char *s = lds + slot * STAGE + (row + lr) * BLOCK;
+#pragma unroll
+        for (int u = 0; u < Q; ++u) to[u] = *(const kge_u32x4 *)(s + (((WIDE ? 2 * step + g : 4 * step + 2 * g + u) ^ swz) << 4));
     };
-    auto read_scales = [&](Scales &x, int slot) {                                 // the words; use_scales takes block kb's bytes from them
-        const uint32_t *s = (const uint32_t *)(lds + slot * STAGE + CODES);
+    auto read_b = [&](int set, int i, int slot, int step) { read(f.b[WIDE ? 0 : set][i], slot, step, wn + 32 * i); };
+    auto read_a = [&](int set, int j, int slot, int step) { read(j < NJ - 1 ? f.a[j < NJ - 1 ? j : 0] : f.l[WIDE ? 0 : set], slot, step, TN + wm + 32 * j); };
+    auto read_scales = [&](int kb) {                                              // the words; use_scales takes block kb's bytes from them
+        const uint32_t *s = (const uint32_t *)(lds + NST * STAGE + (kb >> 2 & 1) * WORDS);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) x.b[i] = s[wn + 32 * i + lr];
+        for (int i = 0; i < NI; ++i) words.b[i] = s[wn + 32 * i + lr];
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) x.a[j] = s[TN + wm + 32 * j + lr];
+        for (int j = 0; j < NJ; ++j) words.a[j] = s[TN + wm + 32 * j + lr];
     };
-    auto use_scales = [&](Scales &x, const Scales &words, int kb) {
-#pragma unroll
-        for (int i = 0; i < NI; ++i) x.b[i] = words.b[i] >> (8 * (kb & 3)) & 255u;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) x.a[j] = words.a[j] >> (8 * (kb & 3)) & 255u;
+    auto use_scales = [&](int kb) {
+        auto pack = [&](const uint32_t *w, int n) {                               // byte kb % 4 of up to four words
+            const uint32_t pick = 0x0c0c0400u + 0x0101u * (kb & 3);               // (of a pair; 0x0c: a zero byte)
+            const uint32_t lo = __builtin_amdgcn_perm(w[1], w[0], pick);
+            return n > 2 ? lo | __builtin_amdgcn_perm(w[n - 1], w[n - 2], pick) << 16 : lo;
+        };
+        xb = pack(words.b, NI);
+        xa = pack(words.a, NJ);
     };
-    // The products of one step; between them, at most one of each at a time, whatever `between` does at its slot.  (Left to itself the compiler puts all reads
-    // in front of all products, and those behind the barrier: a wave that is alone on its SIMD then does either.)
-    auto multiply = [&](const Frags &f, const Scales &x, auto between) {
-        if constexpr (!WIDE) {
-            auto full = [](const kge_u32x4 (&q)[Q]) {
-                return mq_i32x8{(int)q[0][0], (int)q[0][1], (int)q[0][2], (int)q[0][3], (int)q[Q - 1][0], (int)q[Q - 1][1], (int)q[Q - 1][2], (int)q[Q - 1][3]};
-            };
+    static_assert(NI == 2 && (NJ == 2 || NJ == 4), "pairs");
+    auto widen_b = [&](int set, int i, int h) {
+        const kge_u32x4 &q = f.b[0][i][0];
+        v.b[set][i][h] = mq_widen8<FB>(q[2 * h], q[2 * h + 1], __uint_as_float((xb >> (8 * i) & 255u) << 23));
+    };
+    auto widen_a = [&](int set, int j, int h) {
+        const kge_u32x4 &q = j < NJ - 1 ? f.a[j < NJ - 1 ? j : 0][0] : f.l[0][0];
+        const mq_bf16x8 w = mq_widen8<FA>(q[2 * h], q[2 * h + 1], __uint_as_float((xa >> (8 * j) & 255u) << 23));
+        if (j == 0) v.a0[set][h] = w;
+        else v.a[j & 1][h] = w;
+    };
+    // The products of one step and, behind each of them, the reads of the next step's fragments that have their slot there, and whatever `also` does.  (Left to
+    // itself the compiler puts all reads in front of all products, and those behind the barrier.)
+    auto step = [&](int set, int slot, int st, auto also) {                       // slot, st: of the next step
 #pragma unroll
-            for (int t = 0; t < SLOTS; ++t) {
-                const int i = t / NJ, j = t % NJ;
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(full(f.b[i]), full(f.a[j]), acc[i][j], FB, FA, 0, (int)x.b[i], 0, (int)x.a[j]);
-                between(t);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {
-            mq_bf16x8 fb[NI][2], fa[NJ][2];
+        for (int t = 0; t < SLOTS; ++t) {
+            if constexpr (WIDE) {
+                const int j = t / (2 * NI), h = t / NI % 2, i = t % NI, u = t % (2 * NI);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.b[set][i][h], j == 0 ? v.a0[set][h] : v.a[j & 1][h], acc[i][j], 0, 0, 0);
+                also(t);
+                // the next block of A is widened behind the first products of this one, the next step's B and first block of A behind the step's last
+                if (j < NJ - 1 && u < 2) widen_a(set, j + 1, u);
+                if (j == NJ - 1) {
+                    widen_b(set ^ 1, u / 2, u % 2);
+                    if (u < 2) widen_a(set ^ 1, 0, u);
+                }
+                if (t < NI) read_b(set ^ 1, t, slot, st);
+                if (t == NI) read_a(set ^ 1, 0, slot, st);
+                if (j < NJ - 1 && u == 3) read_a(set ^ 1, j + 1, slot, st);
+            } else {
+                const int j = t / NI, i = t % NI;
+                auto full = [](const kge_u32x4 (&q)[Q]) {
+                    return mq_i32x8{(int)q[0][0], (int)q[0][1], (int)q[0][2], (int)q[0][3], (int)q[Q - 1][0], (int)q[Q - 1][1], (int)q[Q - 1][2], (int)q[Q - 1][3]};
+                };
+                // (which byte of a scale register counts is part of the instruction)
+                acc[i][j] = mq_mma<FB, FA>(full(f.b[set][i]), full(j < NJ - 1 ? f.a[j < NJ - 1 ? j : 0] : f.l[set]), acc[i][j], i, j, (int)xb, (int)xa);
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const float sc = __uint_as_float(x.b[i] << 23);
-                fb[i][0] = mq_widen8<FB>(f.b[i][0][0], f.b[i][0][1], sc); fb[i][1] = mq_widen8<FB>(f.b[i][0][2], f.b[i][0][3], sc);
-            }
+                for (int k = 0; k < NI; ++k)
+                    if (t == k * NJ / 2) read_b(set ^ 1, k, slot, st);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const float sc = __uint_as_float(x.a[j] << 23);
-                fa[j][0] = mq_widen8<FA>(f.a[j][0][0], f.a[j][0][1], sc); fa[j][1] = mq_widen8<FA>(f.a[j][0][2], f.a[j][0][3], sc);
+                for (int k = 0; k < NJ - 1; ++k)
+                    if (t == NI * (k + 1) - 1) read_a(set ^ 1, k, slot, st);
+                if (t == NI * NJ / 2) read_a(set ^ 1, NJ - 1, slot, st);
+                also(t);
             }
-#pragma unroll
-            for (int t = 0; t < SLOTS; ++t) {
-                const int h = t / (NI * NJ), i = t / NJ % NI, j = t % NJ;
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[i][h], fa[j][h], acc[i][j], 0, 0, 0);
-                between(t);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
@@ -254,48 +332,49 @@ void matmul_tiles_kernel(const MatmulArgs p) {
 #pragma unroll
         for (int s = 0; s < NST; ++s) {
 #pragma unroll
-            for (int c = 0; c < (s % 2 == 0 ? CP + SC : CP); ++c) copy(s, c);
+            for (int c = 0; c < PER; ++c) copy(s, c);
             advance();
         }
-        mq_wait_vmcnt<(NST - 1) * CP + (NST / 2 - 1) * SC>();
+        mq_wait_vmcnt<(NST - 1) * PER>();
         __syncthreads();
-        Frags f[2];
-        Scales x, words;
 #pragma unroll
-        for (int r = 0; r < READS; ++r) read(f[0], 0, 0, r);
-        read_scales(words, 0);
-        use_scales(x, words, kb0);
-        // reads go with the first two thirds of a step's products, so that the last ones cover their way; copies with all of them
-        constexpr int SPAN = SLOTS * 2 / 3 > 0 ? SLOTS * 2 / 3 : 1;
+        for (int i = 0; i < NI; ++i) read_b(0, i, 0, 0);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) read_a(0, j, 0, 0);
+        read_scales(kb0);
+        use_scales(kb0);
+        if constexpr (WIDE) {                                                     // what the step before the first one would have left
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < NI; ++i) widen_b(0, i, h);
+                widen_a(0, 0, h);
+            }
+        }
+        // the next block's scales are used behind the step's products, or where its first fragments are widened
+        constexpr int READ_SCALES = WIDE ? 1 : SLOTS - 2, USE_SCALES = WIDE ? SLOTS - 2 * NI - 1 : SLOTS - 1;
         int slot = 0;
         for (int kb = kb0; kb < kb1; ++kb) {
+            const int after = slot == NST - 1 ? 0 : slot + 1;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int after = slot == NST - 1 ? 0 : slot + 1, copies = half == 0 ? CP + SC : CP;
-#pragma unroll
-                for (int st = 0; st < STEPS; ++st) {
-                    const bool last = st == STEPS - 1;
-                    if (last) {
-                        mq_wait_vmcnt<(NST - 2) * CP + (NST / 2 - 1) * SC>();     // the next stage has landed ...
-                        __syncthreads();                                          // ... for everyone, and everyone has read this one, which is refilled
-                    }
-                    const int now = STEPS == 2 ? st : half;                       // (which of the two sets of fragments)
-                    multiply(f[now], x, [&](int t) {
-#pragma unroll
-                        for (int r = 0; r < READS; ++r)
-                            if (r * SPAN / READS == t) read(f[now ^ 1], last ? after : slot, last ? 0 : st + 1, r);
-                        if (last) {
-                            if (half == 1 && t == SPAN - 1) read_scales(words, after);
-#pragma unroll
-                            for (int c = 0; c < copies; ++c)
-                                if (c * SLOTS / copies == t) copy(slot, c);
-                        }
-                    });
-                    if (last) advance();
+            for (int st = 0; st < STEPS; ++st) {
+                const bool last = st == STEPS - 1;
+                if (last) {
+                    mq_wait_vmcnt<(NST - 2) * PER>();                             // the next block has landed ...
+                    __syncthreads();                                              // ... for everyone, and everyone has read this one, whose stage is refilled
                 }
-                slot = after;
+                step(st & 1, last ? after : slot, last ? 0 : st + 1, [&](int t) {
+                    if (!last) return;
+                    if (t == READ_SCALES) read_scales(kb + 1);
+                    if (WIDE && t == USE_SCALES) use_scales(kb + 1);
+#pragma unroll
+                    for (int c = 0; c < PER; ++c)
+                        if (c * SLOTS / PER == t) copy(slot, c);
+                });
             }
-            use_scales(x, words, kb + 1);
+            if constexpr (!WIDE) use_scales(kb + 1);
+            advance();
+            slot = after;
         }
         mq_wait_vmcnt<0>();                                                       // no copy may be in flight when the LDS is released
     }
@@ -432,26 +511,26 @@ __global__ __launch_bounds__(64 * SKINNY_WAVES) void matmul_skinny_kernel(const 
 constexpr int SKINNY_ROWS = 64;
 constexpr int64_t WANTED = 512;                                // workgroups that a launch of the smaller tiles aims at
 
-// Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B, and stages
-struct Tile { int wm, wn, nj, ni, nst; };
-constexpr Tile BIG = {2, 4, 4, 2, 4}, MID = {2, 2, 2, 2, 4};
+// Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B; stages; whether matrices may be 4 GiB and more
+struct Tile { int wm, wn, nj, ni, nst; bool far; };
+constexpr Tile BIG = {2, 4, 4, 2, 2, false}, MID = {2, 2, 2, 2, 2, true};
 constexpr int tile_m(const Tile &t) { return 32 * t.wm * t.nj; }
 constexpr int tile_n(const Tile &t) { return 32 * t.wn * t.ni; }
 
 struct Plan { int skinny, big, tiles_m, tiles_n, splits, kb_per; int64_t part_ld, part_bytes; };
 
-Plan make_plan(int64_t m, int64_t n, int64_t k, size_t room) {
+Plan make_plan(int64_t m, int64_t n, int64_t k, size_t room, bool far = false) {
     Plan q = {};
     const int64_t kb = (k + BLOCK - 1) / BLOCK;
     q.splits = 1; q.kb_per = (int)kb;
     if (m <= SKINNY_ROWS) { q.skinny = 1; return q; }
     auto tiles_of = [&](const Tile &t, int64_t &tm, int64_t &tn) { tm = (m + tile_m(t) - 1) / tile_m(t); tn = (n + tile_n(t) - 1) / tile_n(t); return tm * tn; };
     int64_t tm, tn, tiles = tiles_of(BIG, tm, tn);
-    q.big = tiles >= 256;
+    q.big = tiles >= 256 && !far;
     if (!q.big) tiles = tiles_of(MID, tm, tn);
     q.tiles_m = (int)tm; q.tiles_n = (int)tn;
     q.part_ld = (n + 3) / 4 * 4;
-    if (!q.big && tiles * 2 <= WANTED && kb >= 16) {
+    if (!q.big && tiles * 4 <= WANTED && kb >= 16) {
         int64_t s = WANTED / tiles;
         if (s > kb / 8) s = kb / 8;                            // a split of at least eight blocks
         const int64_t one = m * q.part_ld * 4;
@@ -474,8 +553,8 @@ template <bool WIDE, int FA, int FB> void launch(const MatmulArgs &p, const Plan
         return;
     }
     const dim3 grid((unsigned)((p.tiles_m * p.tiles_n * p.splits + 7) / 8 * 8));
-    if (q.big) hipLaunchKernelGGL((matmul_tiles_kernel<BIG.wm, BIG.wn, BIG.nj, BIG.ni, BIG.nst, WIDE, FA, FB>), grid, dim3(64 * BIG.wm * BIG.wn), 0, st, p);
-    else hipLaunchKernelGGL((matmul_tiles_kernel<MID.wm, MID.wn, MID.nj, MID.ni, MID.nst, WIDE, FA, FB>), grid, dim3(64 * MID.wm * MID.wn), 0, st, p);
+    if (q.big) hipLaunchKernelGGL((matmul_tiles_kernel<BIG.wm, BIG.wn, BIG.nj, BIG.ni, BIG.nst, BIG.far, WIDE, FA, FB>), grid, dim3(64 * BIG.wm * BIG.wn), 0, st, p);
+    else hipLaunchKernelGGL((matmul_tiles_kernel<MID.wm, MID.wn, MID.nj, MID.ni, MID.nst, MID.far, WIDE, FA, FB>), grid, dim3(64 * MID.wm * MID.wn), 0, st, p);
     if (p.part) {
         const int64_t blocks = (p.m * (p.part_ld / 4) + 255) / 256;
         hipLaunchKernelGGL(matmul_join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, p);
@@ -503,7 +582,8 @@ int kge_matmul_quantized(const kge_quantized_t *a, const int32_t *rows, int64_t 
     p.m = m; p.n = b->rows; p.out = out; p.out_ld = out_ld; p.out16 = out_dtype == KGE_BF16; p.accumulate = accumulate;
     const int64_t k = a->rows > 0 ? a->cols : 0;               // (a table without rows: nothing may be read, every row of the result is zeros)
     const size_t lost = ws ? (256 - ((uintptr_t)ws & 255)) & 255 : 0;
-    const Plan q = make_plan(m, p.n, k, ws && ws_bytes > lost ? ws_bytes - lost : 0);
+    const bool far = a->rows * a->ld >= (1ll << 32) || b->rows * b->ld >= (1ll << 32);
+    const Plan q = make_plan(m, p.n, k, ws && ws_bytes > lost ? ws_bytes - lost : 0, far);
     if ((int64_t)q.tiles_m * q.tiles_n > (1 << 23) || (q.skinny && p.n > (1 << 26))) return KGE_E_UNSUPPORTED;   // (a grid's limit)
     p.kb = (int)((k + BLOCK - 1) / BLOCK); p.kb_per = q.kb_per; p.splits = q.splits; p.tiles_m = q.tiles_m; p.tiles_n = q.tiles_n;
     p.part_ld = q.part_ld;
