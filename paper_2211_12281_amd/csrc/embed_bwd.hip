@@ -1,7 +1,7 @@
 // Gradient of the token lookup:  G[r, :] (+)= scale sum over i with ids[i] = r of D_i o g[i, :]
 //
 //   1. the positions are sorted by row, stable; every row gets the place of its run in the sorted list
-//   2. sums_kernel: sums of the whole chunks of CHUNK positions inside one run, and the rows whose runs hold no whole chunk
+//   2. sums_kernel: sums of the whole chunks (32 positions, or 8 in lists of up to COLLECT_MAX ids) inside one run, and the rows whose runs hold no whole chunk
 //   3. joins_kernel: the other rows: sums of their whole chunks, and the positions in front of and behind them
 // A gradient row is read once and a table row written once (rows without a position as zeros, or with accumulate not at all), every sum is
 // taken in an order that the sorted list alone decides, in fp32, without atomics.
@@ -22,10 +22,10 @@ constexpr int COLLECT_PARTS = 256;                            // parts of a list
 constexpr int DIGIT_BITS = 8;                                 // of a counting pass inside a part
 constexpr int64_t COLLECT_MAX = 32768, WHOLE_MAX = 4096;
 constexpr int MAX_BLOCKS = 256;                               // blocks of ids of a long list: every one adds up the others' counts
-constexpr int CHUNK = 32;
+constexpr int CHUNK_BITS = 5, SHORT_CHUNK_BITS = 3;           // a chunk's positions in long and in short lists
 constexpr int ROWS = 4;                                       // rows of a slot, whose runs are looked up together
-constexpr int JOIN_LP = 4;                                    // columns of a workgroup of joins_kernel: 2^4 groups, so that sixteen slots share a run
-constexpr int JOIN_CHUNKS = 16;                               // chunks that a workgroup of joins_kernel looks at
+constexpr int JOIN_LP = 5;                                    // columns of a workgroup of joins_kernel: 2^5 groups, so that eight slots share a run
+constexpr int JOIN_CHUNKS = 4;                               // chunks that a workgroup of joins_kernel looks at
 constexpr uint32_t EMPTY = 0xffffffffu;
 
 struct SortArgs {
@@ -72,9 +72,21 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *sums, uint3
     return before + s - v;
 }
 
-// Lanes whose digit equals this lane's (of the lanes with `valid`)
+// Lanes whose digit equals this lane's (of the lanes with `valid`).  The lists that take longest are those of a frequent row: nearly all digits are alike, so
+// the first two digits that occur are looked for by themselves, and the bits of all only where there are more (eight bits are a hundred instructions).
 __device__ __forceinline__ uint64_t peers_of(uint32_t digit, int bits, bool valid) {
-    uint64_t p = __ballot(valid);
+    const uint64_t all = __ballot(valid);
+    uint64_t left = all, p = 0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        if (!left) return p;
+        const uint32_t one = (uint32_t)__builtin_amdgcn_readlane((int)digit, __builtin_ctzll(left));
+        const uint64_t m = __ballot(valid && digit == one);
+        if (digit == one) p = m;
+        left &= ~m;
+    }
+    if (!left) return p;
+    p = all;
     for (int b = 0; b < bits; ++b) {
         const uint64_t m = __ballot(valid && (digit >> b & 1u));
         p &= digit >> b & 1u ? m : ~m;
@@ -206,8 +218,20 @@ __device__ __forceinline__ void sort_part(const SortArgs &a, PartLds &l) {
         const uint32_t mask = (1u << bits) - 1u;
         for (int k = tid; k < WAVES << DIGIT_BITS; k += SORT_NT) (&place[0][0])[k] = 0;
         __syncthreads();
-#pragma unroll 8
-        for (uint32_t i = w0 + lane; i < w1; i += 64) atomicAdd(&place[wave][(ki[i] - r0) >> shift & mask], 1u);
+        // (one addition per row and 64 ids: 64 lanes that add to one word, as a frequent row's do, take turns, 32 us where this takes 13)
+        constexpr int AHEAD = 8;                              // rounds whose loads are in flight (a frequent row's part is one long list)
+        for (uint32_t i0 = w0; i0 < w1; i0 += 64 * AHEAD) {
+            uint32_t key[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) key[u] = ki[min(i0 + 64 * u + lane, w1 - 1)];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const bool valid = i0 + 64 * u + lane < w1;
+                const uint32_t d = (key[u] - r0) >> shift & mask;
+                const uint64_t peers = peers_of(d, bits, valid);
+                if (valid && __popcll(peers & ((1ull << lane) - 1ull)) == 0) atomicAdd(&place[wave][d], (uint32_t)__popcll(peers));
+            }
+        }
         __syncthreads();
         uint32_t c = 0, total;
         if (tid < 1 << DIGIT_BITS)
@@ -222,7 +246,6 @@ __device__ __forceinline__ void sort_part(const SortArgs &a, PartLds &l) {
         }
         __syncthreads();
         volatile uint32_t *mine = place[wave];
-        constexpr int AHEAD = 8;                              // rounds whose loads are in flight (a frequent row's part is one long list)
         for (uint32_t i0 = w0; i0 < w1; i0 += 64 * AHEAD) {
             uint32_t key[AHEAD], pos[AHEAD];
 #pragma unroll
@@ -274,7 +297,8 @@ __global__ __launch_bounds__(SORT_NT) void parts_kernel(const SortArgs a) {
 struct SumArgs {
     const uint32_t *sk, *sp, *count;         // sorted rows and positions, their number
     const uint32_t *first, *last;
-    float *part;                             // [M / CHUNK][8 cg] sums of whole chunks
+    float *part;                             // [M >> lc][8 cg] sums of whole chunks of 2^lc positions
+    int lc;
     const void *g; int64_t g_ld; int64_t M;
     void *out; int64_t out_ld; int64_t n_rows;
     int dim, cg, accumulate; float scale; KgeDropDev drop;
@@ -331,7 +355,7 @@ template <bool OUT16> __device__ __forceinline__ void finish(const SumArgs &a, i
     kge_store8<OUT16>(orow, 8 * grp, n, s);
 }
 
-__device__ __forceinline__ bool holds_chunk(uint32_t k0, uint32_t k1) { return (k0 + CHUNK - 1) / CHUNK * CHUNK + CHUNK <= k1; }
+__device__ __forceinline__ bool holds_chunk(uint32_t k0, uint32_t k1, int lc) { return (((k0 + (1u << lc) - 1) >> lc) + 1) << lc <= k1; }
 
 // The workgroup's slots (THREADS / 2^lp groups of threads, lp <= 6) add up their parts of a sum, through the LDS, in slot order; slot 0 has the sum.
 template <int THREADS> __device__ __forceinline__ void join_slots(float (*red)[8], int lp, float (&s)[8]) {
@@ -406,13 +430,14 @@ __global__ __launch_bounds__(NT) void sums_kernel(const SumArgs a) {
     const int per = 1 << a.lp, sub = threadIdx.x >> a.lp, subs = NT >> a.lp, grp0 = threadIdx.x & (per - 1);
     for (int64_t w = blockIdx.x; w < a.chunk_items + a.row_items; w += gridDim.x) {
         if (w < a.chunk_items) {                               // a chunk: the slots take its positions in turn
-            const int64_t c0 = w * CHUNK;
-            if (c0 + CHUNK > *a.count || a.sk[c0] != a.sk[c0 + CHUNK - 1]) continue;      // (equal ends, equal chunk)
-            const int each = CHUNK / min(subs, CHUNK);
+            const int chunk = 1 << a.lc;
+            const int64_t c0 = w << a.lc;
+            if (c0 + chunk > *a.count || a.sk[c0] != a.sk[c0 + chunk - 1]) continue;      // (equal ends, equal chunk)
+            const int each = chunk / min(subs, chunk);
             for (int g0 = 0; g0 < a.cg; g0 += per) {
                 const int grp = g0 + grp0;
                 float s[8] = {};
-                if (grp < a.cg && sub * each < CHUNK) add_rows<G16>(a, step, a.sp + c0 + sub * each, each, grp, s);
+                if (grp < a.cg && sub * each < chunk) add_rows<G16>(a, step, a.sp + c0 + sub * each, each, grp, s);
                 join_slots<NT>(red, a.lp, s);
                 if (sub == 0 && grp < a.cg) {
                     float *p = a.part + (w * a.cg + grp) * 8;
@@ -431,7 +456,7 @@ __global__ __launch_bounds__(NT) void sums_kernel(const SumArgs a) {
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
                 if (row0 + r >= a.n_rows) break;
-                if (k0[r] == EMPTY ? a.accumulate : holds_chunk(k0[r], k1[r])) continue;
+                if (k0[r] == EMPTY ? a.accumulate : holds_chunk(k0[r], k1[r], a.lc)) continue;
                 for (int grp = grp0; grp < a.cg; grp += per) {
                     float s[8] = {};
                     if (k0[r] != EMPTY) add_rows<G16>(a, step, a.sp + k0[r], (int)(k1[r] - k0[r]), grp, s);
@@ -455,10 +480,11 @@ __global__ __launch_bounds__(NT) void joins_kernel(const SumArgs a, int slices) 
         bool owner = false;
         uint32_t row = 0, k0 = 0, k1 = 0;
         if (threadIdx.x < JOIN_CHUNKS) {
-            const int64_t c = tile * JOIN_CHUNKS + threadIdx.x, c0 = c * CHUNK;
-            if (c < a.chunk_items && c0 + CHUNK <= *a.count) {
+            const int64_t c = tile * JOIN_CHUNKS + threadIdx.x, c0 = c << a.lc;
+            const int chunk = 1 << a.lc;
+            if (c < a.chunk_items && c0 + chunk <= *a.count) {
                 row = a.sk[c0];
-                if (row == a.sk[c0 + CHUNK - 1]) { k0 = a.first[row]; k1 = a.last[row]; owner = (k0 + CHUNK - 1) / CHUNK == c; }
+                if (row == a.sk[c0 + chunk - 1]) { k0 = a.first[row]; k1 = a.last[row]; owner = (k0 + chunk - 1) >> a.lc == c; }
             }
             found[threadIdx.x][0] = owner ? row : EMPTY; found[threadIdx.x][1] = k0; found[threadIdx.x][2] = k1;
         }
@@ -467,12 +493,12 @@ __global__ __launch_bounds__(NT) void joins_kernel(const SumArgs a, int slices) 
         for (int f = 0; f < JOIN_CHUNKS; ++f) {
             const uint32_t r = found[f][0];
             if (r == EMPTY) continue;
-            const uint32_t b0 = found[f][1], b1 = found[f][2], e0 = (b0 + CHUNK - 1) / CHUNK, e1 = b1 / CHUNK;
+            const uint32_t b0 = found[f][1], b1 = found[f][2], e0 = (b0 + (1u << a.lc) - 1) >> a.lc, e1 = b1 >> a.lc;
             float s[8] = {};
             if (grp < a.cg) {
                 // slot by slot: a share of the positions in front, of the chunks, of the positions behind
                 auto share = [&](uint32_t n, uint32_t &lo) { const uint32_t x = (n + subs - 1) / subs; lo = min(n, sub * x); return min(n, lo + x) - lo; };
-                uint32_t lo, n = share(e0 * CHUNK - b0, lo);
+                uint32_t lo, n = share((e0 << a.lc) - b0, lo);
                 add_rows<G16>(a, step, a.sp + b0 + lo, (int)n, grp, s);
                 n = share(e1 - e0, lo);
                 const float *p = a.part + ((int64_t)(e0 + lo) * a.cg + grp) * 8;
@@ -490,8 +516,8 @@ __global__ __launch_bounds__(NT) void joins_kernel(const SumArgs a, int slices) 
                             for (int e = 0; e < 4; ++e) { s[e] += x[u][0][e]; s[4 + e] += x[u][1][e]; }
                         }
                 }
-                n = share(b1 - e1 * CHUNK, lo);
-                add_rows<G16>(a, step, a.sp + e1 * CHUNK + lo, (int)n, grp, s);
+                n = share(b1 - (e1 << a.lc), lo);
+                add_rows<G16>(a, step, a.sp + (e1 << a.lc) + lo, (int)n, grp, s);
             }
             join_slots<NT>(red, a.lp, s);
             if (sub == 0 && grp < a.cg) finish<OUT16>(a, r, grp, s);
@@ -500,7 +526,7 @@ __global__ __launch_bounds__(NT) void joins_kernel(const SumArgs a, int slices) 
     }
 }
 
-struct Ws { SortArgs s; float *part; };
+struct Ws { SortArgs s; float *part; int lc; };
 int bits_of(int64_t n) {                     // of the numbers below n
     int b = 0;
     while ((1ll << b) < n) ++b;
@@ -530,7 +556,8 @@ size_t carve(int64_t M, int64_t n_rows, int dim, void *ws, Ws &w) {
     s.counts = take((size_t)MAX_BLOCKS * (4u << PARTS_BITS));
     s.base = take((4u << PARTS_BITS) + 4);
     s.first = take((size_t)n_rows * 4); s.last = take((size_t)n_rows * 4);
-    w.part = (float *)take((size_t)(M / CHUNK) * ((dim + 7) / 8) * 32);
+    w.lc = M <= COLLECT_MAX ? SHORT_CHUNK_BITS : CHUNK_BITS;
+    w.part = (float *)take((size_t)(M >> w.lc) * ((dim + 7) / 8) * 32);
     return off;
 }
 
@@ -564,7 +591,7 @@ int kge_embed_bwd(const void *g, int32_t g_dtype, int64_t g_ld, const int32_t *i
     SortArgs &s = w.s;
     s.ids = ids;
     const bool odd = ((s.rb + DIGIT_BITS - 1) / DIGIT_BITS & 1) != 0;
-    a.sk = odd ? s.kb : s.ka; a.sp = odd ? s.pb : s.pa; a.count = s.base + s.parts; a.first = s.first; a.last = s.last; a.part = w.part;
+    a.sk = odd ? s.kb : s.ka; a.sp = odd ? s.pb : s.pa; a.count = s.base + s.parts; a.first = s.first; a.last = s.last; a.part = w.part; a.lc = w.lc;
     a.g = g; a.g_ld = g_ld; a.M = M; a.out = g_table; a.out_ld = ld; a.n_rows = n_rows; a.dim = dim; a.cg = (dim + 7) / 8;
     a.accumulate = accumulate; a.scale = scale;
     a.lp = bits_of(a.cg);
@@ -586,7 +613,7 @@ int kge_embed_bwd(const void *g, int32_t g_dtype, int64_t g_ld, const int32_t *i
     SumArgs j = a;                                             // long runs: many slots, few columns each
     if (j.lp > JOIN_LP) j.lp = JOIN_LP;
     const int slots = NT >> a.lp, slices = (a.cg + (1 << j.lp) - 1) >> j.lp;
-    a.chunk_items = j.chunk_items = M / CHUNK;
+    a.chunk_items = j.chunk_items = M >> a.lc;
     a.row_items = (n_rows + slots * ROWS - 1) / (slots * ROWS);
     const dim3 grid = kge_grid_of(a.chunk_items + a.row_items, 1), grid2 = kge_grid_of((a.chunk_items + JOIN_CHUNKS - 1) / JOIN_CHUNKS * slices, 1);
 #define KGE_BWD(G, O)                                                                                           \
