@@ -33,6 +33,7 @@ struct RowsArgs {
     void *out; int64_t out_ld;
     int64_t M; int dim, rows; KgeFastDiv cg;
     float scale; KgeDropDev drop;
+    int stream;                              // the result is stored past the caches
 };
 
 // The lookup and the dropout in one body: a workgroup takes `rows` rows, a thread up to UNROLL groups of eight columns at a time, so that its loads are in
@@ -81,13 +82,16 @@ __global__ __launch_bounds__(NT) void rows_kernel(const RowsArgs a) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[u][e] += z[u][e];
                 }
-            kge_store8<OUT16>((char *)a.out + (r0 + row[u]) * a.out_ld * (OUT16 ? 2 : 4), 8 * grp[u], n[u], v[u]);
+            char *orow = (char *)a.out + (r0 + row[u]) * a.out_ld * (OUT16 ? 2 : 4);
+            if (a.stream) kge_store8<OUT16, true>(orow, 8 * grp[u], n[u], v[u]);
+            else kge_store8<OUT16>(orow, 8 * grp[u], n[u], v[u]);
         }
     }
     }
 }
 
-template <bool LOOKUP> int run_rows(const RowsArgs &a, bool in16, bool out16, hipStream_t st) {
+template <bool LOOKUP> int run_rows(RowsArgs &a, bool in16, bool out16, hipStream_t st) {
+    a.stream = a.M * a.dim * (out16 ? 2 : 4) >= KGE_STREAM_BYTES;
     const dim3 grid = kge_grid_of(a.M, a.rows);
     if (in16 && out16) hipLaunchKernelGGL((rows_kernel<LOOKUP, true, true>), grid, dim3(NT), 0, st, a);
     else if (!in16 && !out16) hipLaunchKernelGGL((rows_kernel<LOOKUP, false, false>), grid, dim3(NT), 0, st, a);

@@ -355,6 +355,19 @@ template <bool OUT16> __device__ __forceinline__ void finish(const SumArgs &a, i
     kge_store8<OUT16>(orow, 8 * grp, n, s);
 }
 
+// A row of zeros, sixteen bytes per lane side by side (the groups' own stores leave every other sixteen bytes of an fp32 line to a second one)
+template <bool OUT16> __device__ __forceinline__ void zero_row(const SumArgs &a, int64_t row, int lane, int lanes) {
+    char *orow = (char *)a.out + row * a.out_ld * (OUT16 ? 2 : 4);
+    const int whole = a.dim * (OUT16 ? 2 : 4) / 16;
+    const kge_u32x4 z = {0u, 0u, 0u, 0u};
+    for (int k = lane; k < whole; k += lanes) *(kge_u32x4_a2 *)(orow + 16 * k) = z;
+    if (lane == 0)
+        for (int c = whole * (OUT16 ? 8 : 4); c < a.dim; ++c) {
+            if constexpr (OUT16) ((uint16_t *)orow)[c] = 0;
+            else ((float *)orow)[c] = 0.f;
+        }
+}
+
 __device__ __forceinline__ bool holds_chunk(uint32_t k0, uint32_t k1, int lc) { return (((k0 + (1u << lc) - 1) >> lc) + 1) << lc <= k1; }
 
 // The workgroup's slots (THREADS / 2^lp groups of threads, lp <= 6) add up their parts of a sum, through the LDS, in slot order; slot 0 has the sum.
@@ -392,9 +405,11 @@ __global__ __launch_bounds__(SORT_NT) void whole_kernel(const SortArgs so, const
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             if (row0 + r >= end) break;
-            const bool none = k0[r] == EMPTY;
-            if (none && a.accumulate) continue;
-            if (!none && k1[r] - k0[r] > FEW) {
+            if (k0[r] == EMPTY) {
+                if (!a.accumulate) zero_row<OUT16>(a, row0 + r, grp0, per);
+                continue;
+            }
+            if (k1[r] - k0[r] > FEW) {
                 if (grp0 == 0) {
                     const uint32_t f = atomicAdd(&n_many, 1u);
                     many[f][0] = (uint32_t)(row0 + r); many[f][1] = k0[r]; many[f][2] = k1[r];
@@ -403,7 +418,7 @@ __global__ __launch_bounds__(SORT_NT) void whole_kernel(const SortArgs so, const
             }
             for (int grp = grp0; grp < a.cg; grp += per) {
                 float s[8] = {};
-                if (!none) add_rows<G16>(a, step, a.sp + k0[r], (int)(k1[r] - k0[r]), grp, s);
+                add_rows<G16>(a, step, a.sp + k0[r], (int)(k1[r] - k0[r]), grp, s);
                 finish<OUT16>(a, row0 + r, grp, s);
             }
         }
@@ -456,10 +471,14 @@ __global__ __launch_bounds__(NT) void sums_kernel(const SumArgs a) {
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
                 if (row0 + r >= a.n_rows) break;
-                if (k0[r] == EMPTY ? a.accumulate : holds_chunk(k0[r], k1[r], a.lc)) continue;
+                if (k0[r] == EMPTY) {
+                    if (!a.accumulate) zero_row<OUT16>(a, row0 + r, grp0, per);
+                    continue;
+                }
+                if (holds_chunk(k0[r], k1[r], a.lc)) continue;
                 for (int grp = grp0; grp < a.cg; grp += per) {
                     float s[8] = {};
-                    if (k0[r] != EMPTY) add_rows<G16>(a, step, a.sp + k0[r], (int)(k1[r] - k0[r]), grp, s);
+                    add_rows<G16>(a, step, a.sp + k0[r], (int)(k1[r] - k0[r]), grp, s);
                     finish<OUT16>(a, row0 + r, grp, s);
                 }
             }

@@ -54,17 +54,22 @@ template <bool BF16> __device__ __forceinline__ void kge_values8(const KgeRaw8<B
     }
 }
 
-template <bool BF16> __device__ __forceinline__ void kge_store8(void *row, int64_t col, int n, const float (&v)[8]) {
+// STREAM: past the caches, for results that are larger than they are
+template <bool BF16, bool STREAM = false> __device__ __forceinline__ void kge_store8(void *row, int64_t col, int n, const float (&v)[8]) {
     if (n >= 8) {
         if constexpr (BF16) {
             typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf2;
             kge_u32x4 r;
 #pragma unroll
             for (int u = 0; u < 4; ++u) r[u] = __builtin_bit_cast(uint32_t, bf2{(__bf16)v[2 * u], (__bf16)v[2 * u + 1]});
-            *(kge_u32x4_a2 *)((uint16_t *)row + col) = r;
+            if constexpr (STREAM) __builtin_nontemporal_store(r, (kge_u32x4_a2 *)((uint16_t *)row + col));
+            else *(kge_u32x4_a2 *)((uint16_t *)row + col) = r;
         } else {
-            *(kge_f32x4_a4 *)((float *)row + col) = kge_f32x4{v[0], v[1], v[2], v[3]};
-            *(kge_f32x4_a4 *)((float *)row + col + 4) = kge_f32x4{v[4], v[5], v[6], v[7]};
+            const kge_f32x4 x = {v[0], v[1], v[2], v[3]}, y = {v[4], v[5], v[6], v[7]};
+            if constexpr (STREAM) {
+                __builtin_nontemporal_store(x, (kge_f32x4_a4 *)((float *)row + col));
+                __builtin_nontemporal_store(y, (kge_f32x4_a4 *)((float *)row + col + 4));
+            } else { *(kge_f32x4_a4 *)((float *)row + col) = x; *(kge_f32x4_a4 *)((float *)row + col + 4) = y; }
         }
     } else {
 #pragma unroll
@@ -86,13 +91,15 @@ struct KgeDropDev {
 
 __device__ __forceinline__ uint32_t kge_drop_step(const KgeDropDev &d) { return d.step + (d.step_counter ? (uint32_t)*d.step_counter : 0u); }
 
+__device__ __forceinline__ uint32_t kge_xor3(uint32_t a, uint32_t b, uint32_t c) { return (uint32_t)__builtin_amdgcn_bitop3_b32((int)a, (int)b, (int)c, 0x96); }
+
 __device__ __forceinline__ void kge_drop8(const KgeDropDev &d, uint32_t step, uint32_t row, uint32_t group, float (&v)[8]) {
     uint32_t c0 = row, c1 = group, c2 = step, c3 = d.tag, k0 = d.k0, k1 = d.k1;
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
-        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0; c1 = (uint32_t)p1;
-        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1; c3 = (uint32_t)p0;
+        c0 = kge_xor3((uint32_t)(p1 >> 32), c1, k0); c1 = (uint32_t)p1;
+        c2 = kge_xor3((uint32_t)(p0 >> 32), c3, k1); c3 = (uint32_t)p0;
         k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
     }
     const uint32_t w[4] = {c0, c1, c2, c3};
@@ -122,3 +129,5 @@ inline bool kge_bad_rows(const void *p, int32_t dtype, int64_t ld, int64_t cols)
 }
 constexpr int64_t KGE_MAX_ROWS = (1ll << 31) - 1, KGE_MAX_LD = 1ll << 31;
 constexpr int KGE_MAX_DIM = 65536;
+// From this size on results are stored past the caches: the L2s hold 32 MB in all
+constexpr int64_t KGE_STREAM_BYTES = 32ll << 20;
