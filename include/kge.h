@@ -450,7 +450,7 @@ size_t kge_encode_workspace_bytes(int op, const kge_encoder_t *enc, int64_t B, i
  * element (no alignment beyond the element's own, except where codes and scales say so).  Types are kge_dtype_t.  The calls only
  * launch kernels and may be captured into a HIP graph.
  *
- * kge_dropout_t: element (row, column) of a matrix is kept iff its 16 random bits are >= thr = round(p * 2^16), and is then
+ * kge_dropout_t: element (row, column) of a matrix is kept iff its 16 random bits are >= thr = round(p * 2^16) (65,535 at most), and is then
  * multiplied by 2^16 / (2^16 - thr).  The bits: Philox4x32-10, key = seed, counter (row, column / 8, step, tag), word (column % 8) / 2, low
  * half for even columns.  The mask is stored nowhere: the backward pass makes it again from the same values.  0 <= p < 1, step < 2^32; with
  * step_counter set (a DEVICE counter, see kge_step_counter_add) the step is step + *step_counter, read when the kernels run.

@@ -5,6 +5,7 @@ stream.  There is no CPU fallback: if the library is missing or a call fails, an
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import functools
 import os
@@ -589,12 +590,47 @@ _DTYPE = {torch.float32: 0, torch.bfloat16: 1}
 _CODES = {"e4m3": 0, "e5m2": 1}
 
 
-def _here(*tensors):
-    """Every given tensor lies on the current device, whose stream the call takes."""
-    dev = torch.cuda.current_device()
+def _here(*tensors) -> int:
+    """The current device, on which every given tensor has to lie (the call takes its stream)."""
+    dev = torch._C._cuda_getDevice()
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise KgeError(f"tensors have to be on the current device cuda:{dev}, got one on {t.device}")
+    return dev
+
+
+def _queue(dev: int, stream) -> int:
+    """The HIP stream of a call: torch's current one of the device, or the given torch.cuda.Stream."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+_stream_ws: dict = {}
+
+
+def _scratch(ws: Workspace | None, nbytes: int, dev: int, stream):
+    """(pointer, size) of a call's scratch space: of the given workspace, or of one that the library keeps for each device and stream, as
+    calls on two streams run side by side.  A call that is being captured into a graph needs one of its own, large enough before
+    the capture begins and kept for that graph: the graph goes on using the address."""
+    if torch.cuda.is_current_stream_capturing():
+        if ws is None or ws.buf is None or ws.buf.numel() < nbytes:
+            raise KgeError(f"a captured call needs a workspace of its own that holds {nbytes} bytes before the capture (ws=Workspace(); ws.get(bytes))")
+        return ws.buf.data_ptr(), ws.buf.numel()
+    if ws is None:
+        key = (dev, _queue(dev, stream))
+        ws = _stream_ws.get(key)
+        if ws is None:
+            ws = _stream_ws[key] = Workspace()
+    with _allocating_for(stream) if ws.buf is None or ws.buf.numel() < nbytes else _nothing:
+        buf = ws.get(nbytes)
+    return buf.data_ptr(), buf.numel()
+
+
+_nothing = contextlib.nullcontext()
+
+
+def _allocating_for(stream):
+    """New tensors belong to the stream that writes them: torch may hand their memory to others only behind its work."""
+    return _nothing if stream is None else torch.cuda.stream(stream)
 
 
 def _matrix(t, what: str):
@@ -611,12 +647,13 @@ def _rows_of(t, n: int, what: str):
     return t.data_ptr()
 
 
-def _new(out, rows: int, cols: int, dtype, what: str):
+def _new(out, rows: int, cols: int, dtype, what: str, stream):
     """(out, pointer, dtype, row stride): the given matrix, or a new one on the current device."""
     if out is None:
         if dtype not in _DTYPE:
             raise KgeError(f"{what}: fp32 or bf16, got {dtype}")
-        out = torch.empty((rows, cols), dtype=dtype, device="cuda")
+        with _allocating_for(stream):
+            out = torch.empty((rows, cols), dtype=dtype, device="cuda")
         return out, out.data_ptr(), _DTYPE[dtype], max(cols, 1)
     if tuple(out.shape) != (rows, cols):
         raise KgeError(f"{what}: out is {tuple(out.shape)}, {(rows, cols)} is wanted")
@@ -638,7 +675,10 @@ class Dropout:
     (step_counter_add) that is added to `step` when the kernels run, for steps replayed from a HIP graph."""
 
     def __init__(self, p: float, seed: int, step: int = 0, tag: int = 0, step_counter=None):
-        _here(step_counter)
+        if not 0 <= seed < 1 << 64 or not 0 <= step < 1 << 32 or not 0 <= tag < 1 << 32:
+            raise KgeError("seed: 64 bits, step and tag: 32 bits")
+        if step_counter is not None:
+            _here(step_counter)
         self.counter = step_counter                        # (kept alive with the struct that points to it)
         self.struct = KgeDropoutT(p, tag, seed, step, _counter(step_counter))
         self.ref = C.byref(self.struct)
@@ -646,10 +686,10 @@ class Dropout:
 
 def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
     """kge_dropout: residual + D o x; on a gradient, without the residual, the backward pass.  out may be x or residual."""
-    _here(x, residual, out)
+    dev = _here(x, residual, out)
     px, dt, ld = _matrix(x, "x")
     rows, cols = x.shape
-    out, po, dto, ldo = _new(out, rows, cols, x.dtype, "kge_dropout")
+    out, po, dto, ldo = _new(out, rows, cols, x.dtype, "kge_dropout", stream)
     pr, ldr = None, 0
     if residual is not None:
         pr, dtr, ldr = _matrix(residual, "residual")
@@ -657,33 +697,33 @@ def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
             raise KgeError("residual has another shape or type than x")
     if dto != dt:
         raise KgeError("out has another type than x")
-    _check(load().kge_dropout(px, ld, pr, ldr, po, ldo, dt, rows, cols, drop.ref, _stream(stream)), "kge_dropout")
+    _check(load().kge_dropout(px, ld, pr, ldr, po, ldo, dt, rows, cols, drop.ref, _queue(dev, stream)), "kge_dropout")
     return out
 
 
 def embed(table, ids, scale: float = 1.0, dropout: Dropout | None = None, dtype=None, out=None, stream=None):
     """kge_embed: rows `ids` of the table times scale, with dropout; dtype of the result: the table's, unless given."""
-    _here(table, ids, out)
+    dev = _here(table, ids, out)
     pt, dt, ld = _matrix(table, "table")
     M, (n_rows, dim) = ids.numel(), table.shape
-    out, po, dto, ldo = _new(out, M, dim, dtype or table.dtype, "kge_embed")
+    out, po, dto, ldo = _new(out, M, dim, dtype or table.dtype, "kge_embed", stream)
     _check(load().kge_embed(pt, dt, n_rows, dim, ld, _rows_of(ids, M, "ids"), M, scale, dropout.ref if dropout else None, po, dto, ldo,
-                            _stream(stream)), "kge_embed")
+                            _queue(dev, stream)), "kge_embed")
     return out
 
 
 def embed_bwd(g, ids, n_rows: int, scale: float = 1.0, dropout: Dropout | None = None, dtype=torch.float32, out=None,
               accumulate: bool = False, ws: Workspace | None = None, stream=None):
     """kge_embed_bwd: the table's gradient [n_rows, dim] from the gradient rows of the positions; accumulate: added to `out`."""
-    _here(g, ids, out)
+    dev = _here(g, ids, out)
     pg, dg, ldg = _matrix(g, "g")
     M, dim = g.shape
     if accumulate and out is None:
         raise KgeError("accumulate needs the gradient to add to")
-    out, po, do, ldo = _new(out, n_rows, dim, dtype, "kge_embed_bwd")
-    buf = (ws or _default_ws).get(_embed_bwd_bytes(M, n_rows, dim))
+    out, po, do, ldo = _new(out, n_rows, dim, dtype, "kge_embed_bwd", stream)
+    wp, wn = _scratch(ws, _embed_bwd_bytes(M, n_rows, dim), dev, stream)
     _check(load().kge_embed_bwd(pg, dg, ldg, _rows_of(ids, M, "ids"), M, scale, dropout.ref if dropout else None, po, do, n_rows, dim, ldo,
-                                1 if accumulate else 0, buf.data_ptr(), buf.numel(), _stream(stream)), "kge_embed_bwd")
+                                1 if accumulate else 0, wp, wn, _queue(dev, stream)), "kge_embed_bwd")
     return out
 
 
@@ -715,32 +755,34 @@ class Quantized:
 def quantize(x, fmt: str = "e4m3", by: str = "row", out=None, stream=None):
     """kge_quantize: x by rows (by="row"), the transposed matrix (by="col"), or the pair of both (by="both") from one read of x.  out: a
     Quantized, or a pair of them, to write to."""
-    _here(x)
+    dev = _here(x)
     px, dt, ld = _matrix(x, "x")
     rows, cols = x.shape
     if by not in ("row", "col", "both"):
         raise KgeError(f"by: row, col or both, got {by!r}")
     if out is None:
-        qr = Quantized.empty(rows, cols, fmt) if by != "col" else None
-        qc = Quantized.empty(cols, rows, fmt) if by != "row" else None
+        with _allocating_for(stream):
+            qr = Quantized.empty(rows, cols, fmt) if by != "col" else None
+            qc = Quantized.empty(cols, rows, fmt) if by != "row" else None
     else:
         qr, qc = out if by == "both" else (out, None) if by == "row" else (None, out)
         for q in (qr, qc):
             if q is not None:
                 _here(q.codes, q.scales)
-    _check(load().kge_quantize(px, dt, rows, cols, ld, qr.ref if qr else None, qc.ref if qc else None, _stream(stream)), "kge_quantize")
+    _check(load().kge_quantize(px, dt, rows, cols, ld, qr.ref if qr else None, qc.ref if qc else None, _queue(dev, stream)), "kge_quantize")
     return (qr, qc) if by == "both" else qr or qc
 
 
 def matmul_quantized(a: Quantized, b: Quantized, rows=None, dtype=torch.bfloat16, out=None, accumulate: bool = False,
                      ws: Workspace | None = None, stream=None):
     """kge_matmul_quantized: a[rows] b^t in fp32 or bf16; accumulate: added to `out`."""
-    _here(a.codes, a.scales, b.codes, b.scales, rows, out)
+    dev = _here(a.codes, a.scales, b.codes, b.scales, rows, out)
     m = a.rows if rows is None else rows.numel()
     if accumulate and out is None:
         raise KgeError("accumulate needs a matrix to add to")
-    out, po, do, ldo = _new(out, m, b.rows, dtype, "kge_matmul_quantized")
-    buf = (ws or _default_ws).get(_matmul_bytes(m, b.rows, a.cols))
+    out, po, do, ldo = _new(out, m, b.rows, dtype, "kge_matmul_quantized", stream)
+    need = _matmul_bytes(m, b.rows, a.cols)
+    wp, wn = _scratch(ws, need, dev, stream) if need > 256 else (None, 0)      # (256: nothing but its alignment)
     _check(load().kge_matmul_quantized(a.ref, None if rows is None else _rows_of(rows, m, "rows"), m, b.ref, 1 if accumulate else 0, po, do, ldo,
-                                       buf.data_ptr(), buf.numel(), _stream(stream)), "kge_matmul_quantized")
+                                       wp, wn, _queue(dev, stream)), "kge_matmul_quantized")
     return out

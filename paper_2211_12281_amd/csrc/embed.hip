@@ -114,7 +114,7 @@ int kge_embed(const void *table, int32_t table_dtype, int64_t n_rows, int32_t di
     if (kge_bad_type(table_dtype) || kge_bad_type(out_dtype) || dim < 1 || dim > KGE_MAX_DIM || n_rows < 0 || n_rows > KGE_MAX_ROWS || M < 0 || M > KGE_MAX_ROWS ||
         ld >= KGE_MAX_LD || out_ld >= KGE_MAX_LD) return KGE_E_INVALID_ARG;
     if (M == 0) return KGE_OK;
-    if ((n_rows > 0 && kge_bad_rows(table, table_dtype, ld, dim)) || !ids || kge_bad_rows(out, out_dtype, out_ld, dim)) return KGE_E_INVALID_ARG;
+    if ((n_rows > 0 && kge_bad_rows(table, table_dtype, ld, dim)) || !ids || ((uintptr_t)ids & 3) != 0 || kge_bad_rows(out, out_dtype, out_ld, dim)) return KGE_E_INVALID_ARG;
     a.x = table; a.x_ld = ld; a.ids = ids; a.n_rows = n_rows; a.out = out; a.out_ld = out_ld; a.M = M; a.dim = dim;
     a.cg = kge_fast_div((uint32_t)(dim + 7) / 8); a.rows = rows_per_block((int)a.cg.d); a.scale = scale;
     return run_rows<true>(a, table_dtype == KGE_BF16, out_dtype == KGE_BF16, (hipStream_t)hip_stream);

@@ -573,7 +573,7 @@ size_t kge_matmul_quantized_workspace_bytes(int64_t m, int64_t n, int64_t k) {
 int kge_matmul_quantized(const kge_quantized_t *a, const int32_t *rows, int64_t m, const kge_quantized_t *b, int32_t accumulate, void *out,
                          int32_t out_dtype, int64_t out_ld, void *ws, size_t ws_bytes, void *hip_stream) {
     if (kge_check_quantized(a) != KGE_OK || kge_check_quantized(b) != KGE_OK || a->cols != b->cols || m < 0 || m >= (1ll << 31) ||
-        (!rows && m != a->rows) || (accumulate != 0 && accumulate != 1) || (out_dtype != KGE_F32 && out_dtype != KGE_BF16)) return KGE_E_INVALID_ARG;
+        (!rows && m != a->rows) || ((uintptr_t)rows & 3) != 0 || (accumulate != 0 && accumulate != 1) || (out_dtype != KGE_F32 && out_dtype != KGE_BF16)) return KGE_E_INVALID_ARG;
     if (m == 0 || b->rows == 0) return KGE_OK;
     if (!out || out_ld < b->rows || out_ld >= (1ll << 31) || ((uintptr_t)out & (out_dtype == KGE_BF16 ? 1 : 3)) != 0) return KGE_E_INVALID_ARG;
     MatmulArgs p = {};
@@ -584,7 +584,7 @@ int kge_matmul_quantized(const kge_quantized_t *a, const int32_t *rows, int64_t 
     const size_t lost = ws ? (256 - ((uintptr_t)ws & 255)) & 255 : 0;
     const bool far = a->rows * a->ld >= (1ll << 32) || b->rows * b->ld >= (1ll << 32);
     const Plan q = make_plan(m, p.n, k, ws && ws_bytes > lost ? ws_bytes - lost : 0, far);
-    if ((int64_t)q.tiles_m * q.tiles_n > (1 << 23) || (q.skinny && p.n > (1 << 26))) return KGE_E_UNSUPPORTED;   // (a grid's limit)
+    if ((int64_t)q.tiles_m * q.tiles_n > (1 << 22) || (q.skinny && p.n > (1 << 26))) return KGE_E_UNSUPPORTED;   // (a grid's limit)
     p.kb = (int)((k + BLOCK - 1) / BLOCK); p.kb_per = q.kb_per; p.splits = q.splits; p.tiles_m = q.tiles_m; p.tiles_n = q.tiles_n;
     p.part_ld = q.part_ld;
     if (q.splits > 1) p.part = (float *)((char *)ws + lost);

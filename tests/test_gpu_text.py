@@ -35,13 +35,13 @@ def _padded(t, pad):
     return wide[:, pad // 2:pad // 2 + t.shape[1]]
 
 
-def _factor(rows, cols, p, step=STEP, seed=SEED, tag=TAG):
-    """float64 [rows, cols]: the dropout factors, from big-integer arithmetic on each counter block."""
+def _factor(rows, cols, p, step=STEP, seed=SEED, tag=TAG, row0=0):
+    """float64 [rows, cols]: the dropout factors of rows row0 and on, from big-integer arithmetic on each counter block."""
     thr = math.floor(p * 65536 + 0.5)
     out = np.zeros((rows, -(-cols // 8) * 8))
     for r in range(rows):
         for g in range(-(-cols // 8)):
-            c, k = [r, g, step, tag], [seed & 0xFFFFFFFF, seed >> 32]
+            c, k = [row0 + r, g, step, tag], [seed & 0xFFFFFFFF, seed >> 32]
             for _ in range(10):
                 p0, p1 = 0xD2511F53 * c[0], 0xCD9E8D57 * c[2]
                 c = [p1 >> 32 ^ c[1] ^ k[0], p1 & 0xFFFFFFFF, p0 >> 32 ^ c[3] ^ k[1], p0 & 0xFFFFFFFF]
@@ -379,6 +379,24 @@ def test_matmul(dt, fa, fb, m, n, k):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("fa,fb,m,n,k", [("e4m3", "e4m3", 4100, 4090, 300), ("e5m2", "e4m3", 4096, 4096, 128), ("e4m3", "e5m2", 65_600, 130, 700),
+                                         ("e5m2", "e5m2", 4353, 3841, 1100)])
+def test_matmul_large_tiles(dt, fa, fb, m, n, k):
+    """256 tiles of 256 x 256 and more: whole ones, rows and columns behind the last whole one, one to nine blocks; gathered, added, into rows with gaps."""
+    a, b = _q(4500, k, fa, 10, k), _q(n, k, fb, 11, k)
+    rows = torch.from_numpy(_rng(56, m).integers(-2, 4502, size=m).astype(np.int32))
+    want, tol = _product(a, b, rows, dt)
+    got = kge.matmul_quantized(a, b, rows=rows.cuda(), dtype=dt)
+    _within(got, want, tol + (want.abs() + tol) * HALF[dt], "matmul")
+    old = torch.ones((m, n), dtype=dt)
+    out = _padded(old, 3)
+    kge.matmul_quantized(a, b, rows=rows.cuda(), out=out, accumulate=True)
+    want += 1
+    tol += want.abs() * U
+    _within(out, want, tol + (want.abs() + tol) * HALF[dt], "matmul")
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
 @pytest.mark.parametrize("m,n,k,pad", [(5, 30, 300, 1), (90, 131, 260, 3), (200, 96, 4200, 2), (1, 7, 128, 0)])
 def test_matmul_gathered_accumulated_strided(dt, m, n, k, pad):
     a, b = _q(50, k, "e4m3", m, 3), _q(n, k, "e4m3", n, 4)
@@ -443,19 +461,19 @@ def test_matmul_splits_only_as_far_as_the_workspace_goes():
 # ---------------------------------------------------------------------------------------------------------------
 # together
 # ---------------------------------------------------------------------------------------------------------------
-def _layer(table, w, ids, dy, drop1, drop2, stream=None):
+def _layer(table, w, ids, dy, drop1, drop2, ws=None):
     """One projection of scaled, dropped-out token embeddings with a residual, and its gradients, as a training step runs it."""
     V, d = table.shape
     x = kge.embed(table, ids, scale=4.0, dropout=drop1, dtype=BF16)
     xr, xc = kge.quantize(x, by="both")
     wr, wc = kge.quantize(w, by="both")
-    y = kge.dropout(kge.matmul_quantized(xr, wr), drop2, residual=x)
+    y = kge.dropout(kge.matmul_quantized(xr, wr, ws=ws), drop2, residual=x)
     dz = kge.dropout(dy, drop2)
     zr, zc = kge.quantize(dz, fmt="e5m2", by="both")
-    dw = kge.matmul_quantized(zc, xc, dtype=F32)
-    dx = kge.matmul_quantized(zr, wc)
+    dw = kge.matmul_quantized(zc, xc, dtype=F32, ws=ws)
+    dx = kge.matmul_quantized(zr, wc, ws=ws)
     dx = (dx.float() + dy.float()).to(BF16)
-    return y, dw, kge.embed_bwd(dx, ids, V, scale=4.0, dropout=drop1)
+    return y, dw, kge.embed_bwd(dx, ids, V, scale=4.0, dropout=drop1, ws=ws)
 
 
 def test_a_training_step_of_them_all():
@@ -485,44 +503,163 @@ def test_a_training_step_of_them_all():
     assert bool(((dt - rdt).abs() <= et * 1.01).all())
 
 
-def test_the_step_in_a_graph_with_a_device_counter():
-    """Captured once, replayed with the counter moving on: every replay equals the eager step of its number, with eager work between them."""
-    V, d, M = 300, 96, 1100
-    table, w, dy = _values((V, d), F32, 64, std=0.1).cuda(), _values((d, d), F32, 65, std=0.1).cuda(), _values((M, d), BF16, 66).cuda()
-    ids = _ids(M, V, 67).cuda()
-    counter = torch.zeros(1, dtype=torch.int64, device="cuda")
-    drops = [kge.Dropout(0.1, SEED, 5, t, step_counter=counter) for t in (1, 2)]
-    eager = [_layer(table, w, ids, dy, kge.Dropout(0.1, SEED, 5 + s, 1), kge.Dropout(0.1, SEED, 5 + s, 2)) for s in range(4)]
+def _graph_inputs(V, d, M, key):
+    table, w, dy = _values((V, d), F32, key, std=0.1).cuda(), _values((d, d), F32, key + 1, std=0.1).cuda(), _values((M, d), BF16, key + 2).cuda()
+    return table, w, _ids(M, V, key + 3).cuda(), dy
+
+
+def _captured(step):
+    graph = torch.cuda.CUDAGraph()
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
-        _layer(table, w, ids, dy, *drops)                              # (sizes of the workspace, first launches)
+        step()                                                          # (the workspace's size, first launches)
     torch.cuda.current_stream().wait_stream(side)
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        out = _layer(table, w, ids, dy, *drops)
-        kge.step_counter_add(counter)
     torch.cuda.synchronize()
-    assert int(counter) == 0
+    with torch.cuda.graph(graph):
+        out = step()
+    return graph, out
+
+
+@pytest.mark.parametrize("V,d,M", [(300, 96, 1100), (500, 64, 40_000)])
+def test_the_step_in_a_graph_with_a_device_counter(V, d, M):
+    """Captured once, replayed with the counter moving on: every replay equals the eager step of its number, with eager work between them."""
+    args = _graph_inputs(V, d, M, 64)
+    counter = torch.zeros(1, dtype=torch.int64, device="cuda")
+    drops = [kge.Dropout(0.1, SEED, 5, t, step_counter=counter) for t in (1, 2)]
+    eager = [_layer(*args, kge.Dropout(0.1, SEED, 5 + s, 1), kge.Dropout(0.1, SEED, 5 + s, 2)) for s in range(4)]
+    ws = kge.Workspace()
+
+    def step():
+        out = _layer(*args, *drops, ws=ws)
+        kge.step_counter_add(counter)
+        return out
+    graph, out = _captured(step)
+    counter.zero_()
     for s in range(4):
         graph.replay()
         torch.cuda.synchronize()
         for got, want in zip(out, eager[s]):
             assert torch.equal(got, want), s
-        other = _layer(table, w, ids, dy, kge.Dropout(0.1, SEED, 90, 1), kge.Dropout(0.1, SEED, 90, 2))   # eager work in between
+        other = _layer(*args, kge.Dropout(0.1, SEED, 90, 1), kge.Dropout(0.1, SEED, 90, 2))   # eager work in between
         assert not torch.equal(other[0], out[0])
 
 
-def test_on_another_stream():
-    table, ids = _values((100, 64), F32, 70).cuda(), _ids(500, 100, 71).cuda()
-    g = _values((500, 64), F32, 72).cuda()
-    ws = kge.Workspace()
-    want = kge.embed_bwd(g, ids, 100), kge.embed(table, ids)
-    s = torch.cuda.Stream()
-    s.wait_stream(torch.cuda.current_stream())
-    got = kge.embed_bwd(g, ids, 100, ws=ws, stream=s, out=torch.empty_like(want[0])), kge.embed(table, ids, stream=s, out=torch.empty_like(want[1]))
-    s.synchronize()
-    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+def test_two_graphs_and_eager_work_with_workspaces_of_their_own():
+    cases = [_graph_inputs(300, 96, 1100, 80), _graph_inputs(900, 64, 36_000, 90)]
+    d = kge.Dropout(0.2, SEED, 1, 1), kge.Dropout(0.3, SEED, 1, 2)
+    want = [_layer(*c, *d) for c in cases]
+    ws = [kge.Workspace() for _ in cases]
+    graphs = [_captured(lambda c=c, w=w: _layer(*c, *d, ws=w)) for c, w in zip(cases, ws)]
+    for order in ((0, 1), (1, 0), (0, 0, 1)):
+        for k in order:
+            graphs[k][0].replay()
+        eager = _layer(*cases[1], *d)
+        torch.cuda.synchronize()
+        for k in (0, 1):
+            for got, ref in zip(graphs[k][1], want[k]):
+                assert torch.equal(got, ref)
+        assert all(torch.equal(x, y) for x, y in zip(eager, want[1]))
+
+
+def test_a_captured_call_without_a_workspace_of_its_own_is_refused():
+    g, ids = _values((50, 64), F32, 95).cuda(), _ids(50, 20, 96).cuda()
+    out = kge.embed_bwd(g, ids, 20)
+    for ws in (None, kge.Workspace()):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            with pytest.raises(kge.KgeError, match="workspace"):
+                kge.embed_bwd(g, ids, 20, out=out, ws=ws)
+            out.add_(1)                                                 # (a graph needs a node)
+
+
+def test_on_other_streams_at_once():
+    """The same calls on three streams side by side, each with the scratch space that the library keeps for its stream."""
+    table, ids = _values((100, 64), F32, 70).cuda(), _ids(40_000, 100, 71).cuda()
+    g = _values((40_000, 64), F32, 72).cuda()
+    q = kge.quantize(g, by="col")
+    calls = [lambda s: kge.embed_bwd(g, ids, 100, stream=s), lambda s: kge.embed(table, ids, stream=s), lambda s: kge.quantize(g, stream=s).codes,
+             lambda s: kge.matmul_quantized(q, q, dtype=F32, stream=s), lambda s: kge.dropout(g, kge.Dropout(0.5, 1), stream=s)]
+    want = [c(None) for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(3):
+        for s in (*streams, None):
+            got += [[c(s) for c in calls]]
+    with torch.cuda.stream(streams[0]):
+        got += [[c(None) for c in calls]]
+    torch.cuda.synchronize()
+    for outs in got:
+        assert all(torch.equal(x, y) for x, y in zip(outs, want))
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# places beyond 32 bits
+# ---------------------------------------------------------------------------------------------------------------
+def test_lookup_and_its_gradient_beyond_32_bits():
+    n, d = 2_300_000, 1000                                              # 4.6 GB in bf16, 9.2 GB in fp32
+    table = torch.zeros((n, d), dtype=BF16, device="cuda")
+    rows = torch.tensor([0, 1, 2_147_483, 2_147_484, n - 1], dtype=torch.int32)
+    v = _values((5, d), BF16, 100)
+    table[rows.long().cuda()] = v.cuda()
+    ids = rows[[4, 2, 0, 3, 1, 4]].cuda()
+    assert torch.equal(kge.embed(table, ids).cpu(), v[[4, 2, 0, 3, 1, 4]])
+    del table
+    g = _values((6, d), F32, 101)
+    for M in (6, 5000):                                                 # (one launch, and three)
+        more = torch.full((M - 6,), -1, dtype=torch.int32, device="cuda")
+        got = kge.embed_bwd(torch.cat([g.cuda(), torch.zeros((M - 6, d), device="cuda")]), torch.cat([ids, more]), n)
+        want = torch.stack([g[2], g[4], g[1], g[3], g[0] + g[5]])
+        assert torch.equal(got[rows.long().cuda()].cpu(), want)
+        got[rows.long().cuda()] = 0
+        assert not bool(got.any())
+        del got
+
+
+def test_dropout_and_quantisation_beyond_32_bits():
+    rows, cols = 4_500_000, 1000
+    x = torch.ones((rows, cols), dtype=BF16, device="cuda")
+    d = kge.Dropout(0.25, SEED, STEP, TAG)
+    q = kge.quantize(x)
+    assert bool((q.codes.view(torch.int64).view(rows, 128)[:, :125] == q.codes.view(torch.int64)[0, 0]).all()) and bool((q.scales[:, :8] == 127 - 8).all())
+    del q
+    kge.dropout(x, d, out=x)
+    for r in (0, 1, 4_294_967, 4_294_968, rows - 1):
+        assert torch.equal(x[r:r + 1].cpu(), _factor(1, cols, 0.25, row0=r).to(BF16))
+
+
+def _random_codes(rows, cols, key):
+    """Codes that stand for +-1, +-1.5, +-2, +-3 (scale 1): sums are whole halves, exact in fp32 whatever their order."""
+    g = torch.Generator(device="cuda").manual_seed(key)
+    pick = torch.tensor([0x38, 0x3C, 0x40, 0x44, 0xB8, 0xBC, 0xC0, 0xC4], dtype=torch.uint8, device="cuda")
+    codes = torch.empty((rows, cols), dtype=torch.uint8, device="cuda")
+    for part in codes.split(1 << 16):
+        part.copy_(pick[torch.randint(0, 8, part.shape, generator=g, device="cuda")])
+    return kge.Quantized(codes, torch.full((rows, -(-cols // 512) * 4), 127, dtype=torch.uint8, device="cuda"), cols)
+
+
+def _values_of(q, rows):
+    return _decode(q.codes[rows].cpu(), "e4m3")
+
+
+def test_product_of_rows_beyond_32_bits():
+    """A gathered table of 4.6 GB (64-bit addresses in every kernel that gathers), and offsets between 2 and 4 GB in the kernel with 32-bit ones."""
+    table = _random_codes(4_500_000, 1024, 1)
+    b = _random_codes(300, 1024, 2)
+    at = torch.tensor([0, 4_194_303, 4_194_304, 4_499_999, 2_097_152])
+    for m in (5, 200):
+        rows = at[torch.arange(m) % 5].to(torch.int32).cuda()
+        got = kge.matmul_quantized(table, b, rows=rows, dtype=F32).double().cpu()
+        want = _values_of(table, at.cuda()) @ _values_of(b, torch.arange(300, device="cuda")).t()
+        assert torch.equal(got, want[torch.arange(m) % 5])
+    near = kge.Quantized(table.codes[:4_100_000], table.scales[:4_100_000], 1024)       # 4.198 GB: just below 2^32
+    rows = torch.arange(4_100_000 - 70_000, 4_100_000, dtype=torch.int32, device="cuda")
+    for dt in (F32, BF16):
+        got = kge.matmul_quantized(near, b, rows=rows, dtype=dt)
+        some = torch.tensor([0, 1, 255, 256, 33_333, 69_999])
+        want = _values_of(near, rows[some.cuda()].long()) @ _values_of(b, torch.arange(300, device="cuda")).t()
+        assert torch.equal(got[some.cuda()].double().cpu(), want.to(dt).double())
 
 
 def test_the_binding_refuses():

@@ -29,7 +29,7 @@ def _embed(lib, **kw):
 
 @pytest.mark.parametrize("bad", [dict(table=None), dict(ids=None), dict(out=None), dict(dt=2), dict(odt=-1), dict(dim=0), dict(dim=65537),
                                  dict(ld=63), dict(old=63), dict(n=-1), dict(M=-1), dict(table=OK + 2), dict(out=OK + 1), dict(n=1 << 31),
-                                 dict(drop=_drop(1.0)), dict(drop=_drop(-0.1)), dict(drop=_drop(float("nan"))), dict(drop=_drop(0.1, 1 << 32))])
+                                 dict(ids=OK + 2), dict(drop=_drop(1.0)), dict(drop=_drop(-0.1)), dict(drop=_drop(float("nan"))), dict(drop=_drop(0.1, 1 << 32))])
 def test_embed_refuses(lib, bad):
     assert _embed(lib, **bad) == INVALID
 
@@ -47,7 +47,7 @@ def _bwd(lib, **kw):
 
 
 @pytest.mark.parametrize("bad", [dict(g=None), dict(ids=None), dict(gt=None), dict(dt=7), dict(tdt=3), dict(dim=0), dict(gld=63), dict(ld=10),
-                                 dict(n=-5), dict(n=1 << 31), dict(M=-1), dict(acc=2), dict(g=OK + 3), dict(gt=OK + 2), dict(drop=_drop(2.0))])
+                                 dict(n=-5), dict(n=1 << 31), dict(M=-1), dict(acc=2), dict(g=OK + 3), dict(gt=OK + 2), dict(ids=OK + 1), dict(drop=_drop(2.0))])
 def test_embed_bwd_refuses(lib, bad):
     assert _bwd(lib, **bad) == INVALID
 
@@ -124,7 +124,7 @@ def test_matmul_refuses_layouts(lib, bad):
     assert _mm(lib, bb=_q(512, **{k: v for k, v in bad.items() if k != "rows"} if "rows" not in bad else dict(format=9))) == INVALID
 
 
-@pytest.mark.parametrize("bad", [dict(m=255), dict(m=-1, rows=OK), dict(acc=2), dict(out=None), dict(dt=5), dict(ld=511), dict(out=OK + 2), dict(ld=1 << 31)])
+@pytest.mark.parametrize("bad", [dict(m=255), dict(m=-1, rows=OK), dict(rows=OK + 2), dict(acc=2), dict(out=None), dict(dt=5), dict(ld=511), dict(out=OK + 2), dict(ld=1 << 31)])
 def test_matmul_refuses(lib, bad):
     assert _mm(lib, **bad) == INVALID
 
