@@ -218,7 +218,7 @@ __device__ __forceinline__ void sort_part(const SortArgs &a, PartLds &l) {
         const uint32_t mask = (1u << bits) - 1u;
         for (int k = tid; k < WAVES << DIGIT_BITS; k += SORT_NT) (&place[0][0])[k] = 0;
         __syncthreads();
-        // (one addition per row and 64 ids: 64 lanes that add to one word, as a frequent row's do, take turns, 32 us where this takes 13)
+        // (one addition per row and 64 ids: lanes that add to one word take turns)
         constexpr int AHEAD = 8;                              // rounds whose loads are in flight (a frequent row's part is one long list)
         for (uint32_t i0 = w0; i0 < w1; i0 += 64 * AHEAD) {
             uint32_t key[AHEAD];
@@ -576,7 +576,9 @@ size_t carve(int64_t M, int64_t n_rows, int dim, void *ws, Ws &w) {
     s.base = take((4u << PARTS_BITS) + 4);
     s.first = take((size_t)n_rows * 4); s.last = take((size_t)n_rows * 4);
     w.lc = M <= COLLECT_MAX ? SHORT_CHUNK_BITS : CHUNK_BITS;
-    w.part = (float *)take((size_t)(M >> w.lc) * ((dim + 7) / 8) * 32);
+    const int64_t most = COLLECT_MAX >> SHORT_CHUNK_BITS;                 // (so that a longer list never needs less)
+    const int64_t chunks = M <= COLLECT_MAX || M >> CHUNK_BITS > most ? M >> w.lc : most;
+    w.part = (float *)take((size_t)chunks * ((dim + 7) / 8) * 32);
     return off;
 }
 

@@ -65,6 +65,18 @@ def test_embed_bwd_wants_its_workspace(lib):
     assert sizes == sorted(sizes)
 
 
+@pytest.mark.parametrize("n,dim", [(0, 1), (50_000, 768), (300, 65536), (2_000_000_000, 8)])
+def test_embed_bwd_workspace_never_falls(lib, n, dim):
+    """What serves a loop's largest call serves its smaller ones."""
+    size = lib.kge_embed_bwd_workspace_bytes
+    by_m = [size(M, n, dim) for M in (*range(0, 300, 7), 4095, 4096, 4097, 32760, 32768, 32769, 32800, 40_000, 131_071, 131_072, 131_073, 1 << 24, (1 << 31) - 1)]
+    assert by_m == sorted(by_m)
+    by_n = [size(M, r, dim) for M in (100, 40_000) for r in (1, 2, 255, 256, 257, 1024, 1025, 70_000, 1 << 30)]
+    assert by_n[:9] == sorted(by_n[:9]) and by_n[9:] == sorted(by_n[9:])
+    by_d = [size(40_000, n, d) for d in (1, 7, 8, 9, 768, 65536)]
+    assert by_d == sorted(by_d)
+
+
 def _dropout(lib, **kw):
     a = dict(x=OK, xld=64, res=None, rld=0, out=OK, old=64, dt=0, rows=4, cols=64, drop=_drop())
     a.update(kw)
@@ -132,7 +144,7 @@ def test_matmul_refuses(lib, bad):
 def test_matmul_refuses_other_widths_and_takes_nothing(lib):
     assert _mm(lib, bb=_q(512, 301)) == INVALID
     assert _mm(lib, bb=_q(0)) == 0 and _mm(lib, a=_q(0), m=0, out=None) == 0
-    assert _mm(lib, bb=_q((1 << 27), 300), a=_q(3), m=3, ld=1 << 27) == UNSUPPORTED        # more workgroups than a grid holds
+    assert _mm(lib, bb=_q((1 << 31) - 1, 300), a=_q(3), m=3, ld=(1 << 31) - 1) == UNSUPPORTED        # more workgroups than a grid holds
     size = lib.kge_matmul_quantized_workspace_bytes
     assert size(-1, 1, 1) == 0 and size(1, 1 << 31, 1) == 0 and size(1, 2048, 2048) >= 256
     assert size(1024, 768, 24576) >= 2 * 4 * 1024 * 768                                    # a long contraction over few tiles is split
