@@ -611,7 +611,9 @@ def _scratch(ws: Workspace | None, nbytes: int, dev: int, stream):
     """(pointer, size) of a call's scratch space: of the given workspace, or of one that the library keeps for each device and stream, as
     calls on two streams run side by side.  A call that is being captured into a graph needs one of its own, large enough before
     the capture begins and kept for that graph: the graph goes on using the address."""
-    if torch.cuda.is_current_stream_capturing():
+    with _allocating_for(stream):
+        capturing = torch.cuda.is_current_stream_capturing()
+    if capturing:
         if ws is None or ws.buf is None or ws.buf.numel() < nbytes:
             raise KgeError(f"a captured call needs a workspace of its own that holds {nbytes} bytes before the capture (ws=Workspace(); ws.get(bytes))")
         return ws.buf.data_ptr(), ws.buf.numel()
@@ -686,7 +688,7 @@ class Dropout:
 
 def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
     """kge_dropout: residual + D o x; on a gradient, without the residual, the backward pass.  out may be x or residual."""
-    dev = _here(x, residual, out)
+    dev = _here(x, residual, out, drop.counter)
     px, dt, ld = _matrix(x, "x")
     rows, cols = x.shape
     out, po, dto, ldo = _new(out, rows, cols, x.dtype, "kge_dropout", stream)
@@ -703,7 +705,7 @@ def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
 
 def embed(table, ids, scale: float = 1.0, dropout: Dropout | None = None, dtype=None, out=None, stream=None):
     """kge_embed: rows `ids` of the table times scale, with dropout; dtype of the result: the table's, unless given."""
-    dev = _here(table, ids, out)
+    dev = _here(table, ids, out, dropout.counter if dropout else None)
     pt, dt, ld = _matrix(table, "table")
     M, (n_rows, dim) = ids.numel(), table.shape
     out, po, dto, ldo = _new(out, M, dim, dtype or table.dtype, "kge_embed", stream)
@@ -715,7 +717,7 @@ def embed(table, ids, scale: float = 1.0, dropout: Dropout | None = None, dtype=
 def embed_bwd(g, ids, n_rows: int, scale: float = 1.0, dropout: Dropout | None = None, dtype=torch.float32, out=None,
               accumulate: bool = False, ws: Workspace | None = None, stream=None):
     """kge_embed_bwd: the table's gradient [n_rows, dim] from the gradient rows of the positions; accumulate: added to `out`."""
-    dev = _here(g, ids, out)
+    dev = _here(g, ids, out, dropout.counter if dropout else None)
     pg, dg, ldg = _matrix(g, "g")
     M, dim = g.shape
     if accumulate and out is None:
@@ -732,6 +734,8 @@ class Quantized:
     (uint8 [rows, ceil(cols / 128) to a multiple of four])."""
 
     def __init__(self, codes, scales, cols: int, fmt: str = "e4m3"):
+        if fmt not in _CODES:
+            raise KgeError(f"fmt: e4m3 or e5m2, got {fmt!r}")
         nb = (cols + 127) // 128
         (rows, wide), (srows, swide) = codes.shape, scales.shape
         if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or rows != srows:
@@ -754,7 +758,7 @@ class Quantized:
 
 def quantize(x, fmt: str = "e4m3", by: str = "row", out=None, stream=None):
     """kge_quantize: x by rows (by="row"), the transposed matrix (by="col"), or the pair of both (by="both") from one read of x.  out: a
-    Quantized, or a pair of them, to write to."""
+    Quantized of that format, or a pair of them, to write to."""
     dev = _here(x)
     px, dt, ld = _matrix(x, "x")
     rows, cols = x.shape
@@ -765,10 +769,14 @@ def quantize(x, fmt: str = "e4m3", by: str = "row", out=None, stream=None):
             qr = Quantized.empty(rows, cols, fmt) if by != "col" else None
             qc = Quantized.empty(cols, rows, fmt) if by != "row" else None
     else:
+        if by == "both" and (not isinstance(out, (tuple, list)) or len(out) != 2):
+            raise KgeError("out: a pair is wanted for both layouts")
         qr, qc = out if by == "both" else (out, None) if by == "row" else (None, out)
         for q in (qr, qc):
             if q is not None:
                 _here(q.codes, q.scales)
+                if q.fmt != fmt:
+                    raise KgeError(f"out has format {q.fmt}, {fmt} is wanted")
     _check(load().kge_quantize(px, dt, rows, cols, ld, qr.ref if qr else None, qc.ref if qc else None, _queue(dev, stream)), "kge_quantize")
     return (qr, qc) if by == "both" else qr or qc
 

@@ -148,7 +148,7 @@ __device__ __forceinline__ bool mq_row_valid(const MatmulArgs &p, int64_t row) {
 // The fragments of the next step are read while this one's are multiplied, across the stages too: the only barrier of a stage stands in front of the
 // products of its last step, whose operands are in registers by then, and the stage that it frees is refilled behind it.
 //
-// FAR: a copy's lanes have 64-bit addresses; else (matrices of less than 4 GiB) a base and 32-bit offsets, which the larger wave tile needs for its registers.
+// FAR: a copy's lanes have 64-bit addresses; else (codes and scales of less than 4 GiB) a base and 32-bit offsets, which the larger wave tile needs for its registers.
 template <int WM, int WN, int NJ, int NI, int NST, bool FAR, bool WIDE, int FA, int FB>
 __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(NI * NJ > 8 ? 1 : 2, NI * NJ > 8 ? 1 : 2)))
 void matmul_tiles_kernel(const MatmulArgs p) {
@@ -439,18 +439,19 @@ __global__ __launch_bounds__(256) void matmul_join_kernel(const MatmulArgs p) {
     }
 }
 
-// Few rows of A (one token, a small batch): the weights are read once and bound the call.  A workgroup takes sixteen rows of B against all rows of A
-// (16 MF at most), its eight waves take the blocks of 128 in turn, straight from memory into fragments, and add up through the LDS in order.
+// Few rows of A (one token, a small batch), and small products of any shape: a workgroup takes sixteen rows of B against 16 MF rows of A, its eight
+// waves take the blocks of 128 in turn, straight from memory into fragments, and add up through the LDS in order.  One token reads the weights
+// once, which bounds it; a small product is over after one or two trips to memory, where a tile's ring makes one for every two blocks.
 constexpr int SKINNY_WAVES = 8;
 template <int MF, bool WIDE, int FA, int FB>
 __global__ __launch_bounds__(64 * SKINNY_WAVES) void matmul_skinny_kernel(const MatmulArgs p) {
     __shared__ float part[SKINNY_WAVES][MF][16][16 + 4];       // [wave][block][row of A][row of B]
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 15, g = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16, rb = n0 + lr < p.n ? n0 + lr : 0;
+    const int64_t n0 = (int64_t)(blockIdx.x % (uint32_t)p.tiles_n) * 16, m0 = (int64_t)(blockIdx.x / (uint32_t)p.tiles_n) * (16 * MF), rb = n0 + lr < p.n ? n0 + lr : 0;
     const uint8_t *gb = p.b + rb * p.b_ld + 32 * g, *sb = p.bs + rb * p.bs_ld, *ga[MF], *sa[MF];
 #pragma unroll
     for (int f = 0; f < MF; ++f) {
-        const int64_t r = 16 * f + lr;
+        const int64_t r = m0 + 16 * f + lr;
         int64_t s = r < p.m ? (p.rows ? (int64_t)p.rows[r] : r) : 0;
         s = s >= 0 && s < p.a_rows ? s : 0;
         ga[f] = p.a + s * p.a_ld + 32 * g; sa[f] = p.as + s * p.as_ld;
@@ -501,15 +502,29 @@ __global__ __launch_bounds__(64 * SKINNY_WAVES) void matmul_skinny_kernel(const 
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[e] += x[e];
         }
-        const int64_t r = 16 * f + row;
+        const int64_t r = m0 + 16 * f + row;
         if (r >= p.m) continue;
         mq_store4(p, r, n0 + c, s, mq_row_valid(p, r));
     }
 }
 
 // ---------------------------------------------------------------------------------------------
-constexpr int SKINNY_ROWS = 64;
-constexpr int64_t WANTED = 512;                                // workgroups that a launch of the smaller tiles aims at
+// Which kernel (times of bf16 output, microseconds, rows of A x rows of B x contraction; those of fp32 output lie the same way):
+//   few rows, or little work   up to 512 workgroups of matmul_skinny_kernel whose waves take at most 12 blocks' worth of rows of A each (blocks in
+//                              turn x sixteens of rows), or up to 16 rows of A against any number of B's with at most four blocks in turn.
+//                              Within: 1 x 4,096 x 4,096 6.7 against 15.6 in tiles, 300 x 256 x 3,000 10.3 against 11.8, 1 x 50,000 x 768
+//                              9.2 against 11.1.  Beyond: 64 x 4,096 x 4,096 16.3 against 13.9, 3,000 x 256 x 768 9.3 against 8.0.
+//   tiles of 256 x 256         from 192 of them on, unless one row of tiles of 128 x 128 holds either side: 3,584 x 3,584 x 4,096 (196 tiles) 61.9 against
+//                              75.7 in tiles of 128 x 128, 160 x 65,536 x 768 20.8 against 25.3; but 32,768 x 256 x 768 (128 tiles) 18.9 against
+//                              14.7 and 128 x 50,000 x 4,096 57.2 against 38.2.
+//   a split contraction        up to 128 tiles, into parts of at least eight blocks and 512 workgroups in all: 200 x 4,096 x 4,096 20.0, with
+//                              parts of four 22.7; 2,000 x 2,000 x 2,000 (256 tiles) 28 split and 16 whole; 768 x 768 x 24,576
+//                              at 256, 512 and 1,024 workgroups 41, 38 and 50.
+constexpr int SKINNY_GROUPS = 512, SKINNY_WORK = 12, SKINNY_LONG = 4;
+constexpr int BIG_TILES = 192;
+constexpr int64_t WANTED = 512;
+constexpr int SPLIT_BLOCKS = 8;
+constexpr int64_t MAX_TILES = 1 << 22;                         // of a launch: a grid has fewer than 2^32 threads
 
 // Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B; stages; whether matrices may be 4 GiB and more
 struct Tile { int wm, wn, nj, ni, nst; bool far; };
@@ -517,22 +532,28 @@ constexpr Tile BIG = {2, 4, 4, 2, 2, false}, MID = {2, 2, 2, 2, 2, true};
 constexpr int tile_m(const Tile &t) { return 32 * t.wm * t.nj; }
 constexpr int tile_n(const Tile &t) { return 32 * t.wn * t.ni; }
 
+// skinny: sixteens of rows of A that a workgroup of matmul_skinny_kernel takes, 0 for tiles
 struct Plan { int skinny, big, tiles_m, tiles_n, splits, kb_per; int64_t part_ld, part_bytes; };
 
 Plan make_plan(int64_t m, int64_t n, int64_t k, size_t room, bool far = false) {
     Plan q = {};
     const int64_t kb = (k + BLOCK - 1) / BLOCK;
     q.splits = 1; q.kb_per = (int)kb;
-    if (m <= SKINNY_ROWS) { q.skinny = 1; return q; }
-    auto tiles_of = [&](const Tile &t, int64_t &tm, int64_t &tn) { tm = (m + tile_m(t) - 1) / tile_m(t); tn = (n + tile_n(t) - 1) / tile_n(t); return tm * tn; };
+    const int mf = m <= 16 ? 1 : m <= 32 ? 2 : 4;
+    const int64_t gm = (m + 16 * mf - 1) / (16 * mf), gn = (n + 15) / 16, rounds = (kb + SKINNY_WAVES - 1) / SKINNY_WAVES;
+    if (gm * gn <= SKINNY_GROUPS ? rounds * mf <= SKINNY_WORK : m <= 16 && gn <= MAX_TILES && rounds <= SKINNY_LONG) {
+        q.skinny = mf; q.tiles_m = (int)gm; q.tiles_n = (int)gn;
+        return q;
+    }
+    const auto tiles_of = [&](const Tile &t, int64_t &tm, int64_t &tn) { tm = (m + tile_m(t) - 1) / tile_m(t); tn = (n + tile_n(t) - 1) / tile_n(t); return tm * tn; };
     int64_t tm, tn, tiles = tiles_of(BIG, tm, tn);
-    q.big = tiles >= 256 && !far;
+    q.big = tiles >= BIG_TILES && m > tile_m(MID) && n > tile_n(MID) && !far;
     if (!q.big) tiles = tiles_of(MID, tm, tn);
     q.tiles_m = (int)tm; q.tiles_n = (int)tn;
     q.part_ld = (n + 3) / 4 * 4;
-    if (!q.big && tiles * 4 <= WANTED && kb >= 16) {
+    if (!q.big && tiles * 4 <= WANTED && kb >= 2 * SPLIT_BLOCKS) {
         int64_t s = WANTED / tiles;
-        if (s > kb / 8) s = kb / 8;                            // a split of at least eight blocks
+        if (s > kb / SPLIT_BLOCKS) s = kb / SPLIT_BLOCKS;
         const int64_t one = m * q.part_ld * 4;
         if (s * one > (int64_t)room) s = (int64_t)room / one;
         if (s > 1) {
@@ -546,9 +567,9 @@ Plan make_plan(int64_t m, int64_t n, int64_t k, size_t room, bool far = false) {
 
 template <bool WIDE, int FA, int FB> void launch(const MatmulArgs &p, const Plan &q, hipStream_t st) {
     if (q.skinny) {
-        const dim3 grid((unsigned)((p.n + 15) / 16)), blk(64 * SKINNY_WAVES);
-        if (p.m <= 16) hipLaunchKernelGGL((matmul_skinny_kernel<1, WIDE, FA, FB>), grid, blk, 0, st, p);
-        else if (p.m <= 32) hipLaunchKernelGGL((matmul_skinny_kernel<2, WIDE, FA, FB>), grid, blk, 0, st, p);
+        const dim3 grid((unsigned)(p.tiles_m * p.tiles_n)), blk(64 * SKINNY_WAVES);
+        if (q.skinny == 1) hipLaunchKernelGGL((matmul_skinny_kernel<1, WIDE, FA, FB>), grid, blk, 0, st, p);
+        else if (q.skinny == 2) hipLaunchKernelGGL((matmul_skinny_kernel<2, WIDE, FA, FB>), grid, blk, 0, st, p);
         else hipLaunchKernelGGL((matmul_skinny_kernel<4, WIDE, FA, FB>), grid, blk, 0, st, p);
         return;
     }
@@ -582,9 +603,10 @@ int kge_matmul_quantized(const kge_quantized_t *a, const int32_t *rows, int64_t 
     p.m = m; p.n = b->rows; p.out = out; p.out_ld = out_ld; p.out16 = out_dtype == KGE_BF16; p.accumulate = accumulate;
     const int64_t k = a->rows > 0 ? a->cols : 0;               // (a table without rows: nothing may be read, every row of the result is zeros)
     const size_t lost = ws ? (256 - ((uintptr_t)ws & 255)) & 255 : 0;
-    const bool far = a->rows * a->ld >= (1ll << 32) || b->rows * b->ld >= (1ll << 32);
+    bool far = false;
+    for (const kge_quantized_t *q : {a, b}) far = far || q->rows * q->ld >= (1ll << 32) || q->rows * q->scales_ld >= (1ll << 32);
     const Plan q = make_plan(m, p.n, k, ws && ws_bytes > lost ? ws_bytes - lost : 0, far);
-    if ((int64_t)q.tiles_m * q.tiles_n > (1 << 22) || (q.skinny && p.n > (1 << 26))) return KGE_E_UNSUPPORTED;   // (a grid's limit)
+    if ((int64_t)q.tiles_m * q.tiles_n > MAX_TILES) return KGE_E_UNSUPPORTED;
     p.kb = (int)((k + BLOCK - 1) / BLOCK); p.kb_per = q.kb_per; p.splits = q.splits; p.tiles_m = q.tiles_m; p.tiles_n = q.tiles_n;
     p.part_ld = q.part_ld;
     if (q.splits > 1) p.part = (float *)((char *)ws + lost);

@@ -365,7 +365,9 @@ def _q(rows, cols, fmt, *key, std=1.0):
 
 
 SHAPES = [(1, 1, 1), (1, 16, 128), (2, 17, 300), (16, 33, 129), (17, 40, 1000), (33, 100, 257), (64, 15, 2048), (65, 130, 128), (100, 64, 384),
-          (128, 128, 640), (129, 257, 100), (300, 200, 2500), (70, 70, 5000), (513, 300, 130), (1000, 3, 260), (66, 1, 127), (3, 5, 0), (80, 90, 0)]
+          (128, 128, 640), (129, 257, 100), (300, 200, 2500), (70, 70, 5000), (513, 300, 130), (1000, 3, 260), (66, 1, 127), (3, 5, 0), (80, 90, 0),
+          # beyond what workgroups of few rows take: tiles, split and whole, with rows and columns behind the last whole one; one token of many columns
+          (1025, 1030, 130), (1100, 900, 260), (40, 9000, 100), (140, 500, 4100), (30, 700, 7000), (2100, 2000, 0), (1, 8200, 2000), (13, 9000, 300), (1, 9000, 5000)]
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
@@ -397,7 +399,7 @@ def test_matmul_large_tiles(dt, fa, fb, m, n, k):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
-@pytest.mark.parametrize("m,n,k,pad", [(5, 30, 300, 1), (90, 131, 260, 3), (200, 96, 4200, 2), (1, 7, 128, 0)])
+@pytest.mark.parametrize("m,n,k,pad", [(5, 30, 300, 1), (90, 131, 260, 3), (200, 96, 4200, 2), (1, 7, 128, 0), (1030, 1029, 200, 3), (300, 1700, 1300, 1)])
 def test_matmul_gathered_accumulated_strided(dt, m, n, k, pad):
     a, b = _q(50, k, "e4m3", m, 3), _q(n, k, "e4m3", n, 4)
     rows = torch.from_numpy(_rng(52, m).integers(0, 50, size=m).astype(np.int32))
@@ -417,26 +419,27 @@ def test_matmul_gathered_accumulated_strided(dt, m, n, k, pad):
 
 def test_matmul_gathers_nothing_from_an_empty_table():
     b = _q(20, 256, "e4m3", 5)
-    out = kge.matmul_quantized(kge.Quantized.empty(0, 256), b, rows=torch.zeros(70, dtype=torch.int32, device="cuda"), dtype=F32)
-    assert out.shape == (70, 20) and not bool(out.any())
+    for m in (70, 70_000):
+        out = kge.matmul_quantized(kge.Quantized.empty(0, 256), b, rows=torch.zeros(m, dtype=torch.int32, device="cuda"), dtype=F32)
+        assert out.shape == (m, 20) and not bool(out.any())
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
-@pytest.mark.parametrize("m", [3, 70])
-def test_matmul_nan_stays_in_its_row(dt, m):
-    x, w = _values((m, 200), F32, 54), _values((30, 200), F32, 55)
+@pytest.mark.parametrize("m,n", [(3, 30), (70, 30), (1100, 1000), (5000, 4100)])
+def test_matmul_nan_stays_in_its_row(dt, m, n):
+    x, w = _values((m, 200), F32, 54), _values((n, 200), F32, 55)
     x[1, 7], w[4, 100] = float("nan"), float("nan")
     got = kge.matmul_quantized(kge.quantize(x.cuda()), kge.quantize(w.cuda()), dtype=dt).cpu()
-    want = torch.zeros((m, 30), dtype=torch.bool)
+    want = torch.zeros((m, n), dtype=torch.bool)
     want[1], want[:, 4] = True, True
     assert torch.equal(torch.isnan(got), want)
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
-@pytest.mark.parametrize("m", [2, 100])
-def test_matmul_far_scales(dt, m):
+@pytest.mark.parametrize("m,n", [(2, 40), (100, 40), (1100, 1000)])
+def test_matmul_far_scales(dt, m, n):
     """Scale bytes from one end to the other: products in and around fp32's range."""
-    a, b = _q(m, 512, "e4m3", 6), _q(40, 512, "e4m3", 7)
+    a, b = _q(m, 512, "e4m3", 6), _q(n, 512, "e4m3", 7)
     for i, s in enumerate((0, 1, 120, 220)):
         a.scales[:, i], b.scales[:, i] = s, 245 - s
     got = kge.matmul_quantized(a, b, dtype=dt)
@@ -648,7 +651,7 @@ def test_product_of_rows_beyond_32_bits():
     table = _random_codes(4_500_000, 1024, 1)
     b = _random_codes(300, 1024, 2)
     at = torch.tensor([0, 4_194_303, 4_194_304, 4_499_999, 2_097_152])
-    for m in (5, 200):
+    for m in (5, 200, 3000):
         rows = at[torch.arange(m) % 5].to(torch.int32).cuda()
         got = kge.matmul_quantized(table, b, rows=rows, dtype=F32).double().cpu()
         want = _values_of(table, at.cuda()) @ _values_of(b, torch.arange(300, device="cuda")).t()
@@ -660,6 +663,21 @@ def test_product_of_rows_beyond_32_bits():
         some = torch.tensor([0, 1, 255, 256, 33_333, 69_999])
         want = _values_of(near, rows[some.cuda()].long()) @ _values_of(b, torch.arange(300, device="cuda")).t()
         assert torch.equal(got[some.cuda()].double().cpu(), want.to(dt).double())
+
+
+def test_product_of_scales_beyond_32_bits():
+    """Scales with gaps, 5.2 GB from the first to the last, of a matrix whose codes are small."""
+    a, b = _random_codes(5000, 128, 3), _random_codes(700, 128, 4)
+    far = torch.zeros((5000, 1 << 20), dtype=torch.uint8, device="cuda")
+    far[:, 0] = 127 + (torch.arange(5000, device="cuda") % 5).to(torch.uint8)
+    a = kge.Quantized(a.codes, far[:, :4], 128)
+    rows = torch.arange(20_000, dtype=torch.int32) % 5000
+    some = torch.tensor([0, 1, 4095, 4096, 4999, 19_998])
+    want = _values_of(a, rows[some].long().cuda()) * 2.0 ** (rows[some] % 5).double().unsqueeze(1) @ _values_of(b, torch.arange(700, device="cuda")).t()
+    for m in (100, 20_000):
+        got = kge.matmul_quantized(a, b, rows=rows[:m].cuda(), dtype=F32)
+        ok = some < m
+        assert torch.equal(got[some[ok].cuda()].double().cpu(), want[ok])
 
 
 def test_the_binding_refuses():
@@ -674,6 +692,8 @@ def test_the_binding_refuses():
                  lambda: kge.quantize(x, by="rows"), lambda: kge.Quantized(q.codes[:, :64], q.scales, 64), lambda: kge.Quantized(q.codes, q.scales[:, :1], 64),
                  lambda: kge.Quantized(q.codes, q.scales, 200), lambda: kge.matmul_quantized(q, kge.quantize(torch.zeros((4, 200), device="cuda"))),
                  lambda: kge.matmul_quantized(q, q, accumulate=True), lambda: kge.matmul_quantized(q, q, rows=ids.long()),
-                 lambda: kge.matmul_quantized(q, q, out=torch.empty((4, 5), device="cuda")), lambda: kge.dropout(x.expand(4, 64)[:, :1].expand(4, 64), d)]:
+                 lambda: kge.matmul_quantized(q, q, out=torch.empty((4, 5), device="cuda")), lambda: kge.dropout(x.expand(4, 64)[:, :1].expand(4, 64), d),
+                 lambda: kge.quantize(x, fmt="e3m4"), lambda: kge.quantize(x, fmt="e5m2", out=q), lambda: kge.quantize(x, by="both", out=q),
+                 lambda: kge.Quantized(q.codes, q.scales, 64, "fp8")]:
         with pytest.raises(kge.KgeError):
             call()
