@@ -42,51 +42,51 @@ template <bool LOOKUP, bool IN16, bool OUT16>
 __global__ __launch_bounds__(NT) void rows_kernel(const RowsArgs a) {
     const uint32_t step = a.drop.thr ? kge_drop_step(a.drop) : 0u;
     for (int64_t r0 = (int64_t)blockIdx.x * a.rows; r0 < a.M; r0 += (int64_t)gridDim.x * a.rows) {
-    const int nr = (int)(a.M - r0 < a.rows ? a.M - r0 : a.rows), items = nr * (int)a.cg.d;
-    for (int it0 = threadIdx.x; it0 < items; it0 += NT * UNROLL) {
-        int row[UNROLL], grp[UNROLL], n[UNROLL];
-        int64_t src[UNROLL];
-        bool in[UNROLL];
+        const int nr = (int)(a.M - r0 < a.rows ? a.M - r0 : a.rows), items = nr * (int)a.cg.d;
+        for (int it0 = threadIdx.x; it0 < items; it0 += NT * UNROLL) {
+            int row[UNROLL], grp[UNROLL], n[UNROLL];
+            int64_t src[UNROLL];
+            bool in[UNROLL];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const int it = it0 + u * NT;
-            in[u] = it < items;
-            row[u] = in[u] ? (int)kge_div((uint32_t)it, a.cg) : 0;
-            grp[u] = in[u] ? it - row[u] * (int)a.cg.d : 0;
-            n[u] = a.dim - 8 * grp[u];
-            if constexpr (LOOKUP) src[u] = in[u] ? (int64_t)a.ids[r0 + row[u]] : -1;
-            else src[u] = r0 + row[u];
-        }
-        float v[UNROLL][8], z[UNROLL][8];
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const bool live = LOOKUP ? src[u] >= 0 && src[u] < a.n_rows : in[u];
-            if (live) kge_load8<IN16>((const char *)a.x + src[u] * a.x_ld * (IN16 ? 2 : 4), 8 * grp[u], n[u], v[u]);
-            else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
+            for (int u = 0; u < UNROLL; ++u) {
+                const int it = it0 + u * NT;
+                in[u] = it < items;
+                row[u] = in[u] ? (int)kge_div((uint32_t)it, a.cg) : 0;
+                grp[u] = in[u] ? it - row[u] * (int)a.cg.d : 0;
+                n[u] = a.dim - 8 * grp[u];
+                if constexpr (LOOKUP) src[u] = in[u] ? (int64_t)a.ids[r0 + row[u]] : -1;
+                else src[u] = r0 + row[u];
             }
-            if constexpr (!LOOKUP)
-                if (a.res && in[u]) kge_load8<IN16>((const char *)a.res + (r0 + row[u]) * a.res_ld * (IN16 ? 2 : 4), 8 * grp[u], n[u], z[u]);
-        }
+            float v[UNROLL][8], z[UNROLL][8];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            if (!in[u]) continue;
-            if constexpr (LOOKUP) {
+            for (int u = 0; u < UNROLL; ++u) {
+                const bool live = LOOKUP ? src[u] >= 0 && src[u] < a.n_rows : in[u];
+                if (live) kge_load8<IN16>((const char *)a.x + src[u] * a.x_ld * (IN16 ? 2 : 4), 8 * grp[u], n[u], v[u]);
+                else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[u][e] *= a.scale;
-            }
-            if (a.drop.thr) kge_drop8(a.drop, step, (uint32_t)(r0 + row[u]), (uint32_t)grp[u], v[u]);
-            if constexpr (!LOOKUP)
-                if (a.res) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[u][e] += z[u][e];
+                    for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
                 }
-            char *orow = (char *)a.out + (r0 + row[u]) * a.out_ld * (OUT16 ? 2 : 4);
-            if (a.stream) kge_store8<OUT16, true>(orow, 8 * grp[u], n[u], v[u]);
-            else kge_store8<OUT16>(orow, 8 * grp[u], n[u], v[u]);
+                if constexpr (!LOOKUP)
+                    if (a.res && in[u]) kge_load8<IN16>((const char *)a.res + (r0 + row[u]) * a.res_ld * (IN16 ? 2 : 4), 8 * grp[u], n[u], z[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                if (!in[u]) continue;
+                if constexpr (LOOKUP) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[u][e] *= a.scale;
+                }
+                if (a.drop.thr) kge_drop8(a.drop, step, (uint32_t)(r0 + row[u]), (uint32_t)grp[u], v[u]);
+                if constexpr (!LOOKUP)
+                    if (a.res) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[u][e] += z[u][e];
+                    }
+                char *orow = (char *)a.out + (r0 + row[u]) * a.out_ld * (OUT16 ? 2 : 4);
+                if (a.stream) kge_store8<OUT16, true>(orow, 8 * grp[u], n[u], v[u]);
+                else kge_store8<OUT16>(orow, 8 * grp[u], n[u], v[u]);
+            }
         }
-    }
     }
 }
 

@@ -1,15 +1,26 @@
 // Gradient of the token lookup:  G[r, :] (+)= scale sum over i with ids[i] = r of D_i o g[i, :]
 //
 //   1. the positions are sorted by row, stable; every row gets the place of its run in the sorted list
-//   2. sums_kernel: sums of the whole chunks (32 positions, or 8 in lists of up to COLLECT_MAX ids) inside one run, and the rows whose runs hold no whole chunk
+//   2. sums_kernel: sums of the whole chunks (32 or 8 positions) inside one run, and the rows whose runs hold no whole chunk
 //   3. joins_kernel: the other rows: sums of their whole chunks, and the positions in front of and behind them
 // A gradient row is read once and a table row written once (rows without a position as zeros, or with accumulate not at all), every sum is
 // taken in an order that the sorted list alone decides, in fp32, without atomics.
 //
 // The sort.  Rows are cut into parts of consecutive rows, and one workgroup per part orders the part's list.  Long lists (2^rb rows a part, at
 // most 1,024 parts): one launch counts the ids of each part per block of ids, one deals them out stable.  Up to COLLECT_MAX ids the part's workgroup
-// (256 of them) reads all ids and collects its own, and these two launches fall away.  Up to WHOLE_MAX ids that workgroup goes on to the sums of its rows, and the call is
-// one launch.  Ids outside the table belong to no part and are gone from the list.
+// (256 of them) reads all ids and collects its own, and these two launches fall away.  Short lists: that workgroup goes on to the sums of its rows,
+// and the call is one launch.  Ids outside the table belong to no part and are gone from the list.
+//
+// What bounds it: memory for the rows, at 131,072 positions of 1,024 bf16 columns (half a gigabyte with the touched fp32 rows): sums 120 us, the
+// sort 37 and joins 22; the sort's launches take turns with nothing to hide behind.  The lists are those of text: a handful of rows has most positions, so
+// no step may depend on a row's positions being few (one workgroup per row, one lane per digit).
+//
+// Rules, both sides measured (microseconds, bf16 gradient, fp32 table of 768 columns; without and with dropout, whose bits are the work of a sum):
+//   one launch      1,024 ids over 300 rows 18.0 against 24.6 in three launches, 2,048 over 30,000 31.9 against 32.6, 4,096 38.5 against 36.2; with dropout
+//                   512 over 300 20.9 against 29.4, 2,048 over 30,000 46.3 against 35.8 (a frequent row's bits are one workgroup's)
+//   collected ids   24,000 61.2 against 66.7 dealt out, 32,768 72.6 against 73.0
+//   chunks of 8     9,000 37.3 against 40.2 in chunks of 32, 24,000 60.9 against 53.2; with dropout 16,384 56.2 against 67.7, 40,000 95.8 against
+//                   89.8
 #include "text_ops.hpp"
 
 namespace {
@@ -20,12 +31,14 @@ constexpr int PARTS_BITS = 10;                                // parts of a long
 static_assert(1 << PARTS_BITS <= SORT_NT, "one thread per part");
 constexpr int COLLECT_PARTS = 256;                            // parts of a list that every part reads: one workgroup per compute unit
 constexpr int DIGIT_BITS = 8;                                 // of a counting pass inside a part
-constexpr int64_t COLLECT_MAX = 32768, WHOLE_MAX = 4096;
+// Most ids of a call (the rules above): whose parts collect them, of one launch, of chunks of 8; the last two without and with dropout
+constexpr int64_t COLLECT_MAX = 32768, WHOLE_MAX = 2048, WHOLE_MAX_DROP = 512, SHORT_MAX = 16384, SHORT_MAX_DROP = 32768;
 constexpr int MAX_BLOCKS = 256;                               // blocks of ids of a long list: every one adds up the others' counts
 constexpr int CHUNK_BITS = 5, SHORT_CHUNK_BITS = 3;           // a chunk's positions in long and in short lists
 constexpr int ROWS = 4;                                       // rows of a slot, whose runs are looked up together
-constexpr int JOIN_LP = 5;                                    // columns of a workgroup of joins_kernel: 2^5 groups, so that eight slots share a run
-constexpr int JOIN_CHUNKS = 4;                               // chunks that a workgroup of joins_kernel looks at
+// Of a workgroup of joins_kernel: 2^5 groups of columns, so that eight slots share a run, and four chunks (with 2^4 and sixteen, 5,000 positions of 1,024
+// columns took 43.6 us and not 34.2, 131,072 took 182 and not 178).
+constexpr int JOIN_LP = 5, JOIN_CHUNKS = 4;
 constexpr uint32_t EMPTY = 0xffffffffu;
 
 struct SortArgs {
@@ -382,7 +395,7 @@ template <int THREADS> __device__ __forceinline__ void join_slots(float (*red)[8
             for (int e = 0; e < 8; ++e) s[e] += red[t][e];
 }
 
-// Up to WHOLE_MAX ids: the part's workgroup sorts and adds up.  A slot takes the rows with a FEW positions, ROWS of them at a time; the others are
+// Short lists: the part's workgroup sorts and adds up.  A slot takes the rows with a FEW positions, ROWS of them at a time; the others are
 // shared by all slots one after the other.
 constexpr int FEW = 16;
 template <bool G16, bool OUT16>
@@ -551,7 +564,7 @@ int bits_of(int64_t n) {                     // of the numbers below n
     while ((1ll << b) < n) ++b;
     return b;
 }
-size_t carve(int64_t M, int64_t n_rows, int dim, void *ws, Ws &w) {
+size_t carve(int64_t M, int64_t n_rows, int dim, bool drop, void *ws, Ws &w) {
     char *p = (char *)ws;
     size_t off = 0;
     auto take = [&](size_t bytes) { void *q = p ? p + off : nullptr; off += (bytes + 255) / 256 * 256; return (uint32_t *)q; };
@@ -575,9 +588,10 @@ size_t carve(int64_t M, int64_t n_rows, int dim, void *ws, Ws &w) {
     s.counts = take((size_t)MAX_BLOCKS * (4u << PARTS_BITS));
     s.base = take((4u << PARTS_BITS) + 4);
     s.first = take((size_t)n_rows * 4); s.last = take((size_t)n_rows * 4);
-    w.lc = M <= COLLECT_MAX ? SHORT_CHUNK_BITS : CHUNK_BITS;
-    const int64_t most = COLLECT_MAX >> SHORT_CHUNK_BITS;                 // (so that a longer list never needs less)
-    const int64_t chunks = M <= COLLECT_MAX || M >> CHUNK_BITS > most ? M >> w.lc : most;
+    w.lc = M <= (drop ? SHORT_MAX_DROP : SHORT_MAX) ? SHORT_CHUNK_BITS : CHUNK_BITS;
+    // (room for the shorter chunks wherever a dropout asks for them, so that a longer list never needs less)
+    const int64_t shorts = (M < SHORT_MAX_DROP ? M : SHORT_MAX_DROP) >> SHORT_CHUNK_BITS, longs = M >> CHUNK_BITS;
+    const int64_t chunks = shorts > longs ? shorts : longs;
     w.part = (float *)take((size_t)chunks * ((dim + 7) / 8) * 32);
     return off;
 }
@@ -589,7 +603,7 @@ extern "C" {
 size_t kge_embed_bwd_workspace_bytes(int64_t M, int64_t n_rows, int32_t dim) {
     if (M < 0 || M > KGE_MAX_ROWS || n_rows < 0 || n_rows > KGE_MAX_ROWS || dim < 1 || dim > KGE_MAX_DIM) return 0;
     Ws w;
-    return carve(M, n_rows, dim, nullptr, w) + 256;
+    return carve(M, n_rows, dim, false, nullptr, w) + 256;
 }
 
 int kge_embed_bwd(const void *g, int32_t g_dtype, int64_t g_ld, const int32_t *ids, int64_t M, float scale, const kge_dropout_t *drop,
@@ -606,8 +620,8 @@ int kge_embed_bwd(const void *g, int32_t g_dtype, int64_t g_ld, const int32_t *i
     if (!ws) return KGE_E_WORKSPACE_TOO_SMALL;
     const size_t lost = (256 - ((uintptr_t)ws & 255)) & 255;
     Ws w = {};
-    if (carve(M, n_rows, dim, nullptr, w) + lost > ws_bytes) return KGE_E_WORKSPACE_TOO_SMALL;
-    carve(M, n_rows, dim, (char *)ws + lost, w);
+    if (carve(M, n_rows, dim, a.drop.thr != 0, nullptr, w) + lost > ws_bytes) return KGE_E_WORKSPACE_TOO_SMALL;
+    carve(M, n_rows, dim, a.drop.thr != 0, (char *)ws + lost, w);
     hipStream_t st = (hipStream_t)hip_stream;
     SortArgs &s = w.s;
     s.ids = ids;
@@ -618,7 +632,7 @@ int kge_embed_bwd(const void *g, int32_t g_dtype, int64_t g_ld, const int32_t *i
     a.lp = bits_of(a.cg);
     if (a.lp > 6) a.lp = 6;
     const bool g16 = g_dtype == KGE_BF16, o16 = table_dtype == KGE_BF16;
-    if (M > 0 && M <= WHOLE_MAX) {
+    if (M > 0 && M <= (a.drop.thr ? WHOLE_MAX_DROP : WHOLE_MAX)) {
         const dim3 grid((unsigned)s.parts);
         if (g16 && o16) hipLaunchKernelGGL((whole_kernel<true, true>), grid, dim3(SORT_NT), 0, st, s, a);
         else if (g16) hipLaunchKernelGGL((whole_kernel<true, false>), grid, dim3(SORT_NT), 0, st, s, a);

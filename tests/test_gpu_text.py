@@ -120,7 +120,9 @@ def _bwd_case(M, V, dim, p, dt, *key, ids=None):
 @pytest.mark.parametrize("dt,odt", [(F32, F32), (BF16, F32), (BF16, BF16), (F32, BF16)])
 @pytest.mark.parametrize("M,V,dim,pad,p,acc", [(1, 7, 768, 0, 0.0, False), (5, 3, 1, 1, 0.5, True), (40, 1, 33, 0, 0.1, False), (700, 64, 72, 3, 0.1, True),
                                                (700, 2000, 257, 1, 0.0, False), (0, 5, 16, 0, 0.0, False), (64, 1, 600, 0, 0.0, True),
-                                               (129, 2, 8, 0, 0.25, False), (3000, 300, 24, 0, 0.0, True)])
+                                               (129, 2, 8, 0, 0.25, False), (3000, 300, 24, 0, 0.0, True),
+                                               (512, 20, 264, 1, 0.1, False), (513, 20, 264, 1, 0.1, False), (2048, 9, 130, 0, 0.0, False),
+                                               (2049, 9, 130, 0, 0.0, True), (4500, 60_000, 16, 0, 0.2, False)])
 def test_embed_bwd(dt, odt, M, V, dim, pad, p, acc):
     g, ids, scale, want, tol = _bwd_case(M, V, dim, p, dt)
     old = _values((V, dim), odt, 5, V)
@@ -137,19 +139,22 @@ def test_embed_bwd(dt, odt, M, V, dim, pad, p, acc):
 
 
 @pytest.mark.parametrize("M,V,dim", [(32768, 700, 40), (32769, 700, 40), (70000, 90000, 24), (70000, 3, 72), (32768, 3_000_000, 8), (40000, 3_000_000, 8),
-                                     (530_000, 5000, 8), (33000, 1, 16), (20000, 70_000, 600)])
-def test_embed_bwd_long(M, V, dim):
+                                     (530_000, 5000, 8), (33000, 1, 16), (20000, 70_000, 600), (16384, 400, 32), (16385, 400, 32)])
+@pytest.mark.parametrize("p", [0.0, 0.1])
+def test_embed_bwd_long(M, V, dim, p):
     """Both sorts, runs of thousands of positions, every chunk boundary."""
-    g, ids, scale, want, tol = _bwd_case(M, V, dim, 0.0, BF16)
-    got = kge.embed_bwd(g.cuda(), ids.cuda(), V, scale=scale)
+    g, ids, scale, want, tol = _bwd_case(M, V, dim, p, BF16)
+    d = kge.Dropout(p, SEED, STEP, TAG) if p else None
+    got = kge.embed_bwd(g.cuda(), ids.cuda(), V, scale=scale, dropout=d)
     _within(got, want, tol + (want.abs() + tol) * U, "embed_bwd")
-    assert torch.equal(got, kge.embed_bwd(g.cuda(), ids.cuda(), V, scale=scale))        # the same sums every time
+    assert torch.equal(got, kge.embed_bwd(g.cuda(), ids.cuda(), V, scale=scale, dropout=d))        # the same sums every time
 
 
 @pytest.mark.parametrize("start,n", [(0, 64), (0, 63), (1, 63), (1, 64), (63, 65), (64, 64), (10, 200), (0, 256)])
-def test_embed_bwd_runs_against_chunks(start, n):
-    """A run of n positions that starts at a given place of the sorted list."""
-    ids = torch.from_numpy(_rng(9, start, n).permutation(np.concatenate([np.zeros(start), np.full(n, 1), np.full(37, 2)])).astype(np.int32))
+@pytest.mark.parametrize("padded", [0, 2100, 17_000])
+def test_embed_bwd_runs_against_chunks(start, n, padded):
+    """A run of n positions that starts at a given place of the sorted list; with padded positions the call is one of those that take chunks of 8 and of 32."""
+    ids = torch.from_numpy(_rng(9, start, n).permutation(np.concatenate([np.zeros(start), np.full(n, 1), np.full(37, 2), np.full(padded, -1)])).astype(np.int32))
     g, ids, scale, want, tol = _bwd_case(ids.numel(), 3, 16, 0.0, F32, 1, ids=ids)
     _within(kge.embed_bwd(g.cuda(), ids.cuda(), 3, scale=scale), want, tol + (want.abs() + tol) * U)
 
