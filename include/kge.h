@@ -453,7 +453,7 @@ size_t kge_encode_workspace_bytes(int op, const kge_encoder_t *enc, int64_t B, i
  * kge_dropout_t: element (row, column) of a matrix is kept iff its 16 random bits are >= thr = round(p * 2^16) (65,535 at most), and is then
  * multiplied by 2^16 / (2^16 - thr).  The bits: Philox4x32-10, key = seed, counter (row, column / 8, step, tag), word (column % 8) / 2, low
  * half for even columns.  The mask is stored nowhere: the backward pass makes it again from the same values.  0 <= p < 1, step < 2^32; with
- * step_counter set (a DEVICE counter, see kge_step_counter_add) the step is step + *step_counter, read when the kernels run.
+ * step_counter set (a DEVICE counter, see kge_step_counter_add) the step is step + *step_counter modulo 2^32, read when the kernels run.
  */
 typedef struct {
     float p;
@@ -473,7 +473,8 @@ int kge_dropout(const void *x, int64_t x_ld, const void *residual, int64_t resid
 
 /*
  * kge_embed: out[i, :] = D_i o (scale * table[ids[i], :]), i < M, in fp32, rounded once to out_dtype; D from `drop` with row i (NULL: no
- * dropout).  ids: device int32[M]; an id outside [0, n_rows) - a padded position - gives a row of zeros.  dim <= 65,536.
+ * dropout).  ids: device int32[M]; an id outside [0, n_rows) - a padded position - gives a row of zeros.  dim <= 65,536.  out must not overlap
+ * the table.
  * kge_embed_bwd: g_table[r, :] = scale * sum over i with ids[i] = r of D_i o g[i, :], rows without a position zeros; with accumulate = 1 it is added
  * to g_table, and rows without a position are neither read nor written.  The positions of a row are added in a fixed order, in fp32, and
  * rounded once to table_dtype: results do not depend on scheduling.  g: [M, dim]; workspace from kge_embed_bwd_workspace_bytes (0 for invalid
@@ -507,7 +508,8 @@ typedef struct {
  * kge_quantize: writes x [rows, cols] quantised by rows (by_row: [rows, cols], blocks of 128 columns) and / or the transposed matrix (by_col:
  * [cols, rows], blocks of 128 rows), padding included; x is read once.  Of a block's finite elements the largest magnitude decides
  * the scale, the smallest power of two that no finite element outgrows the format with; codes are rounded to nearest even.  NaN stays NaN; an
- * infinity stays one in e5m2 and becomes NaN in e4m3.  A block of zeros has scale byte 0.  Both layouts have the same format.
+ * infinity stays one in e5m2 and becomes NaN in e4m3.  A block of zeros has scale byte 0.  Both layouts have the same format and
+ * overlap neither each other nor x.  KGE_E_UNSUPPORTED: by_col with 2^24 and more tiles of 128 x 128.
  */
 int kge_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, const kge_quantized_t *by_row,
                  const kge_quantized_t *by_col, void *hip_stream);
@@ -521,8 +523,10 @@ int kge_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64
  * result on normal values); sums of these groups in fp32, one rounding at the end.  A value that needs more than fp32's range (a block that holds numbers next to the largest
  * fp32 one) overflows.
  * Few rows over many blocks are split along k into partial sums in the workspace, which are added in order: the size to give is
- * kge_matmul_quantized_workspace_bytes (k = a->cols); with less (NULL too) the call takes fewer splits, and sums are associated accordingly.
- * out must not overlap the operands.
+ * kge_matmul_quantized_workspace_bytes (k = a->cols; of that call: a call with more rows may need less, and more than 256 bytes only if it
+ * is split); with less (NULL too) the call takes fewer splits, and sums are associated accordingly.
+ * out must not overlap the operands.  KGE_E_UNSUPPORTED: more than 2^22 tiles of 128 x 128 (where both sides have more than 128 rows and the operands less
+ * than 4 GiB each: of 256 x 256).
  */
 int kge_matmul_quantized(const kge_quantized_t *a, const int32_t *rows, int64_t m, const kge_quantized_t *b, int32_t accumulate, void *out,
                          int32_t out_dtype, int64_t out_ld, void *ws, size_t ws_bytes, void *hip_stream);

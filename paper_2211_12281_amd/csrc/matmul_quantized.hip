@@ -10,6 +10,11 @@
 //                result on normal values (2-norm), 1 / 100 of the output's own rounding.
 //   fp32 output  the codes are widened to bf16 with their scale, which is exact, and multiplied with 32 x 32 x 16 bf16
 //                instructions and fp32 sums: 1e-7, at half the rate.
+//
+// What bounds it: large products the matrix pipe and the clock that it leaves (16,384 x 4,096 x 4,096: bf16 output 230 us, 2.39 PFLOP/s, of
+// which first fragments and the last tiles' stores are a tenth, matrix pipe 62 % busy at 1.9 GHz; fp32 output 425 us, 1.29 PFLOP/s, 73 % busy at 1.78 GHz);
+// products of a few hundred tiles the trips to memory of a tile's start and end (24,576 gathered rows x 256 x 768, fp32 output: 22 us, of which its bytes are 10);
+// one token the weights' bytes or the launch (1 x 2,048 x 2,048 4.1 us, 1 x 4,096 x 16,384 17.4, 3.9 TB/s).
 #include "text_ops.hpp"
 #include <type_traits>
 

@@ -129,5 +129,6 @@ inline bool kge_bad_rows(const void *p, int32_t dtype, int64_t ld, int64_t cols)
 }
 constexpr int64_t KGE_MAX_ROWS = (1ll << 31) - 1, KGE_MAX_LD = 1ll << 31;
 constexpr int KGE_MAX_DIM = 65536;
-// From this size on results are stored past the caches: the L2s hold 32 MB in all
+// From this size on results are stored past the caches (the L2s hold 32 MB in all).  Dropout with residual, past them and through them: 128 MB 65.5 and
+// 82.4 us, 32 MB 16.8 and 19.4, 8 MB 7.6 and 7.7; followed by a reader of the result 128 MB 127 and 140, 64 MB 61.7 and 60.7, 24 MB 26.9 and 27.7.
 constexpr int64_t KGE_STREAM_BYTES = 32ll << 20;
