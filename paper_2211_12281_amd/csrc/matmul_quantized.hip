@@ -532,6 +532,7 @@ constexpr int SPLIT_BLOCKS = 8;
 constexpr int64_t MAX_TILES = 1 << 22;                         // of a launch: a grid has fewer than 2^32 threads
 
 // Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B; stages; whether matrices may be 4 GiB and more
+// (2,816 x 2,816 x 4,096 in tiles of 128 x 128 37.5 us, of 64 x 128 54.8, with three stages, hence one workgroup per compute unit, 43.8.)
 struct Tile { int wm, wn, nj, ni, nst; bool far; };
 constexpr Tile BIG = {2, 4, 4, 2, 2, false}, MID = {2, 2, 2, 2, 2, true};
 constexpr int tile_m(const Tile &t) { return 32 * t.wm * t.nj; }
