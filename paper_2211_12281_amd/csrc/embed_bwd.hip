@@ -1,8 +1,8 @@
 // Gradient of the token lookup:  G[r, :] (+)= scale sum over i with ids[i] = r of D_i o g[i, :]
 //
 //   1. the positions are sorted by row, stable; every row gets the place of its run in the sorted list
-//   2. sums_kernel: sums of the whole chunks (32 or 8 positions) inside one run, and the rows whose runs hold no whole chunk
-//   3. joins_kernel: the other rows: sums of their whole chunks, and the positions in front of and behind them
+//   2. chunks_kernel: sums of the whole chunks (32 or 8 positions) inside one run
+//   3. run_rows_kernel: the rows that hold one: sums of their whole chunks, and the positions in front of and behind them; then all other rows
 // A gradient row is read once and a table row written once (rows without a position as zeros, or with accumulate not at all), every sum is
 // taken in an order that the sorted list alone decides, in fp32, without atomics.
 //
@@ -36,7 +36,7 @@ constexpr int64_t COLLECT_MAX = 32768, WHOLE_MAX = 2048, WHOLE_MAX_DROP = 512, S
 constexpr int MAX_BLOCKS = 256;                               // blocks of ids of a long list: every one adds up the others' counts
 constexpr int CHUNK_BITS = 5, SHORT_CHUNK_BITS = 3;           // a chunk's positions in long and in short lists
 constexpr int ROWS = 4;                                       // rows of a slot, whose runs are looked up together
-// Of a workgroup of joins_kernel: 2^5 groups of columns, so that eight slots share a run, and four chunks (with 2^4 and sixteen, 5,000 positions of 1,024
+// Of a workgroup of run_rows_kernel that joins long runs: 2^5 groups of columns, so that eight slots share a run, and four chunks (with 2^4 and sixteen, 5,000 positions of 1,024
 // columns took 43.6 us and not 34.2, 131,072 took 182 and not 178).
 constexpr int JOIN_LP = 5, JOIN_CHUNKS = 4;
 constexpr uint32_t EMPTY = 0xffffffffu;
@@ -315,8 +315,8 @@ struct SumArgs {
     const void *g; int64_t g_ld; int64_t M;
     void *out; int64_t out_ld; int64_t n_rows;
     int dim, cg, accumulate; float scale; KgeDropDev drop;
-    int64_t chunk_items, row_items;          // workgroups of sums_kernel's two halves
-    int lp;                                  // 2^lp threads take the groups of a row
+    int64_t chunk_items, row_items;          // chunks; workgroups for the short rows
+    int lp, join_lp;                         // 2^lp threads take the groups of a row; of a long run's, 2^join_lp
 };
 
 // s += D_i o g[i, group] of the positions sp[0 .. n), in order, 8 (fp32: 4) rows in flight
@@ -451,63 +451,71 @@ __global__ __launch_bounds__(SORT_NT) void whole_kernel(const SortArgs so, const
     }
 }
 
-template <bool G16, bool OUT16>
-__global__ __launch_bounds__(NT) void sums_kernel(const SumArgs a) {
+// A chunk per workgroup, if it lies inside one run: the slots take its positions in turn.
+template <bool G16>
+__global__ __launch_bounds__(NT) void chunks_kernel(const SumArgs a) {
     __shared__ float red[NT][8];
     const uint32_t step = a.drop.thr ? kge_drop_step(a.drop) : 0u;
     const int per = 1 << a.lp, sub = threadIdx.x >> a.lp, subs = NT >> a.lp, grp0 = threadIdx.x & (per - 1);
-    for (int64_t w = blockIdx.x; w < a.chunk_items + a.row_items; w += gridDim.x) {
-        if (w < a.chunk_items) {                               // a chunk: the slots take its positions in turn
-            const int chunk = 1 << a.lc;
-            const int64_t c0 = w << a.lc;
-            if (c0 + chunk > *a.count || a.sk[c0] != a.sk[c0 + chunk - 1]) continue;      // (equal ends, equal chunk)
-            const int each = chunk / min(subs, chunk);
-            for (int g0 = 0; g0 < a.cg; g0 += per) {
-                const int grp = g0 + grp0;
-                float s[8] = {};
-                if (grp < a.cg && sub * each < chunk) add_rows<G16>(a, step, a.sp + c0 + sub * each, each, grp, s);
-                join_slots<NT>(red, a.lp, s);
-                if (sub == 0 && grp < a.cg) {
-                    float *p = a.part + (w * a.cg + grp) * 8;
-                    *(kge_f32x4 *)p = kge_f32x4{s[0], s[1], s[2], s[3]};
-                    *(kge_f32x4 *)(p + 4) = kge_f32x4{s[4], s[5], s[6], s[7]};
-                }
-            }
-        } else {                                               // ROWS rows per slot
-            const int64_t row0 = ((w - a.chunk_items) * subs + sub) * ROWS;
-            uint32_t k0[ROWS], k1[ROWS];
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                const bool in = row0 + r < a.n_rows && a.M;
-                k0[r] = in ? a.first[row0 + r] : EMPTY; k1[r] = in ? a.last[row0 + r] : EMPTY;
-            }
-#pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                if (row0 + r >= a.n_rows) break;
-                if (k0[r] == EMPTY) {
-                    if (!a.accumulate) zero_row<OUT16>(a, row0 + r, grp0, per);
-                    continue;
-                }
-                if (holds_chunk(k0[r], k1[r], a.lc)) continue;
-                for (int grp = grp0; grp < a.cg; grp += per) {
-                    float s[8] = {};
-                    add_rows<G16>(a, step, a.sp + k0[r], (int)(k1[r] - k0[r]), grp, s);
-                    finish<OUT16>(a, row0 + r, grp, s);
-                }
+    for (int64_t w = blockIdx.x; w < a.chunk_items; w += gridDim.x) {
+        const int chunk = 1 << a.lc;
+        const int64_t c0 = w << a.lc;
+        if (c0 + chunk > *a.count || a.sk[c0] != a.sk[c0 + chunk - 1]) continue;      // (equal ends, equal chunk)
+        const int each = chunk / min(subs, chunk);
+        for (int g0 = 0; g0 < a.cg; g0 += per) {
+            const int grp = g0 + grp0;
+            float s[8] = {};
+            if (grp < a.cg && sub * each < chunk) add_rows<G16>(a, step, a.sp + c0 + sub * each, each, grp, s);
+            join_slots<NT>(red, a.lp, s);
+            if (sub == 0 && grp < a.cg) {
+                float *p = a.part + (w * a.cg + grp) * 8;
+                *(kge_f32x4 *)p = kge_f32x4{s[0], s[1], s[2], s[3]};
+                *(kge_f32x4 *)(p + 4) = kge_f32x4{s[4], s[5], s[6], s[7]};
             }
         }
     }
 }
 
-// One workgroup per JOIN_CHUNKS chunks and 2^lp groups of columns: of the chunks that are a run's first whole one, it adds up the run.
+// ROWS rows per slot: rows without a position, and those whose runs hold no whole chunk
+template <bool G16, bool OUT16> __device__ __forceinline__ void short_rows(const SumArgs &a, uint32_t step, int64_t item) {
+    const int per = 1 << a.lp, sub = threadIdx.x >> a.lp, subs = NT >> a.lp, grp0 = threadIdx.x & (per - 1);
+    const int64_t row0 = (item * subs + sub) * ROWS;
+    uint32_t k0[ROWS], k1[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const bool in = row0 + r < a.n_rows && a.M;
+        k0[r] = in ? a.first[row0 + r] : EMPTY; k1[r] = in ? a.last[row0 + r] : EMPTY;
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        if (row0 + r >= a.n_rows) break;
+        if (k0[r] == EMPTY) {
+            if (!a.accumulate) zero_row<OUT16>(a, row0 + r, grp0, per);
+            continue;
+        }
+        if (holds_chunk(k0[r], k1[r], a.lc)) continue;
+        for (int grp = grp0; grp < a.cg; grp += per) {
+            float s[8] = {};
+            add_rows<G16>(a, step, a.sp + k0[r], (int)(k1[r] - k0[r]), grp, s);
+            finish<OUT16>(a, row0 + r, grp, s);
+        }
+    }
+}
+
+// The rows: first the long runs, one workgroup per JOIN_CHUNKS chunks and 2^join_lp groups of columns: of the chunks that are a run's first whole one, it adds
+// up the run.  Behind them, so that their chains of loads are covered, the short rows.
 template <bool G16, bool OUT16>
-__global__ __launch_bounds__(NT) void joins_kernel(const SumArgs a, int slices) {
+__global__ __launch_bounds__(NT) void run_rows_kernel(const SumArgs a) {
     __shared__ float red[NT][8];
     __shared__ uint32_t found[JOIN_CHUNKS][3];
     const uint32_t step = a.drop.thr ? kge_drop_step(a.drop) : 0u;
-    const int per = 1 << a.lp, sub = threadIdx.x >> a.lp, subs = NT >> a.lp;
-    const int64_t tiles = (a.chunk_items + JOIN_CHUNKS - 1) / JOIN_CHUNKS;
-    for (int64_t w = blockIdx.x; w < tiles * slices; w += gridDim.x) {
+    const int per = 1 << a.join_lp, sub = threadIdx.x >> a.join_lp, subs = NT >> a.join_lp, slices = (a.cg + per - 1) >> a.join_lp;
+    const int64_t joins = (a.chunk_items + JOIN_CHUNKS - 1) / JOIN_CHUNKS * slices;
+    for (int64_t w = blockIdx.x; w < joins + a.row_items; w += gridDim.x) {
+        if (w >= joins) {
+            short_rows<G16, OUT16>(a, step, w - joins);
+            continue;
+        }
         const int64_t tile = w / slices;
         bool owner = false;
         uint32_t row = 0, k0 = 0, k1 = 0;
@@ -551,7 +559,7 @@ __global__ __launch_bounds__(NT) void joins_kernel(const SumArgs a, int slices) 
                 n = share(b1 - (e1 << a.lc), lo);
                 add_rows<G16>(a, step, a.sp + (e1 << a.lc) + lo, (int)n, grp, s);
             }
-            join_slots<NT>(red, a.lp, s);
+            join_slots<NT>(red, a.join_lp, s);
             if (sub == 0 && grp < a.cg) finish<OUT16>(a, r, grp, s);
         }
         __syncthreads();                                       // (found is written again)
@@ -645,16 +653,16 @@ int kge_embed_bwd(const void *g, int32_t g_dtype, int64_t g_ld, const int32_t *i
         hipLaunchKernelGGL(deal_kernel, dim3(s.blocks), dim3(SORT_NT), 0, st, s);
         hipLaunchKernelGGL(parts_kernel<false>, dim3(s.parts), dim3(SORT_NT), 0, st, s);
     } else if (M > 0) hipLaunchKernelGGL(parts_kernel<true>, dim3(s.parts), dim3(SORT_NT), 0, st, s);
-    SumArgs j = a;                                             // long runs: many slots, few columns each
-    if (j.lp > JOIN_LP) j.lp = JOIN_LP;
-    const int slots = NT >> a.lp, slices = (a.cg + (1 << j.lp) - 1) >> j.lp;
-    a.chunk_items = j.chunk_items = M >> a.lc;
+    const int slots = NT >> a.lp;
+    a.join_lp = a.lp < JOIN_LP ? a.lp : JOIN_LP;               // (many slots, few columns each)
+    a.chunk_items = M >> a.lc;
     a.row_items = (n_rows + slots * ROWS - 1) / (slots * ROWS);
-    const dim3 grid = kge_grid_of(a.chunk_items + a.row_items, 1), grid2 = kge_grid_of((a.chunk_items + JOIN_CHUNKS - 1) / JOIN_CHUNKS * slices, 1);
+    const int64_t joins = (a.chunk_items + JOIN_CHUNKS - 1) / JOIN_CHUNKS * ((a.cg + (1 << a.join_lp) - 1) >> a.join_lp);
+    const dim3 chunks = kge_grid_of(a.chunk_items, 1), rows = kge_grid_of(joins + a.row_items, 1);
 #define KGE_BWD(G, O)                                                                                           \
     do {                                                                                                        \
-        hipLaunchKernelGGL((sums_kernel<G, O>), grid, dim3(NT), 0, st, a);                                      \
-        if (a.chunk_items > 0) hipLaunchKernelGGL((joins_kernel<G, O>), grid2, dim3(NT), 0, st, j, slices);     \
+        if (a.chunk_items > 0) hipLaunchKernelGGL(chunks_kernel<G>, chunks, dim3(NT), 0, st, a);                \
+        hipLaunchKernelGGL((run_rows_kernel<G, O>), rows, dim3(NT), 0, st, a);                                      \
     } while (0)
     if (g16 && o16) KGE_BWD(true, true);
     else if (g16) KGE_BWD(true, false);
