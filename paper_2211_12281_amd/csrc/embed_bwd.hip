@@ -11,16 +11,17 @@
 // (256 of them) reads all ids and collects its own, and these two launches fall away.  Short lists: that workgroup goes on to the sums of its rows,
 // and the call is one launch.  Ids outside the table belong to no part and are gone from the list.
 //
-// What bounds it: memory for the rows, at 131,072 positions of 1,024 bf16 columns (half a gigabyte with the touched fp32 rows): sums 120 us, the
-// sort 37 and joins 22; the sort's launches take turns with nothing to hide behind.  The lists are those of text: a handful of rows has most positions, so
+// What bounds it: memory for the rows, at 131,072 positions of 1,024 bf16 columns (half a gigabyte with the touched fp32 rows) 165 us in all; the
+// sort's launches are 37 of them and have nothing to hide behind.  The lists are those of text: a handful of rows has most positions, so
 // no step may depend on a row's positions being few (one workgroup per row, one lane per digit).
 //
-// Rules, both sides measured (microseconds, bf16 gradient, fp32 table of 768 columns; without and with dropout, whose bits are the work of a sum):
-//   one launch      1,024 ids over 300 rows 18.0 against 24.6 in three launches, 2,048 over 30,000 31.9 against 32.6, 4,096 38.5 against 36.2; with dropout
-//                   512 over 300 20.9 against 29.4, 2,048 over 30,000 46.3 against 35.8 (a frequent row's bits are one workgroup's)
-//   collected ids   24,000 61.2 against 66.7 dealt out, 32,768 72.6 against 73.0
-//   chunks of 8     9,000 37.3 against 40.2 in chunks of 32, 24,000 60.9 against 53.2; with dropout 16,384 56.2 against 67.7, 40,000 95.8 against
-//                   89.8
+// Rules, both sides measured (microseconds, bf16 gradient, fp32 table of 768 columns and 30,000 rows where nothing else is said; without and with
+// dropout, whose bits are the work of a sum):
+//   one launch      1,024 ids over 300 rows 18.4 against 23.3 in three launches, 2,048 23.8 against 23.2 (50,000 rows of 256: 21.0 and 24.8), 3,000 over
+//                   300 26.2 against 25.3; with dropout 512 27.1 against 32.6, 1,024 35.5 against 32.3 (a frequent row's bits are one workgroup's)
+//   collected ids   24,000 51.3 against 63.4 dealt out, 32,768 62.0 against 69.9 (where the bits of a thread's own ids end)
+//   chunks of 8     9,000 34.0 against 38.2 in chunks of 32, 24,000 53.5 against 51.4, 50,000 85.7 against 73.3; with dropout 16,384 51.8 against 68.4,
+//                   32,768 72.2 against 84.5, 50,000 over 300 rows 69.8 against 68.6
 #include "text_ops.hpp"
 
 namespace {
@@ -35,10 +36,13 @@ constexpr int DIGIT_BITS = 8;                                 // of a counting p
 constexpr int64_t COLLECT_MAX = 32768, WHOLE_MAX = 2048, WHOLE_MAX_DROP = 512, SHORT_MAX = 16384, SHORT_MAX_DROP = 32768;
 constexpr int MAX_BLOCKS = 256;                               // blocks of ids of a long list: every one adds up the others' counts
 constexpr int CHUNK_BITS = 5, SHORT_CHUNK_BITS = 3;           // a chunk's positions in long and in short lists
-constexpr int ROWS = 4;                                       // rows of a slot, whose runs are looked up together
-// Of a workgroup of run_rows_kernel that joins long runs: 2^5 groups of columns, so that eight slots share a run, and four chunks (with 2^4 and sixteen, 5,000 positions of 1,024
-// columns took 43.6 us and not 34.2, 131,072 took 182 and not 178).
-constexpr int JOIN_LP = 5, JOIN_CHUNKS = 4;
+// Rows of a slot, whose runs are looked up together: one where the table's rows do not fill the chip (300 rows of 1,024 columns, 5,000 ids with dropout: 28.8 us
+// with two rows, 34.6 with four)
+constexpr int ROWS = 4;
+constexpr int64_t FEW_ROWS = 2048;                            // workgroups of one row per slot
+// Of a workgroup of run_rows_kernel that joins long runs: 2^5 groups of columns, so that eight slots share a run, and eight chunks (131,072 x 1,024 with 2^4
+// groups 175 us, not 167; 131,072 x 768 with dropout and four chunks 152, not 150; 5,000 x 256 with sixteen 28, not 23).
+constexpr int JOIN_LP = 5, JOIN_CHUNKS = 8;
 constexpr uint32_t EMPTY = 0xffffffffu;
 
 struct SortArgs {
@@ -316,6 +320,7 @@ struct SumArgs {
     void *out; int64_t out_ld; int64_t n_rows;
     int dim, cg, accumulate; float scale; KgeDropDev drop;
     int64_t chunk_items, row_items;          // chunks; workgroups for the short rows
+    int rows;                                // of a slot among the short rows
     int lp, join_lp;                         // 2^lp threads take the groups of a row; of a long run's, 2^join_lp
 };
 
@@ -476,19 +481,19 @@ __global__ __launch_bounds__(NT) void chunks_kernel(const SumArgs a) {
     }
 }
 
-// ROWS rows per slot: rows without a position, and those whose runs hold no whole chunk
+// a.rows rows per slot: rows without a position, and those whose runs hold no whole chunk
 template <bool G16, bool OUT16> __device__ __forceinline__ void short_rows(const SumArgs &a, uint32_t step, int64_t item) {
     const int per = 1 << a.lp, sub = threadIdx.x >> a.lp, subs = NT >> a.lp, grp0 = threadIdx.x & (per - 1);
-    const int64_t row0 = (item * subs + sub) * ROWS;
+    const int64_t row0 = (item * subs + sub) * a.rows;
     uint32_t k0[ROWS], k1[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-        const bool in = row0 + r < a.n_rows && a.M;
+        const bool in = r < a.rows && row0 + r < a.n_rows && a.M;
         k0[r] = in ? a.first[row0 + r] : EMPTY; k1[r] = in ? a.last[row0 + r] : EMPTY;
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-        if (row0 + r >= a.n_rows) break;
+        if (r >= a.rows || row0 + r >= a.n_rows) break;
         if (k0[r] == EMPTY) {
             if (!a.accumulate) zero_row<OUT16>(a, row0 + r, grp0, per);
             continue;
@@ -656,7 +661,8 @@ int kge_embed_bwd(const void *g, int32_t g_dtype, int64_t g_ld, const int32_t *i
     const int slots = NT >> a.lp;
     a.join_lp = a.lp < JOIN_LP ? a.lp : JOIN_LP;               // (many slots, few columns each)
     a.chunk_items = M >> a.lc;
-    a.row_items = (n_rows + slots * ROWS - 1) / (slots * ROWS);
+    a.rows = n_rows <= FEW_ROWS * slots ? 1 : ROWS;
+    a.row_items = (n_rows + slots * a.rows - 1) / (slots * a.rows);
     const int64_t joins = (a.chunk_items + JOIN_CHUNKS - 1) / JOIN_CHUNKS * ((a.cg + (1 << a.join_lp) - 1) >> a.join_lp);
     const dim3 chunks = kge_grid_of(a.chunk_items, 1), rows = kge_grid_of(joins + a.row_items, 1);
 #define KGE_BWD(G, O)                                                                                           \
