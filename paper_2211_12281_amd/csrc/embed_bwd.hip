@@ -236,13 +236,14 @@ __device__ __forceinline__ void sort_part(const SortArgs &a, PartLds &l) {
         for (int k = tid; k < WAVES << DIGIT_BITS; k += SORT_NT) (&place[0][0])[k] = 0;
         __syncthreads();
         // (one addition per row and 64 ids: lanes that add to one word take turns)
-        constexpr int AHEAD = 8;                              // rounds whose loads are in flight (a frequent row's part is one long list)
+        constexpr int AHEAD = 4;                              // rounds whose loads are in flight (parts of 131,072 ids: 4 21.3 us, 8 21.9, 16 25.3)
         for (uint32_t i0 = w0; i0 < w1; i0 += 64 * AHEAD) {
             uint32_t key[AHEAD];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) key[u] = ki[min(i0 + 64 * u + lane, w1 - 1)];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
+                if (i0 + 64 * u >= w1) break;
                 const bool valid = i0 + 64 * u + lane < w1;
                 const uint32_t d = (key[u] - r0) >> shift & mask;
                 const uint64_t peers = peers_of(d, bits, valid);
