@@ -43,6 +43,10 @@ constexpr int64_t FEW_ROWS = 2048;                            // workgroups of o
 // Of a workgroup of run_rows_kernel that joins long runs: 2^5 groups of columns, so that eight slots share a run, and eight chunks (131,072 x 1,024 with 2^4
 // groups 175 us, not 167; 131,072 x 768 with dropout and four chunks 152, not 150; 5,000 x 256 with sixteen 28, not 23).
 constexpr int JOIN_LP = 5, JOIN_CHUNKS = 8;
+// The table's gradient goes past the caches where it would push the positions' gradient out of them (the last one holds 256 MB) before that is read, and
+// only there, as what stays is what the next step reads: 131,072 ids into 30,000 x 768 101 us past and 126 through them, into 120,000 x 1,024 207 and 241; 65,536
+// into 30,000 x 768 74.0 and 75.1, 32,768 into 50,000 x 768 70.9 and 67.5, 2,000 into 70,000 x 1,024 75.7 and 63.3.
+constexpr int64_t STREAM_READ = 64ll << 20, STREAM_BYTES = 256ll << 20;
 constexpr uint32_t EMPTY = 0xffffffffu;
 
 struct SortArgs {
@@ -319,7 +323,7 @@ struct SumArgs {
     int lc;
     const void *g; int64_t g_ld; int64_t M;
     void *out; int64_t out_ld; int64_t n_rows;
-    int dim, cg, accumulate; float scale; KgeDropDev drop;
+    int dim, cg, accumulate, stream; float scale; KgeDropDev drop;         // stream: the table's rows are stored past the caches
     int64_t chunk_items, row_items;          // chunks; workgroups for the short rows
     int rows;                                // of a slot among the short rows
     int lp, join_lp;                         // 2^lp threads take the groups of a row; of a long run's, 2^join_lp
@@ -371,7 +375,8 @@ template <bool OUT16> __device__ __forceinline__ void finish(const SumArgs &a, i
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e] += o[e];
     }
-    kge_store8<OUT16>(orow, 8 * grp, n, s);
+    if (a.stream) kge_store8<OUT16, true>(orow, 8 * grp, n, s);
+    else kge_store8<OUT16>(orow, 8 * grp, n, s);
 }
 
 // A row of zeros, sixteen bytes per lane side by side (the groups' own stores leave every other sixteen bytes of an fp32 line to a second one)
@@ -379,7 +384,10 @@ template <bool OUT16> __device__ __forceinline__ void zero_row(const SumArgs &a,
     char *orow = (char *)a.out + row * a.out_ld * (OUT16 ? 2 : 4);
     const int whole = a.dim * (OUT16 ? 2 : 4) / 16;
     const kge_u32x4 z = {0u, 0u, 0u, 0u};
-    for (int k = lane; k < whole; k += lanes) *(kge_u32x4_a2 *)(orow + 16 * k) = z;
+    if (a.stream)
+        for (int k = lane; k < whole; k += lanes) __builtin_nontemporal_store(z, (kge_u32x4_a2 *)(orow + 16 * k));
+    else
+        for (int k = lane; k < whole; k += lanes) *(kge_u32x4_a2 *)(orow + 16 * k) = z;
     if (lane == 0)
         for (int c = whole * (OUT16 ? 8 : 4); c < a.dim; ++c) {
             if constexpr (OUT16) ((uint16_t *)orow)[c] = 0;
@@ -643,6 +651,8 @@ int kge_embed_bwd(const void *g, int32_t g_dtype, int64_t g_ld, const int32_t *i
     a.sk = odd ? s.kb : s.ka; a.sp = odd ? s.pb : s.pa; a.count = s.base + s.parts; a.first = s.first; a.last = s.last; a.part = w.part; a.lc = w.lc;
     a.g = g; a.g_ld = g_ld; a.M = M; a.out = g_table; a.out_ld = ld; a.n_rows = n_rows; a.dim = dim; a.cg = (dim + 7) / 8;
     a.accumulate = accumulate; a.scale = scale;
+    const int64_t read = M * dim * (g_dtype == KGE_BF16 ? 2 : 4), written = n_rows * dim * (table_dtype == KGE_BF16 ? 2 : 4);
+    a.stream = !accumulate && read >= STREAM_READ && read + written >= STREAM_BYTES;
     a.lp = bits_of(a.cg);
     if (a.lp > 6) a.lp = 6;
     const bool g16 = g_dtype == KGE_BF16, o16 = table_dtype == KGE_BF16;

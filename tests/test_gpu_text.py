@@ -159,6 +159,21 @@ def test_embed_bwd_runs_against_chunks(start, n, padded):
     _within(kge.embed_bwd(g.cuda(), ids.cuda(), 3, scale=scale), want, tol + (want.abs() + tol) * U)
 
 
+@pytest.mark.parametrize("odt", [F32, BF16])
+def test_embed_bwd_past_the_caches(odt):
+    """A gradient of 90 MB into 200 MB and more, with rows of odd widths and gaps: whole values, exact in any order."""
+    M, V, dim = 45_000, 102_500, 1001
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    g = torch.randint(-2, 3, (M, dim), generator=gen, device="cuda").to(BF16)
+    ids = (torch.rand(M, generator=gen, device="cuda") ** 4 * (V + 1000)).to(torch.int32) - 100
+    ids[::3] = 7
+    out = torch.full((V, dim + 3), 5.0, dtype=odt, device="cuda")
+    kge.embed_bwd(g, ids, V, out=out[:, :dim])
+    ok = (ids >= 0) & (ids < V)
+    want = torch.zeros((V, dim), dtype=torch.float32, device="cuda").index_add_(0, ids[ok].long(), g[ok].float())
+    assert torch.equal(out[:, :dim], want.to(odt)) and bool((out[:, dim:] == 5).all())
+
+
 def test_embed_bwd_only_padded_positions():
     ids = torch.full((100,), -1, dtype=torch.int32, device="cuda")
     g = torch.full((100, 16), float("nan"), device="cuda")
