@@ -11,8 +11,8 @@
 // (256 of them) reads all ids and collects its own, and these two launches fall away.  Short lists: that workgroup goes on to the sums of its rows,
 // and the call is one launch.  Ids outside the table belong to no part and are gone from the list.
 //
-// What bounds it: memory for the rows, at 131,072 positions of 1,024 bf16 columns (half a gigabyte with the touched fp32 rows) 165 us in all; the
-// sort's launches are 37 of them and have nothing to hide behind.  The lists are those of text: a handful of rows has most positions, so
+// What bounds it: memory for the rows, at 131,072 positions of 1,024 bf16 columns (half a gigabyte with the touched fp32 rows) 167 us in all; the
+// sort's launches are 36 of them and have nothing to hide behind.  The lists are those of text: a handful of rows has most positions, so
 // no step may depend on a row's positions being few (one workgroup per row, one lane per digit).
 //
 // Rules, both sides measured (microseconds, bf16 gradient, fp32 table of 768 columns and 30,000 rows where nothing else is said; without and with

@@ -630,7 +630,7 @@ def test_lookup_and_its_gradient_beyond_32_bits():
     assert torch.equal(kge.embed(table, ids).cpu(), v[[4, 2, 0, 3, 1, 4]])
     del table
     g = _values((6, d), F32, 101)
-    for M in (6, 5000):                                                 # (one launch, and three)
+    for M in (6, 5000, 40_000):                                         # (one launch, three, and five)
         more = torch.full((M - 6,), -1, dtype=torch.int32, device="cuda")
         got = kge.embed_bwd(torch.cat([g.cuda(), torch.zeros((M - 6, d), device="cuda")]), torch.cat([ids, more]), n)
         want = torch.stack([g[2], g[4], g[1], g[3], g[0] + g[5]])
