@@ -194,7 +194,8 @@ def _i32(t):
 
 
 class Workspace:
-    """A grow-only device buffer handed to the library as its scratch space."""
+    """A grow-only device buffer handed to the library as its scratch space, for the calls of one stream and one host thread at a time: the kernels of
+    calls that overlap, and a call that runs while another one makes the buffer grow, would write over each other."""
 
     def __init__(self):
         self.buf = None
@@ -604,27 +605,17 @@ def _queue(dev: int, stream) -> int:
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
-_stream_ws: dict = {}
-
-
-def _scratch(ws: Workspace | None, nbytes: int, dev: int, stream):
-    """(pointer, size) of a call's scratch space: of the given workspace, or of one that the library keeps for each device and stream, as
-    calls on two streams run side by side.  A call that is being captured into a graph needs one of its own, large enough before
+def _scratch(ws: Workspace | None, nbytes: int, stream):
+    """A call's scratch space, which the caller holds until the call has returned: the given workspace's buffer, or memory of this call alone.  Torch
+    hands that out again only behind the stream's work, so calls of two host threads, whose launches may alternate on one
+    stream, never share it, and nothing is kept.  A call that is being captured into a graph needs a workspace of its own, large enough before
     the capture begins and kept for that graph: the graph goes on using the address."""
     with _allocating_for(stream):
-        capturing = torch.cuda.is_current_stream_capturing()
-    if capturing:
-        if ws is None or ws.buf is None or ws.buf.numel() < nbytes:
-            raise KgeError(f"a captured call needs a workspace of its own that holds {nbytes} bytes before the capture (ws=Workspace(); ws.get(bytes))")
-        return ws.buf.data_ptr(), ws.buf.numel()
-    if ws is None:
-        key = (dev, _queue(dev, stream))
-        ws = _stream_ws.get(key)
-        if ws is None:
-            ws = _stream_ws[key] = Workspace()
-    with _allocating_for(stream) if ws.buf is None or ws.buf.numel() < nbytes else _nothing:
-        buf = ws.get(nbytes)
-    return buf.data_ptr(), buf.numel()
+        if torch.cuda.is_current_stream_capturing():
+            if ws is None or ws.buf is None or ws.buf.numel() < nbytes:
+                raise KgeError(f"a captured call needs a workspace of its own that holds {nbytes} bytes before the capture (ws=Workspace(); ws.get(bytes))")
+            return ws.buf
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if ws is None else ws.get(nbytes)
 
 
 _nothing = contextlib.nullcontext()
@@ -723,9 +714,9 @@ def embed_bwd(g, ids, n_rows: int, scale: float = 1.0, dropout: Dropout | None =
     if accumulate and out is None:
         raise KgeError("accumulate needs the gradient to add to")
     out, po, do, ldo = _new(out, n_rows, dim, dtype, "kge_embed_bwd", stream)
-    wp, wn = _scratch(ws, _embed_bwd_bytes(M, n_rows, dim), dev, stream)
+    buf = _scratch(ws, max(_embed_bwd_bytes(M, n_rows, dim), 256), stream)
     _check(load().kge_embed_bwd(pg, dg, ldg, _rows_of(ids, M, "ids"), M, scale, dropout.ref if dropout else None, po, do, n_rows, dim, ldo,
-                                1 if accumulate else 0, wp, wn, _queue(dev, stream)), "kge_embed_bwd")
+                                1 if accumulate else 0, buf.data_ptr(), buf.numel(), _queue(dev, stream)), "kge_embed_bwd")
     return out
 
 
@@ -790,7 +781,7 @@ def matmul_quantized(a: Quantized, b: Quantized, rows=None, dtype=torch.bfloat16
         raise KgeError("accumulate needs a matrix to add to")
     out, po, do, ldo = _new(out, m, b.rows, dtype, "kge_matmul_quantized", stream)
     need = _matmul_bytes(m, b.rows, a.cols)
-    wp, wn = _scratch(ws, need, dev, stream) if need > 256 else (None, 0)      # (256: nothing but its alignment)
+    buf = _scratch(ws, need, stream) if need > 256 else None                   # (256: nothing but its alignment)
     _check(load().kge_matmul_quantized(a.ref, None if rows is None else _rows_of(rows, m, "rows"), m, b.ref, 1 if accumulate else 0, po, do, ldo,
-                                       wp, wn, _queue(dev, stream)), "kge_matmul_quantized")
+                                       _ptr(buf), 0 if buf is None else buf.numel(), _queue(dev, stream)), "kge_matmul_quantized")
     return out

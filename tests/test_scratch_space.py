@@ -1,0 +1,118 @@
+"""Scratch space of calls that are given none: calls that run at once - two host threads on torch's default stream, whose launches may alternate -
+never hold the same memory, and it belongs to the stream that the kernels run on.  Decided on the host: the library is a stand-in that
+notes what it is handed, memory comes from the CPU."""
+import contextlib
+import threading
+
+import pytest
+import torch
+
+import paper_2211_12281_amd.binding as b
+
+
+class Streams:
+    """Stands for torch.cuda.stream: notes the stream that is current in each thread."""
+
+    def __init__(self):
+        self.local = threading.local()
+
+    @property
+    def current(self):
+        return getattr(self.local, "stream", None)
+
+    @contextlib.contextmanager
+    def __call__(self, stream):
+        before, self.local.stream = self.current, stream
+        yield
+        self.local.stream = before
+
+
+class Library:
+    """Notes address and size of the scratch space of every call, which returns when `together` calls are in."""
+
+    def __init__(self, together):
+        self.gate, self.seen, self.lock = threading.Barrier(together, timeout=20), [], threading.Lock()
+
+    def __getattr__(self, name):
+        if name.endswith("workspace_bytes"):
+            return lambda *a: 3 << 20
+
+        def call(*args):
+            at = [i for i, x in enumerate(args) if isinstance(x, int) and x >= 3 << 20 and (args[i + 1:i + 2] or [None])[0] == 3 << 20]
+            assert len(at) == 1, (name, args)
+            with self.lock:
+                self.seen.append((args[at[0]], args[at[0] + 1]))
+            self.gate.wait()
+            return 0
+        return call
+
+
+@pytest.fixture
+def on_the_host(monkeypatch):
+    streams, owner, real = Streams(), {}, torch.empty
+
+    def empty(*a, **k):
+        t = real(*a, **{**k, "device": "cpu"})
+        owner[t.data_ptr()] = streams.current
+        return t
+    monkeypatch.setattr(torch, "empty", empty)
+    monkeypatch.setattr(torch.cuda, "stream", streams)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(b, "_here", lambda *t: 0)
+    monkeypatch.setattr(b, "_queue", lambda dev, stream: stream.cuda_stream if stream else 7)
+    monkeypatch.setattr(b, "_embed_bwd_bytes", lambda *a: 3 << 20)
+    monkeypatch.setattr(b, "_matmul_bytes", lambda *a: 3 << 20)
+    return owner
+
+
+class FakeStream:
+    cuda_stream = 11
+
+
+def _embed_bwd(ws=None, stream=None):
+    b.embed_bwd(torch.zeros((5, 8)), torch.zeros(5, dtype=torch.int32), 9, ws=ws, stream=stream)
+
+
+def _matmul(ws=None, stream=None):
+    q = b.Quantized(torch.zeros((5, 128), dtype=torch.uint8), torch.zeros((5, 4), dtype=torch.uint8), 100)
+    b.matmul_quantized(q, q, ws=ws, stream=stream)
+
+
+def _at_once(monkeypatch, calls):
+    lib = Library(len(calls))
+    monkeypatch.setattr(b, "load", lambda: lib)
+    errors = []
+
+    def run(c):
+        try:
+            c()
+        except Exception as e:      # noqa: BLE001
+            errors.append(e)
+    threads = [threading.Thread(target=run, args=(c,)) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    return lib.seen
+
+
+@pytest.mark.parametrize("calls", [(_embed_bwd, _embed_bwd), (_matmul, _matmul), (_embed_bwd, _matmul)])
+def test_text_calls_of_two_threads_hold_memory_of_their_own(monkeypatch, on_the_host, calls):
+    for _ in range(2):                                       # (the second time with what the first one left behind)
+        (p, n), (q, m) = _at_once(monkeypatch, calls)
+        assert p + n <= q or q + m <= p
+
+
+@pytest.mark.parametrize("call", [_embed_bwd, _matmul])
+def test_text_calls_take_memory_of_the_stream_they_run_on(monkeypatch, on_the_host, call):
+    for stream in (None, FakeStream()):
+        ((p, _),) = _at_once(monkeypatch, [lambda: call(stream=stream)])
+        assert on_the_host[p] is stream
+
+
+@pytest.mark.parametrize("call", [_embed_bwd, _matmul])
+def test_a_given_workspace_is_used(monkeypatch, on_the_host, call):
+    ws = b.Workspace()
+    ((p, n),) = _at_once(monkeypatch, [lambda: call(ws=ws)])
+    assert (p, n) == (ws.buf.data_ptr(), ws.buf.numel())
