@@ -152,7 +152,7 @@ class TrainWorkload:
             self.loss_kw["reg_l3"] = reg_l3
         self.main = torch.cuda.current_stream()
         self.eager_now = False
-        self.ws_ent, self.ws_rel, self.ws_relw = kge.Workspace(), kge.Workspace(), kge.Workspace()
+        self.ws, self.ws_ent, self.ws_rel, self.ws_relw = (kge.Workspace() for _ in range(4))
         self.enc = None
         if feat_dim > 0:
             # text features stand-ins: fixed U(-0.5, 0.5) rows; projections start at U(-0.05, 0.05)
@@ -226,7 +226,7 @@ class TrainWorkload:
                 kge.sparse_adam(q["p"], q["sh"], q["m"], q["v"], self.rows_d, gm, lr, step=i + 1)
         else:
             # batches drawn by the sampler: the ids that the update sorts are the ones kge_loss_bwd lists beside its gradient rows
-            kge.loss_bwd(self.model, self.P["loss"], h, r, t, self.neg, out=self.out, stream=self.main, **self.loss_kw)
+            kge.loss_bwd(self.model, self.P["loss"], h, r, t, self.neg, out=self.out, ws=self.ws, stream=self.main, **self.loss_kw)
             plans = [(self.n_ent, self.d, self.out["g_ent_idx"], self.ws_ent), (self.n_rel, self.rel.shape[1], r, self.ws_rel)]
             if self.relw is not None:
                 plans.append((self.n_rel, self.d, r, self.ws_relw))
@@ -258,7 +258,7 @@ class TrainWorkload:
         plans = [(self.n_ent, self.d, ids, self.ws_ent), (self.n_rel, self.rel.shape[1], r, self.ws_rel)]
         if self.relw is not None:
             plans.append((self.n_rel, self.d, r, self.ws_relw))
-        kge.loss_bwd(self.model, self.P["loss"], h, r, t, ids[2 * self.B:], out=self.out, stream=main,
+        kge.loss_bwd(self.model, self.P["loss"], h, r, t, ids[2 * self.B:], out=self.out, ws=self.ws, stream=main,
                      draw=(ks.BASE_SEED, i, ks.TAG_NEG, lo, hi), plans=plans, **self.loss_kw)
         kge.sparse_adam_apply_tables(self._tables(), self.P["lr"], step=i + 1, stream=main)
 
@@ -271,7 +271,7 @@ class TrainWorkload:
         plans = [(self.n_ent, self.d, ids, self.ws_ent), (self.n_rel, self.rel.shape[1], r, self.ws_rel)]
         if self.relw is not None:
             plans.append((self.n_rel, self.d, r, self.ws_relw))
-        kge.loss_bwd(self.model, self.P["loss"], h, r, t, ids[2 * self.B:], out=self.out, stream=main,
+        kge.loss_bwd(self.model, self.P["loss"], h, r, t, ids[2 * self.B:], out=self.out, ws=self.ws, stream=main,
                      draw=(ks.BASE_SEED, 0, ks.TAG_NEG, lo, hi, c), plans=plans, **self.loss_kw)
         kge.sparse_adam_apply_tables(self._tables(), self.P["lr"], step=1, stream=main, step_counter=c)
         kge.step_counter_add(c, 1, stream=main)

@@ -207,7 +207,22 @@ class Workspace:
         return self.buf
 
 
-_default_ws = Workspace()
+_nothing = contextlib.nullcontext()
+
+
+def _allocating_for(stream):
+    """New tensors belong to the stream that writes them: torch may hand their memory to others only behind its work."""
+    return _nothing if stream is None else torch.cuda.stream(stream)
+
+
+def _buffer(ws: Workspace | None, nbytes: int, stream=None):
+    """A call's scratch space, which the caller holds until the call has returned: the given workspace's buffer, or memory of this call alone, of the
+    stream that it runs on.  Torch hands that out again only behind the stream's work, so calls on two streams, and calls of two host
+    threads, whose launches may alternate on one stream, never share it, and nothing is kept."""
+    if ws is not None and ws.buf is not None and ws.buf.numel() >= nbytes:
+        return ws.buf
+    with _allocating_for(stream):
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device="cuda") if ws is None else ws.get(nbytes)
 
 
 class Model:
@@ -276,9 +291,7 @@ def score(model: Model, h, r, t, neg, want_neg: bool = True, ws: Workspace | Non
     B, N = h.numel(), neg.numel()
     pos = torch.empty(B, dtype=torch.float32, device="cuda")
     blk = torch.empty((B, N), dtype=torch.float32, device="cuda") if want_neg else None
-    ws = ws or _default_ws
-    nbytes = workspace_bytes(OP_SCORE, model, B, N)
-    buf = ws.get(nbytes)
+    buf = _buffer(ws, workspace_bytes(OP_SCORE, model, B, N))
     _check(load().kge_score(model.ref, _ptr(_i32(h)), _ptr(_i32(r)), _ptr(_i32(t)), B, _ptr(_i32(neg)), N,
                             _ptr(pos), _ptr(blk), _ptr(buf), buf.numel(), _stream()), "kge_score")
     return pos, blk
@@ -302,8 +315,7 @@ def loss_bwd(model: Model, loss: str, h, r, t, neg, gamma: float = 0.0, adv_temp
             "g_rel_idx": torch.empty(B, dtype=torch.int32, device="cuda"),
         }
     cfg = KgeLossCfgT(LOSSES[loss], gamma, adv_temp, loss_scale, n_ent_for_c, reg_l3, 0)
-    ws = ws or _default_ws
-    buf = ws.get(workspace_bytes(OP_LOSS_BWD, model, B, N))
+    buf = _buffer(ws, workspace_bytes(OP_LOSS_BWD, model, B, N), stream)
     if draw is not None:
         assert neg.is_cuda and neg.dtype == torch.int32 and neg.is_contiguous()
         dr = KgeNegDrawT(draw[0], draw[1], _counter(draw[5]) if len(draw) > 5 else None, draw[2], 0, draw[3], draw[4])
@@ -337,8 +349,7 @@ def sparse_adam(param, shadow, m, v, idx, grads, lr: float, beta1: float = 0.9, 
         assert shadow.dtype == torch.bfloat16 and shadow.stride() == param.stride()
     M, d = idx.numel(), param.shape[1]
     cfg = KgeAdamCfgT(lr, beta1, beta2, eps, step, _counter(step_counter))
-    ws = ws or _default_ws
-    buf = ws.get(workspace_bytes(OP_SPARSE_ADAM, None, M, d))
+    buf = _buffer(ws, workspace_bytes(OP_SPARSE_ADAM, None, M, d))
     _check(load().kge_sparse_adam(_ptr(param), _ptr(shadow), _ptr(m), _ptr(v), param.shape[0], d, param.stride(0),
                                   _ptr(_i32(idx)), _ptr(grads), M, C.byref(cfg), _ptr(buf), buf.numel(), _stream()),
            "kge_sparse_adam")
@@ -424,8 +435,7 @@ def topk(model: Model, h, r, cand_lo: int, cand_hi: int, K: int, true_t=None, ws
     out_idx = torch.empty((Q, K), dtype=torch.int32, device="cuda")
     out_score = torch.empty((Q, K), dtype=torch.float32, device="cuda")
     rank = torch.empty(Q, dtype=torch.int64, device="cuda") if true_t is not None else None
-    ws = ws or _default_ws
-    buf = ws.get(workspace_bytes(OP_TOPK, model, Q, cand_hi - cand_lo, K))
+    buf = _buffer(ws, workspace_bytes(OP_TOPK, model, Q, cand_hi - cand_lo, K))
     _check(load().kge_topk(model.ref, _ptr(_i32(h)), _ptr(_i32(r)), Q, cand_lo, cand_hi, K, _ptr(out_idx),
                            _ptr(out_score), _ptr(true_t), _ptr(rank), _ptr(buf), buf.numel(), _stream()), "kge_topk")
     return out_idx, out_score, rank
@@ -493,8 +503,7 @@ def partition_triples(h, t, part_size: int, D: int, ws: Workspace | None = None)
     n = h.numel()
     offsets = torch.empty(D * D + 1, dtype=torch.int64, device="cuda")
     order = torch.empty(n, dtype=torch.int64, device="cuda")
-    ws = ws or _default_ws
-    buf = ws.get(workspace_bytes(OP_PARTITION, None, n, D))
+    buf = _buffer(ws, workspace_bytes(OP_PARTITION, None, n, D))
     _check(load().kge_partition_triples(_ptr(_i32(h)), _ptr(_i32(t)), n, part_size, D, _ptr(offsets), _ptr(order),
                                         _ptr(buf), buf.numel(), _stream()), "kge_partition_triples")
     return offsets, order
@@ -510,8 +519,7 @@ class TripleSampler:
         self.order = torch.empty(max(n, 1), dtype=torch.int64, device="cuda")[:n]
         self.rel_offsets = torch.empty(groups + 1, dtype=torch.int64, device="cuda")
         self.cdf = torch.empty(groups, dtype=torch.int64, device="cuda")       # bit pattern of uint64
-        ws = ws or _default_ws
-        buf = ws.get(workspace_bytes(OP_SAMPLER_BUILD, None, n, D))
+        buf = _buffer(ws, workspace_bytes(OP_SAMPLER_BUILD, None, n, D))
         _check(load().kge_sampler_build(_ptr(self.h), _ptr(self.r), _ptr(self.t), n, part_size, D, n_rel,
                                         _ptr(self.order), _ptr(self.rel_offsets), _ptr(self.cdf), _ptr(buf),
                                         buf.numel(), _stream()), "kge_sampler_build")
@@ -553,11 +561,10 @@ class Encoder:
                                m_h.stride(0), dropout, reg_t, reg_s, reg_f)
 
     def _ws(self, op, B, N, ws):
-        ws = ws or _default_ws
         n = load().kge_encode_workspace_bytes(op, C.byref(self.ref), B, N)
         if n == 0:
             raise KgeError("kge_encode_workspace_bytes: invalid arguments")
-        return ws.get(n)
+        return _buffer(ws, n)
 
     def encode(self, h, t, neg, seed: int = 0, step: int = 0, ws: Workspace | None = None):
         """(e [(2B+N), dim] in the table dtype, proj fp32 [(2B+N), dim], reg fp32 [1])."""
@@ -606,24 +613,13 @@ def _queue(dev: int, stream) -> int:
 
 
 def _scratch(ws: Workspace | None, nbytes: int, stream):
-    """A call's scratch space, which the caller holds until the call has returned: the given workspace's buffer, or memory of this call alone.  Torch
-    hands that out again only behind the stream's work, so calls of two host threads, whose launches may alternate on one
-    stream, never share it, and nothing is kept.  A call that is being captured into a graph needs a workspace of its own, large enough before
-    the capture begins and kept for that graph: the graph goes on using the address."""
+    """The same for a call that may be captured into a graph: then it needs a workspace of its own, large enough before the capture
+    begins and kept for that graph, which goes on using the address."""
     with _allocating_for(stream):
-        if torch.cuda.is_current_stream_capturing():
-            if ws is None or ws.buf is None or ws.buf.numel() < nbytes:
-                raise KgeError(f"a captured call needs a workspace of its own that holds {nbytes} bytes before the capture (ws=Workspace(); ws.get(bytes))")
-            return ws.buf
-        return torch.empty(nbytes, dtype=torch.uint8, device="cuda") if ws is None else ws.get(nbytes)
-
-
-_nothing = contextlib.nullcontext()
-
-
-def _allocating_for(stream):
-    """New tensors belong to the stream that writes them: torch may hand their memory to others only behind its work."""
-    return _nothing if stream is None else torch.cuda.stream(stream)
+        capturing = torch.cuda.is_current_stream_capturing()
+    if capturing and (ws is None or ws.buf is None or ws.buf.numel() < nbytes):
+        raise KgeError(f"a captured call needs a workspace of its own that holds {nbytes} bytes before the capture (ws=Workspace(); ws.get(bytes))")
+    return _buffer(ws, nbytes, stream)
 
 
 def _matrix(t, what: str):
@@ -714,7 +710,7 @@ def embed_bwd(g, ids, n_rows: int, scale: float = 1.0, dropout: Dropout | None =
     if accumulate and out is None:
         raise KgeError("accumulate needs the gradient to add to")
     out, po, do, ldo = _new(out, n_rows, dim, dtype, "kge_embed_bwd", stream)
-    buf = _scratch(ws, max(_embed_bwd_bytes(M, n_rows, dim), 256), stream)
+    buf = _scratch(ws, _embed_bwd_bytes(M, n_rows, dim), stream)
     _check(load().kge_embed_bwd(pg, dg, ldg, _rows_of(ids, M, "ids"), M, scale, dropout.ref if dropout else None, po, do, n_rows, dim, ldo,
                                 1 if accumulate else 0, buf.data_ptr(), buf.numel(), _queue(dev, stream)), "kge_embed_bwd")
     return out

@@ -116,3 +116,84 @@ def test_a_given_workspace_is_used(monkeypatch, on_the_host, call):
     ws = b.Workspace()
     ((p, n),) = _at_once(monkeypatch, [lambda: call(ws=ws)])
     assert (p, n) == (ws.buf.data_ptr(), ws.buf.numel())
+
+
+# ---------------------------------------------------------------------------------------------
+# the path's calls
+# ---------------------------------------------------------------------------------------------
+def _ids(n):
+    return torch.zeros(n, dtype=torch.int32)
+
+
+def _model():
+    m = object.__new__(b.Model)
+    m.struct, m.dim, m.rel, m.relw = b.KgeModelT(), 8, torch.zeros((3, 8)), None
+    return m
+
+
+def _score(ws=None):
+    b.score(_model(), _ids(4), _ids(4), _ids(4), _ids(6), ws=ws)
+
+
+def _loss_bwd(ws=None, stream=None):
+    b.loss_bwd(_model(), "logsigmoid", _ids(4), _ids(4), _ids(4), _ids(6), ws=ws, stream=stream)
+
+
+def _sparse_adam(ws=None):
+    b.sparse_adam(torch.zeros((9, 8)), None, torch.zeros((9, 8)), torch.zeros((9, 8)), _ids(4), torch.zeros((4, 8)), 0.1, ws=ws)
+
+
+def _topk(ws=None):
+    b.topk(_model(), _ids(4), _ids(4), 0, 9, 2, ws=ws)
+
+
+def _partition(ws=None):
+    b.partition_triples(_ids(4), _ids(4), 3, 2, ws=ws)
+
+
+def _sampler(ws=None):
+    b.TripleSampler(_ids(4), _ids(4), _ids(4), 3, 2, 3, ws=ws)
+
+
+def _encoder():
+    e = object.__new__(b.Encoder)
+    e.ref, e.ent_s, e.dim, e.feat_dim = b.KgeEncoderT(), torch.zeros((9, 8)), 8, 16
+    return e
+
+
+def _encode(ws=None):
+    _encoder().encode(_ids(4), _ids(4), _ids(6), ws=ws)
+
+
+def _encode_bwd(ws=None):
+    _encoder().encode_bwd(_ids(4), _ids(4), _ids(6), torch.zeros((14, 8)), torch.zeros((14, 8)), ws=ws)
+
+
+PATH = [_score, _loss_bwd, _sparse_adam, _topk, _partition, _sampler, _encode, _encode_bwd]
+
+
+@pytest.fixture
+def path_on_the_host(monkeypatch, on_the_host):
+    monkeypatch.setattr(b, "_i32", lambda t: t)
+    monkeypatch.setattr(b, "_stream", lambda stream=None: stream.cuda_stream if stream else 7)
+    return on_the_host
+
+
+@pytest.mark.parametrize("call", PATH)
+def test_calls_of_two_threads_hold_memory_of_their_own(monkeypatch, path_on_the_host, call):
+    for other in (call, _embed_bwd, _score):
+        (p, n), (q, m) = _at_once(monkeypatch, [call, other])
+        assert p + n <= q or q + m <= p
+
+
+@pytest.mark.parametrize("call", PATH)
+def test_a_workspace_given_to_the_path_is_used(monkeypatch, path_on_the_host, call):
+    ws = b.Workspace()
+    ((p, n),) = _at_once(monkeypatch, [lambda: call(ws=ws)])
+    assert (p, n) == (ws.buf.data_ptr(), ws.buf.numel())
+
+
+def test_loss_bwd_takes_memory_of_the_stream_it_runs_on(monkeypatch, path_on_the_host):
+    stream = FakeStream()
+    ((p, _),) = _at_once(monkeypatch, [lambda: _loss_bwd(stream=stream)])
+    assert path_on_the_host[p] is stream
