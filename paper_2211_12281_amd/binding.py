@@ -274,7 +274,8 @@ def step_counter_add(counter, inc: int = 1, stream=None):
 def sample_negatives_dev(seed: int, counter, step_offset: int, tag: int, lo: int, hi: int, n: int, out=None, stream=None):
     """kge_sample_negatives_dev: the ids of step step_offset + counter[0], the counter being read on the device."""
     if out is None:
-        out = torch.empty(n, dtype=torch.int32, device="cuda")
+        with _allocating_for(stream):
+            out = torch.empty(n, dtype=torch.int32, device="cuda")
     _check(load().kge_sample_negatives_dev(seed, _counter(counter), step_offset, tag, lo, hi, n, _ptr(out), _stream(stream)),
            "kge_sample_negatives_dev")
     return out
@@ -282,7 +283,8 @@ def sample_negatives_dev(seed: int, counter, step_offset: int, tag: int, lo: int
 
 def sample_negatives(seed: int, step: int, tag: int, lo: int, hi: int, n: int, out=None, stream=None):
     if out is None:
-        out = torch.empty(n, dtype=torch.int32, device="cuda")
+        with _allocating_for(stream):
+            out = torch.empty(n, dtype=torch.int32, device="cuda")
     _check(load().kge_sample_negatives(seed, step, tag, lo, hi, n, _ptr(out), _stream(stream)), "kge_sample_negatives")
     return out
 
@@ -306,14 +308,15 @@ def loss_bwd(model: Model, loss: str, h, r, t, neg, gamma: float = 0.0, adv_temp
     B, N, d = h.numel(), neg.numel(), model.dim
     k = model.rel.shape[1]
     if out is None:
-        out = {
-            "loss": torch.empty(1, dtype=torch.float32, device="cuda"),
-            "g_ent": torch.empty((2 * B + N, d), dtype=torch.float32, device="cuda"),
-            "g_ent_idx": torch.empty(2 * B + N, dtype=torch.int32, device="cuda"),
-            "g_rel": torch.empty((B, k), dtype=torch.float32, device="cuda"),
-            "g_relw": torch.empty((B, d), dtype=torch.float32, device="cuda") if model.relw is not None else None,
-            "g_rel_idx": torch.empty(B, dtype=torch.int32, device="cuda"),
-        }
+        with _allocating_for(stream):
+            out = {
+                "loss": torch.empty(1, dtype=torch.float32, device="cuda"),
+                "g_ent": torch.empty((2 * B + N, d), dtype=torch.float32, device="cuda"),
+                "g_ent_idx": torch.empty(2 * B + N, dtype=torch.int32, device="cuda"),
+                "g_rel": torch.empty((B, k), dtype=torch.float32, device="cuda"),
+                "g_relw": torch.empty((B, d), dtype=torch.float32, device="cuda") if model.relw is not None else None,
+                "g_rel_idx": torch.empty(B, dtype=torch.int32, device="cuda"),
+            }
     cfg = KgeLossCfgT(LOSSES[loss], gamma, adv_temp, loss_scale, n_ent_for_c, reg_l3, 0)
     buf = _buffer(ws, workspace_bytes(OP_LOSS_BWD, model, B, N), stream)
     if draw is not None:

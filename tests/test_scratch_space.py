@@ -197,3 +197,14 @@ def test_loss_bwd_takes_memory_of_the_stream_it_runs_on(monkeypatch, path_on_the
     stream = FakeStream()
     ((p, _),) = _at_once(monkeypatch, [lambda: _loss_bwd(stream=stream)])
     assert path_on_the_host[p] is stream
+
+
+@pytest.mark.parametrize("stream", [None, FakeStream()])
+def test_outputs_belong_to_the_stream_that_writes_them(monkeypatch, path_on_the_host, stream):
+    calls = [lambda: [b.sample_negatives(1, 2, 3, 0, 9, 5, stream=stream)],
+             lambda: [b.sample_negatives_dev(1, None, 2, 3, 0, 9, 5, stream=stream)],
+             lambda: list(filter(torch.is_tensor, b.loss_bwd(_model(), "logsigmoid", _ids(4), _ids(4), _ids(4), _ids(6), stream=stream).values()))]
+    monkeypatch.setattr(b, "load", lambda: type("Lib", (), {"__getattr__": lambda self, name: lambda *a: 3 << 20 if name.endswith("bytes") else 0})())
+    for call in calls:
+        for t in call():
+            assert path_on_the_host[t.data_ptr()] is stream
