@@ -74,9 +74,10 @@ __global__ __launch_bounds__(NT) void rows_kernel(const RowsArgs a) {
 #pragma unroll
             for (int u = 0; u < UNROLL; ++u) {
                 if (!in[u]) continue;
-                if constexpr (LOOKUP) {
+                if constexpr (LOOKUP) {                        // (a row of zeros stays one whatever the scale is)
+                    const float scale = src[u] >= 0 && src[u] < a.n_rows ? a.scale : 0.f;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[u][e] *= a.scale;
+                    for (int e = 0; e < 8; ++e) v[u][e] *= scale;
                 }
                 if (a.drop.thr) kge_drop8(a.drop, step, (uint32_t)(r0 + row[u]), (uint32_t)grp[u], v[u]);
                 if constexpr (!LOOKUP)

@@ -42,3 +42,16 @@ def test_two_threads_on_one_stream():
     assert not errors, errors
     for k, out in got[0] + got[1]:
         assert torch.equal(out, want[k])
+
+
+@pytest.mark.parametrize("p", [0.0, 0.5])
+@pytest.mark.parametrize("dt,odt", [(F32, F32), (BF16, F32), (F32, BF16), (BF16, BF16)])
+@pytest.mark.parametrize("scale", [float("inf"), float("nan"), -2.0])
+def test_padded_positions_are_zeros_whatever_the_scale(scale, dt, odt, p):
+    table = torch.randn((4, 23), device="cuda").to(dt)
+    ids = torch.tensor([0, -1, 4, 3, -2**31, 2**31 - 1], dtype=torch.int32, device="cuda")
+    out = kge.embed(table, ids, scale=scale, dropout=kge.Dropout(p, 1) if p else None, dtype=odt).float()
+    dead = out[[1, 2, 4, 5]]
+    assert not bool(dead.any()) and not bool(torch.signbit(dead).any())
+    if not p:
+        assert torch.equal(torch.nan_to_num(out[[0, 3]], 7.0), torch.nan_to_num((table[[0, 3]].float() * scale).to(odt).float(), 7.0))
