@@ -518,7 +518,9 @@ int kge_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64
  * kge_matmul_quantized: out[i, j] = sum over k of a[rows[i], k] * b[j, k], i < m, j < b->rows; rows NULL: row i itself (m = a->rows); a row
  * number outside [0, a->rows) gives a row of zeros.  With accumulate = 1 the product is added to out.  A layer y = x W^t is (x by row, W by
  * row), its dx = dy W (dy by row, W by column), dW = dy^t x (dy by column, x by column).
- * Arithmetic: out_dtype KGE_F32: the codes widened exactly to bf16, fp32 sums on the bf16 matrix cores.  KGE_BF16: the 8-bit
+ * Arithmetic: out_dtype KGE_F32: the codes widened with their scale to bf16, fp32 sums on the bf16 matrix cores.  Widening is exact under scale bytes
+ * 3..246 (e4m3) and 10..239 (e5m2); below them an element is rounded to a multiple of 2^-133, above them one of 2^128 and more
+ * is infinite.  KGE_BF16: the 8-bit
  * matrix cores, twice as fast, which align every eight products to the largest of them and drop what lies 2^-13 below it (1.4e-5 of the
  * result on normal values); sums of these groups in fp32, one rounding at the end.  A value that needs more than fp32's range (a block that holds numbers next to the largest
  * fp32 one) overflows.

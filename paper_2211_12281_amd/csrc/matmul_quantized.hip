@@ -8,8 +8,10 @@
 //   bf16 output  32 x 32 x 64 matrix instructions on the 8-bit codes themselves, which take the scales as exponent bytes.  They align
 //                every eight products to the largest of them and drop what lies 13 bits below it (groups are added in fp32): 1.4e-5 of the
 //                result on normal values (2-norm), 1 / 100 of the output's own rounding.
-//   fp32 output  the codes are widened to bf16 with their scale, which is exact, and multiplied with 32 x 32 x 16 bf16
-//                instructions and fp32 sums: 1e-7, at half the rate.
+//   fp32 output  the codes are widened to bf16 with their scale and multiplied with 32 x 32 x 16 bf16 instructions and fp32 sums: 1e-7, at half
+//                the rate.  Widening is exact for every code under scale bytes 3..246 (e4m3) or 10..239 (e5m2); below, what is no multiple of
+//                2^-133, bf16's smallest number, is rounded to one, and above, codes of 2^128 and more become infinite.  (The 8-bit
+//                instructions add the scales' exponents and know neither end.)
 //
 // What bounds it: large products the matrix pipe and the clock that it leaves (16,384 x 4,096 x 4,096: bf16 output 230 us, 2.39 PFLOP/s, of
 // which first fragments and the last tiles' stores are a tenth, matrix pipe 62 % busy at 1.9 GHz; fp32 output 425 us, 1.29 PFLOP/s, 73 % busy at 1.78 GHz);

@@ -55,3 +55,37 @@ def test_padded_positions_are_zeros_whatever_the_scale(scale, dt, odt, p):
     assert not bool(dead.any()) and not bool(torch.signbit(dead).any())
     if not p:
         assert torch.equal(torch.nan_to_num(out[[0, 3]], 7.0), torch.nan_to_num((table[[0, 3]].float() * scale).to(odt).float(), 7.0))
+
+
+FLOAT8 = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("m", [16, 1280])                       # (few rows, tiles)
+@pytest.mark.parametrize("side", ["a", "b"])
+@pytest.mark.parametrize("fmt,exact", [("e4m3", range(3, 247)), ("e5m2", range(10, 240))])
+def test_product_of_every_code_under_scales_from_end_to_end(fmt, exact, side, m, dt):
+    """One code times a power of two that brings it back into range.  fp32 output: exact under the bytes of `exact`; below them the element is rounded to a
+    multiple of 2^-133 (off by half of one), above them infinite from 2^128 on.  bf16 output: exact, as such a product has four bits at most."""
+    codes = torch.zeros((1280, 128), dtype=torch.uint8, device="cuda")
+    codes[:, 5] = (torch.arange(1280, device="cuda") % 256).to(torch.uint8)
+    value = codes[:256, 5].cpu().view(FLOAT8[fmt]).double()
+    ones = torch.zeros((1280, 128), dtype=torch.uint8, device="cuda")
+    ones[:, 5] = 0x38                                           # 1 in e4m3
+    for s in (*range(0, 14), 120, 127, *range(236, 255)):
+        t = min(254 - s, 246)                                   # (code * 2^(s + t - 254): in range)
+        scales = [torch.zeros((1280, 4), dtype=torch.uint8, device="cuda") for _ in range(2)]
+        scales[0][:, 0], scales[1][:, 0] = s, t
+        q, one = kge.Quantized(codes, scales[0], 128, fmt), kge.Quantized(ones[:m], scales[1][:m], 128)
+        got = kge.matmul_quantized(q, one, dtype=dt)[:256, 0] if side == "a" else kge.matmul_quantized(one, q, dtype=dt)[0, :256]
+        got, element, want = got.double().cpu(), value * 2.0 ** (s - 127), value * 2.0 ** (s + t - 254)
+        assert torch.equal(torch.isnan(got), torch.isnan(want)), s
+        ok = torch.isfinite(want)
+        if dt == F32:
+            big = ok & (element.abs() >= 2.0 ** 128)
+            assert torch.equal(got[big], want[big] * float("inf")) and (not bool(big.any()) or s > exact[-1])
+            ok &= ~big
+            tol = torch.zeros_like(want) if s in exact or s > exact[-1] else torch.full_like(want, 2.0 ** -134 * 2.0 ** (t - 127))
+        else:
+            tol = torch.zeros_like(want)                        # (four bits times a power of two)
+        assert bool(((got - want).abs() <= tol)[ok].all()), s
