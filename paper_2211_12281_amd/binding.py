@@ -599,6 +599,7 @@ class Encoder:
 # ---------------------------------------------------------------------------------------------
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1}
 _CODES = {"e4m3": 0, "e5m2": 1}
+KGE_FP32_SUMS = 0x100
 
 
 def _here(*tensors) -> int:
@@ -772,13 +773,16 @@ def quantize(x, fmt: str = "e4m3", by: str = "row", out=None, stream=None):
 
 
 def matmul_quantized(a: Quantized, b: Quantized, rows=None, dtype=torch.bfloat16, out=None, accumulate: bool = False,
-                     ws: Workspace | None = None, stream=None):
-    """kge_matmul_quantized: a[rows] b^t in fp32 or bf16; accumulate: added to `out`."""
+                     ws: Workspace | None = None, stream=None, fp32_sums: bool = False):
+    """kge_matmul_quantized: a[rows] b^t in fp32 or bf16; accumulate: added to `out`.  A bf16 result comes from the 8-bit matrix cores, whose sums are
+    shorter than fp32's, unless fp32_sums asks for the arithmetic of an fp32 result (half the rate where the matrix cores are the bound)."""
     dev = _here(a.codes, a.scales, b.codes, b.scales, rows, out)
     m = a.rows if rows is None else rows.numel()
     if accumulate and out is None:
         raise KgeError("accumulate needs a matrix to add to")
     out, po, do, ldo = _new(out, m, b.rows, dtype, "kge_matmul_quantized", stream)
+    if fp32_sums and do == 1:
+        do |= KGE_FP32_SUMS
     need = _matmul_bytes(m, b.rows, a.cols)
     buf = _scratch(ws, need, stream) if need > 256 else None                   # (256: nothing but its alignment)
     _check(load().kge_matmul_quantized(a.ref, None if rows is None else _rows_of(rows, m, "rows"), m, b.ref, 1 if accumulate else 0, po, do, ldo,

@@ -5,10 +5,11 @@
 // The rows of A may be gathered (rows): the projection of the features of a step's slots reads them straight from the entities' table.
 //
 // Two kinds of products:
-//   bf16 output  32 x 32 x 64 matrix instructions on the 8-bit codes themselves, which take the scales as exponent bytes.  They align
+//   bf16 output  (unless fp32 sums are asked for) 32 x 32 x 64 matrix instructions on the 8-bit codes themselves, which take the scales as exponent bytes.  They align
 //                every eight products to the largest of them and drop what lies 13 bits below it (groups are added in fp32): 1.4e-5 of the
-//                result on normal values (2-norm), 1 / 100 of the output's own rounding.
-//   fp32 output  the codes are widened to bf16 with their scale and multiplied with 32 x 32 x 16 bf16 instructions and fp32 sums: 1e-7, at half
+//                result on normal values (2-norm), 1 / 100 of the output's own rounding.  Where products cancel the cut stays: up to 7 x 2^-13 of the largest
+//                of each eight.
+//   fp32 sums    the codes are widened to bf16 with their scale and multiplied with 32 x 32 x 16 bf16 instructions and fp32 sums: 1e-7, at half
 //                the rate.  Widening is exact for every code under scale bytes 3..246 (e4m3) or 10..239 (e5m2); below, what is no multiple of
 //                2^-133, bf16's smallest number, is rounded to one, and above, codes of 2^128 and more become infinite.  (The 8-bit
 //                instructions add the scales' exponents and know neither end.)
@@ -602,7 +603,10 @@ size_t kge_matmul_quantized_workspace_bytes(int64_t m, int64_t n, int64_t k) {
 int kge_matmul_quantized(const kge_quantized_t *a, const int32_t *rows, int64_t m, const kge_quantized_t *b, int32_t accumulate, void *out,
                          int32_t out_dtype, int64_t out_ld, void *ws, size_t ws_bytes, void *hip_stream) {
     if (kge_check_quantized(a) != KGE_OK || kge_check_quantized(b) != KGE_OK || a->cols != b->cols || m < 0 || m >= (1ll << 31) ||
-        (!rows && m != a->rows) || ((uintptr_t)rows & 3) != 0 || (accumulate != 0 && accumulate != 1) || (out_dtype != KGE_F32 && out_dtype != KGE_BF16)) return KGE_E_INVALID_ARG;
+        (!rows && m != a->rows) || ((uintptr_t)rows & 3) != 0 || (accumulate != 0 && accumulate != 1)) return KGE_E_INVALID_ARG;
+    const bool wide = out_dtype != KGE_BF16;
+    if (out_dtype == (KGE_BF16 | KGE_FP32_SUMS)) out_dtype = KGE_BF16;
+    if (out_dtype != KGE_F32 && out_dtype != KGE_BF16) return KGE_E_INVALID_ARG;
     if (m == 0 || b->rows == 0) return KGE_OK;
     if (!out || out_ld < b->rows || out_ld >= (1ll << 31) || ((uintptr_t)out & (out_dtype == KGE_BF16 ? 1 : 3)) != 0) return KGE_E_INVALID_ARG;
     MatmulArgs p = {};
@@ -623,8 +627,8 @@ int kge_matmul_quantized(const kge_quantized_t *a, const int32_t *rows, int64_t 
 #define KGE_MQ(W)                                                                                                                        \
     (a4 ? (b4 ? launch<W, KGE_E4M3, KGE_E4M3>(p, q, st) : launch<W, KGE_E4M3, KGE_E5M2>(p, q, st))                                      \
         : (b4 ? launch<W, KGE_E5M2, KGE_E4M3>(p, q, st) : launch<W, KGE_E5M2, KGE_E5M2>(p, q, st)))
-    if (p.out16) KGE_MQ(false);
-    else KGE_MQ(true);
+    if (wide) KGE_MQ(true);
+    else KGE_MQ(false);
 #undef KGE_MQ
     return kge_launch_status();
 }

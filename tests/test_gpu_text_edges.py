@@ -89,3 +89,25 @@ def test_product_of_every_code_under_scales_from_end_to_end(fmt, exact, side, m,
         else:
             tol = torch.zeros_like(want)                        # (four bits times a power of two)
         assert bool(((got - want).abs() <= tol)[ok].all()), s
+
+
+def _cancelling(m, n, k):
+    """64 * 64 - 64 * 64 + 2^-3 beside zeros, in different places of the rows: 2^-3 whatever the order of fp32 sums."""
+    a, b = torch.zeros((m, k), device="cuda"), torch.zeros((n, k), device="cuda")
+    a[:, 0], a[:, 1], a[:, 2], b[:, 0], b[:, 1], b[:, 2] = 64, 64, 0.5, 64, -64, 0.25
+    return kge.quantize(a), kge.quantize(b)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 300, 100), (16, 4096, 1000), (40, 300, 700), (300, 700, 900), (1100, 900, 260), (140, 500, 4100), (4100, 4090, 300)])
+def test_bf16_output_with_fp32_sums(m, n, k):
+    """The sums of the fp32 output, rounded once, from every kernel: few rows, tiles, split and whole, large tiles; gathered and added too."""
+    gen = torch.Generator(device="cuda").manual_seed(m + n)
+    a, b = (kge.quantize(torch.randn((r, k), generator=gen, device="cuda")) for r in (m, n))
+    assert torch.equal(kge.matmul_quantized(a, b, fp32_sums=True), kge.matmul_quantized(a, b, dtype=F32).to(BF16))
+    rows = torch.randint(-1, m + 1, (m,), generator=gen, device="cuda", dtype=torch.int32)
+    got = kge.matmul_quantized(a, b, rows=rows, fp32_sums=True, out=torch.ones((m, n), dtype=BF16, device="cuda"), accumulate=True)
+    assert torch.equal(got, (kge.matmul_quantized(a, b, rows=rows, dtype=F32) + 1).to(BF16))
+    assert torch.equal(kge.matmul_quantized(a, b, dtype=F32, fp32_sums=True), kge.matmul_quantized(a, b, dtype=F32))
+    a, b = _cancelling(m, n, k)
+    assert bool((kge.matmul_quantized(a, b, fp32_sums=True) == 0.125).all())
+    assert bool(((kge.matmul_quantized(a, b).float() - 0.125).abs() <= 7 * 2.0 ** -13 * 4096).all())
