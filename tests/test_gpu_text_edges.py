@@ -111,3 +111,110 @@ def test_bf16_output_with_fp32_sums(m, n, k):
     a, b = _cancelling(m, n, k)
     assert bool((kge.matmul_quantized(a, b, fp32_sums=True) == 0.125).all())
     assert bool(((kge.matmul_quantized(a, b).float() - 0.125).abs() <= 7 * 2.0 ** -13 * 4096).all())
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# what lies between the rows stays
+# ---------------------------------------------------------------------------------------------------------------
+def _gapped(values, front, back):
+    """The values in rows between gaps of a pattern, and a check that the gaps, a row above and a row below still hold it."""
+    rows, cols = values.shape
+    wide = torch.full((rows + 2, front + cols + back), 77.0, dtype=values.dtype, device="cuda")
+    inner = wide[1:rows + 1, front:front + cols]
+    inner.copy_(values)
+
+    def untouched():
+        w = wide.clone()
+        w[1:rows + 1, front:front + cols] = 77.0
+        return bool((w == 77.0).all())
+    return inner, untouched
+
+
+@pytest.mark.parametrize("odt", [F32, BF16])
+@pytest.mark.parametrize("acc", [False, True])
+@pytest.mark.parametrize("M,V,dim", [(1, 3, 1), (5, 9, 7), (300, 40, 33), (513, 20, 264), (2048, 9, 130), (2049, 300, 131), (20_000, 500, 9), (40_000, 700, 13), (40_000, 3000, 257)])
+def test_embed_bwd_writes_its_rows_alone(M, V, dim, acc, odt):
+    gen = torch.Generator(device="cuda").manual_seed(M + dim)
+    g = torch.randint(-2, 3, (M, dim), generator=gen, device="cuda").float()                # whole values: exact in any order
+    ids = (torch.rand(M, generator=gen, device="cuda") ** 4 * (V + 2)).to(torch.int32) - 1
+    for front, back in ((0, 1), (1, 0), (3, 2), (8, 8)):
+        out, untouched = _gapped(torch.ones((V, dim), dtype=odt, device="cuda"), front, back)
+        kge.embed_bwd(g, ids, V, out=out, accumulate=acc)
+        ok = (ids >= 0) & (ids < V)
+        want = torch.full((V, dim), 1.0 if acc else 0.0, device="cuda").index_add_(0, ids[ok].long(), g[ok])
+        assert torch.equal(out, want.to(odt)) and untouched()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("acc", [False, True])
+@pytest.mark.parametrize("m,n,k", [(1, 1, 100), (3, 30, 300), (20, 17, 200), (70, 131, 260), (200, 97, 4200), (1030, 1029, 200), (300, 1700, 1300), (4353, 3841, 130)])
+def test_matmul_writes_its_rows_alone(m, n, k, acc, dt):
+    """Every kernel and the launch that adds up splits: rows and columns behind the last whole tile, group of four and of eight."""
+    gen = torch.Generator(device="cuda").manual_seed(m + n + k)
+    a, b = (kge.quantize(torch.randint(-1, 2, (r, k), generator=gen, device="cuda").float()) for r in (m, n))
+    plain = kge.matmul_quantized(a, b, dtype=F32)
+    for front, back in ((0, 1), (1, 0), (3, 2), (8, 8)):
+        out, untouched = _gapped(torch.ones((m, n), dtype=dt, device="cuda"), front, back)
+        kge.matmul_quantized(a, b, out=out, accumulate=acc)
+        assert torch.equal(out, (plain + 1.0 if acc else plain).to(dt)) and untouched()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (130, 64), (5, 767), (40, 8193), (40_000, 1001)])
+def test_dropout_and_lookup_write_their_rows_alone(rows, cols, dt):
+    gen = torch.Generator(device="cuda").manual_seed(rows + cols)
+    x, r = (torch.randn((rows, cols), generator=gen, device="cuda").to(dt) for _ in range(2))
+    ids = torch.randint(-1, rows + 1, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    d = kge.Dropout(0.3, 5)
+    for front, back in ((0, 1), (1, 0), (3, 2), (8, 8)):
+        xs, rs = _gapped(x, back, front)[0], _gapped(r, 5, 0)[0]
+        for res, gapped in ((None, None), (r, rs)):
+            out, untouched = _gapped(torch.ones((rows, cols), dtype=dt, device="cuda"), front, back)
+            kge.dropout(xs, d, residual=gapped, out=out)
+            assert torch.equal(out, kge.dropout(x, d, residual=res)) and untouched()
+        out, untouched = _gapped(torch.ones((rows, cols), dtype=dt, device="cuda"), front, back)
+        kge.embed(xs, ids, dropout=d, out=out)
+        assert torch.equal(out, kge.embed(x, ids, dropout=d)) and untouched()
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# gradient: three digits, numbers that are not finite
+# ---------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("M,V", [(20_000, 20_000_000), (40_000, 80_000_000)])
+def test_embed_bwd_sorts_in_three_passes(M, V):
+    """Parts of 2^17 rows, by eight bits at a time, of collected and of dealt out ids."""
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    pool = torch.randint(0, V, (M // 3,), generator=gen, device="cuda")
+    ids = pool[torch.randint(0, M // 3, (M,), generator=gen, device="cuda")]
+    ids[::50], ids[1::50], ids[2::50], ids[3::50] = 0, V - 1, -1, V // 2                    # runs of whole chunks
+    ids = ids.to(torch.int32)
+    g = torch.randint(-3, 4, (M, 1), generator=gen, device="cuda").float()
+    ok = ids >= 0
+    got = kge.embed_bwd(g, ids, V)
+    assert torch.equal(got, torch.zeros((V, 1), device="cuda").index_add_(0, ids[ok].long(), g[ok]))
+    ones = torch.ones((V, 1), device="cuda")
+    assert torch.equal(kge.embed_bwd(g, ids, V, out=ones, accumulate=True), got + 1)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("M,V", [(400, 30), (1500, 30), (9000, 300), (40_000, 300)])
+def test_embed_bwd_of_numbers_that_are_not_finite(M, V, dt):
+    """NaN and infinities in a live element reach their row and column alone; in a dropped one and at a padded position they reach nothing."""
+    dim, p = 24, 0.5
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    ids = (torch.rand(M, generator=gen, device="cuda") ** 3 * V).to(torch.int32)
+    ids[::9] = -1
+    ids[::11] = V
+    g = torch.randint(-2, 3, (M, dim), generator=gen, device="cuda").to(dt)
+    d = kge.Dropout(p, 3, step=2, tag=1)
+    kept = kge.dropout(torch.ones((M, dim), device="cuda"), d) > 0
+    dead = ~kept | (ids < 0).unsqueeze(1) | (ids >= V).unsqueeze(1)
+    clean = kge.embed_bwd(g, ids, V, dropout=d)
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        assert torch.equal(kge.embed_bwd(torch.where(dead, torch.full_like(g, bad), g), ids, V, dropout=d), clean)
+        live = (~dead).nonzero()[::97]
+        x = g.clone()
+        x[live[:, 0], live[:, 1]] = bad
+        want = clean.clone()
+        want[ids[live[:, 0]].long(), live[:, 1]] = bad
+        assert torch.equal(torch.nan_to_num(kge.embed_bwd(x, ids, V, dropout=d), 1e9, 2e9, -2e9), torch.nan_to_num(want, 1e9, 2e9, -2e9))
