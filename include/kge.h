@@ -493,7 +493,7 @@ size_t kge_embed_bwd_workspace_bytes(int64_t M, int64_t n_rows, int32_t dim);
  *     element (i, k) = code(i, k) * 2^(scales[i * scales_ld + k / 128] - 127)
  * codes: OCP e4m3 (largest value 448, no infinity) or e5m2 (57,344), a row's codes padded with zeros to a multiple of 128 (ld a multiple of 16
  * and at least that; codes 16-byte aligned); scales: exponent bytes 0..254, a row's padded with zeros to a multiple of 4 (scales_ld a multiple
- * of 4 and at least that; 4-byte aligned).  90M text features of 768 take 74 GB in this form, 138 GB in bf16.
+ * of 4 and at least that; 4-byte aligned).  90M text features of 768 take 70 GB in this form, 138 GB in bf16.
  */
 typedef enum { KGE_E4M3 = 0, KGE_E5M2 = 1 } kge_float_code_t;
 typedef struct {
@@ -517,7 +517,8 @@ int kge_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64
 /*
  * kge_matmul_quantized: out[i, j] = sum over k of a[rows[i], k] * b[j, k], i < m, j < b->rows; rows NULL: row i itself (m = a->rows); a row
  * number outside [0, a->rows) gives a row of zeros.  With accumulate = 1 the product is added to out.  A layer y = x W^t is (x by row, W by
- * row), its dx = dy W (dy by row, W by column), dW = dy^t x (dy by column, x by column).
+ * row), its dx = dy W (dy by row, W by column), dW = dy^t x (dy by column, x by column).  With gathered rows x by column is quantised from the
+ * slots' own fp32 or bf16 rows: no call makes it from a table's codes, whose blocks run along the other side.
  * Arithmetic: out_dtype KGE_F32: the codes widened with their scale to bf16, fp32 sums on the bf16 matrix cores.  Widening is exact under scale bytes
  * 3..246 (e4m3) and 10..239 (e5m2); below them an element is rounded to a multiple of 2^-133, above them one of 2^128 and more
  * is infinite.  KGE_BF16: the 8-bit matrix cores, twice as fast and exact under all scales, which align every eight products to the largest of them and drop

@@ -4,8 +4,8 @@
 //   dropout   out       = residual + D o x
 //
 // Both move every element once and compute next to nothing: memory bounds them, and a launch where there are few rows.  D is made where it is used
-// (text_ops.hpp).  Measured: 131,072 x 768 from an fp32 table to bf16 with dropout 54 us (201 MB written, the table's 154 MB mostly from the caches;
-// a plain copy of as many bytes takes 80); 65,536 x 1,024 bf16 dropout with residual 76 us, 5.3 TB/s; one row 2-3 us.
+// (text_ops.hpp).  Measured: 131,072 x 768 from an fp32 table to bf16 with dropout 54 us (201 MB written, 16,600 distinct rows of 51 MB
+// read: 57 at a plain copy's rate); 65,536 x 1,024 bf16 dropout with residual 76 us, 5.3 TB/s; one row 2-3 us.
 #include "text_ops.hpp"
 #include <math.h>
 

@@ -129,6 +129,8 @@ inline bool kge_bad_rows(const void *p, int32_t dtype, int64_t ld, int64_t cols)
 }
 constexpr int64_t KGE_MAX_ROWS = (1ll << 31) - 1, KGE_MAX_LD = 1ll << 31;
 constexpr int KGE_MAX_DIM = 65536;
-// From this size on results are stored past the caches (the L2s hold 32 MB in all).  Dropout with residual, past them and through them: 128 MB 65.5 and
-// 82.4 us, 32 MB 16.8 and 19.4, 8 MB 7.6 and 7.7; followed by a reader of the result 128 MB 127 and 140, 64 MB 61.7 and 60.7, 24 MB 26.9 and 27.7.
+// From this size on results are stored past the caches (the L2s hold 32 MB in all).  Dropout with residual, past them and through them, fresh matrices in
+// turn: 128 MB 76.6 and 82.4 us, 64 MB 40.5 and 44.7, 32 MB 22.3 and 24.6, 24 MB 19.2 and 20.7, 8 MB 10.8 and 11.7; followed by a reader of the result
+// 128 MB 128 and 141, 64 MB 69.1 and 72.4, 24 MB 32.4 and 33.3, 8 MB 16.5 and 16.5.  (The same matrices again and again come from the last
+// cache: 128 MB 64.7 and 81.9.)
 constexpr int64_t KGE_STREAM_BYTES = 32ll << 20;
