@@ -323,7 +323,7 @@ def loss_bwd(model: Model, loss: str, h, r, t, neg, gamma: float = 0.0, adv_temp
         assert neg.is_cuda and neg.dtype == torch.int32 and neg.is_contiguous()
         dr = KgeNegDrawT(draw[0], draw[1], _counter(draw[5]) if len(draw) > 5 else None, draw[2], 0, draw[3], draw[4])
         if plans is not None:
-            arr = _plan_array(plans)
+            arr = _plan_array(plans, stream)
             _check(load().kge_loss_bwd_sampled_planned(model.ref, C.byref(cfg), _ptr(_i32(h)), _ptr(_i32(r)), _ptr(_i32(t)), B,
                                                        C.byref(dr), _ptr(neg), N, _ptr(out["loss"]), _ptr(out["g_ent"]),
                                                        _ptr(out["g_ent_idx"]), _ptr(out["g_rel"]), _ptr(out["g_relw"]),
@@ -379,7 +379,7 @@ def sparse_adam_static(param, shadow, m, v, idx, grads, lr: float, beta1: float 
 def sparse_adam_plan(n_rows: int, dim: int, idx, ws: Workspace, stream=None):
     """Sorts the row ids of a later sparse_adam_apply into `ws` (which must be kept for that call alone)."""
     M = idx.numel()
-    buf = ws.get(workspace_bytes(OP_SPARSE_ADAM, None, M, dim))
+    buf = _buffer(ws, workspace_bytes(OP_SPARSE_ADAM, None, M, dim), stream)
     _check(load().kge_sparse_adam_plan(n_rows, dim, _ptr(_i32(idx)), M, _ptr(buf), buf.numel(), _stream(stream)),
            "kge_sparse_adam_plan")
 
@@ -393,7 +393,7 @@ def sparse_adam_apply(param, shadow, m, v, grads, ws: Workspace, lr: float, beta
         assert shadow.dtype == torch.bfloat16 and shadow.stride() == param.stride()
     M, d = grads.shape[0], param.shape[1]
     cfg = KgeAdamCfgT(lr, beta1, beta2, eps, step, _counter(step_counter))
-    buf = ws.get(workspace_bytes(OP_SPARSE_ADAM, None, M, d))
+    buf = _buffer(ws, workspace_bytes(OP_SPARSE_ADAM, None, M, d), stream)
     _check(load().kge_sparse_adam_apply(_ptr(param), _ptr(shadow), _ptr(m), _ptr(v), param.shape[0], d, param.stride(0),
                                         _ptr(grads), M, C.byref(cfg), _ptr(buf), buf.numel(), _stream(stream)),
            "kge_sparse_adam_apply")
@@ -401,14 +401,14 @@ def sparse_adam_apply(param, shadow, m, v, grads, ws: Workspace, lr: float, beta
 
 def sparse_adam_plan_tables(plans, stream=None):
     """kge_sparse_adam_plan_tables: plans = [(n_rows, dim, idx, ws), ...]; the sorts of up to 32,768 ids share one launch."""
-    _check(load().kge_sparse_adam_plan_tables(_plan_array(plans), len(plans), _stream(stream)), "kge_sparse_adam_plan_tables")
+    _check(load().kge_sparse_adam_plan_tables(_plan_array(plans, stream), len(plans), _stream(stream)), "kge_sparse_adam_plan_tables")
 
 
-def _plan_array(plans):
+def _plan_array(plans, stream):
     rows = []
     for n_rows, dim, idx, ws in plans:
         M = idx.numel()
-        buf = ws.get(workspace_bytes(OP_SPARSE_ADAM, None, M, dim))
+        buf = _buffer(ws, workspace_bytes(OP_SPARSE_ADAM, None, M, dim), stream)
         rows.append((n_rows, dim, _i32(idx).data_ptr(), M, buf.data_ptr(), buf.numel()))
     return (KgeAdamPlanT * len(rows))(*rows)
 
@@ -425,7 +425,7 @@ def sparse_adam_apply_tables(tables, lr: float, beta1: float = 0.9, beta2: float
         if shadow is not None:
             assert shadow.dtype == torch.bfloat16 and shadow.stride() == strides
         (n_rows, d), M = param.shape, grads.shape[0]
-        buf = ws.get(workspace_bytes(OP_SPARSE_ADAM, None, M, d))
+        buf = _buffer(ws, workspace_bytes(OP_SPARSE_ADAM, None, M, d), stream)
         rows.append((param.data_ptr(), _ptr(shadow), m.data_ptr(), v.data_ptr(), n_rows, d, strides[0], grads.data_ptr(), M,
                      buf.data_ptr(), buf.numel()))
     arr = (KgeAdamTableT * len(rows))(*rows)

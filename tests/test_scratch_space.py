@@ -3,6 +3,7 @@ never hold the same memory, and it belongs to the stream that the kernels run on
 notes what it is handed, memory comes from the CPU."""
 import contextlib
 import threading
+import types
 
 import pytest
 import torch
@@ -208,3 +209,19 @@ def test_outputs_belong_to_the_stream_that_writes_them(monkeypatch, path_on_the_
     for call in calls:
         for t in call():
             assert path_on_the_host[t.data_ptr()] is stream
+
+
+@pytest.mark.parametrize("stream", [None, FakeStream()])
+def test_a_plan_s_workspace_grows_on_the_stream_that_sorts_into_it(monkeypatch, path_on_the_host, stream):
+    t = torch.zeros((9, 8))
+    neg = types.SimpleNamespace(numel=lambda: 6, is_cuda=True, dtype=torch.int32, is_contiguous=lambda: True, data_ptr=lambda: 1 << 20)
+    calls = [lambda ws: b.sparse_adam_plan(9, 8, _ids(4), ws, stream=stream),
+             lambda ws: b.sparse_adam_plan_tables([(9, 8, _ids(4), ws)], stream=stream),
+             lambda ws: b.sparse_adam_apply(t, None, t, t, torch.zeros((4, 8)), ws, 0.1, stream=stream),
+             lambda ws: b.sparse_adam_apply_tables([(t, None, t, t, torch.zeros((4, 8)), ws)], 0.1, stream=stream),
+             lambda ws: b.loss_bwd(_model(), "logsigmoid", _ids(4), _ids(4), _ids(4), neg, draw=(1, 2, 3, 0, 9), plans=[(9, 8, _ids(14), ws)], stream=stream)]
+    monkeypatch.setattr(b, "load", lambda: type("Lib", (), {"__getattr__": lambda self, name: lambda *a: 3 << 20 if name.endswith("bytes") else 0})())
+    for call in calls:
+        ws = b.Workspace()
+        call(ws)
+        assert path_on_the_host[ws.buf.data_ptr()] is stream
