@@ -521,8 +521,8 @@ int kge_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64
  * slots' own fp32 or bf16 rows: no call makes it from a table's codes, whose blocks run along the other side.
  * Arithmetic: out_dtype KGE_F32: the codes widened with their scale to bf16, fp32 sums on the bf16 matrix cores.  Widening is exact under scale bytes
  * 3..246 (e4m3) and 10..239 (e5m2); below them an element is rounded to a multiple of 2^-133, above them one of 2^128 and more
- * is infinite.  KGE_BF16: the 8-bit matrix cores, twice as fast and exact under all scales, which align every eight products to the largest of them and drop
- * what lies 2^-13 below it (1.4e-5 of the result on normal values; where products cancel, up to 7 * 2^-13 of the largest of each eight); sums of
+ * is infinite.  KGE_BF16: the 8-bit matrix cores, twice as fast and without these ends of the scales, which align every eight products to the largest of them
+ * and drop what lies 2^-13 below it (1.4e-5 of the result on normal values; where products cancel, up to 7 * 2^-13 of the largest of each eight); sums of
  * these groups in fp32, one rounding at the end.  KGE_BF16 | KGE_FP32_SUMS: the arithmetic of KGE_F32, rounded once to bf16.  A value that needs more than
  * fp32's range (a block that holds numbers next to the largest fp32 one) overflows.
  * Few rows over many blocks are split along k into partial sums in the workspace, which are added in order: the size to give is

@@ -218,3 +218,43 @@ def test_embed_bwd_of_numbers_that_are_not_finite(M, V, dt):
         want = clean.clone()
         want[ids[live[:, 0]].long(), live[:, 1]] = bad
         assert torch.equal(torch.nan_to_num(kge.embed_bwd(x, ids, V, dropout=d), 1e9, 2e9, -2e9), torch.nan_to_num(want, 1e9, 2e9, -2e9))
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# in front of the path
+# ---------------------------------------------------------------------------------------------------------------
+def test_entities_from_an_8_bit_feature_table_through_the_loss():
+    """e = e_S + D o (M e_F) of a step's slots, with e_F in 8 bits and gathered by the product, through kge_loss_bwd, whose gradient rows come back as a dense one
+    of e_S.  The front part against 64 bits, the loss and its gradient against the same call on entities made in 64 bits and rounded."""
+    n_ent, n_rel, d, f, B, N = 400, 5, 64, 200, 96, 160
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda")                                          # noqa: E731
+    e_s, m, rel = rand(n_ent, d) * 0.3, rand(d, f) * 0.05, rand(n_rel, d) * 0.3
+    feat, proj = kge.quantize(rand(n_ent, f)), kge.quantize(m)
+    ids = torch.randint(0, n_ent, (2 * B + N,), generator=gen, device="cuda", dtype=torch.int32)
+    r = torch.randint(0, n_rel, (B,), generator=gen, device="cuda", dtype=torch.int32)
+    slot = torch.arange(2 * B + N, dtype=torch.int32, device="cuda")
+    drop = kge.Dropout(0.25, 7, step=3, tag=12)
+    e = kge.dropout(kge.matmul_quantized(feat, proj, rows=ids, dtype=F32), drop, residual=kge.embed(e_s, ids))
+
+    def values(q):
+        v = q.codes.view(FLOAT8[q.fmt]).double()
+        return v * torch.exp2(q.scales[:, :v.shape[1] // 128].double() - 127).repeat_interleave(128, dim=1)
+    kept = (kge.dropout(torch.ones((2 * B + N, d), device="cuda"), drop) > 0).double() / 0.75
+    p, mag = (x[ids.long()] @ y.t() for x, y in ((values(feat), values(proj)), (values(feat).abs(), values(proj).abs())))
+    want = e_s[ids.long()].double() + kept * p
+    # (256 products in any order, factor, its product, sum)
+    assert bool(((e.double() - want).abs() <= kept * mag * (256 + 3) * 2.0 ** -24 + want.abs() * 2.0 ** -24).all())
+
+    def loss(x):
+        return kge.loss_bwd(kge.Model("distmult", x, rel), "logsigmoid", slot[:B], r, slot[B:2 * B], slot[2 * B:], gamma=2.0)
+    got, ref = loss(e), loss(want.float())
+    assert torch.equal(got["g_ent_idx"], slot)
+    for key in ("loss", "g_ent", "g_rel"):
+        # e is off by 256 * 2^-24 = 1.5e-5 of its terms at most; what comes out is smooth in it, and a call's own sums are good to 1e-5
+        assert float((got[key] - ref[key]).double().norm()) <= 1e-4 * float(ref[key].double().norm()), key
+    dense = kge.embed_bwd(got["g_ent"], ids, n_ent)
+    zero = torch.zeros((n_ent, d), dtype=torch.float64, device="cuda")
+    sums, sizes = (zero.index_add(0, ids.long(), x) for x in (got["g_ent"].double(), got["g_ent"].double().abs()))
+    count = torch.bincount(ids.long(), minlength=n_ent).unsqueeze(1)
+    assert bool(((dense.double() - sums).abs() <= sizes * count * 2.0 ** -24).all())
