@@ -537,6 +537,124 @@ int kge_matmul_quantized(const kge_quantized_t *a, const int32_t *rows, int64_t 
 size_t kge_matmul_quantized_workspace_bytes(int64_t m, int64_t n, int64_t k);
 
 /*
+ * Norms around a block of the text side's layers, fused with the block's gate and residual scale: of a residual stream x and a block's output y
+ *     h = x + s o g o N_post(y),    z = N_pre(h),    N(v) = w o v^ + b,  v^ = (v - mu) / sqrt(var + eps)
+ * (KGE_NORM_LAYER: mu and var of the row; KGE_NORM_RMS: mu = 0, so that var is the mean square).  Each part may be absent: post = NULL uses y itself,
+ * pre = NULL leaves z out, scale and gate = NULL are ones, a norm's weight = NULL is ones and its bias = NULL zeros; without y (then post, scale and gate
+ * are NULL too) the call is z = N_pre(x).  gate: [ceil(rows / gate_rows), dim] of block_dtype, one row for each gate_rows consecutive rows (1: a gate
+ * of its own for every row; rows and more: one gate for all).  x, h and their gradients are of stream_dtype, y, z, gate and theirs of block_dtype, vectors
+ * float[dim].  Everything is computed in fp32 and rounded once, z from h before its rounding; squares of elements have to fit fp32.  1 <= dim <= 16,384
+ * (KGE_E_UNSUPPORTED beyond), rows < 2^31, 0 < eps.
+ */
+typedef enum { KGE_NORM_RMS = 0, KGE_NORM_LAYER = 1 } kge_norm_kind_t;
+typedef struct {
+    int32_t kind;                     /* kge_norm_kind_t */
+    float eps;
+    const float *weight, *bias;       /* device, [dim] or NULL */
+} kge_norm_t;
+typedef struct {
+    int32_t dim;
+    int32_t stream_dtype, block_dtype;/* kge_dtype_t */
+    int32_t reserved;                 /* 0 */
+    const kge_norm_t *post, *pre;     /* HOST structs, or NULL */
+    const float *scale;               /* s: device, [dim] or NULL */
+    const void *gate;                 /* g: device or NULL */
+    int64_t gate_ld, gate_rows;
+} kge_norm_block_t;
+
+/*
+ * kge_norm_block: writes h (NULL: not wanted, only with pre; without y it is x and has to be NULL) and z (exactly with pre).  x NULL: zeros.  h may be x with the
+ * same row stride; otherwise outputs overlap neither inputs nor each other.
+ *
+ * kge_norm_block_bwd: from dh (the gradient of h by its other uses; NULL: zeros, only with pre) and dz (exactly with pre) the gradients dx and
+ * dy (each NULL: not wanted) and those of the vectors and gates that grads (a HOST struct, may be NULL) names; a name may be set only if the part is
+ * there.  h is the forward pass's result (without y: its x; not read without pre), y its input; the norms' statistics are computed again from them.  The vectors'
+ * gradients are fp32 sums over the rows in a fixed order; with accumulate = 1 they are added to what is there.  A gate's gradient, the
+ * sum over its rows, is rounded once to block_dtype and never accumulated.  dx may be dh with the same row stride; otherwise outputs overlap nothing.
+ * Workspace (only for sums over rows: any vector's gradient, or a gate's) from kge_norm_block_bwd_workspace_bytes, which never falls as rows
+ * grows and returns 0 for invalid arguments.
+ */
+typedef struct {
+    float *post_weight, *post_bias, *pre_weight, *pre_bias, *scale;     /* device, [dim] or NULL */
+    void *gate; int64_t gate_ld;      /* device, as the gate, or NULL */
+    int32_t accumulate;
+    int32_t reserved;                 /* 0 */
+} kge_norm_block_grads_t;
+int kge_norm_block(const kge_norm_block_t *blk, const void *x, int64_t x_ld, const void *y, int64_t y_ld, int64_t rows, void *h, int64_t h_ld,
+                   void *z, int64_t z_ld, void *hip_stream);
+int kge_norm_block_bwd(const kge_norm_block_t *blk, const void *h, int64_t h_ld, const void *y, int64_t y_ld, const void *dh, int64_t dh_ld,
+                       const void *dz, int64_t dz_ld, int64_t rows, void *dx, int64_t dx_ld, void *dy, int64_t dy_ld,
+                       const kge_norm_block_grads_t *grads, void *ws, size_t ws_bytes, void *hip_stream);
+size_t kge_norm_block_bwd_workspace_bytes(const kge_norm_block_t *blk, int64_t rows);
+
+/*
+ * A matrix [rows, cols] in 8-bit integers with one scale per row (a token, an output channel, an entity's features):
+ *     element (i, k) = codes[i * ld + k] * scales[i]
+ * codes: -127..127, a row padded with zeros to a multiple of 128 (ld a multiple of 16 and at least that; 16-byte aligned); scales: float[rows].  cols <=
+ * 131,071, so that sums of products stay below 2^31 (KGE_E_UNSUPPORTED beyond).
+ */
+typedef struct {
+    int64_t rows, cols;
+    int8_t *codes; int64_t ld;
+    float *scales;
+} kge_rowwise_t;
+
+/*
+ * kge_quantize_rowwise: writes x [rows, cols] by rows (by_row: [rows, cols]) and / or the transposed matrix (by_col: [cols, rows], a scale for each column
+ * of x), padding included.  With a the largest magnitude of the row, but 2^-100 at least: scale = a / 127, code = x * (127 / a) rounded to nearest even,
+ * each operation rounded to fp32.  A row that holds a NaN or an infinity gets a NaN for its scale and codes of 0: 8-bit integers have neither, and a product of
+ * that row is NaN.  The layouts overlap neither each other nor x.  by_col needs a workspace (kge_quantize_rowwise_workspace_bytes; 0 for
+ * invalid arguments).  KGE_E_UNSUPPORTED: by_col with 2^24 and more tiles of 128 x 128.
+ *
+ * kge_matmul_rowwise: out[i, j] = a.scales[rows[i]] * b.scales[j] * sum over k of a.codes[rows[i], k] * b.codes[j, k], i < m, j < b->rows; rows NULL: row i itself
+ * (m = a->rows); a row number outside [0, a->rows) gives a row of zeros.  The sums are exact (8-bit matrix cores, 32-bit integers); then three
+ * fp32 roundings ((float)sum * a's scale * b's, in this order: an intermediate result beyond fp32's range is infinite) and that of out_dtype.  accumulate = 1: added to out, in fp32.  The products
+ * of a layer's backward pass are those of kge_matmul_quantized, each with a scale per row of its own operands.  Few rows over long contractions are
+ * split along k into partial sums in the workspace (kge_matmul_rowwise_workspace_bytes, k = a->cols; 256 bytes where nothing is split); with less
+ * the call takes fewer splits: the result is the same.  out must not overlap the operands.  KGE_E_UNSUPPORTED: more than 2^22 tiles of 128 x 128.
+ */
+int kge_quantize_rowwise(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, const kge_rowwise_t *by_row,
+                         const kge_rowwise_t *by_col, void *ws, size_t ws_bytes, void *hip_stream);
+size_t kge_quantize_rowwise_workspace_bytes(int64_t rows, int64_t cols);
+int kge_matmul_rowwise(const kge_rowwise_t *a, const int32_t *rows, int64_t m, const kge_rowwise_t *b, int32_t accumulate, void *out, int32_t out_dtype,
+                       int64_t out_ld, void *ws, size_t ws_bytes, void *hip_stream);
+size_t kge_matmul_rowwise_workspace_bytes(int64_t m, int64_t n, int64_t k);
+
+/*
+ * kge_adamw: one AdamW step over many dense tensors at once (the encoder's and the text side's projections, norms and embedding tables; rows
+ * taken by id are kge_sparse_adam's).  Every element of every tensor:
+ *     g <- grad * *grad_scale (if given);   m <- b1 m + (1 - b1) g;   v <- b2 v + (1 - b2) g^2
+ *     theta <- theta (1 - lr * weight_decay) - lr * (m / (1 - b1^step)) / (sqrt(v / (1 - b2^step)) + eps)
+ * in fp32; the moments' operations are rounded one by one.  param_bf16, if not NULL, is rewritten as RNE(theta).  Tensors are contiguous, of any length (0
+ * too) and at any element, and must not overlap; n < 2^34.  Launches take 40 tensors each.
+ *
+ * state_bits 32: m and v are float[n].  state_bits 8: m in e4m3, v in e5m2 codes, each the single row of a kge_quantized_t of n columns (codes padded to a
+ * multiple of 128 and 16-byte aligned, m_scales and v_scales an exponent byte per 128 elements).  The update uses the moments before they are rounded.  A block's byte is
+ * kge_quantize's; a code is one of the two neighbours of the value, the upper one with probability equal to its nearness (stochastic
+ * rounding: with b2 = 0.999 a step changes v by a thousandth, far less than half a spacing, and rounding to nearest would never move it); a
+ * positive v is never rounded to 0.  Sixteen random bits each: Philox4x32-10, key = seed, counter (element / 4, tensor's place in the call, step, tag),
+ * word element % 4, low half for m.  So v carries a relative noise of about 0.3 at b2 = 0.999, without bias.  NaN stays NaN; an infinite m becomes NaN, an infinite v stays.  Codes
+ * behind the last element are written as zeros.
+ * step as in kge_adam_cfg_t (adam.step_counter too; the generator takes its low 32 bits).
+ */
+typedef struct {
+    float *param_f32; void *param_bf16;
+    const void *grad; int32_t grad_dtype;                  /* kge_dtype_t */
+    int32_t state_bits;                                    /* 32 or 8 */
+    void *m, *v; uint8_t *m_scales, *v_scales;             /* scales: state_bits 8 */
+    int64_t n;
+    float weight_decay;
+    int32_t reserved;                                      /* 0 */
+} kge_adamw_tensor_t;
+typedef struct {
+    kge_adam_cfg_t adam;
+    const float *grad_scale;                               /* device, or NULL */
+    uint64_t seed; uint32_t tag;                           /* state_bits 8 */
+    uint32_t reserved;                                     /* 0 */
+} kge_adamw_cfg_t;
+int kge_adamw(const kge_adamw_tensor_t *tensors, int32_t n_tensors, const kge_adamw_cfg_t *cfg, void *hip_stream);
+
+/*
  * Workspace size in bytes for one call (pure function; host only).  Meaning of (B, N, K):
  *   KGE_OP_SCORE, KGE_OP_LOSS_BWD  B triples, N shared negatives, K unused
  *   KGE_OP_SPARSE_ADAM             B = M gradient rows, N = dim, K unused; model may be NULL

@@ -26,7 +26,9 @@ EXPORTS = ["kge_sample_negatives", "kge_score", "kge_loss_bwd", "kge_sparse_adam
            "kge_calibrate_mfma", "kge_calibrate_mfma_varied", "kge_calibrate_copy", "kge_step_counter_add", "kge_sample_negatives_dev",
            "kge_sparse_adam_apply_tables", "kge_sparse_adam_plan_tables", "kge_loss_bwd_sampled",
            "kge_loss_bwd_sampled_planned", "kge_dropout", "kge_embed", "kge_embed_bwd", "kge_embed_bwd_workspace_bytes",
-           "kge_quantize", "kge_matmul_quantized", "kge_matmul_quantized_workspace_bytes"]
+           "kge_quantize", "kge_matmul_quantized", "kge_matmul_quantized_workspace_bytes", "kge_norm_block", "kge_norm_block_bwd",
+           "kge_norm_block_bwd_workspace_bytes", "kge_quantize_rowwise", "kge_quantize_rowwise_workspace_bytes", "kge_matmul_rowwise",
+           "kge_matmul_rowwise_workspace_bytes", "kge_adamw"]
 PROF_SLOTS = {"block_score": 0, "block_fwd": 1, "block_gradt": 2, "adam": 3, "sort": 4, "topk_scan": 5,
               "enc_fwd": 6, "enc_bwd": 7, "gather": 8, "finish": 9}
 
@@ -78,6 +80,34 @@ class KgeDropoutT(C.Structure):
 class KgeQuantizedT(C.Structure):
     _fields_ = [("format", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64), ("codes", C.c_void_p),
                 ("ld", C.c_int64), ("scales", C.c_void_p), ("scales_ld", C.c_int64)]
+
+
+class KgeNormT(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("eps", C.c_float), ("weight", C.c_void_p), ("bias", C.c_void_p)]
+
+
+class KgeNormBlockT(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("stream_dtype", C.c_int32), ("block_dtype", C.c_int32), ("reserved", C.c_int32), ("post", C.c_void_p),
+                ("pre", C.c_void_p), ("scale", C.c_void_p), ("gate", C.c_void_p), ("gate_ld", C.c_int64), ("gate_rows", C.c_int64)]
+
+
+class KgeNormBlockGradsT(C.Structure):
+    _fields_ = [("post_weight", C.c_void_p), ("post_bias", C.c_void_p), ("pre_weight", C.c_void_p), ("pre_bias", C.c_void_p), ("scale", C.c_void_p),
+                ("gate", C.c_void_p), ("gate_ld", C.c_int64), ("accumulate", C.c_int32), ("reserved", C.c_int32)]
+
+
+class KgeRowwiseT(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("codes", C.c_void_p), ("ld", C.c_int64), ("scales", C.c_void_p)]
+
+
+class KgeAdamwTensorT(C.Structure):
+    _fields_ = [("param_f32", C.c_void_p), ("param_bf16", C.c_void_p), ("grad", C.c_void_p), ("grad_dtype", C.c_int32), ("state_bits", C.c_int32),
+                ("m", C.c_void_p), ("v", C.c_void_p), ("m_scales", C.c_void_p), ("v_scales", C.c_void_p), ("n", C.c_int64),
+                ("weight_decay", C.c_float), ("reserved", C.c_int32)]
+
+
+class KgeAdamwCfgT(C.Structure):
+    _fields_ = [("adam", KgeAdamCfgT), ("grad_scale", C.c_void_p), ("seed", C.c_uint64), ("tag", C.c_uint32), ("reserved", C.c_uint32)]
 
 
 class KgeError(RuntimeError):
@@ -162,6 +192,20 @@ def load():
                                              C.c_void_p, C.c_size_t, C.c_void_p]
         lib.kge_matmul_quantized_workspace_bytes.restype = C.c_size_t
         lib.kge_matmul_quantized_workspace_bytes.argtypes = [C.c_int64] * 3
+        lib.kge_norm_block.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                       C.c_int64, C.c_void_p]
+        lib.kge_norm_block_bwd.argtypes = [C.c_void_p] + [C.c_void_p, C.c_int64] * 4 + [C.c_int64] + [C.c_void_p, C.c_int64] * 2 + \
+            [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.kge_norm_block_bwd_workspace_bytes.restype = C.c_size_t
+        lib.kge_norm_block_bwd_workspace_bytes.argtypes = [C.c_void_p, C.c_int64]
+        lib.kge_quantize_rowwise.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                             C.c_void_p]
+        lib.kge_quantize_rowwise_workspace_bytes.restype = C.c_size_t
+        lib.kge_quantize_rowwise_workspace_bytes.argtypes = [C.c_int64] * 2
+        lib.kge_matmul_rowwise.argtypes = lib.kge_matmul_quantized.argtypes
+        lib.kge_matmul_rowwise_workspace_bytes.restype = C.c_size_t
+        lib.kge_matmul_rowwise_workspace_bytes.argtypes = [C.c_int64] * 3
+        lib.kge_adamw.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
         _lib = lib
     return _lib
 
@@ -788,3 +832,301 @@ def matmul_quantized(a: Quantized, b: Quantized, rows=None, dtype=torch.bfloat16
     _check(load().kge_matmul_quantized(a.ref, None if rows is None else _rows_of(rows, m, "rows"), m, b.ref, 1 if accumulate else 0, po, do, ldo,
                                        _ptr(buf), 0 if buf is None else buf.numel(), _queue(dev, stream)), "kge_matmul_quantized")
     return out
+
+
+# ---------------------------------------------------------------------------------------------
+# Text side: norms around a block, 8-bit integers with a scale per row, dense AdamW
+# ---------------------------------------------------------------------------------------------
+_NORMS = {"rms": 0, "layer": 1}
+
+
+def _vector(t, dim: int, what: str):
+    """Pointer of an fp32 vector of `dim` elements, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.dim() != 1 or t.numel() != dim or not t.is_contiguous():
+        raise KgeError(f"{what}: a contiguous fp32 tensor of {dim} entries is wanted, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+class Norm:
+    """kge_norm_t: a layer ("layer") or root-mean-square ("rms") norm with its weight and bias (fp32 vectors, either may be absent)."""
+
+    def __init__(self, kind: str = "rms", weight=None, bias=None, eps: float = 1e-6):
+        if kind not in _NORMS:
+            raise KgeError(f"kind: rms or layer, got {kind!r}")
+        self.weight, self.bias = weight, bias
+        some = weight if weight is not None else bias
+        self.dim = None if some is None else some.numel()
+        self.struct = KgeNormT(_NORMS[kind], eps, None if weight is None else _vector(weight, self.dim, "weight"),
+                               None if bias is None else _vector(bias, self.dim, "bias"))
+
+
+def _block(dim, stream_dtype, block_dtype, post, pre, scale, gate, gate_rows, rows):
+    """(kge_norm_block_t, tensors that it points to)"""
+    s = KgeNormBlockT(dim, stream_dtype, block_dtype)
+    for name, norm in (("post", post), ("pre", pre)):
+        if norm is not None:
+            if norm.dim not in (None, dim):
+                raise KgeError(f"{name}: a norm of {norm.dim} elements over rows of {dim}")
+            setattr(s, name, C.addressof(norm.struct))
+    s.scale = _vector(scale, dim, "scale")
+    if gate is not None:
+        s.gate, gdt, s.gate_ld = _matrix(gate, "gate")
+        if gate_rows is None:
+            gate_rows = 1 if gate.shape[0] == rows else 0
+        if gdt != block_dtype or gate_rows < 1 or tuple(gate.shape) != (-(-rows // gate_rows), dim):
+            raise KgeError(f"gate: {-(-rows // max(gate_rows, 1))} rows of {dim} (one for each gate_rows rows) of y's type are wanted, got {gate.dtype} "
+                           f"{tuple(gate.shape)} with gate_rows = {gate_rows}")
+        s.gate_rows = gate_rows
+    elif gate_rows is not None and gate_rows < 1:
+        raise KgeError("gate_rows: one row at least")
+    return s
+
+
+def _on_norms(*norms):
+    return [t for n in norms if n is not None for t in (n.weight, n.bias)]
+
+
+def _like(t, rows: int, dim: int, dtype: int, what: str):
+    """(pointer, row stride) of an input matrix, or of none"""
+    if t is None:
+        return None, 0
+    p, dt, ld = _matrix(t, what)
+    if tuple(t.shape) != (rows, dim) or dt != dtype:
+        raise KgeError(f"{what}: {(rows, dim)} of another type is wanted, got {t.dtype} {tuple(t.shape)}")
+    return p, ld
+
+
+def norm_block(x, y=None, post: Norm | None = None, pre: Norm | None = None, scale=None, gate=None, gate_rows: int | None = None, dtype=None,
+               out_h=None, out_z=None, want_h: bool = True, stream=None):
+    """kge_norm_block: (h, z) with h = x + scale o gate o post(y) and z = pre(h); without y (z alone) h is x itself.  x may be None (then the stream has y's
+    type).  gate: one row for each gate_rows rows (1 where it has as many rows as y).  dtype: z's, where there is no y (else it is y's).  out_h may
+    be x.  want_h=False: z alone (h is None)."""
+    some = y if y is not None else x
+    if some is None:
+        raise KgeError("kge_norm_block: x or y is wanted")
+    dev = _here(x, y, scale, gate, out_h, out_z, *_on_norms(post, pre))
+    rows, dim = some.shape
+    sdt = _matrix(x if x is not None else y, "x")[1]
+    bdt = _matrix(y, "y")[1] if y is not None else _DTYPE.get(dtype or x.dtype)
+    if bdt is None or (y is not None and dtype is not None and dtype != y.dtype):
+        raise KgeError(f"dtype: y's, or fp32 or bf16 without y, got {dtype}")
+    blk = _block(dim, sdt, bdt, post, pre, scale, gate, gate_rows, rows)
+    px, ldx = _like(x, rows, dim, sdt, "x")
+    py, ldy = _like(y, rows, dim, bdt, "y")
+    h, ph, ldh, z, pz, ldz = (x if y is None else None), None, 0, None, None, 0
+    if y is not None and (want_h or pre is None):
+        h, ph, dt, ldh = _new(out_h, rows, dim, some.dtype if x is None else x.dtype, "kge_norm_block", stream)
+        if dt != sdt:
+            raise KgeError("out_h has another type than x")
+    elif out_h is not None:
+        raise KgeError("out_h: there is no h to write")
+    if pre is not None:
+        z, pz, dt, ldz = _new(out_z, rows, dim, y.dtype if y is not None else dtype or x.dtype, "kge_norm_block", stream)
+        if dt != bdt:
+            raise KgeError("out_z has another type than wanted")
+    elif out_z is not None:
+        raise KgeError("out_z: there is no norm behind h")
+    _check(load().kge_norm_block(C.byref(blk), px, ldx, py, ldy, rows, ph, ldh, pz, ldz, _queue(dev, stream)), "kge_norm_block")
+    return h, z
+
+
+_BLOCK_GRADS = ("post_weight", "post_bias", "pre_weight", "pre_bias", "scale")
+
+
+def norm_block_bwd(h, y=None, dh=None, dz=None, post: Norm | None = None, pre: Norm | None = None, scale=None, gate=None,
+                   gate_rows: int | None = None, want=None, out=None, accumulate: bool = False, ws: Workspace | None = None, stream=None):
+    """kge_norm_block_bwd: a dict of gradients, "x", "y", "gate", "scale", "post_weight", "post_bias", "pre_weight", "pre_bias", of what the block has; want: the
+    names wanted of these (all unless given).  h: the forward pass's (without y: its x; may be None without pre).  out: a dict of tensors to write
+    to, "x" may be dh; accumulate: the vectors' gradients are added to those in `out`."""
+    out = dict(out or {})
+    first = h if h is not None else dh
+    if first is None:
+        raise KgeError("kge_norm_block_bwd: h or dh is wanted")
+    dev = _here(h, y, dh, dz, scale, gate, *_on_norms(post, pre), *out.values())
+    rows, dim = first.shape
+    sdt = _matrix(first, "h")[1]
+    block = y if y is not None else dz if dz is not None else first
+    bdt = _matrix(block, "y")[1]
+    blk = _block(dim, sdt, bdt, post, pre, scale, gate, gate_rows, rows)
+    there = {"x": True, "y": y is not None, "gate": gate is not None, "scale": scale is not None}
+    for name, norm in (("post", post), ("pre", pre)):
+        there[name + "_weight"], there[name + "_bias"] = (norm is not None and norm.weight is not None), (norm is not None and norm.bias is not None)
+    names = [k for k, t in there.items() if t] if want is None else list(want)
+    for k in (*names, *out):
+        if not there.get(k) or k not in names:
+            raise KgeError(f"{k!r}: no gradient of the block that is wanted")
+    if accumulate and any(k in names and k not in out for k in _BLOCK_GRADS):
+        raise KgeError("accumulate needs the gradients to add to")
+    args = [a for t, dt, what in ((h, sdt, "h"), (y, bdt, "y"), (dh, sdt, "dh"), (dz, bdt, "dz")) for a in _like(t, rows, dim, dt, what)]
+    grads, to = KgeNormBlockGradsT(), [None, 0, None, 0]
+    for i, (k, like, dt) in enumerate((("x", first, sdt), ("y", block, bdt), ("gate", gate, bdt))):
+        if k not in names:
+            continue
+        out[k], p, got, ld = _new(out.get(k), rows if k != "gate" else gate.shape[0], dim, like.dtype, "kge_norm_block_bwd", stream)
+        if got != dt:
+            raise KgeError(f"out[{k!r}] has another type than wanted")
+        if k == "gate":
+            grads.gate, grads.gate_ld = p, ld
+        else:
+            to[2 * i], to[2 * i + 1] = p, ld
+    sums = [k for k in _BLOCK_GRADS if k in names]
+    if any(k not in out for k in sums):
+        with _allocating_for(stream):
+            for k in sums:
+                if k not in out:
+                    out[k] = torch.empty(dim, dtype=torch.float32, device="cuda")
+    for k in sums:
+        setattr(grads, k, _vector(out[k], dim, f"out[{k!r}]"))
+    grads.accumulate = 1 if accumulate else 0
+    buf = None
+    if sums or (gate is not None and "gate" in names and blk.gate_rows > 1):
+        buf = _scratch(ws, int(load().kge_norm_block_bwd_workspace_bytes(C.byref(blk), rows)), stream)
+    _check(load().kge_norm_block_bwd(C.byref(blk), *args, rows, *to, C.byref(grads), _ptr(buf), 0 if buf is None else buf.numel(), _queue(dev, stream)),
+           "kge_norm_block_bwd")
+    return {k: out[k] for k in names}
+
+
+class Rowwise:
+    """kge_rowwise_t: a matrix [rows, cols] in 8-bit integers (int8 [rows, 128 ceil(cols / 128)], zeros behind a row's end) with a scale per row (fp32)."""
+
+    def __init__(self, codes, scales, cols: int):
+        if codes.dtype != torch.int8 or codes.dim() != 2 or codes.shape[1] < -(-cols // 128) * 128 or (codes.shape[0] > 0 and cols > 0 and codes.stride(1) != 1):
+            raise KgeError(f"codes: contiguous int8 rows of {-(-cols // 128) * 128} (padded to a multiple of 128) are wanted, got {codes.dtype} {tuple(codes.shape)}")
+        rows = codes.shape[0]
+        if scales.get_device() != codes.get_device():
+            raise KgeError("codes and scales are on different devices")
+        ld = codes.stride(0) if rows > 1 and cols > 0 else -(-cols // 128) * 128      # (else torch gives strides of its own choice)
+        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
+        self.struct = KgeRowwiseT(rows, cols, codes.data_ptr(), ld, _vector(scales, rows, "scales"))
+        self.ref = C.byref(self.struct)
+
+    @staticmethod
+    def empty(rows: int, cols: int, device="cuda"):
+        return Rowwise(torch.empty((rows, -(-cols // 128) * 128), dtype=torch.int8, device=device),
+                       torch.empty(rows, dtype=torch.float32, device=device), cols)
+
+
+@functools.lru_cache(maxsize=1024)
+def _rowwise_bytes(rows: int, cols: int) -> int:
+    return int(load().kge_quantize_rowwise_workspace_bytes(rows, cols))
+
+
+@functools.lru_cache(maxsize=1024)
+def _matmul_rowwise_bytes(m: int, n: int, k: int) -> int:
+    return int(load().kge_matmul_rowwise_workspace_bytes(m, n, k))
+
+
+def quantize_rowwise(x, by: str = "row", out=None, ws: Workspace | None = None, stream=None):
+    """kge_quantize_rowwise: x by rows (by="row"), the transposed matrix with a scale per column of x (by="col"), or the pair of both (by="both").  out: a
+    Rowwise, or a pair of them, to write to."""
+    dev = _here(x)
+    px, dt, ld = _matrix(x, "x")
+    rows, cols = x.shape
+    if by not in ("row", "col", "both"):
+        raise KgeError(f"by: row, col or both, got {by!r}")
+    if out is None:
+        with _allocating_for(stream):
+            qr = Rowwise.empty(rows, cols) if by != "col" else None
+            qc = Rowwise.empty(cols, rows) if by != "row" else None
+    else:
+        if by == "both" and (not isinstance(out, (tuple, list)) or len(out) != 2):
+            raise KgeError("out: a pair is wanted for both layouts")
+        qr, qc = out if by == "both" else (out, None) if by == "row" else (None, out)
+        for q in (qr, qc):
+            if q is not None:
+                _here(q.codes, q.scales)
+    buf = _scratch(ws, _rowwise_bytes(rows, cols), stream) if qc is not None else None
+    _check(load().kge_quantize_rowwise(px, dt, rows, cols, ld, qr.ref if qr else None, qc.ref if qc else None, _ptr(buf),
+                                       0 if buf is None else buf.numel(), _queue(dev, stream)), "kge_quantize_rowwise")
+    return (qr, qc) if by == "both" else qr or qc
+
+
+def matmul_rowwise(a: Rowwise, b: Rowwise, rows=None, dtype=torch.bfloat16, out=None, accumulate: bool = False, ws: Workspace | None = None, stream=None):
+    """kge_matmul_rowwise: a[rows] b^t in fp32 or bf16, sums of the codes' products exact; accumulate: added to `out`."""
+    dev = _here(a.codes, a.scales, b.codes, b.scales, rows, out)
+    m = a.rows if rows is None else rows.numel()
+    if accumulate and out is None:
+        raise KgeError("accumulate needs a matrix to add to")
+    out, po, do, ldo = _new(out, m, b.rows, dtype, "kge_matmul_rowwise", stream)
+    need = _matmul_rowwise_bytes(m, b.rows, a.cols)
+    buf = _scratch(ws, need, stream) if need > 256 else None                   # (256: nothing but its alignment)
+    _check(load().kge_matmul_rowwise(a.ref, None if rows is None else _rows_of(rows, m, "rows"), m, b.ref, 1 if accumulate else 0, po, do, ldo,
+                                     _ptr(buf), 0 if buf is None else buf.numel(), _queue(dev, stream)), "kge_matmul_rowwise")
+    return out
+
+
+class AdamWState:
+    """The moments of one tensor of kge_adamw: fp32 (m, v), or 8-bit codes (uint8, e4m3 and e5m2, padded to a multiple of 128) with a scale byte per 128
+    elements (uint8, padded to a multiple of four)."""
+
+    def __init__(self, m, v, m_scales=None, v_scales=None):
+        self.m, self.v, self.m_scales, self.v_scales = m, v, m_scales, v_scales
+        self.bits = 32 if m_scales is None else 8
+        if (m_scales is None) != (v_scales is None):
+            raise KgeError("scales: of both moments or of none")
+
+    @staticmethod
+    def zeros(n: int, bits: int = 32, device="cuda"):
+        if bits not in (32, 8):
+            raise KgeError(f"bits: 32 or 8, got {bits}")
+        nb = -(-n // 128)
+        size, dt = (n, torch.float32) if bits == 32 else (128 * nb, torch.uint8)
+        m, v = (torch.zeros(size, dtype=dt, device=device) for _ in range(2))
+        return AdamWState(m, v) if bits == 32 else AdamWState(m, v, *(torch.zeros(-(-nb // 4) * 4, dtype=torch.uint8, device=device) for _ in range(2)))
+
+
+class AdamW:
+    """kge_adamw over a fixed list of tensors: `params` (fp32, contiguous, any shape), their moments, and optionally bf16 shadows (entries may be None) that
+    step() rewrites.  bits: of new moments, which are zeros (a number, or one for each tensor); weight_decay: likewise.  seed and tag: of the generator that rounds 8-bit
+    moments (another tag for each AdamW of a program)."""
+
+    def __init__(self, params, states=None, shadows=None, bits=32, weight_decay=0.01, seed: int = 0, tag: int = 0):
+        self.params = list(params)
+        k = len(self.params)
+        each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * k       # noqa: E731
+        self.states = [AdamWState.zeros(p.numel(), b, p.device) for p, b in zip(self.params, each(bits), strict=True)] if states is None else list(states)
+        self.shadows = [None] * k if shadows is None else list(shadows)
+        decays = each(weight_decay)
+        if not len(self.states) == len(self.shadows) == len(decays) == k:
+            raise KgeError("states, shadows and weight_decay: one for each tensor")
+        if not 0 <= seed < 1 << 64 or not 0 <= tag < 1 << 32:
+            raise KgeError("seed: 64 bits, tag: 32 bits")
+        self.seed, self.tag, self.sizes, self.dev = seed, tag, [p.numel() for p in self.params], None
+        self.structs = (KgeAdamwTensorT * max(k, 1))()
+        for s, p, st, sh, wd, n in zip(self.structs, self.params, self.states, self.shadows, decays, self.sizes):
+            nb = -(-n // 128)
+            want = (n, n, torch.float32) if st.bits == 32 else (128 * nb, -(-nb // 4) * 4, torch.uint8)
+            dev = p.get_device()
+            if p.dtype != torch.float32 or not p.is_contiguous() or dev < 0 or (self.dev is not None and dev != self.dev):
+                raise KgeError(f"params: contiguous fp32 tensors of one GPU are wanted, got {p.dtype} {tuple(p.shape)} on {p.device}")
+            self.dev = dev
+            for t, size, dt in ((st.m, want[0], want[2]), (st.v, want[0], want[2]), (st.m_scales, want[1], torch.uint8), (st.v_scales, want[1], torch.uint8),
+                                (sh, n, torch.bfloat16)):
+                if t is not None and (t.dtype != dt or t.numel() != size or not t.is_contiguous() or t.get_device() != dev):
+                    raise KgeError(f"moments and shadows: {size} contiguous {dt} on {p.device} are wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
+            s.param_f32, s.param_bf16, s.state_bits, s.n, s.weight_decay = p.data_ptr(), _ptr(sh), st.bits, n, wd
+            s.m, s.v, s.m_scales, s.v_scales = st.m.data_ptr(), st.v.data_ptr(), _ptr(st.m_scales), _ptr(st.v_scales)
+
+    def step(self, grads, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale=None, step_counter=None,
+             stream=None):
+        """One update with `grads`, one (fp32 or bf16, contiguous) for each tensor.  step: 1 for the first; with step_counter (a device counter) step + counter[0].
+        grad_scale: an fp32 number on the GPU that every gradient is multiplied by (a clipping factor, 1 / loss scale)."""
+        dev = _here(grad_scale, step_counter)
+        if len(grads) != len(self.params):
+            raise KgeError(f"grads: {len(self.params)} are wanted, got {len(grads)}")
+        if not grads:
+            return
+        if self.dev != dev:
+            raise KgeError(f"the tensors are on cuda:{self.dev}, the current device is cuda:{dev}")
+        if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+            raise KgeError("grad_scale: one fp32 number on the GPU")
+        arr = (KgeAdamwTensorT * len(grads)).from_buffer_copy(self.structs)       # (of this call: two may run at once)
+        for s, g, n in zip(arr, grads, self.sizes):
+            dt = _DTYPE.get(g.dtype)
+            if dt is None or g.numel() != n or not g.is_contiguous() or g.get_device() != dev:
+                raise KgeError(f"grads: {n} contiguous fp32 or bf16 elements on cuda:{dev} are wanted, got {g.dtype} {tuple(g.shape)} on {g.device}")
+            s.grad, s.grad_dtype = g.data_ptr(), dt
+        cfg = KgeAdamwCfgT(KgeAdamCfgT(lr, beta1, beta2, eps, step, _counter(step_counter)), _ptr(grad_scale), self.seed, self.tag, 0)
+        _check(load().kge_adamw(C.byref(arr), len(grads), C.byref(cfg), _queue(dev, stream)), "kge_adamw")

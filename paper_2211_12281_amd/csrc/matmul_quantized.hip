@@ -18,6 +18,7 @@
 // which first fragments and the last tiles' stores are a tenth, matrix pipe 62 % busy at 1.9 GHz; fp32 output 425 us, 1.29 PFLOP/s, 73 % busy at 1.78 GHz);
 // products of a few hundred tiles the trips to memory of a tile's start and end (24,576 gathered rows x 256 x 768, fp32 output: 22 us, of which its bytes are 10);
 // one token the weights' bytes or the launch (1 x 2,048 x 2,048 4.1 us, 1 x 4,096 x 16,384 17.4, 3.9 TB/s).
+#include "lds_copy.hpp"
 #include "text_ops.hpp"
 #include <type_traits>
 
@@ -56,25 +57,6 @@ struct MatmulArgs {
     float *part; int64_t part_ld;                             // partial sums [split][m][part_ld] (null: one split)
     int kb, kb_per, splits, tiles_m, tiles_n;
 };
-
-__device__ __forceinline__ void mq_copy16(const void *g, uint32_t lds) {
-    // lane l's 16 bytes go to LDS address lds + 16 l; tracked by vmcnt, unseen by the compiler
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(g) : "memory");
-}
-__device__ __forceinline__ void mq_copy4(const void *g, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(g) : "memory");
-}
-// the same from base + a 32-bit offset of each lane
-__device__ __forceinline__ void mq_copy16(const uint8_t *base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
-}
-__device__ __forceinline__ void mq_copy4(const uint8_t *base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
-}
-template <int N> __device__ __forceinline__ void mq_wait_vmcnt() {
-    static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit counter");
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 
 // Two codes (low or high half of a word) as two bf16 numbers with their scale 2^(byte - 127), given as a float's bits byte << 23
 template <int FMT, bool HI> __device__ __forceinline__ uint32_t mq_widen2(uint32_t w, float scale) {
@@ -225,16 +207,16 @@ void matmul_tiles_kernel(const MatmulArgs p) {
     auto copy = [&](int slot, int c) {
         if (c >= SC) {
             const uint32_t to = lds0 + (uint32_t)slot * STAGE + (uint32_t)(CP * wave + c - SC) * 1024;
-            if constexpr (FAR) mq_copy16(gc[c - SC], to);
-            else mq_copy16(base, oc[c - SC], to);
+            if constexpr (FAR) kge_copy16(gc[c - SC], to);
+            else kge_copy16(base, oc[c - SC], to);
         } else {
             // scales first.  Where the word has been copied before, all lanes take one address and write to the third place: no branch, which would
             // take the products of the step before behind the barrier, and no lines fetched again
             const bool need = (next & 3) == 0 || next == kb0;
             const uint32_t to = lds0 + NST * STAGE + (need ? (uint32_t)(next >> 2 & 1) : 2u) * WORDS + (uint32_t)(SC * wave + c) * 256;
             const int off = (next >> 2) * 4;
-            if constexpr (FAR) mq_copy4((need ? gs[c] : p.bs) + off, to);
-            else mq_copy4(sbase + off, os & (need ? 0xffffffffu : 0u), to);
+            if constexpr (FAR) kge_copy4((need ? gs[c] : p.bs) + off, to);
+            else kge_copy4(sbase + off, os & (need ? 0xffffffffu : 0u), to);
         }
     };
     auto advance = [&] {                                                          // past the end: the last block again, harmless
@@ -343,7 +325,7 @@ void matmul_tiles_kernel(const MatmulArgs p) {
             for (int c = 0; c < PER; ++c) copy(s, c);
             advance();
         }
-        mq_wait_vmcnt<(NST - 1) * PER>();
+        kge_wait_vmcnt<(NST - 1) * PER>();
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < NI; ++i) read_b(0, i, 0, 0);
@@ -368,7 +350,7 @@ void matmul_tiles_kernel(const MatmulArgs p) {
             for (int st = 0; st < STEPS; ++st) {
                 const bool last = st == STEPS - 1;
                 if (last) {
-                    mq_wait_vmcnt<(NST - 2) * PER>();                             // the next block has landed ...
+                    kge_wait_vmcnt<(NST - 2) * PER>();                             // the next block has landed ...
                     __syncthreads();                                              // ... for everyone, and everyone has read this one, whose stage is refilled
                 }
                 step(st & 1, last ? after : slot, last ? 0 : st + 1, [&](int t) {
@@ -384,7 +366,7 @@ void matmul_tiles_kernel(const MatmulArgs p) {
             advance();
             slot = after;
         }
-        mq_wait_vmcnt<0>();                                                       // no copy may be in flight when the LDS is released
+        kge_wait_vmcnt<0>();                                                       // no copy may be in flight when the LDS is released
     }
 
     // Accumulator layout: lane holds row lr of A's block; element e is B's row 8 (e / 4) + 4 g + e % 4.  Stored from there a row gets sixteen bytes at a

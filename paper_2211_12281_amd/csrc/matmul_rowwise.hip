@@ -1,0 +1,429 @@
+// Product of two matrices in 8-bit integers with one scale per row (quantize_rowwise.hip), both contiguous along the contraction:
+//
+//   out[i, j] (+)= sa[rows[i]] sb[j]  sum over k of A[rows[i], k] B[j, k]
+//
+// The sums are exact: 8-bit matrix instructions with 32-bit integer accumulators (k <= 131,071 keeps them below 2^31), partial sums of a split contraction too, so the
+// result does not depend on tiles or splits.  The scales are applied once, as the sums leave the accumulators.
+#include "lds_copy.hpp"
+#include "text_ops.hpp"
+#include <type_traits>
+
+typedef int mi_i32x4 __attribute__((ext_vector_type(4)));
+typedef int mi_i32x16 __attribute__((ext_vector_type(16)));
+
+int kge_check_rowwise(const kge_rowwise_t *q);
+
+namespace {
+
+constexpr int BLOCK = 128;                                    // bytes of a row that a stage holds
+
+struct MatmulArgs {
+    const int8_t *a, *b; const float *as, *bs; int64_t a_ld, b_ld; const int32_t *rows; int64_t a_rows;
+    int64_t m, n;
+    void *out; int64_t out_ld; int out16, accumulate;
+    int32_t *part; int64_t part_ld;                           // partial sums [split][m][part_ld] (null: one split)
+    int kb, kb_per, splits, tiles_m, tiles_n;
+};
+
+// eight (bf16 output) or four (fp32 output) consecutive columns of an output row, of which n are inside
+template <int C> __device__ __forceinline__ void put(const MatmulArgs &p, int64_t row, int64_t col, float (&v)[C]) {
+    const int n = (int)(p.n - col < C ? p.n - col : C);
+    if (n <= 0) return;
+    if (p.out16) {
+        uint16_t *q = (uint16_t *)p.out + row * p.out_ld + col;
+        if (p.accumulate) {
+#pragma unroll
+            for (int e = 0; e < C; ++e)
+                if (e < n) v[e] += __uint_as_float((uint32_t)q[e] << 16);
+        }
+        if constexpr (C == 8) kge_store8<true>(q, 0, n, v);
+        else if (n == 4) {
+            typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf2;
+            *(kge_u32x2_a2 *)q = kge_u32x2{__builtin_bit_cast(uint32_t, bf2{(__bf16)v[0], (__bf16)v[1]}), __builtin_bit_cast(uint32_t, bf2{(__bf16)v[2], (__bf16)v[3]})};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (e < n) ((__bf16 *)q)[e] = (__bf16)v[e];
+        }
+    } else {
+        float *q = (float *)p.out + row * p.out_ld + col;
+        if (n == C) {
+#pragma unroll
+            for (int e = 0; e < C; e += 4) {
+                kge_f32x4 r = {v[e], v[e + 1], v[e + 2], v[e + 3]};
+                if (p.accumulate) {
+                    const kge_f32x4 o = *(const kge_f32x4_a4 *)(q + e);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) r[u] += o[u];
+                }
+                *(kge_f32x4_a4 *)(q + e) = r;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < C - 1; ++e)
+                if (e < n) q[e] = p.accumulate ? q[e] + v[e] : v[e];
+        }
+    }
+}
+// row of A of an output row, -1: a row of zeros
+__device__ __forceinline__ int64_t source(const MatmulArgs &p, int64_t row) {
+    if (!p.rows) return row;
+    const int64_t r = p.rows[row];
+    return r >= 0 && r < p.a_rows ? r : -1;
+}
+// four columns' scales; columns beyond the matrix take the last one's
+__device__ __forceinline__ kge_f32x4 scales4(const MatmulArgs &p, int64_t col) {
+    kge_f32x4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = p.bs[min(col + e, p.n - 1)];
+    return r;
+}
+
+// Workgroup = WM x WN waves = TM rows of A x TN rows of B, wave = NJ x NI blocks of 32 x 32.  Stages of 128 bytes of every row pass through a ring of NST
+// stages in the LDS, filled by asynchronous copies of whole lines.  A row's 16-byte pieces lie XOR-swizzled by (row / 2) % 8, so that the
+// fragment reads of sixteen consecutive rows fall into different ones of the 64 banks.  Rows beyond the matrices are read from row 0 and not
+// stored.  Which bytes a lane half contracts first does not matter as long as both operands agree.
+//
+// A stage is four steps of 32 bytes; the fragments of the next step are read while this one's are multiplied, across the stages too: the only barrier of a stage
+// stands in front of the products of its last step, whose operands are in registers by then, and the stage that it frees is refilled behind it.
+//
+// FAR: a copy's lanes have 64-bit addresses; else (codes of less than 4 GiB) a base and 32-bit offsets.
+template <int WM, int WN, int NJ, int NI, int NST, int OCC, bool FAR>
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
+void matmul_tiles_kernel(const MatmulArgs p) {
+    constexpr int NW = WM * WN, TM = 32 * NJ * WM, TN = 32 * NI * WN, ROWS = TM + TN, CP = ROWS / 8 / NW;      // copies of a wave per stage
+    constexpr int STAGE = ROWS * BLOCK, STEPS = 4, SLOTS = NI * NJ;
+    static_assert(ROWS % (8 * NW) == 0 && NST >= 2 && (NST - 1) * CP < 64 && NST * STAGE <= 160 * 1024, "tile");
+    __shared__ __attribute__((aligned(16))) char lds[NST * STAGE];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, g = lane >> 5;
+    // ids go round-robin to the 8 dies: a die takes a run of tiles, eight tiles of A deep, so that both operands' rows meet in its L2
+    const int total = p.tiles_m * p.tiles_n * p.splits, per = (total + 7) >> 3;
+    int w = ((int)blockIdx.x & 7) * per + ((int)blockIdx.x >> 3);
+    if (((int)blockIdx.x >> 3) >= per || w >= total) return;
+    const int split = __builtin_amdgcn_readfirstlane(w / (p.tiles_m * p.tiles_n));
+    w -= split * p.tiles_m * p.tiles_n;
+    const int band = w / (8 * p.tiles_n), deep = min(8, p.tiles_m - 8 * band), in = w - band * 8 * p.tiles_n;
+    const int64_t m0 = (int64_t)(8 * band + in % deep) * TM, n0 = (int64_t)(in / deep) * TN;
+    const int kb0 = split * p.kb_per, kb1 = min(p.kb, kb0 + p.kb_per);
+
+    // Row r of the stage: B's tile first, then A's.  Copy j of this wave takes rows 8 (CP wave + j) .. + 7
+    auto b_row = [&](int r) { const int64_t s = n0 + r; return s < p.n ? s : 0; };
+    auto a_row = [&](int r) -> int64_t {
+        const int64_t s = m0 + r, t = s < p.m ? source(p, s) : 0;
+        return t < 0 ? 0 : t;
+    };
+    auto swizzle = [](int r) { return (r >> 1) & 7; };
+    static_assert(FAR || TN % (8 * CP) == 0, "all rows that a wave copies are of one operand");
+    const bool of_b = 8 * CP * wave < TN;                                          // (not FAR)
+    const uint8_t *base = (const uint8_t *)(of_b ? p.b : p.a), *gc[FAR ? CP : 1];
+    uint32_t oc[FAR ? 1 : CP];
+#pragma unroll
+    for (int j = 0; j < CP; ++j) {
+        const int r0 = 8 * (CP * wave + j), r = r0 + (lane >> 3), piece = ((lane & 7) ^ swizzle(r)) * 16;
+        if constexpr (FAR) gc[j] = (const uint8_t *)(r0 < TN ? p.b + b_row(r) * p.b_ld : p.a + a_row(r - TN) * p.a_ld) + piece + (int64_t)kb0 * BLOCK;   // (a copy's rows are of one operand)
+        else oc[j] = (uint32_t)(of_b ? b_row(r) * p.b_ld : a_row(r - TN) * p.a_ld) + piece;
+    }
+    if constexpr (!FAR) base += (int64_t)kb0 * BLOCK;
+    // (the gathered row numbers have to be there before the loop: a wait of the compiler's inside it would drain the ring)
+#pragma unroll
+    for (int j = 0; j < CP; ++j) {
+        if constexpr (FAR) asm volatile("" : "+v"(gc[j]));
+        else asm volatile("" : "+v"(oc[j]));
+    }
+    int next = kb0;                                                               // block that the next copies fetch, and their addresses'
+    auto copy = [&](int slot, int c) {
+        const uint32_t to = lds0 + (uint32_t)slot * STAGE + (uint32_t)(CP * wave + c) * 1024;
+        if constexpr (FAR) kge_copy16(gc[c], to);
+        else kge_copy16(base, oc[c], to);
+    };
+    auto advance = [&] {                                                          // past the end: the last block again, harmless
+        const int d = next + 1 < kb1 ? 1 : 0;
+        next += d;
+        if constexpr (FAR) {
+#pragma unroll
+            for (int j = 0; j < CP; ++j) gc[j] += d * BLOCK;
+        } else base += d * BLOCK;
+    };
+    const int wn = (wave % WN) * 32 * NI, wm = (wave / WN) * 32 * NJ;
+    mi_i32x16 acc[NI][NJ];
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+
+    mi_i32x4 fb[2][NI], fa[2][NJ];                                                // this step's fragments and the next one's
+    const int swz = swizzle(lr);
+    auto read = [&](mi_i32x4 &to, int slot, int step, int row) {
+        to = *(const mi_i32x4 *)(lds + slot * STAGE + (row + lr) * BLOCK + (((2 * step + g) ^ swz) << 4));
+    };
+    // fragment r in the order in which a step wants them: the first of A, all of B, the others of A
+    auto read_next = [&](int set, int r, int slot, int st) {
+        if (r == 0) read(fa[set][0], slot, st, TN + wm);
+        else if (r <= NI) read(fb[set][r - 1], slot, st, wn + 32 * (r - 1));
+        else read(fa[set][r - NI], slot, st, TN + wm + 32 * (r - NI));
+    };
+    // The products of one step and, behind each of them, a read of the next step's fragments and whatever `also` does.  (Left to itself the compiler puts all reads
+    // in front of all products, and those behind the barrier.)
+    auto step = [&](int set, int slot, int st, auto also) {                       // slot, st: of the next step
+#pragma unroll
+        for (int t = 0; t < SLOTS; ++t) {
+            const int j = t / NI, i = t % NI;
+            acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[set][i], fa[set][j], acc[i][j], 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < NI + NJ; ++r)
+                if (r * SLOTS / (NI + NJ) / (SLOTS >= 2 * (NI + NJ) ? 2 : 1) == t) read_next(set ^ 1, r, slot, st);
+            also(t);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    if (kb0 < kb1) {
+#pragma unroll
+        for (int s = 0; s < NST; ++s) {
+#pragma unroll
+            for (int c = 0; c < CP; ++c) copy(s, c);
+            advance();
+        }
+        kge_wait_vmcnt<(NST - 1) * CP>();
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < NI + NJ; ++r) read_next(0, r, 0, 0);
+        int slot = 0;
+        for (int kb = kb0; kb < kb1; ++kb) {
+            const int after = slot == NST - 1 ? 0 : slot + 1;
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) {
+                const bool last = st == STEPS - 1;
+                if (last) {
+                    kge_wait_vmcnt<(NST - 2) * CP>();                             // the next block has landed ...
+                    __syncthreads();                                              // ... for everyone, and everyone has read this one, whose stage is refilled
+                }
+                step(st & 1, last ? after : slot, last ? 0 : st + 1, [&](int t) {
+                    if (!last) return;
+#pragma unroll
+                    for (int c = 0; c < CP; ++c)
+                        if (c * SLOTS / CP == t) copy(slot, c);
+                });
+            }
+            advance();
+            slot = after;
+        }
+        kge_wait_vmcnt<0>();                                                      // no copy may be in flight when the LDS is released
+    }
+
+    // Accumulator layout: lane holds row lr of A's block; element e is B's row 8 (e / 4) + 4 g + e % 4.  Stored from there a row gets sixteen bytes at a
+    // time; so 32 rows of the wave at a time go through the LDS, and rows leave in whole lines.  (Row stride one piece more than
+    // the row: writes and reads of sixteen lanes fall into different banks.)
+    constexpr int LD = 32 * NI + 4;
+    static_assert(NW * 32 * LD * 4 <= NST * STAGE, "the waves' rows fit the ring");
+    int32_t *mine = (int32_t *)lds + wave * (32 * LD);
+    __syncthreads();                                                              // everyone is done with the ring
+    const int64_t col0 = n0 + wn;
+    auto store = [&](auto wide) {                                                 // wide: eight columns per lane, else four
+        constexpr int C = decltype(wide)::value ? 8 : 4, LPR = 32 * NI / C, RPI = 64 / LPR;         // lanes per row, rows at a time
+        const int c = C * (lane % LPR);
+        kge_f32x4 sb[C / 4];
+#pragma unroll
+        for (int e = 0; e < C / 4; ++e) sb[e] = scales4(p, col0 + c + 4 * e);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *(mi_i32x4 *)(mine + lr * LD + 32 * i + 8 * q + 4 * g) = mi_i32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+            __builtin_amdgcn_wave_barrier();
+            const int64_t row0 = m0 + wm + 32 * j;
+#pragma unroll
+            for (int r0 = 0; r0 < 32; r0 += RPI) {
+                const int r = r0 + lane / LPR;
+                const int64_t row = row0 + r;
+                mi_i32x4 x[C / 4];
+#pragma unroll
+                for (int e = 0; e < C / 4; ++e) x[e] = *(const mi_i32x4 *)(mine + r * LD + c + 4 * e);
+                if (row >= p.m) continue;
+                if constexpr (C == 4)
+                    if (p.part) {
+                        if (col0 + c < p.part_ld) *(mi_i32x4 *)(p.part + ((int64_t)split * p.m + row) * p.part_ld + col0 + c) = x[0];
+                        continue;
+                    }
+                const int64_t from = source(p, row);
+                const float sa = from < 0 ? 0.f : p.as[from];
+                float v[C];
+#pragma unroll
+                for (int e = 0; e < C; ++e) v[e] = from < 0 ? 0.f : (float)x[e >> 2][e & 3] * sa * sb[e >> 2][e & 3];
+                put<C>(p, row, col0 + c, v);
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+    if (p.part || !p.out16) store(std::false_type());
+    else store(std::true_type());
+}
+
+// Sums the splits' partial results.
+__global__ __launch_bounds__(256) void matmul_join_kernel(const MatmulArgs p) {
+    const int64_t per = p.part_ld / 4, total = p.m * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / per, col = (i - row * per) * 4;
+        mi_i32x4 s = {0, 0, 0, 0};
+        for (int k = 0; k < p.splits; ++k) s += *(const mi_i32x4 *)(p.part + ((int64_t)k * p.m + row) * p.part_ld + col);
+        const int64_t from = source(p, row);
+        const kge_f32x4 sb = scales4(p, col);
+        const float sa = from < 0 ? 0.f : p.as[from];
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = from < 0 ? 0.f : (float)s[e] * sa * sb[e];
+        put<4>(p, row, col, v);
+    }
+}
+
+// Few rows of A (one token, a small batch), and small products of any shape: a workgroup takes sixteen rows of B against 16 MF rows of A, its eight
+// waves take the blocks of 128 in turn, straight from memory into fragments, and add up through the LDS.
+constexpr int SKINNY_WAVES = 8;
+template <int MF> __global__ __launch_bounds__(64 * SKINNY_WAVES) void matmul_skinny_kernel(const MatmulArgs p) {
+    __shared__ int32_t part[SKINNY_WAVES][MF][16][16 + 4];     // [wave][block][row of A][row of B]
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 15, g = lane >> 4;
+    const int64_t n0 = (int64_t)(blockIdx.x % (uint32_t)p.tiles_n) * 16, m0 = (int64_t)(blockIdx.x / (uint32_t)p.tiles_n) * (16 * MF), rb = n0 + lr < p.n ? n0 + lr : 0;
+    const int8_t *gb = p.b + rb * p.b_ld + 32 * g, *ga[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f) {
+        const int64_t r = m0 + 16 * f + lr, s = r < p.m ? source(p, r) : 0;
+        ga[f] = p.a + (s < 0 ? 0 : s) * p.a_ld + 32 * g;
+    }
+    mi_i32x4 acc[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f) acc[f] = mi_i32x4{0, 0, 0, 0};
+    for (int kb = wave; kb < p.kb; kb += SKINNY_WAVES) {
+        const mi_i32x4 b0 = *(const mi_i32x4 *)(gb + (int64_t)kb * BLOCK), b1 = *(const mi_i32x4 *)(gb + (int64_t)kb * BLOCK + 16);
+        mi_i32x4 a0[MF], a1[MF];
+#pragma unroll
+        for (int f = 0; f < MF; ++f) { a0[f] = *(const mi_i32x4 *)(ga[f] + (int64_t)kb * BLOCK); a1[f] = *(const mi_i32x4 *)(ga[f] + (int64_t)kb * BLOCK + 16); }
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+            acc[f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b0, a0[f], acc[f], 0, 0, 0);
+            acc[f] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b1, a1[f], acc[f], 0, 0, 0);
+        }
+    }
+    // lane holds A's row lr; element e is B's row 4 g + e
+#pragma unroll
+    for (int f = 0; f < MF; ++f) *(mi_i32x4 *)&part[wave][f][lr][4 * g] = acc[f];
+    __syncthreads();
+    for (int i = tid; i < MF * 64; i += 64 * SKINNY_WAVES) {
+        const int f = i >> 6, row = (i >> 2) & 15, c = (i & 3) * 4;
+        mi_i32x4 s = {0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < SKINNY_WAVES; ++k) s += *(const mi_i32x4 *)&part[k][f][row][c];
+        const int64_t r = m0 + 16 * f + row;
+        if (r >= p.m) continue;
+        const int64_t from = source(p, r);
+        const kge_f32x4 sb = scales4(p, n0 + c);
+        const float sa = from < 0 ? 0.f : p.as[from];
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = from < 0 ? 0.f : (float)s[e] * sa * sb[e];
+        put<4>(p, r, n0 + c, v);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+constexpr int SKINNY_GROUPS = 512, SKINNY_WORK = 12, SKINNY_LONG = 4;
+constexpr int BIG_TILES = 192;
+constexpr int64_t WANTED = 512;
+constexpr int SPLIT_BLOCKS = 8;
+constexpr int64_t MAX_TILES = 1 << 22;                         // of a launch: a grid has fewer than 2^32 threads
+
+// Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B; stages; waves per SIMD; whether matrices may be 4 GiB and more
+struct Tile { int wm, wn, nj, ni, nst, occ; bool far; };
+constexpr Tile BIG = {2, 2, 4, 4, 2, 1, false}, MID = {2, 2, 2, 2, 2, 2, true};
+constexpr int tile_m(const Tile &t) { return 32 * t.wm * t.nj; }
+constexpr int tile_n(const Tile &t) { return 32 * t.wn * t.ni; }
+
+// skinny: sixteens of rows of A that a workgroup of matmul_skinny_kernel takes, 0 for tiles
+struct Plan { int skinny, big, tiles_m, tiles_n, splits, kb_per; int64_t part_ld, part_bytes; };
+
+Plan make_plan(int64_t m, int64_t n, int64_t k, size_t room, bool far = false) {
+    Plan q = {};
+    const int64_t kb = (k + BLOCK - 1) / BLOCK;
+    q.splits = 1; q.kb_per = (int)kb;
+    const int mf = m <= 16 ? 1 : m <= 32 ? 2 : 4;
+    const int64_t gm = (m + 16 * mf - 1) / (16 * mf), gn = (n + 15) / 16, rounds = (kb + SKINNY_WAVES - 1) / SKINNY_WAVES;
+    if (gm * gn <= SKINNY_GROUPS ? rounds * mf <= SKINNY_WORK : m <= 16 && gn <= MAX_TILES && rounds <= SKINNY_LONG) {
+        q.skinny = mf; q.tiles_m = (int)gm; q.tiles_n = (int)gn;
+        return q;
+    }
+    const auto tiles_of = [&](const Tile &t, int64_t &tm, int64_t &tn) { tm = (m + tile_m(t) - 1) / tile_m(t); tn = (n + tile_n(t) - 1) / tile_n(t); return tm * tn; };
+    int64_t tm, tn, tiles = tiles_of(BIG, tm, tn);
+    q.big = tiles >= BIG_TILES && m > tile_m(MID) && n > tile_n(MID) && !far;
+    if (!q.big) tiles = tiles_of(MID, tm, tn);
+    q.tiles_m = (int)tm; q.tiles_n = (int)tn;
+    q.part_ld = (n + 3) / 4 * 4;
+    if (!q.big && tiles * 4 <= WANTED && kb >= 2 * SPLIT_BLOCKS) {
+        int64_t s = WANTED / tiles;
+        if (s > kb / SPLIT_BLOCKS) s = kb / SPLIT_BLOCKS;
+        const int64_t one = m * q.part_ld * 4;
+        if (s * one > (int64_t)room) s = (int64_t)room / one;
+        if (s > 1) {
+            q.kb_per = (int)((kb + s - 1) / s);
+            q.splits = (int)((kb + q.kb_per - 1) / q.kb_per);
+            q.part_bytes = q.splits * one;
+        }
+    }
+    return q;
+}
+
+void launch(const MatmulArgs &p, const Plan &q, hipStream_t st) {
+    if (q.skinny) {
+        const dim3 grid((unsigned)(p.tiles_m * p.tiles_n)), blk(64 * SKINNY_WAVES);
+        if (q.skinny == 1) hipLaunchKernelGGL((matmul_skinny_kernel<1>), grid, blk, 0, st, p);
+        else if (q.skinny == 2) hipLaunchKernelGGL((matmul_skinny_kernel<2>), grid, blk, 0, st, p);
+        else hipLaunchKernelGGL((matmul_skinny_kernel<4>), grid, blk, 0, st, p);
+        return;
+    }
+    const dim3 grid((unsigned)((p.tiles_m * p.tiles_n * p.splits + 7) / 8 * 8));
+    if (q.big) hipLaunchKernelGGL((matmul_tiles_kernel<BIG.wm, BIG.wn, BIG.nj, BIG.ni, BIG.nst, BIG.occ, BIG.far>), grid, dim3(64 * BIG.wm * BIG.wn), 0, st, p);
+    else hipLaunchKernelGGL((matmul_tiles_kernel<MID.wm, MID.wn, MID.nj, MID.ni, MID.nst, MID.occ, MID.far>), grid, dim3(64 * MID.wm * MID.wn), 0, st, p);
+    if (p.part) {
+        const int64_t blocks = (p.m * (p.part_ld / 4) + 255) / 256;
+        hipLaunchKernelGGL(matmul_join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, p);
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t kge_matmul_rowwise_workspace_bytes(int64_t m, int64_t n, int64_t k) {
+    if (m < 0 || n < 0 || k < 0 || m >= (1ll << 31) || n >= (1ll << 31) || k >= (1ll << 31)) return 0;
+    return (size_t)make_plan(m, n, k, ~0ull >> 1).part_bytes + 256;
+}
+
+int kge_matmul_rowwise(const kge_rowwise_t *a, const int32_t *rows, int64_t m, const kge_rowwise_t *b, int32_t accumulate, void *out, int32_t out_dtype,
+                       int64_t out_ld, void *ws, size_t ws_bytes, void *hip_stream) {
+    const int ca = kge_check_rowwise(a), cb = kge_check_rowwise(b);
+    if (ca == KGE_E_INVALID_ARG || cb == KGE_E_INVALID_ARG || a->cols != b->cols || m < 0 || m >= (1ll << 31) || (!rows && m != a->rows) ||
+        ((uintptr_t)rows & 3) != 0 || (accumulate != 0 && accumulate != 1) || kge_bad_type(out_dtype)) return KGE_E_INVALID_ARG;
+    if (m > 0 && b->rows > 0 && (kge_bad_rows(out, out_dtype, out_ld, b->rows) || out_ld >= KGE_MAX_LD)) return KGE_E_INVALID_ARG;
+    if (ca != KGE_OK || cb != KGE_OK) return KGE_E_UNSUPPORTED;
+    if (m == 0 || b->rows == 0) return KGE_OK;
+    MatmulArgs p = {};
+    p.a = a->codes; p.as = a->scales; p.a_ld = a->ld; p.rows = rows; p.a_rows = a->rows;
+    p.b = b->codes; p.bs = b->scales; p.b_ld = b->ld;
+    p.m = m; p.n = b->rows; p.out = out; p.out_ld = out_ld; p.out16 = out_dtype == KGE_BF16; p.accumulate = accumulate;
+    const int64_t k = a->rows > 0 ? a->cols : 0;               // (a table without rows: nothing may be read, every row of the result is zeros)
+    const size_t lost = ws ? (256 - ((uintptr_t)ws & 255)) & 255 : 0;
+    bool far = false;
+    for (const kge_rowwise_t *q : {a, b}) far = far || q->rows * q->ld >= (1ll << 32);
+    const Plan q = make_plan(m, p.n, k, ws && ws_bytes > lost ? ws_bytes - lost : 0, far);
+    if ((int64_t)q.tiles_m * q.tiles_n > MAX_TILES) return KGE_E_UNSUPPORTED;
+    p.kb = (int)((k + BLOCK - 1) / BLOCK); p.kb_per = q.kb_per; p.splits = q.splits; p.tiles_m = q.tiles_m; p.tiles_n = q.tiles_n;
+    p.part_ld = q.part_ld;
+    if (q.splits > 1) p.part = (int32_t *)((char *)ws + lost);
+    launch(p, q, (hipStream_t)hip_stream);
+    return kge_launch_status();
+}
+
+}  // extern "C"

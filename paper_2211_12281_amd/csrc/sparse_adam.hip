@@ -3,6 +3,7 @@
 //   2. every run of equal rows is reduced in increasing position order (fixed order, no atomics)
 //   3. one Adam step on each distinct row, fp32 master weights + moments, optional bf16 shadow
 // Only rows that occur in idx are read or written (arXiv 2211.12281, Section 1: sparse access).
+#include "adam_ops.hpp"
 #include "kge_internal.h"
 #include "prep_kernels.h"
 #include "row_finish.hpp"
@@ -153,17 +154,6 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 }
 
 struct AdamConst { float lr, b1, b2, eps, omb1, omb2, inv_bc1, inv_bc2; const uint64_t *step_counter; uint64_t step; };
-
-// 1 / (1 - beta^step) by binary powering in fp64: products only, so the host (plain calls) and the device (steps read
-// from a counter in device memory) arrive at the same bits.
-__host__ __device__ inline float adam_inv_bias(float beta, uint64_t step) {
-    double p = 1.0, b = (double)beta;
-    for (; step; step >>= 1) {
-        if (step & 1) p *= b;
-        b *= b;
-    }
-    return (float)(1.0 / (1.0 - p));
-}
 
 // With a device counter the corrections belong to step + *counter and are formed by the wave that is about to update.
 __device__ __forceinline__ void adam_resolve(AdamConst &c) {
