@@ -17,22 +17,22 @@ using namespace kge_norm;
 // ---------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------
-template <bool S16, bool B16, int NG, int NT>
-__global__ __launch_bounds__(NT) void norm_fwd_kernel(const FwdArgs a) {
-    __shared__ float red[2][NT / 64][2];
+// A team takes a row at a time; the vectors stand in the LDS (rows of more than 4,096 columns: in memory).
+enum { VEC_POST = 0, VEC_POST_BIAS = 1, VEC_SCALE = 2, VEC_PRE = 3, VEC_PRE_BIAS = 4, VECTORS = 5 };
+template <bool S16, bool B16, int NG, int LAST, int NT, int OCC>
+__global__ __launch_bounds__(NT, OCC) void norm_fwd_kernel(const FwdArgs a) {
+    constexpr bool LDS = NT == 256;
+    __shared__ float red[2][NT / 64][1];
+    extern __shared__ __attribute__((aligned(16))) float vec[];
     const Team t(a.waves);
-    Reduce<2, NT> reduce(red, t);
+    Reduce<1, NT> reduce(red, t);
+    const Columns<NG, LAST> c(a.dim, t.lane, t.size);
     const float inv_dim = 1.f / (float)a.dim;
-    int col[NG], n[NG];
-    Vec postw[NG], postb[NG], scale[NG], prew[NG], preb[NG];
-#pragma unroll
-    for (int k = 0; k < NG; ++k) {
-        col[k] = 8 * (t.lane + k * t.size);
-        n[k] = a.dim - col[k];
-        postw[k].vector(a.post.w, col[k], n[k], 1.f); postb[k].vector(a.post.b, col[k], n[k], 0.f);
-        prew[k].vector(a.pre.w, col[k], n[k], 1.f); preb[k].vector(a.pre.b, col[k], n[k], 0.f);
-        scale[k].vector(a.scale, col[k], n[k], 1.f);
-    }
+    const int wide = 4 * t.size * NG;
+    const float *const from[VECTORS] = {a.post.w, a.post.b, a.scale, a.pre.w, a.pre.b};
+    auto vector = [&](int which, int k) {
+        return LDS ? *(const kge_f32x4 *)(vec + which * wide + c.col(k)) : vector4(from[which], c.col(k), a.dim, which == VEC_POST_BIAS || which == VEC_PRE_BIAS ? 0.f : 1.f);
+    };
     const int64_t step = (int64_t)gridDim.x * t.teams, first = (int64_t)blockIdx.x * t.teams;
     Raw<S16> x[NG];
     Raw<B16> y[NG], g[NG];
@@ -40,317 +40,173 @@ __global__ __launch_bounds__(NT) void norm_fwd_kernel(const FwdArgs a) {
         const bool in = row < a.rows;
 #pragma unroll
         for (int k = 0; k < NG; ++k) {
-            const int m = in ? n[k] : 0;
-            x[k].load(a.x.row(row), col[k], a.x.p ? m : 0);
-            y[k].load(a.y.row(row), col[k], a.y.p ? m : 0);
-            g[k].load(a.gate.row(a.gate.p && in ? (uint32_t)row / a.gate_rows : 0), col[k], a.gate.p ? m : 0);
+            x[k].load(a.x.row(row), c, k, in && a.x.p);
+            y[k].load(a.y.row(row), c, k, in && a.y.p);
+            g[k].load(a.gate.row(a.gate.p && in ? (uint32_t)row / a.gate_rows : 0), c, k, in && a.gate.p);
         }
     };
-    load(first + t.team);
+    load(first + t.team);                                         // (under the loads of the vectors; later rows' wait for nobody but their own wave)
+    if constexpr (LDS) {
+        for (int i = 4 * threadIdx.x; i < wide; i += 4 * NT)
+#pragma unroll
+            for (int v = 0; v < VECTORS; ++v)
+                *(kge_f32x4 *)(vec + v * wide + i) = vector4(from[v], i, a.dim, v == VEC_POST_BIAS || v == VEC_PRE_BIAS ? 0.f : 1.f);
+        __syncthreads();
+    }
     for (int64_t r0 = first; r0 < a.rows; r0 += step) {           // (every team goes round equally often: the waves of one meet at barriers)
+        if constexpr (!LDS) asm volatile("" ::: "memory");        // (the vectors are read for every row: no registers for them in between)
         const int64_t row = r0 + t.team;
         const bool in = row < a.rows;
-        Vec h[NG], u[NG], gv[NG];
+        if (r0 > first) load(row);
+        kge_f32x4 h[NG], u[NG], f[NG];
 #pragma unroll
-        for (int k = 0; k < NG; ++k) { x[k].values(h[k]); y[k].values(u[k]); g[k].values(gv[k]); }
-        if (r0 + step < a.rows) load(row + step);
+        for (int k = 0; k < NG; ++k) { h[k] = x[k].values(); u[k] = y[k].values(); f[k] = g[k].values(); }
         if (a.y.p) {
             if (a.post.on) {
-                const Stats s = statistics<NG>(u, n, a.post, inv_dim, reduce);
+                normalise(u, c, a.post, inv_dim, reduce);
 #pragma unroll
-                for (int k = 0; k < NG; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) u[k].v[e] = fmaf((u[k].v[e] - s.mean) * s.r, postw[k].v[e], postb[k].v[e]);
+                for (int k = 0; k < NG; ++k) u[k] = fma4(u[k], vector(VEC_POST, k), vector(VEC_POST_BIAS, k));
             }
 #pragma unroll
             for (int k = 0; k < NG; ++k) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) h[k].v[e] = fmaf(u[k].v[e], scale[k].v[e] * (a.gate.p ? gv[k].v[e] : 1.f), h[k].v[e]);
-                if (a.h.p && in) kge_store8<S16>(a.h.row(row), col[k], n[k], h[k].v);
+                if (a.scale) u[k] *= vector(VEC_SCALE, k);
+                h[k] = a.gate.p ? fma4(u[k], f[k], h[k]) : u[k] + h[k];
+                if (a.h.p && in && c.inside(k)) store<S16>(a.h.row(row), c, k, h[k]);
             }
         }
         if (a.pre.on) {
-            const Stats s = statistics<NG>(h, n, a.pre, inv_dim, reduce);
-#pragma unroll
-            for (int k = 0; k < NG; ++k) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) h[k].v[e] = fmaf((h[k].v[e] - s.mean) * s.r, prew[k].v[e], preb[k].v[e]);
-                if (in) kge_store8<B16>(a.z.row(row), col[k], n[k], h[k].v);
-            }
-        }
-    }
-}
-
-// ---------------------------------------------------------------------------------------------
-// backward: rows
-// ---------------------------------------------------------------------------------------------
-// A workgroup takes a run of rows, its teams every teams-th row of it, and keeps the run's column sums in registers.  Gates of groups of rows: a run holds
-// whole groups (their gradients are written here) or a part of one (the join writes them).
-template <bool S16, bool B16, int NG, int NT>
-__global__ __launch_bounds__(NT) void norm_bwd_kernel(const BwdArgs a) {
-    __shared__ float red[2][NT / 64][4];
-    __shared__ __attribute__((aligned(16))) float sums[NT][8];
-    const Team t(a.waves);
-    Reduce<4, NT> reduce(red, t);
-    const float inv_dim = 1.f / (float)a.dim;
-    int col[NG], n[NG];
-    Vec postw[NG], prew[NG], scale[NG];
-    Vec A[NG], B[NG], C[NG], D[NG], ga[NG], gb[NG];
-#pragma unroll
-    for (int k = 0; k < NG; ++k) {
-        col[k] = 8 * (t.lane + k * t.size);
-        n[k] = a.dim - col[k];
-        postw[k].vector(a.post.w, col[k], n[k], 1.f);
-        prew[k].vector(a.pre.w, col[k], n[k], 1.f);
-        scale[k].vector(a.scale, col[k], n[k], 1.f);
-        A[k].zero(); B[k].zero(); C[k].zero(); D[k].zero(); ga[k].zero(); gb[k].zero();
-    }
-    // adds the teams' sums; afterwards team 0's are the workgroup's, the others' zeros
-    auto join = [&](Vec (&s)[NG]) {
-        if (t.teams == 1) return;
-#pragma unroll
-        for (int k = 0; k < NG; ++k) {
-            if (t.team > 0) {
-                *(kge_f32x4 *)&sums[threadIdx.x][0] = kge_f32x4{s[k].v[0], s[k].v[1], s[k].v[2], s[k].v[3]};
-                *(kge_f32x4 *)&sums[threadIdx.x][4] = kge_f32x4{s[k].v[4], s[k].v[5], s[k].v[6], s[k].v[7]};
-            }
-            __syncthreads();
-            if (t.team == 0) {
-                for (int i = 1; i < t.teams; ++i)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) s[k].v[e] += sums[threadIdx.x + i * t.size][e];
-            } else s[k].zero();
-            __syncthreads();
-        }
-    };
-    const bool grouped = a.gate.p && a.gate_rows > 1;
-    const int64_t run = blockIdx.x;
-    int64_t r0, r1;                                               // rows of the run, and of its first group
-    if (a.parts > 1) {                                            // a part of a group
-        const int64_t group = run / a.parts, part = run - group * a.parts, g0 = group * a.gate_rows, g1 = min(g0 + a.gate_rows, a.rows);
-        r0 = min(g0 + part * a.run, g1); r1 = min(r0 + a.run, g1);
-    } else { r0 = run * a.run; r1 = min(r0 + a.run, a.rows); }
-
-    Raw<S16> rh[NG], rd[NG];
-    Raw<B16> ry[NG], rz[NG], rg[NG];
-    auto load = [&](int64_t row, int64_t end) {
-        const bool in = row < end;
-#pragma unroll
-        for (int k = 0; k < NG; ++k) {
-            const int m = in ? n[k] : 0;
-            rh[k].load(a.h.row(row), col[k], a.pre.on ? m : 0);
-            rd[k].load(a.dh.row(row), col[k], a.dh.p ? m : 0);
-            rz[k].load(a.dz.row(row), col[k], a.pre.on ? m : 0);
-            ry[k].load(a.y.row(row), col[k], a.y.p ? m : 0);
-            if (a.gate.p && !grouped) rg[k].load(a.gate.row(row), col[k], m);
-        }
-    };
-    int64_t g0 = r0;                                              // of the group at hand
-    do {
-        const int64_t g1 = grouped && a.parts <= 1 ? min(g0 + a.gate_rows, r1) : r1;
-        Vec gate[NG];
-#pragma unroll
-        for (int k = 0; k < NG; ++k) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) gate[k].v[e] = 1.f;
-            if (grouped && g0 < g1) {
-                Raw<B16> q;
-                q.load(a.gate.row((uint32_t)g0 / a.gate_rows), col[k], n[k]);
-                q.values(gate[k]);
-                ga[k].zero(); gb[k].zero();
-            }
-        }
-        load(g0 + t.team, g1);
-        for (int64_t q0 = g0; q0 < g1; q0 += t.teams) {
-            const int64_t row = q0 + t.team;
-            const bool in = row < g1;
-            Vec h[NG], d[NG], z[NG], y[NG];
-#pragma unroll
-            for (int k = 0; k < NG; ++k) {
-                rh[k].values(h[k]); rd[k].values(d[k]); rz[k].values(z[k]); ry[k].values(y[k]);
-                if (a.gate.p && !grouped) rg[k].values(gate[k]);
-            }
-            if (q0 + t.teams < g1) load(row + t.teams, g1);
-            // statistics: of rms norms with the sum of dz's products at once, of layer norms after the means
-            float v[4] = {0.f, 0.f, 0.f, 0.f}, rp = 1.f, ry1 = 1.f, c1 = 0.f, c2 = 0.f;
-            if (a.pre.layer || a.post.layer) {
-#pragma unroll
-                for (int k = 0; k < NG; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) { v[0] += h[k].v[e]; v[1] += y[k].v[e]; }
-                reduce(v, 2);
-                const float mh = a.pre.layer ? v[0] * inv_dim : 0.f, my = a.post.layer ? v[1] * inv_dim : 0.f;
-#pragma unroll
-                for (int k = 0; k < NG; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        h[k].v[e] = e < n[k] ? h[k].v[e] - mh : 0.f;
-                        y[k].v[e] = e < n[k] ? y[k].v[e] - my : 0.f;
-                    }
-            }
-            if (a.pre.on || a.post.on) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = 0.f;
-#pragma unroll
-                for (int k = 0; k < NG; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float q = z[k].v[e] * prew[k].v[e];
-                        v[0] = fmaf(h[k].v[e], h[k].v[e], v[0]); v[1] = fmaf(y[k].v[e], y[k].v[e], v[1]);
-                        v[2] = fmaf(q, h[k].v[e], v[2]); v[3] += q;
-                    }
-                reduce(v, 4);
-                if (a.post.on) ry1 = inv_sqrt(fmaf(v[1], inv_dim, a.post.eps));
-                if (a.pre.on) {
-                    rp = inv_sqrt(fmaf(v[0], inv_dim, a.pre.eps));
-                    c2 = v[2] * rp * inv_dim;
-                    c1 = a.pre.layer ? v[3] * inv_dim : 0.f;
-                }
-            }
-            float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < NG; ++k) {
-                if (a.pre.on) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float hat = h[k].v[e] * rp;
-                        C[k].v[e] = fmaf(z[k].v[e], hat, C[k].v[e]);
-                        D[k].v[e] += z[k].v[e];
-                        d[k].v[e] = fmaf(fmaf(-hat, c2, z[k].v[e] * prew[k].v[e] - c1), rp, d[k].v[e]);
-                    }
-                }
-                if (a.dx.p && in) kge_store8<S16>(a.dx.row(row), col[k], n[k], d[k].v);
-                if (!a.y.p) continue;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float hat = y[k].v[e] * ry1, x = e < n[k] ? d[k].v[e] : 0.f;
-                    y[k].v[e] = hat;
-                    if (grouped) { ga[k].v[e] = fmaf(x, hat, ga[k].v[e]); gb[k].v[e] += x; }
-                    else {
-                        A[k].v[e] = fmaf(x * gate[k].v[e], hat, A[k].v[e]);
-                        B[k].v[e] = fmaf(x, gate[k].v[e], B[k].v[e]);
-                    }
-                }
-                if (a.g_gate.p && !grouped && in) {               // a gate of the row's own: s o d o u
-                    Vec q, b;
-                    b.vector(a.post.b, col[k], n[k], 0.f);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) q.v[e] = d[k].v[e] * scale[k].v[e] * fmaf(y[k].v[e], postw[k].v[e], b.v[e]);
-                    kge_store8<B16>(a.g_gate.row(row), col[k], n[k], q.v);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    d[k].v[e] *= scale[k].v[e] * gate[k].v[e] * postw[k].v[e];
-                    if (e < n[k]) { s[0] += d[k].v[e]; s[1] = fmaf(d[k].v[e], y[k].v[e], s[1]); }
-                }
-            }
-            if (!a.y.p || !a.dy.p) continue;
-            if (a.post.on) {
-                reduce(s, 2);
-                const float m1 = a.post.layer ? s[0] * inv_dim : 0.f, m2 = s[1] * inv_dim;
-#pragma unroll
-                for (int k = 0; k < NG; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) d[k].v[e] = (d[k].v[e] - m1 - y[k].v[e] * m2) * ry1;
-            }
+            normalise(h, c, a.pre, inv_dim, reduce);
 #pragma unroll
             for (int k = 0; k < NG; ++k)
-                if (in) kge_store8<B16>(a.dy.row(row), col[k], n[k], d[k].v);
+                if (in && c.inside(k)) store<B16>(a.z.row(row), c, k, fma4(h[k], vector(VEC_PRE, k), vector(VEC_PRE_BIAS, k)));
         }
-        if (grouped) {
-            join(ga); join(gb);
-            if (t.team == 0) {
-#pragma unroll
-                for (int k = 0; k < NG; ++k) {
-                    if (a.parts > 1) { A[k] = ga[k]; B[k] = gb[k]; continue; }
-                    if (a.g_gate.p && g0 < g1) {
-                        Vec q, b;
-                        b.vector(a.post.b, col[k], n[k], 0.f);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) q.v[e] = scale[k].v[e] * fmaf(postw[k].v[e], ga[k].v[e], b.v[e] * gb[k].v[e]);
-                        kge_store8<B16>(a.g_gate.row((uint32_t)g0 / a.gate_rows), col[k], n[k], q.v);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        A[k].v[e] = fmaf(gate[k].v[e], ga[k].v[e], A[k].v[e]);
-                        B[k].v[e] = fmaf(gate[k].v[e], gb[k].v[e], B[k].v[e]);
-                    }
-                }
-            }
-        }
-        g0 = g1;
-    } while (g0 < r1);
-    // the run's sums
-    auto keep = [&](Vec (&s)[NG], int which, bool joined) {
-        if (!(a.want >> which & 1)) return;
-        if (!joined) join(s);
-        if (t.team == 0)
-#pragma unroll
-            for (int k = 0; k < NG; ++k)
-                if (n[k] > 0) {
-                    float *p = a.part + ((int64_t)which * a.runs + run) * a.part_ld + col[k];
-                    *(kge_f32x4 *)p = kge_f32x4{s[k].v[0], s[k].v[1], s[k].v[2], s[k].v[3]};
-                    *(kge_f32x4 *)(p + 4) = kge_f32x4{s[k].v[4], s[k].v[5], s[k].v[6], s[k].v[7]};
-                }
-    };
-    keep(A, SUM_A, grouped); keep(B, SUM_B, grouped); keep(C, SUM_C, false); keep(D, SUM_D, false);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
 // backward: column sums
 // ---------------------------------------------------------------------------------------------
-// 32 columns and 32 slices of the rows per workgroup; the slices are added in order.
-constexpr int JC = 32, JS = 32;
-__device__ __forceinline__ float column_sum(const float *p, int64_t ld, int64_t n, float (&lds)[JS][JC + 1]) {
-    const int c = threadIdx.x & (JC - 1), s = threadIdx.x / JC;
-    float v = 0.f;
-#pragma unroll 8
-    for (int64_t r = s; r < n; r += JS) v += p[r * ld + c];
-    lds[s][c] = v;
-    __syncthreads();
-    float sum = 0.f;
-    for (int i = 0; i < JS; ++i) sum += lds[i][c];
-    __syncthreads();
-    return sum;
-}
-
-// Groups whose rows were several runs: their gates' gradients, and their sums times the gates in the place of their first run's
-template <bool B16> __global__ __launch_bounds__(JC * JS) void norm_groups_kernel(const BwdArgs a) {
-    __shared__ float lds[JS][JC + 1];
-    const int tiles = (int)(a.part_ld / JC), c = threadIdx.x & (JC - 1);
-    const int64_t group = blockIdx.x / (uint32_t)tiles, col = (int64_t)(blockIdx.x - group * tiles) * JC;
-    float s[2] = {0.f, 0.f};
+// 32 columns (eight lanes of four) and 128 slices of the rows per workgroup; the slices' sums are added in a fixed order, two of them at once.
+constexpr int JC = 32, JS = 128, JT = 1024;
+typedef float JoinLds[2][JS][JC + 1];
+__device__ __forceinline__ void add_slices(const kge_f32x4 (&v)[2], float (&sum)[2], JoinLds &lds) {
+    const int l = threadIdx.x & 7, s = threadIdx.x >> 3, c = threadIdx.x & (JC - 1), q = threadIdx.x / JC;
 #pragma unroll
-    for (int w = 0; w < 2; ++w)
-        if (a.want >> w & 1) s[w] = column_sum(a.part + ((int64_t)w * a.runs + group * a.parts) * a.part_ld + col, a.part_ld, a.parts, lds);
-    if (threadIdx.x >= JC || col + c >= a.dim) return;
-    const float g = load1<B16>(a.gate.row(group), col + c);
-    if (a.g_gate.p) {
-        const float sc = a.scale ? a.scale[col + c] : 1.f, w = a.post.w ? a.post.w[col + c] : 1.f, b = a.post.b ? a.post.b[col + c] : 0.f;
-        store1<B16>(a.g_gate.row(group), col + c, sc * fmaf(w, s[0], b * s[1]));
-    }
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int w = 0; w < 2; ++w)
-        if (a.want >> w & 1) a.part[((int64_t)w * a.runs + group * a.parts) * a.part_ld + col + c] = g * s[w];
-}
-
-// Sums over all runs, and the gradients of the vectors
-__global__ __launch_bounds__(JC * JS) void norm_join_kernel(const BwdArgs a) {
-    __shared__ float lds[JS][JC + 1];
-    const int c = threadIdx.x & (JC - 1);
-    const int64_t col = (int64_t)blockIdx.x * JC;
-    const bool branch = blockIdx.y == 0;
-    const bool folded = branch && a.parts > 1;                    // (one row of sums for each group)
-    float s[2] = {0.f, 0.f};
+        for (int e = 0; e < 4; ++e) lds[i][s][4 * l + e] = v[i][e];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) sum[i] = (lds[i][4 * q][c] + lds[i][4 * q + 1][c]) + (lds[i][4 * q + 2][c] + lds[i][4 * q + 3][c]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) lds[i][q][c] = sum[i];
+    __syncthreads();
+    if (threadIdx.x >= JC) return;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int w = branch ? i : 2 + i;
-        if (a.want >> w & 1)
-            s[i] = column_sum(a.part + (int64_t)w * a.runs * a.part_ld + col, folded ? a.parts * a.part_ld : a.part_ld, folded ? a.runs / a.parts : a.runs, lds);
+        sum[i] = 0.f;
+#pragma unroll
+        for (int k = 0; k < JT / JC; ++k) sum[i] += lds[i][k][c];
     }
-    if (threadIdx.x >= JC || col + c >= a.dim) return;
-    auto put = [&](float *p, float v) {
-        if (p) p[col + c] = a.accumulate ? p[col + c] + v : v;
+}
+
+// v[i] += rows r0, r0 + step, ... of p[i], as far as they are wanted; four of them in flight, at the end too
+__device__ __forceinline__ void add_rows(const float *const (&p)[2], kge_f32x4 (&v)[2], uint32_t want, int64_t r0, int64_t end, int64_t step, int64_t ld) {
+    for (int64_t r = r0; r < end; r += 4 * step) {
+        kge_f32x4 x[4][2];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                x[k][i] = splat(0.f);
+                if ((want >> i & 1) && r + k * step < end) x[k][i] = *(const kge_f32x4 *)(p[i] + (r + k * step) * ld);
+            }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) v[i] += x[k][i];
+    }
+}
+
+// Groups whose rows were many runs: their gates' gradients, and their sums times the gates in the place of their first run's.  A lane has four columns; sixteen
+// waves share a group's runs.
+constexpr int GROUP_SLICES = 16;
+template <bool B16> __global__ __launch_bounds__(64 * GROUP_SLICES) void norm_groups_kernel(const BwdArgs a) {
+    __shared__ kge_f32x4 lds[GROUP_SLICES][64];
+    const int tiles = (int)((a.part_ld + 255) / 256), lane = threadIdx.x & 63, slice = threadIdx.x >> 6;
+    const int64_t group = blockIdx.x / (uint32_t)tiles, col = (int64_t)(blockIdx.x - group * tiles) * 256 + 4 * lane;
+    kge_f32x4 s[2] = {splat(0.f), splat(0.f)};
+    float *const p0 = a.part + group * a.parts * a.part_ld + col;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        if (!(a.want >> w & 1)) continue;
+        if (col < a.part_ld) {
+            const float *p = p0 + (int64_t)w * a.runs * a.part_ld;
+#pragma unroll 8
+            for (int r = slice; r < a.parts; r += GROUP_SLICES) s[w] += *(const kge_f32x4 *)(p + r * a.part_ld);
+        }
+        lds[slice][lane] = s[w];
+        __syncthreads();
+        s[w] = lds[0][lane];
+#pragma unroll
+        for (int i = 1; i < GROUP_SLICES; ++i) s[w] += lds[i][lane];
+        __syncthreads();
+    }
+    if (slice > 0) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (col + e >= a.dim) break;
+        const float g = load1<B16>(a.gate.row(group), col + e);
+        if (a.g_gate.p) {
+            const float sc = a.scale ? a.scale[col + e] : 1.f, w = a.post.w ? a.post.w[col + e] : 1.f, b = a.post.b ? a.post.b[col + e] : 0.f;
+            store1<B16>(a.g_gate.row(group), col + e, sc * fmaf(w, s[0][e], b * s[1][e]));
+        }
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+            if (a.want >> w & 1) p0[(int64_t)w * a.runs * a.part_ld + e] = g * s[w][e];
+    }
+}
+
+// Sums over all runs, and the gradients of the vectors; where a group is a few runs (each), the gates' gradients too.  FOLDED: norm_groups_kernel has left one
+// row of sums for each group.
+template <bool B16> __global__ __launch_bounds__(JT) void norm_join_kernel(const BwdArgs a, const bool folded) {
+    __shared__ JoinLds lds;
+    const int l = threadIdx.x & 7, slice = threadIdx.x >> 3;
+    const int64_t col = (int64_t)blockIdx.x * JC;
+    const bool branch = blockIdx.y == 0, each = branch && a.parts > 1 && !folded;
+    const uint32_t want = branch ? a.want : a.want >> 2;
+    const float *p[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p[i] = a.part + (int64_t)(branch ? i : 2 + i) * a.runs * a.part_ld + col + 4 * l;
+    kge_f32x4 v[2] = {splat(0.f), splat(0.f)};
+    if (each) {
+        const kge_f32x4 sc = vector4(a.scale, (int)col + 4 * l, a.dim, 1.f), w = vector4(a.post.w, (int)col + 4 * l, a.dim, 1.f), b = vector4(a.post.b, (int)col + 4 * l, a.dim, 0.f);
+        const int64_t groups = a.runs / a.parts;
+        for (int64_t g = slice; g < groups; g += JS) {
+            kge_f32x4 s[2] = {splat(0.f), splat(0.f)}, gate;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) gate[e] = col + 4 * l + e < a.dim ? load1<B16>(a.gate.row(g), col + 4 * l + e) : 0.f;
+            add_rows(p, s, want, g * a.parts, (g + 1) * a.parts, 1, a.part_ld);
+            if (a.g_gate.p) {
+                const kge_f32x4 d = sc * fma4(w, s[0], b * s[1]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + 4 * l + e < a.dim) store1<B16>(a.g_gate.row(g), col + 4 * l + e, d[e]);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) v[i] = fma4(gate, s[i], v[i]);
+        }
+    } else {
+        const int64_t ld = branch && folded ? a.parts * a.part_ld : a.part_ld, n = branch && folded ? a.runs / a.parts : a.runs;
+        add_rows(p, v, want, slice, n, JS, ld);
+    }
+    float s[2];
+    add_slices(v, s, lds);
+    const int c = threadIdx.x;
+    if (c >= JC || col + c >= a.dim) return;
+    auto put = [&](float *q, float x) {
+        if (q) q[col + c] = a.accumulate ? q[col + c] + x : x;
     };
     if (!branch) { put(a.g_prew, s[0]); put(a.g_preb, s[1]); return; }
     const float sc = a.scale ? a.scale[col + c] : 1.f, w = a.post.w ? a.post.w[col + c] : 1.f, b = a.post.b ? a.post.b[col + c] : 0.f;
@@ -362,8 +218,9 @@ __global__ __launch_bounds__(JC * JS) void norm_join_kernel(const BwdArgs a) {
 // ---------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------
-constexpr int64_t FWD_GROUPS = 2048, BWD_RUNS = 1024;
-constexpr int MIN_RUN = 4;
+constexpr int64_t FWD_GROUPS = 2048, BWD_RUNS = 1024;      // BWD_RUNS: at most
+constexpr int MIN_RUN = 1;
+constexpr int64_t MANY_PARTS = 16;                              // runs of a group from which on its sums are a launch of their own
 
 bool bad_norm(const kge_norm_t *n) {
     return n && ((n->kind != KGE_NORM_RMS && n->kind != KGE_NORM_LAYER) || !(n->eps > 0.f) || n->eps > 3e38f || ((uintptr_t)n->weight & 3) != 0 ||
@@ -383,19 +240,13 @@ bool bad_matrix(const void *p, int32_t dtype, int64_t ld, int64_t cols) { return
 Norm norm_of(const kge_norm_t *n) {
     return n ? Norm{true, n->kind == KGE_NORM_LAYER, n->eps, n->weight, n->bias} : Norm{false, false, 1.f, nullptr, nullptr};
 }
-// Waves of a row, a power of two: 512 columns each, or 1,024 in rows of more than 4,096.  (Sixteen waves leave a thread 128 registers.)
-int waves_of(int dim) {
-    int w = 1;
-    while (w < 8 && 512 * w < dim) w *= 2;
-    return dim > 8192 ? 16 : w;
-}
-
-// Runs of rows of the backward pass: about BWD_RUNS of them, of at least MIN_RUN rows for each team, of whole groups of rows where a run holds
+// Runs of rows of the backward pass: as many as the chip holds at once, of at least MIN_RUN rows for each team, of whole groups of rows where a run holds
 // several and of parts of one where it is longer.
 struct Runs { int64_t run, runs, parts; };
 Runs runs_of(const kge_norm_block_t *b, int64_t rows) {
     const int w = waves_of(b->dim), teams = w < 4 ? 4 / w : 1;
-    int64_t run = (rows + BWD_RUNS - 1) / BWD_RUNS;
+    const int64_t wanted = BWD_RUNS / 4 * (w > 4 ? 1 : occ_of(groups_of(b->dim)));
+    int64_t run = (rows + wanted - 1) / wanted;
     if (run < MIN_RUN * teams) run = MIN_RUN * teams;
     Runs q = {run, (rows + run - 1) / run, 1};
     if (b->gate && b->gate_rows > 1) {
@@ -421,22 +272,27 @@ int64_t most_runs(const kge_norm_block_t *b, int64_t rows) {
 int64_t part_ld_of(int dim) { return (dim + JC - 1) / JC * JC; }
 
 template <bool S16, bool B16> void launch_fwd(const FwdArgs &a, hipStream_t st) {
-    const int teams = a.waves < 4 ? 4 / a.waves : 1;
+    const int teams = a.waves < 4 ? 4 / a.waves : 1, ng = groups_of(a.dim);
     int64_t groups = (a.rows + teams - 1) / teams;
     if (groups > FWD_GROUPS) groups = FWD_GROUPS;
     const dim3 grid((unsigned)groups), blk(64 * a.waves * teams);
-    if (a.waves <= 4) hipLaunchKernelGGL((norm_fwd_kernel<S16, B16, 1, 256>), grid, blk, 0, st, a);
-    else if (a.dim <= 4096) hipLaunchKernelGGL((norm_fwd_kernel<S16, B16, 1, 512>), grid, blk, 0, st, a);
-    else if (a.dim <= 8192) hipLaunchKernelGGL((norm_fwd_kernel<S16, B16, 2, 512>), grid, blk, 0, st, a);
-    else hipLaunchKernelGGL((norm_fwd_kernel<S16, B16, 2, 1024>), grid, blk, 0, st, a);
-}
-template <bool S16, bool B16> void launch_bwd(const BwdArgs &a, hipStream_t st) {
-    const int teams = a.waves < 4 ? 4 / a.waves : 1;
-    const dim3 grid((unsigned)a.runs), blk(64 * a.waves * teams);
-    if (a.waves <= 4) hipLaunchKernelGGL((norm_bwd_kernel<S16, B16, 1, 256>), grid, blk, 0, st, a);
-    else if (a.dim <= 4096) hipLaunchKernelGGL((norm_bwd_kernel<S16, B16, 1, 512>), grid, blk, 0, st, a);
-    else if (a.dim <= 8192) hipLaunchKernelGGL((norm_bwd_kernel<S16, B16, 2, 512>), grid, blk, 0, st, a);
-    else hipLaunchKernelGGL((norm_bwd_kernel<S16, B16, 2, 1024>), grid, blk, 0, st, a);
+    const int lds = a.waves <= 4 ? VECTORS * 256 * a.waves * ng * (int)sizeof(float) : 0;                   // 80 KB at most
+#define KGE_FWD(NG, LAST, NT, OCC)                                                                                              \
+    do {                                                                                                                        \
+        static KgeLdsLimit limit;                                                                                               \
+        const auto kern = norm_fwd_kernel<S16, B16, NG, LAST, NT, OCC>;                                                         \
+        if (lds > 48 * 1024 && limit.set((const void *)kern, 80 * 1024) != KGE_OK) return;                                      \
+        hipLaunchKernelGGL(kern, grid, blk, lds, st, a);                                                                        \
+    } while (0)
+    if (a.waves == 16) KGE_FWD(4, 2, 1024, 4);
+    else if (a.waves == 8) KGE_FWD(4, 2, 512, 2);
+    else switch (ng) {
+    case 1: KGE_FWD(1, 1, 256, 8); break;
+    case 2: KGE_FWD(2, 1, 256, 6); break;
+    case 3: KGE_FWD(3, 1, 256, 5); break;
+    default: KGE_FWD(4, 1, 256, 4);
+    }
+#undef KGE_FWD
 }
 
 }  // namespace
@@ -513,19 +369,23 @@ int kge_norm_block_bwd(const kge_norm_block_t *blk, const void *h, int64_t h_ld,
         if (need && (!ws || ws_bytes < lost + need)) return KGE_E_WORKSPACE_TOO_SMALL;
         a.part = (float *)((char *)ws + lost);
     }
+    const bool folded = q.parts > MANY_PARTS && (a.want & 3);
     hipStream_t st = (hipStream_t)hip_stream;
     if (rows > 0) {
-        if (s16) b16 ? launch_bwd<true, true>(a, st) : launch_bwd<true, false>(a, st);
-        else b16 ? launch_bwd<false, true>(a, st) : launch_bwd<false, false>(a, st);
-        if (q.parts > 1 && (a.want & 3)) {
-            const dim3 grid((unsigned)(q.runs / q.parts * (a.part_ld / JC)));
-            if (b16) hipLaunchKernelGGL((norm_groups_kernel<true>), grid, dim3(JC * JS), 0, st, a);
-            else hipLaunchKernelGGL((norm_groups_kernel<false>), grid, dim3(JC * JS), 0, st, a);
+        if (s16) rows_bwd16(a, b16, st);
+        else rows_bwd32(a, b16, st);
+        if (folded) {
+            const dim3 grid((unsigned)(q.runs / q.parts * ((a.part_ld + 255) / 256)));
+            if (b16) hipLaunchKernelGGL((norm_groups_kernel<true>), grid, dim3(64 * GROUP_SLICES), 0, st, a);
+            else hipLaunchKernelGGL((norm_groups_kernel<false>), grid, dim3(64 * GROUP_SLICES), 0, st, a);
         }
     }
     const bool vectors = w.scale || w.post_weight || w.post_bias || w.pre_weight || w.pre_bias;
-    if (vectors)
-        hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)(a.part_ld / JC), 2), dim3(JC * JS), 0, st, a);
+    if (vectors || (of_group && !folded && rows > 0)) {
+        const dim3 grid((unsigned)(a.part_ld / JC), a.want >> 2 ? 2 : 1);
+        if (b16) hipLaunchKernelGGL(norm_join_kernel<true>, grid, dim3(JT), 0, st, a, folded);
+        else hipLaunchKernelGGL(norm_join_kernel<false>, grid, dim3(JT), 0, st, a, folded);
+    }
     return rows > 0 || vectors ? kge_launch_status() : KGE_OK;
 }
 

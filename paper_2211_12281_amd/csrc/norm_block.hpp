@@ -4,44 +4,105 @@
 
 namespace kge_norm {
 
-constexpr int MAX_DIM = 16384;                                    // 1,024 threads of sixteen columns
+constexpr int MAX_DIM = 16384;                                    // sixteen waves of sixteen columns a lane
 
-// Eight columns of a thread
-struct Vec {
-    float v[8];
-    __device__ __forceinline__ void zero() {
+__device__ __forceinline__ kge_f32x4 splat(float x) { return kge_f32x4{x, x, x, x}; }
+__device__ __forceinline__ kge_f32x4 fma4(kge_f32x4 a, kge_f32x4 b, kge_f32x4 c) {
+    return kge_f32x4{fmaf(a[0], b[0], c[0]), fmaf(a[1], b[1], c[1]), fmaf(a[2], b[2], c[2]), fmaf(a[3], b[3], c[3])};
+}
+
+struct Matrix {
+    char *p; int64_t ld;                                          // ld in bytes
+    __device__ __forceinline__ char *row(int64_t r) const { return p + r * ld; }
+};
+inline Matrix matrix(void *p, int64_t ld, bool b16) { return Matrix{(char *)p, ld * (b16 ? 2 : 4)}; }
+
+// Columns i .. i + 3 of a vector of parameters, which may be absent; zeros behind its end
+__device__ __forceinline__ kge_f32x4 vector4(const float *p, int i, int dim, float otherwise) {
+    kge_f32x4 r = splat(0.f);
+    if (i + 4 <= dim) r = p ? *(const kge_f32x4_a4 *)(p + i) : splat(otherwise);
+    else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+        for (int e = 0; e < 3; ++e)
+            if (i + e < dim) r[e] = p ? p[i + e] : otherwise;
     }
-    // of a vector of parameters, which may be absent; zeros behind the row's end, so that what is scaled by it is zero there and counts in no sum
-    __device__ __forceinline__ void vector(const float *p, int col, int n, float otherwise) {
-        if (p) kge_load8<false>(p, col, n > 8 ? 8 : n, v);
-        else
+    return r;
+}
+
+// A thread's share of a row: NG groups of four columns, the team's lanes side by side.  Only the last LAST groups may reach past the row's end; `mask` is 1 on
+// their columns that are inside and 0 on the others, whose values are kept zero: a mean is subtracted as fma(-mean, mask, x).
+template <int NG, int LAST> struct Columns {
+    int dim, lane, size;
+    kge_f32x4 mask[LAST];
+    __device__ __forceinline__ Columns(int d, int l, int s) : dim(d), lane(l), size(s) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < n ? otherwise : 0.f;
+        for (int k = 0; k < LAST; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mask[k][e] = col(NG - LAST + k) + e < d ? 1.f : 0.f;
+    }
+    __device__ __forceinline__ int col(int k) const { return 4 * (lane + size * k); }
+    __device__ __forceinline__ int left(int k) const { return dim - col(k); }
+    __device__ __forceinline__ bool inside(int k) const { return k < NG - LAST || left(k) > 0; }
+    // x - m on the columns that are inside
+    __device__ __forceinline__ kge_f32x4 minus(int k, kge_f32x4 x, float m) const {
+        return k < NG - LAST ? x - splat(m) : fma4(splat(-m), mask[k - (NG - LAST)], x);
     }
 };
 
-// The same of a row as it lies in memory; n: columns left of the row, none or fewer for threads past its end
+// Four columns as they lie in memory.  Where the row ends inside them, the row's last four are read and moved down: one load for all lanes (rows of fewer
+// than four elements take them one by one).
 template <bool B16> struct Raw {
-    KgeRaw8<B16> r;
-    __device__ __forceinline__ void load(const void *row, int col, int n) {
-        if (n >= 8) r = kge_raw8<B16>(row, col);
-        else {
-#pragma unroll
-            for (int i = 0; i < (B16 ? 1 : 2); ++i) r.w[i] = kge_u32x4{0u, 0u, 0u, 0u};
-            if (n > 0) {
-#pragma unroll
-                for (int e = 0; e < 7; ++e)
-                    if (e < n) {
-                        if constexpr (B16) r.w[0][e >> 1] |= (uint32_t)((const uint16_t *)row)[col + e] << (16 * (e & 1));
-                        else r.w[e >> 2][e & 3] = ((const uint32_t *)row)[col + e];
-                    }
+    kge_u32x4 w;                                                  // (bf16: two words)
+    template <int NG, int LAST> __device__ __forceinline__ void load(const char *row, const Columns<NG, LAST> &c, int k, bool in) {
+        w = kge_u32x4{0u, 0u, 0u, 0u};
+        const bool whole = k < NG - LAST;
+        const int n = c.left(k);
+        if (!in || (!whole && n <= 0)) return;
+        if (whole || c.dim >= 4) {
+            const int sh = whole || n >= 4 ? 0 : 4 - n, at = c.col(k) - sh;
+            if constexpr (B16) {
+                const kge_u32x2 r = *(const kge_u32x2_a2 *)((const uint16_t *)row + at);
+                w[0] = r[0]; w[1] = r[1];
+            } else w = *(const kge_u32x4_a4 *)((const uint32_t *)row + at);
+            if (!whole && (c.dim & 3)) {
+                if constexpr (B16) {
+                    const uint64_t v = ((uint64_t)w[1] << 32 | w[0]) >> (16 * sh);
+                    w[0] = (uint32_t)v; w[1] = (uint32_t)(v >> 32);
+                } else {
+                    if (sh & 1) w = kge_u32x4{w[1], w[2], w[3], 0u};
+                    if (sh & 2) w = kge_u32x4{w[2], w[3], 0u, 0u};
+                }
             }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (e < n) {
+                    if constexpr (B16) w[e >> 1] |= (uint32_t)((const uint16_t *)row)[e] << (16 * (e & 1));
+                    else w[e] = ((const uint32_t *)row)[e];
+                }
         }
     }
-    __device__ __forceinline__ void values(Vec &x) const { kge_values8<B16>(r, x.v); }
+    __device__ __forceinline__ kge_f32x4 values() const {
+        if constexpr (B16) return kge_f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u), __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
+        else return kge_f32x4{__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3])};
+    }
 };
+template <bool B16, int NG, int LAST> __device__ __forceinline__ void store(char *row, const Columns<NG, LAST> &c, int k, kge_f32x4 v) {
+    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf2;
+    const int n = k < NG - LAST ? 4 : c.left(k), at = c.col(k);
+    if (n >= 4) {
+        if constexpr (B16)
+            *(kge_u32x2_a2 *)((uint16_t *)row + at) = kge_u32x2{__builtin_bit_cast(uint32_t, bf2{(__bf16)v[0], (__bf16)v[1]}), __builtin_bit_cast(uint32_t, bf2{(__bf16)v[2], (__bf16)v[3]})};
+        else *(kge_f32x4_a4 *)((float *)row + at) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) {
+                if constexpr (B16) ((__bf16 *)row)[at + e] = (__bf16)v[e];
+                else ((float *)row)[at + e] = v[e];
+            }
+    }
+}
 template <bool B16> __device__ __forceinline__ float load1(const void *row, int64_t col) {
     return B16 ? __uint_as_float((uint32_t)((const uint16_t *)row)[col] << 16) : ((const float *)row)[col];
 }
@@ -71,71 +132,60 @@ __device__ __forceinline__ float wave_sum(float x) {
     return (s0 + s1) + (s2 + s3);
 }
 
-// Sums of up to K values over the threads of a team, for all of them.  Two places in turn: who writes to one again has passed the barrier of the sums in
+// Sums of N values over the threads of a team, for all of them.  Two places in turn: who writes to one again has passed the barrier of the sums in
 // between, behind which nobody reads it any more.  (Teams of one wave need no barrier, and go round as they like.)
 template <int K, int NT> struct Reduce {
     float (&lds)[2][NT / 64][K];
     const Team &t;
     int place = 0;
     __device__ __forceinline__ Reduce(float (&l)[2][NT / 64][K], const Team &team) : lds(l), t(team) {}
-    __device__ __forceinline__ void operator()(float *v, int n) {
+    template <int N> __device__ __forceinline__ void operator()(float (&v)[N]) {
+        static_assert(N <= K, "sums at once");
 #pragma unroll
-        for (int i = 0; i < K; ++i)
-            if (i < n) v[i] = wave_sum(v[i]);
+        for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
         if (t.waves == 1) return;
         const int wave = (int)threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-            for (int i = 0; i < K; ++i)
-                if (i < n) lds[place][wave][i] = v[i];
+            for (int i = 0; i < N; ++i) lds[place][wave][i] = v[i];
         }
         __syncthreads();
         const int w0 = t.team * t.waves;
 #pragma unroll
-        for (int i = 0; i < K; ++i)
-            if (i < n) v[i] = lds[place][w0][i];
+        for (int i = 0; i < N; ++i) v[i] = lds[place][w0][i];
         for (int w = 1; w < t.waves; ++w)
 #pragma unroll
-            for (int i = 0; i < K; ++i)
-                if (i < n) v[i] += lds[place][w0 + w][i];
+            for (int i = 0; i < N; ++i) v[i] += lds[place][w0 + w][i];
         place ^= 1;
     }
 };
 
+__device__ __forceinline__ float sum4(kge_f32x4 v, float s) { return s + ((v[0] + v[1]) + (v[2] + v[3])); }
+__device__ __forceinline__ float dot4(kge_f32x4 a, kge_f32x4 b, float s) { return fmaf(a[3], b[3], fmaf(a[2], b[2], fmaf(a[1], b[1], fmaf(a[0], b[0], s)))); }
 __device__ __forceinline__ float inv_sqrt(float x) { return 1.f / sqrtf(x); }
 
 struct Norm { bool on, layer; float eps; const float *w, *b; };
-struct Stats { float mean, r; };
 
-template <int NG, class R> __device__ __forceinline__ Stats statistics(const Vec (&x)[NG], const int (&n)[NG], const Norm &norm, float inv_dim, R &reduce) {
-    Stats s = {0.f, 1.f};
+// x -> x^ = (x - mean) / deviation
+template <int NG, int LAST, class R>
+__device__ __forceinline__ void normalise(kge_f32x4 (&x)[NG], const Columns<NG, LAST> &c, const Norm &norm, float inv_dim, R &reduce) {
     float v[1] = {0.f};
     if (norm.layer) {
 #pragma unroll
-        for (int k = 0; k < NG; ++k)
+        for (int k = 0; k < NG; ++k) v[0] = sum4(x[k], v[0]);
+        reduce(v);
+        const float mean = v[0] * inv_dim;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[0] += x[k].v[e];
-        reduce(v, 1);
-        s.mean = v[0] * inv_dim;
+        for (int k = 0; k < NG; ++k) x[k] = c.minus(k, x[k], mean);
         v[0] = 0.f;
     }
 #pragma unroll
-    for (int k = 0; k < NG; ++k)
+    for (int k = 0; k < NG; ++k) v[0] = dot4(x[k], x[k], v[0]);
+    reduce(v);
+    const float r = inv_sqrt(fmaf(v[0], inv_dim, norm.eps));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float q = e < n[k] ? x[k].v[e] - s.mean : 0.f;
-            v[0] = fmaf(q, q, v[0]);
-        }
-    reduce(v, 1);
-    s.r = inv_sqrt(fmaf(v[0], inv_dim, norm.eps));
-    return s;
+    for (int k = 0; k < NG; ++k) x[k] *= splat(r);
 }
-
-struct Matrix {
-    char *p; int64_t ld;                                          // ld in bytes
-    __device__ __forceinline__ char *row(int64_t r) const { return p + r * ld; }
-};
-inline Matrix matrix(void *p, int64_t ld, bool b16) { return Matrix{(char *)p, ld * (b16 ? 2 : 4)}; }
 
 struct FwdArgs {
     int dim, waves; int64_t rows;
@@ -155,5 +205,23 @@ struct BwdArgs {
     float *part;                                                  // [sum][run][part_ld]
     float *g_postw, *g_postb, *g_prew, *g_preb, *g_scale; int accumulate;
 };
+
+// Waves of a row, a power of two: a lane holds up to sixteen columns.  (Sixteen waves leave a thread 128 registers, and the backward pass spills.)
+inline int waves_of(int dim) {
+    int w = 1;
+    while (1024 * w < dim) w *= 2;
+    return w;
+}
+// groups of four columns of a lane; five to eight waves and more take four whatever the width
+inline int groups_of(int dim) {
+    const int w = waves_of(dim);
+    return w > 4 ? 4 : (dim + 256 * w - 1) / (256 * w);
+}
+// waves per SIMD that the backward pass' registers leave room for
+constexpr int occ_of(int groups) { return groups <= 2 ? 4 : groups == 3 ? 3 : 2; }
+
+// rows of the backward pass, by the stream's type
+void rows_bwd16(const BwdArgs &a, bool b16, hipStream_t st);
+void rows_bwd32(const BwdArgs &a, bool b16, hipStream_t st);
 
 }  // namespace kge_norm
