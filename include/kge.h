@@ -543,7 +543,7 @@ size_t kge_matmul_quantized_workspace_bytes(int64_t m, int64_t n, int64_t k);
  * pre = NULL leaves z out, scale and gate = NULL are ones, a norm's weight = NULL is ones and its bias = NULL zeros; without y (then post, scale and gate
  * are NULL too) the call is z = N_pre(x).  gate: [ceil(rows / gate_rows), dim] of block_dtype, one row for each gate_rows consecutive rows (1: a gate
  * of its own for every row; rows and more: one gate for all).  x, h and their gradients are of stream_dtype, y, z, gate and theirs of block_dtype, vectors
- * float[dim].  Everything is computed in fp32 and rounded once, z from h before its rounding; squares of elements have to fit fp32.  1 <= dim <= 16,384
+ * float[dim].  Everything is computed in fp32 and rounded once, z from h before its rounding; squares of elements have to fit fp32.  1 <= dim <= 8,192
  * (KGE_E_UNSUPPORTED beyond), rows < 2^31, 0 < eps.
  */
 typedef enum { KGE_NORM_RMS = 0, KGE_NORM_LAYER = 1 } kge_norm_kind_t;

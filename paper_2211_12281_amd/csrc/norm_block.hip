@@ -86,11 +86,11 @@ __global__ __launch_bounds__(NT, OCC) void norm_fwd_kernel(const FwdArgs a) {
 // ---------------------------------------------------------------------------------------------
 // backward: column sums
 // ---------------------------------------------------------------------------------------------
-// 32 columns (eight lanes of four) and 128 slices of the rows per workgroup; the slices' sums are added in a fixed order, two of them at once.
-constexpr int JC = 32, JS = 128, JT = 1024;
+// Sixteen columns (four lanes of four) and 256 slices of the rows per workgroup; the slices' sums are added in a fixed order, two of them at once.
+constexpr int JC = 16, JT = 1024, JL = JC / 4, JS = JT / JL;
 typedef float JoinLds[2][JS][JC + 1];
 __device__ __forceinline__ void add_slices(const kge_f32x4 (&v)[2], float (&sum)[2], JoinLds &lds) {
-    const int l = threadIdx.x & 7, s = threadIdx.x >> 3, c = threadIdx.x & (JC - 1), q = threadIdx.x / JC;
+    const int l = threadIdx.x % JL, s = threadIdx.x / JL, c = threadIdx.x % JC, q = threadIdx.x / JC;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -111,21 +111,20 @@ __device__ __forceinline__ void add_slices(const kge_f32x4 (&v)[2], float (&sum)
     }
 }
 
-// v[i] += rows r0, r0 + step, ... of p[i], as far as they are wanted; four of them in flight, at the end too
-__device__ __forceinline__ void add_rows(const float *const (&p)[2], kge_f32x4 (&v)[2], uint32_t want, int64_t r0, int64_t end, int64_t step, int64_t ld) {
+// v[i] += rows r0, r0 + step, ... of p[i]; four of them in flight, at the end too (the last one's again, which do not count)
+__device__ __forceinline__ void add_rows(const float *const (&p)[2], kge_f32x4 (&v)[2], int64_t r0, int64_t end, int64_t step, int64_t ld) {
     for (int64_t r = r0; r < end; r += 4 * step) {
         kge_f32x4 x[4][2];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                x[k][i] = splat(0.f);
-                if ((want >> i & 1) && r + k * step < end) x[k][i] = *(const kge_f32x4 *)(p[i] + (r + k * step) * ld);
-            }
+            for (int i = 0; i < 2; ++i) x[k][i] = *(const kge_f32x4 *)(p[i] + (r + k * step < end ? r + k * step : r) * ld);
 #pragma unroll
         for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) v[i] += x[k][i];
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[i][e] += r + k * step < end ? x[k][i][e] : 0.f;
     }
 }
 
@@ -172,13 +171,14 @@ template <bool B16> __global__ __launch_bounds__(64 * GROUP_SLICES) void norm_gr
 // row of sums for each group.
 template <bool B16> __global__ __launch_bounds__(JT) void norm_join_kernel(const BwdArgs a, const bool folded) {
     __shared__ JoinLds lds;
-    const int l = threadIdx.x & 7, slice = threadIdx.x >> 3;
+    const int l = threadIdx.x % JL, slice = threadIdx.x / JL;
     const int64_t col = (int64_t)blockIdx.x * JC;
-    const bool branch = blockIdx.y == 0, each = branch && a.parts > 1 && !folded;
+    const bool branch = blockIdx.y == 0, each = branch && a.parts > 0 && !folded;
     const uint32_t want = branch ? a.want : a.want >> 2;
     const float *p[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) p[i] = a.part + (int64_t)(branch ? i : 2 + i) * a.runs * a.part_ld + col + 4 * l;
+    for (int i = 0; i < 2; ++i)                                   // (a sum that is not wanted is not there: the other one's again, for nothing)
+        p[i] = a.part + (int64_t)((branch ? 0 : 2) + (want >> i & 1 ? i : 1 - i)) * a.runs * a.part_ld + col + 4 * l;
     kge_f32x4 v[2] = {splat(0.f), splat(0.f)};
     if (each) {
         const kge_f32x4 sc = vector4(a.scale, (int)col + 4 * l, a.dim, 1.f), w = vector4(a.post.w, (int)col + 4 * l, a.dim, 1.f), b = vector4(a.post.b, (int)col + 4 * l, a.dim, 0.f);
@@ -187,7 +187,7 @@ template <bool B16> __global__ __launch_bounds__(JT) void norm_join_kernel(const
             kge_f32x4 s[2] = {splat(0.f), splat(0.f)}, gate;
 #pragma unroll
             for (int e = 0; e < 4; ++e) gate[e] = col + 4 * l + e < a.dim ? load1<B16>(a.gate.row(g), col + 4 * l + e) : 0.f;
-            add_rows(p, s, want, g * a.parts, (g + 1) * a.parts, 1, a.part_ld);
+            add_rows(p, s, g * a.parts, (g + 1) * a.parts, 1, a.part_ld);
             if (a.g_gate.p) {
                 const kge_f32x4 d = sc * fma4(w, s[0], b * s[1]);
 #pragma unroll
@@ -199,7 +199,7 @@ template <bool B16> __global__ __launch_bounds__(JT) void norm_join_kernel(const
         }
     } else {
         const int64_t ld = branch && folded ? a.parts * a.part_ld : a.part_ld, n = branch && folded ? a.runs / a.parts : a.runs;
-        add_rows(p, v, want, slice, n, JS, ld);
+        if (want & 3) add_rows(p, v, slice, n, JS, ld);
     }
     float s[2];
     add_slices(v, s, lds);
@@ -218,8 +218,7 @@ template <bool B16> __global__ __launch_bounds__(JT) void norm_join_kernel(const
 // ---------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------
-constexpr int64_t FWD_GROUPS = 2048, BWD_RUNS = 1024;      // BWD_RUNS: at most
-constexpr int MIN_RUN = 1;
+constexpr int64_t FWD_GROUPS = 2048;
 constexpr int64_t MANY_PARTS = 16;                              // runs of a group from which on its sums are a launch of their own
 
 bool bad_norm(const kge_norm_t *n) {
@@ -240,18 +239,17 @@ bool bad_matrix(const void *p, int32_t dtype, int64_t ld, int64_t cols) { return
 Norm norm_of(const kge_norm_t *n) {
     return n ? Norm{true, n->kind == KGE_NORM_LAYER, n->eps, n->weight, n->bias} : Norm{false, false, 1.f, nullptr, nullptr};
 }
-// Runs of rows of the backward pass: as many as the chip holds at once, of at least MIN_RUN rows for each team, of whole groups of rows where a run holds
-// several and of parts of one where it is longer.
+// Runs of rows of the backward pass: as many as the chip holds at once, of a row for each team at least; of parts of one group of rows, where a group is as long as
+// a run, else of whole groups.
 struct Runs { int64_t run, runs, parts; };
 Runs runs_of(const kge_norm_block_t *b, int64_t rows) {
-    const int w = waves_of(b->dim), teams = w < 4 ? 4 / w : 1;
-    const int64_t wanted = BWD_RUNS / 4 * (w > 4 ? 1 : occ_of(groups_of(b->dim)));
+    const int64_t wanted = bwd_runs_of(b->dim), teams = bwd_teams_of(b->dim);
     int64_t run = (rows + wanted - 1) / wanted;
-    if (run < MIN_RUN * teams) run = MIN_RUN * teams;
-    Runs q = {run, (rows + run - 1) / run, 1};
+    if (run < teams) run = teams;
+    Runs q = {run, (rows + run - 1) / run, 0};
     if (b->gate && b->gate_rows > 1) {
         const int64_t len = b->gate_rows < rows ? b->gate_rows : rows;
-        if (len > run) {
+        if (len >= run) {
             q.parts = (len + run - 1) / run;
             q.run = (len + q.parts - 1) / q.parts;
             q.runs = (rows + len - 1) / len * q.parts;
@@ -262,12 +260,11 @@ Runs runs_of(const kge_norm_block_t *b, int64_t rows) {
     }
     return q;
 }
-// No call of up to so many rows has more runs.  With r rows at least in a run before the groups' ends are looked at: groups of len > r rows are
+// No call of up to so many rows has more runs.  With r rows in a run before the groups' ends are looked at: groups of len >= r rows are
 // ceil(rows / len) ceil(len / r) < rows / r + rows / len + len / r + 1 runs, shorter ones less than 2 rows / r + 1.
 int64_t most_runs(const kge_norm_block_t *b, int64_t rows) {
-    const int w = waves_of(b->dim), teams = w < 4 ? 4 / w : 1;
-    const int64_t short_runs = 3 * (rows / (MIN_RUN * teams) + 1) + 1, all = 3 * BWD_RUNS + 1;
-    return rows == 0 ? 0 : short_runs < all ? short_runs : all;
+    const int64_t few = 3 * (rows / bwd_teams_of(b->dim) + 1) + 1, all = 3 * bwd_runs_of(b->dim) + 1;
+    return rows == 0 ? 0 : few < all ? few : all;
 }
 int64_t part_ld_of(int dim) { return (dim + JC - 1) / JC * JC; }
 
@@ -284,8 +281,7 @@ template <bool S16, bool B16> void launch_fwd(const FwdArgs &a, hipStream_t st) 
         if (lds > 48 * 1024 && limit.set((const void *)kern, 80 * 1024) != KGE_OK) return;                                      \
         hipLaunchKernelGGL(kern, grid, blk, lds, st, a);                                                                        \
     } while (0)
-    if (a.waves == 16) KGE_FWD(4, 2, 1024, 4);
-    else if (a.waves == 8) KGE_FWD(4, 2, 512, 2);
+    if (a.waves == 8) KGE_FWD(4, 2, 512, 2);
     else switch (ng) {
     case 1: KGE_FWD(1, 1, 256, 8); break;
     case 2: KGE_FWD(2, 1, 256, 6); break;
@@ -357,9 +353,9 @@ int kge_norm_block_bwd(const kge_norm_block_t *blk, const void *h, int64_t h_ld,
     a.h = matrix((void *)h, h_ld, s16); a.y = matrix((void *)y, y_ld, b16); a.dh = matrix((void *)dh, dh_ld, s16); a.dz = matrix((void *)dz, dz_ld, b16);
     a.dx = matrix(dx, dx_ld, s16); a.dy = matrix(dy, dy_ld, b16); a.g_gate = matrix(w.gate, w.gate_ld, b16);
     a.g_postw = w.post_weight; a.g_postb = w.post_bias; a.g_prew = w.pre_weight; a.g_preb = w.pre_bias; a.g_scale = w.scale; a.accumulate = w.accumulate;
-    const Runs q = rows > 0 ? runs_of(blk, rows) : Runs{0, 0, 1};
+    const Runs q = rows > 0 ? runs_of(blk, rows) : Runs{0, 0, 0};
     a.run = q.run; a.runs = q.runs; a.parts = (int)q.parts; a.part_ld = part_ld_of(blk->dim);
-    const bool bias = blk->post && blk->post->bias, of_group = w.gate && q.parts > 1;         // (parts: of gates of groups alone)
+    const bool bias = blk->post && blk->post->bias, of_group = w.gate && q.parts > 0;         // (parts: of gates of groups alone)
     if (w.scale || w.post_weight || of_group) a.want |= 1u << SUM_A;
     if (w.post_bias || (bias && (w.scale || of_group))) a.want |= 1u << SUM_B;
     if (w.pre_weight) a.want |= 1u << SUM_C;

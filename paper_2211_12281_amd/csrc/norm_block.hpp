@@ -4,7 +4,7 @@
 
 namespace kge_norm {
 
-constexpr int MAX_DIM = 16384;                                    // sixteen waves of sixteen columns a lane
+constexpr int MAX_DIM = 8192;                                     // eight waves of sixteen columns a lane
 
 __device__ __forceinline__ kge_f32x4 splat(float x) { return kge_f32x4{x, x, x, x}; }
 __device__ __forceinline__ kge_f32x4 fma4(kge_f32x4 a, kge_f32x4 b, kge_f32x4 c) {
@@ -200,25 +200,35 @@ struct BwdArgs {
     Norm post, pre; const float *scale;
     Matrix gate; uint32_t gate_rows;
     Matrix h, y, dh, dz, dx, dy, g_gate;
-    int64_t run, runs, part_ld; int parts;                        // rows of a run, runs, and of a group
+    int64_t run, runs, part_ld; int parts;                        // rows of a run; runs; runs of a group, 0 where a run is not of one group
     uint32_t want;                                                // sums that are kept
     float *part;                                                  // [sum][run][part_ld]
     float *g_postw, *g_postb, *g_prew, *g_preb, *g_scale; int accumulate;
 };
 
-// Waves of a row, a power of two: a lane holds up to sixteen columns.  (Sixteen waves leave a thread 128 registers, and the backward pass spills.)
+// Waves of a row, a power of two: a lane holds up to sixteen columns.
 inline int waves_of(int dim) {
     int w = 1;
     while (1024 * w < dim) w *= 2;
     return w;
 }
-// groups of four columns of a lane; five to eight waves and more take four whatever the width
+// groups of four columns of a lane; eight waves take four whatever the width
 inline int groups_of(int dim) {
     const int w = waves_of(dim);
     return w > 4 ? 4 : (dim + 256 * w - 1) / (256 * w);
 }
-// waves per SIMD that the backward pass' registers leave room for
-constexpr int occ_of(int groups) { return groups <= 2 ? 4 : groups == 3 ? 3 : 2; }
+// Teams of a workgroup of the backward pass.  Of one wave (no barriers between rows): as many as the registers leave room for on a compute unit, so that there are 256 runs'
+// sums to join and not 768 (24,576 x 768: 9.4 MB of sums, 11 us); of more, whose waves meet at barriers, few.
+constexpr int TEAMS_OF_ONE[4] = {16, 16, 12, 8};
+inline int bwd_teams_of(int dim) {
+    const int w = waves_of(dim);
+    return w == 1 ? TEAMS_OF_ONE[groups_of(dim) - 1] : w == 2 ? 2 : 1;
+}
+// workgroups that the chip holds at once
+inline int64_t bwd_runs_of(int dim) {
+    const int w = waves_of(dim);
+    return 256 * (w == 1 || w == 8 ? 1 : groups_of(dim) == 3 ? 3 : 2);
+}
 
 // rows of the backward pass, by the stream's type
 void rows_bwd16(const BwdArgs &a, bool b16, hipStream_t st);

@@ -69,9 +69,9 @@ def test_norm_block_bwd_refuses(lib, bad):
 
 
 def test_norm_block_limits(lib):
-    wide = dict(dim=16385, gate_ld=16385)
-    assert _fwd(lib, wide, xld=16385, yld=16385, hld=16385, zld=16385) == UNSUPPORTED
-    assert _bwd(lib, wide, dict(gate_ld=16385), ld=16385) == UNSUPPORTED
+    wide = dict(dim=8193, gate_ld=8193)
+    assert _fwd(lib, wide, xld=8193, yld=8193, hld=8193, zld=8193) == UNSUPPORTED
+    assert _bwd(lib, wide, dict(gate_ld=8193), ld=8193) == UNSUPPORTED
     assert _fwd(lib, rows=0) == 0 and _bwd(lib, rows=0, grads=dict(post_weight=None, pre_bias=None)) == 0
     assert _fwd(lib, rows=0, x=None, y=None, h=None, z=None) == 0
     size = lib.kge_norm_block_bwd_workspace_bytes
@@ -79,7 +79,7 @@ def test_norm_block_limits(lib):
     assert need > 256 and _bwd(lib, rows=100) == SMALL and _bwd(lib, rows=100, ws=OK + 8, wsb=255) == SMALL
     assert size(C.byref(_blk()), -1) == 0 and size(C.byref(_blk()), 1 << 31) == 0
     for gate_rows in (1, 2, 3, 100, 1 << 40):
-        for dim in (1, 64, 600, 16384):
+        for dim in (1, 64, 600, 1500, 4000, 8192):
             blk = _blk(dim=dim, gate_ld=dim, gate_rows=gate_rows)
             sizes = [size(C.byref(blk), r) for r in (*range(0, 200, 7), 4096, 4097, 24_576, 1 << 20, (1 << 31) - 1)]
             assert sizes == sorted(sizes) and sizes[-1] < 1 << 30
