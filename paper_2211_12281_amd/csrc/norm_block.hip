@@ -71,14 +71,14 @@ __global__ __launch_bounds__(NT, OCC) void norm_fwd_kernel(const FwdArgs a) {
             for (int k = 0; k < NG; ++k) {
                 if (a.scale) u[k] *= vector(VEC_SCALE, k);
                 h[k] = a.gate.p ? fma4(u[k], f[k], h[k]) : u[k] + h[k];
-                if (a.h.p && in && c.inside(k)) store<S16>(a.h.row(row), c, k, h[k]);
+                if (a.h.p && in && c.inside(k)) store<S16>(a.h.row(row), c, k, h[k], a.stream);
             }
         }
         if (a.pre.on) {
             normalise(h, c, a.pre, inv_dim, reduce);
 #pragma unroll
             for (int k = 0; k < NG; ++k)
-                if (in && c.inside(k)) store<B16>(a.z.row(row), c, k, fma4(h[k], vector(VEC_PRE, k), vector(VEC_PRE_BIAS, k)));
+                if (in && c.inside(k)) store<B16>(a.z.row(row), c, k, fma4(h[k], vector(VEC_PRE, k), vector(VEC_PRE_BIAS, k)), a.stream);
         }
     }
 }
@@ -312,6 +312,7 @@ int kge_norm_block(const kge_norm_block_t *blk, const void *x, int64_t x_ld, con
     a.post = norm_of(blk->post); a.pre = norm_of(blk->pre); a.scale = blk->scale;
     a.gate = matrix((void *)blk->gate, blk->gate_ld, b16); a.gate_rows = (uint32_t)(blk->gate_rows < rows ? blk->gate_rows : rows);
     a.x = matrix((void *)x, x_ld, s16); a.y = matrix((void *)y, y_ld, b16); a.h = matrix(h, h_ld, s16); a.z = matrix(z, z_ld, b16);
+    a.stream = rows * blk->dim * ((h ? (s16 ? 2 : 4) : 0) + (z ? (b16 ? 2 : 4) : 0)) >= KGE_STREAM_BYTES;
     hipStream_t st = (hipStream_t)hip_stream;
     if (s16) b16 ? launch_fwd<true, true>(a, st) : launch_fwd<true, false>(a, st);
     else b16 ? launch_fwd<false, true>(a, st) : launch_fwd<false, false>(a, st);
@@ -353,6 +354,7 @@ int kge_norm_block_bwd(const kge_norm_block_t *blk, const void *h, int64_t h_ld,
     a.h = matrix((void *)h, h_ld, s16); a.y = matrix((void *)y, y_ld, b16); a.dh = matrix((void *)dh, dh_ld, s16); a.dz = matrix((void *)dz, dz_ld, b16);
     a.dx = matrix(dx, dx_ld, s16); a.dy = matrix(dy, dy_ld, b16); a.g_gate = matrix(w.gate, w.gate_ld, b16);
     a.g_postw = w.post_weight; a.g_postb = w.post_bias; a.g_prew = w.pre_weight; a.g_preb = w.pre_bias; a.g_scale = w.scale; a.accumulate = w.accumulate;
+    a.stream = rows * blk->dim * ((dx ? (s16 ? 2 : 4) : 0) + (dy ? (b16 ? 2 : 4) : 0)) >= KGE_STREAM_BYTES;
     const Runs q = rows > 0 ? runs_of(blk, rows) : Runs{0, 0, 0};
     a.run = q.run; a.runs = q.runs; a.parts = (int)q.parts; a.part_ld = part_ld_of(blk->dim);
     const bool bias = blk->post && blk->post->bias, of_group = w.gate && q.parts > 0;         // (parts: of gates of groups alone)

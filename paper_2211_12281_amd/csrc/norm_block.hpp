@@ -87,12 +87,16 @@ template <bool B16> struct Raw {
         else return kge_f32x4{__uint_as_float(w[0]), __uint_as_float(w[1]), __uint_as_float(w[2]), __uint_as_float(w[3])};
     }
 };
-template <bool B16, int NG, int LAST> __device__ __forceinline__ void store(char *row, const Columns<NG, LAST> &c, int k, kge_f32x4 v) {
+// stream: past the caches (KGE_STREAM_BYTES)
+template <bool B16, int NG, int LAST> __device__ __forceinline__ void store(char *row, const Columns<NG, LAST> &c, int k, kge_f32x4 v, bool stream) {
     typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf2;
     const int n = k < NG - LAST ? 4 : c.left(k), at = c.col(k);
     if (n >= 4) {
-        if constexpr (B16)
-            *(kge_u32x2_a2 *)((uint16_t *)row + at) = kge_u32x2{__builtin_bit_cast(uint32_t, bf2{(__bf16)v[0], (__bf16)v[1]}), __builtin_bit_cast(uint32_t, bf2{(__bf16)v[2], (__bf16)v[3]})};
+        if constexpr (B16) {
+            const kge_u32x2 w = {__builtin_bit_cast(uint32_t, bf2{(__bf16)v[0], (__bf16)v[1]}), __builtin_bit_cast(uint32_t, bf2{(__bf16)v[2], (__bf16)v[3]})};
+            if (stream) __builtin_nontemporal_store(w, (kge_u32x2_a2 *)((uint16_t *)row + at));
+            else *(kge_u32x2_a2 *)((uint16_t *)row + at) = w;
+        } else if (stream) __builtin_nontemporal_store(v, (kge_f32x4_a4 *)((float *)row + at));
         else *(kge_f32x4_a4 *)((float *)row + at) = v;
     } else {
 #pragma unroll
@@ -191,7 +195,7 @@ struct FwdArgs {
     int dim, waves; int64_t rows;
     Norm post, pre; const float *scale;
     Matrix gate; uint32_t gate_rows;
-    Matrix x, y, h, z;
+    Matrix x, y, h, z; bool stream;
 };
 
 enum { SUM_A = 0, SUM_B = 1, SUM_C = 2, SUM_D = 3 };
@@ -199,7 +203,7 @@ struct BwdArgs {
     int dim, waves; int64_t rows;
     Norm post, pre; const float *scale;
     Matrix gate; uint32_t gate_rows;
-    Matrix h, y, dh, dz, dx, dy, g_gate;
+    Matrix h, y, dh, dz, dx, dy, g_gate; bool stream;
     int64_t run, runs, part_ld; int parts;                        // rows of a run; runs; runs of a group, 0 where a run is not of one group
     uint32_t want;                                                // sums that are kept
     float *part;                                                  // [sum][run][part_ld]

@@ -141,12 +141,12 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
                     if (sum_d) D[k] += z[k];
                     d[k] = fma4(fma4(splat(-c2), h[k], c.minus(k, z[k] * vector(VEC_PRE, k), c1)), splat(rp), d[k]);
                 }
-                if (a.dx.p && in && c.inside(k)) store<S16>(a.dx.row(row), c, k, d[k]);
+                if (a.dx.p && in && c.inside(k)) store<S16>(a.dx.row(row), c, k, d[k], a.stream);
                 if (!a.y.p) continue;
                 y[k] *= splat(rq);                                // y^, or y itself
                 if constexpr (OF_ROW) {
                     if (a.g_gate.p && in && c.inside(k))          // s o d o u
-                        store<B16>(a.g_gate.row(row), c, k, d[k] * fma4(y[k], vector(VEC_F, k), vector(VEC_SB, k)));
+                        store<B16>(a.g_gate.row(row), c, k, d[k] * fma4(y[k], vector(VEC_F, k), vector(VEC_SB, k)), a.stream);
                     d[k] *= gate[k];
                 }
                 A[k] = fma4(d[k], y[k], A[k]);
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
             }
 #pragma unroll
             for (int k = 0; k < NG; ++k)
-                if (in && c.inside(k)) store<B16>(a.dy.row(row), c, k, d[k]);
+                if (in && c.inside(k)) store<B16>(a.dy.row(row), c, k, d[k], a.stream);
         }
         if constexpr (GROUPS) {                                   // the group's gate, and its sums times the gate
             const int64_t group = (uint32_t)g0 / a.gate_rows;
