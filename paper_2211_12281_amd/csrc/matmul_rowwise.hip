@@ -79,21 +79,23 @@ __device__ __forceinline__ kge_f32x4 scales4(const MatmulArgs &p, int64_t col) {
     return r;
 }
 
-// Workgroup = WM x WN waves = TM rows of A x TN rows of B, wave = NJ x NI blocks of 32 x 32.  Stages of 128 bytes of every row pass through a ring of NST
-// stages in the LDS, filled by asynchronous copies of whole lines.  A row's 16-byte pieces lie XOR-swizzled by (row / 2) % 8, so that the
+// Workgroup = WM x WN waves = TM rows of A x TN rows of B, wave = NJ x NI blocks of 32 x 32.  Stages of 128 bytes of every row pass through two places in the
+// LDS, filled by asynchronous copies of whole lines.  A row's 16-byte pieces lie XOR-swizzled by (row / 2) % 8, so that the
 // fragment reads of sixteen consecutive rows fall into different ones of the 64 banks.  Rows beyond the matrices are read from row 0 and not
 // stored.  Which bytes a lane half contracts first does not matter as long as both operands agree.
 //
-// A stage is four steps of 32 bytes; the fragments of the next step are read while this one's are multiplied, across the stages too: the only barrier of a stage
-// stands in front of the products of its last step, whose operands are in registers by then, and the stage that it frees is refilled behind it.
+// A stage is four steps of 32 bytes.  Its fragments are all in registers before its products begin: those of the next stage are read during the second half of this
+// one, into the registers of the steps that are over (the last step's have two places in turn).  So a place of the LDS is read in half a stage and
+// free for a stage and a half, which is what the copies from the L2 have to arrive in: with reads one step ahead it was one stage, and half of the time went by waiting
+// (16,384 x 4,096 x 4,096: 268 us).  The copies are issued over half a stage, as fast as the address unit takes them.
 //
 // FAR: a copy's lanes have 64-bit addresses; else (codes of less than 4 GiB) a base and 32-bit offsets.
-template <int WM, int WN, int NJ, int NI, int NST, int OCC, bool FAR>
+template <int WM, int WN, int NJ, int NI, int OCC, bool FAR>
 __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 void matmul_tiles_kernel(const MatmulArgs p) {
     constexpr int NW = WM * WN, TM = 32 * NJ * WM, TN = 32 * NI * WN, ROWS = TM + TN, CP = ROWS / 8 / NW;      // copies of a wave per stage
-    constexpr int STAGE = ROWS * BLOCK, STEPS = 4, SLOTS = NI * NJ;
-    static_assert(ROWS % (8 * NW) == 0 && NST >= 2 && (NST - 1) * CP < 64 && NST * STAGE <= 160 * 1024, "tile");
+    constexpr int NST = 2, STAGE = ROWS * BLOCK, SLOTS = NI * NJ, FRAGS = NI + NJ;
+    static_assert(ROWS % (8 * NW) == 0 && CP < 64 && NST * STAGE <= 160 * 1024, "tile");
     __shared__ __attribute__((aligned(16))) char lds[NST * STAGE];
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, g = lane >> 5;
@@ -154,30 +156,44 @@ void matmul_tiles_kernel(const MatmulArgs p) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
-    mi_i32x4 fb[2][NI], fa[2][NJ];                                                // this step's fragments and the next one's
+    mi_i32x4 f[4][FRAGS];                                                         // of the steps: of B, then of A
     const int swz = swizzle(lr);
-    auto read = [&](mi_i32x4 &to, int slot, int step, int row) {
-        to = *(const mi_i32x4 *)(lds + slot * STAGE + (row + lr) * BLOCK + (((2 * step + g) ^ swz) << 4));
+    auto read = [&](int slot, int r) {                                            // fragment r of a stage in the order of the steps
+        const int st = r / FRAGS, k = r % FRAGS, row = k < NI ? wn + 32 * k : TN + wm + 32 * (k - NI);
+        f[st][k] = *(const mi_i32x4 *)(lds + slot * STAGE + (row + lr) * BLOCK + (((2 * st + g) ^ swz) << 4));
     };
-    // fragment r in the order in which a step wants them: the first of A, all of B, the others of A
-    auto read_next = [&](int set, int r, int slot, int st) {
-        if (r == 0) read(fa[set][0], slot, st, TN + wm);
-        else if (r <= NI) read(fb[set][r - 1], slot, st, wn + 32 * (r - 1));
-        else read(fa[set][r - NI], slot, st, TN + wm + 32 * (r - NI));
-    };
-    // The products of one step and, behind each of them, a read of the next step's fragments and whatever `also` does.  (Left to itself the compiler puts all reads
-    // in front of all products, and those behind the barrier.)
-    auto step = [&](int set, int slot, int st, auto also) {                       // slot, st: of the next step
+    // products of a stage: in whose shadow the last step's fragments are read; between two copies; copies in front of the second half
+    constexpr int FREE = SLOTS, GAP = SLOTS >= CP ? 2 : 1, ISSUED = SLOTS / GAP < CP ? SLOTS / GAP : CP;
+    constexpr int READS = 3 * FRAGS <= 2 * SLOTS ? 1 : 2;                         // reads behind a product
+    static_assert(READS * SLOTS >= FRAGS && READS * 2 * SLOTS >= 3 * FRAGS && FREE + GAP * (CP - 1) < 4 * SLOTS, "slots");
+    // What stands behind each product keeps its place (the compiler would put all reads in front of all products).
+    auto stage = [&](int P) {
 #pragma unroll
-        for (int t = 0; t < SLOTS; ++t) {
-            const int j = t / NI, i = t % NI;
-            acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[set][i], fa[set][j], acc[i][j], 0, 0, 0);
+        for (int st = 0; st < 4; ++st)
 #pragma unroll
-            for (int r = 0; r < NI + NJ; ++r)
-                if (r * SLOTS / (NI + NJ) / (SLOTS >= 2 * (NI + NJ) ? 2 : 1) == t) read_next(set ^ 1, r, slot, st);
-            also(t);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int i = 0; i < NI; ++i) {
+                    const int t = st * SLOTS + j * NI + i, set = st;
+                    if (t == FREE) {
+                        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                        __syncthreads();                                          // everyone has this stage's fragments: its place takes the stage after the next
+                    }
+                    if (t == 2 * SLOTS) {
+                        kge_wait_vmcnt<ISSUED>();
+                        __syncthreads();                                          // the next stage has landed for everyone
+                    }
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[set][i], f[set][NI + j], acc[i][j], 0, 0, 0);
+                    if (t >= FREE && (t - FREE) % GAP == 0 && (t - FREE) / GAP < CP) copy(P, (t - FREE) / GAP);
+#pragma unroll
+                    for (int u = 0; u < READS; ++u) {
+                        const int r = READS * (t - 2 * SLOTS) + u, last = READS * t + u;
+                        if (t >= 2 * SLOTS && r < 3 * FRAGS) read(P ^ 1, r);      // (step r / FRAGS is over: the first two were before, the third in the shadow of the fourth)
+                        if (t < SLOTS && last < FRAGS) read(P, 3 * FRAGS + last);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+        advance();
     };
 
     if (kb0 < kb1) {
@@ -187,41 +203,32 @@ void matmul_tiles_kernel(const MatmulArgs p) {
             for (int c = 0; c < CP; ++c) copy(s, c);
             advance();
         }
-        kge_wait_vmcnt<(NST - 1) * CP>();
+        kge_wait_vmcnt<CP>();
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < NI + NJ; ++r) read_next(0, r, 0, 0);
-        int slot = 0;
-        for (int kb = kb0; kb < kb1; ++kb) {
-            const int after = slot == NST - 1 ? 0 : slot + 1;
-#pragma unroll
-            for (int st = 0; st < STEPS; ++st) {
-                const bool last = st == STEPS - 1;
-                if (last) {
-                    kge_wait_vmcnt<(NST - 2) * CP>();                             // the next block has landed ...
-                    __syncthreads();                                              // ... for everyone, and everyone has read this one, whose stage is refilled
-                }
-                step(st & 1, last ? after : slot, last ? 0 : st + 1, [&](int t) {
-                    if (!last) return;
-#pragma unroll
-                    for (int c = 0; c < CP; ++c)
-                        if (c * SLOTS / CP == t) copy(slot, c);
-                });
-            }
-            advance();
-            slot = after;
-        }
+        for (int r = 0; r < 3 * FRAGS; ++r) read(0, r);
+        for (int kb = kb0; kb < kb1; ++kb) stage((kb - kb0) & 1);
         kge_wait_vmcnt<0>();                                                      // no copy may be in flight when the LDS is released
     }
 
     // Accumulator layout: lane holds row lr of A's block; element e is B's row 8 (e / 4) + 4 g + e % 4.  Stored from there a row gets sixteen bytes at a
     // time; so 32 rows of the wave at a time go through the LDS, and rows leave in whole lines.  (Row stride one piece more than
     // the row: writes and reads of sixteen lanes fall into different banks.)
-    constexpr int LD = 32 * NI + 4;
-    static_assert(NW * 32 * LD * 4 <= NST * STAGE, "the waves' rows fit the ring");
-    int32_t *mine = (int32_t *)lds + wave * (32 * LD);
-    __syncthreads();                                                              // everyone is done with the ring
+    // The scales of the wave's rows stand beside them: read for each row from memory, every row's store would be waited for.
+    constexpr int LD = 32 * NI + 4, MINE = 32 * LD + 64 * NJ;
+    static_assert(NW * MINE * 4 <= NST * STAGE, "the waves' rows fit the ring");
+    int32_t *mine = (int32_t *)lds + wave * MINE;
+    float *scale = (float *)(mine + 32 * LD);                                     // [row], then whether there is such a row of A
     const int64_t col0 = n0 + wn;
+    __syncthreads();                                                              // everyone is done with the ring
+    if (!p.part) {
+#pragma unroll
+        for (int j = 0; j < NJ; j += 2) {
+            const int64_t row = m0 + wm + 32 * j + lane, from = row < p.m ? source(p, row) : -1;
+            scale[32 * j + lane] = from < 0 ? 0.f : p.as[from];
+            mine[32 * LD + 32 * NJ + 32 * j + lane] = from >= 0;
+        }
+    }
     auto store = [&](auto wide) {                                                 // wide: eight columns per lane, else four
         constexpr int C = decltype(wide)::value ? 8 : 4, LPR = 32 * NI / C, RPI = 64 / LPR;         // lanes per row, rows at a time
         const int c = C * (lane % LPR);
@@ -237,24 +244,24 @@ void matmul_tiles_kernel(const MatmulArgs p) {
                     *(mi_i32x4 *)(mine + lr * LD + 32 * i + 8 * q + 4 * g) = mi_i32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
             __builtin_amdgcn_wave_barrier();
             const int64_t row0 = m0 + wm + 32 * j;
-#pragma unroll
+#pragma unroll 4
             for (int r0 = 0; r0 < 32; r0 += RPI) {
                 const int r = r0 + lane / LPR;
                 const int64_t row = row0 + r;
                 mi_i32x4 x[C / 4];
 #pragma unroll
                 for (int e = 0; e < C / 4; ++e) x[e] = *(const mi_i32x4 *)(mine + r * LD + c + 4 * e);
-                if (row >= p.m) continue;
                 if constexpr (C == 4)
                     if (p.part) {
-                        if (col0 + c < p.part_ld) *(mi_i32x4 *)(p.part + ((int64_t)split * p.m + row) * p.part_ld + col0 + c) = x[0];
+                        if (row < p.m && col0 + c < p.part_ld) *(mi_i32x4 *)(p.part + ((int64_t)split * p.m + row) * p.part_ld + col0 + c) = x[0];
                         continue;
                     }
-                const int64_t from = source(p, row);
-                const float sa = from < 0 ? 0.f : p.as[from];
+                const float sa = scale[32 * j + r];
+                const bool there = mine[32 * LD + 32 * NJ + 32 * j + r];
+                if (row >= p.m) continue;
                 float v[C];
 #pragma unroll
-                for (int e = 0; e < C; ++e) v[e] = from < 0 ? 0.f : (float)x[e >> 2][e & 3] * sa * sb[e >> 2][e & 3];
+                for (int e = 0; e < C; ++e) v[e] = there ? (float)x[e >> 2][e & 3] * sa * sb[e >> 2][e & 3] : 0.f;
                 put<C>(p, row, col0 + c, v);
             }
             __builtin_amdgcn_wave_barrier();
@@ -336,9 +343,12 @@ constexpr int64_t WANTED = 512;
 constexpr int SPLIT_BLOCKS = 8;
 constexpr int64_t MAX_TILES = 1 << 22;                         // of a launch: a grid has fewer than 2^32 threads
 
-// Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B; stages; waves per SIMD; whether matrices may be 4 GiB and more
-struct Tile { int wm, wn, nj, ni, nst, occ; bool far; };
-constexpr Tile BIG = {2, 2, 4, 4, 2, 1, false}, MID = {2, 2, 2, 2, 2, 2, true};
+// Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B; waves per SIMD; whether matrices may be 4 GiB and more
+struct Tile { int wm, wn, nj, ni, occ; bool far; };
+#ifndef BIGT
+#define BIGT {2, 2, 4, 4, 1, false}
+#endif
+constexpr Tile BIG = BIGT, MID = {2, 2, 2, 2, 2, true};
 constexpr int tile_m(const Tile &t) { return 32 * t.wm * t.nj; }
 constexpr int tile_n(const Tile &t) { return 32 * t.wn * t.ni; }
 
@@ -384,8 +394,8 @@ void launch(const MatmulArgs &p, const Plan &q, hipStream_t st) {
         return;
     }
     const dim3 grid((unsigned)((p.tiles_m * p.tiles_n * p.splits + 7) / 8 * 8));
-    if (q.big) hipLaunchKernelGGL((matmul_tiles_kernel<BIG.wm, BIG.wn, BIG.nj, BIG.ni, BIG.nst, BIG.occ, BIG.far>), grid, dim3(64 * BIG.wm * BIG.wn), 0, st, p);
-    else hipLaunchKernelGGL((matmul_tiles_kernel<MID.wm, MID.wn, MID.nj, MID.ni, MID.nst, MID.occ, MID.far>), grid, dim3(64 * MID.wm * MID.wn), 0, st, p);
+    if (q.big) hipLaunchKernelGGL((matmul_tiles_kernel<BIG.wm, BIG.wn, BIG.nj, BIG.ni, BIG.occ, BIG.far>), grid, dim3(64 * BIG.wm * BIG.wn), 0, st, p);
+    else hipLaunchKernelGGL((matmul_tiles_kernel<MID.wm, MID.wn, MID.nj, MID.ni, MID.occ, MID.far>), grid, dim3(64 * MID.wm * MID.wn), 0, st, p);
     if (p.part) {
         const int64_t blocks = (p.m * (p.part_ld / 4) + 255) / 256;
         hipLaunchKernelGGL(matmul_join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, p);
