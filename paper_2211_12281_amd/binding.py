@@ -844,7 +844,7 @@ def _vector(t, dim: int, what: str):
     """Pointer of an fp32 vector of `dim` elements, or None."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.dim() != 1 or t.numel() != dim or not t.is_contiguous():
+    if t.dtype is not torch.float32 or t.dim() != 1 or t.numel() != dim or not t.is_contiguous():
         raise KgeError(f"{what}: a contiguous fp32 tensor of {dim} entries is wanted, got {t.dtype} {tuple(t.shape)}")
     return t.data_ptr()
 
@@ -853,49 +853,65 @@ class Norm:
     """kge_norm_t: a layer ("layer") or root-mean-square ("rms") norm with its weight and bias (fp32 vectors, either may be absent)."""
 
     def __init__(self, kind: str = "rms", weight=None, bias=None, eps: float = 1e-6):
-        if kind not in _NORMS:
+        code = _NORMS.get(kind)
+        if code is None:
             raise KgeError(f"kind: rms or layer, got {kind!r}")
         self.weight, self.bias = weight, bias
-        some = weight if weight is not None else bias
-        self.dim = None if some is None else some.numel()
-        self.struct = KgeNormT(_NORMS[kind], eps, None if weight is None else _vector(weight, self.dim, "weight"),
-                               None if bias is None else _vector(bias, self.dim, "bias"))
+        self.dim = weight.numel() if weight is not None else bias.numel() if bias is not None else None
+        self.struct = KgeNormT(code, eps, _vector(weight, self.dim, "weight"), _vector(bias, self.dim, "bias"))
+        self.address = C.addressof(self.struct)
 
 
-def _block(dim, stream_dtype, block_dtype, post, pre, scale, gate, gate_rows, rows):
-    """(kge_norm_block_t, tensors that it points to)"""
-    s = KgeNormBlockT(dim, stream_dtype, block_dtype)
-    for name, norm in (("post", post), ("pre", pre)):
-        if norm is not None:
-            if norm.dim not in (None, dim):
-                raise KgeError(f"{name}: a norm of {norm.dim} elements over rows of {dim}")
-            setattr(s, name, C.addressof(norm.struct))
-    s.scale = _vector(scale, dim, "scale")
-    if gate is not None:
-        s.gate, gdt, s.gate_ld = _matrix(gate, "gate")
-        if gate_rows is None:
-            gate_rows = 1 if gate.shape[0] == rows else 0
-        if gdt != block_dtype or gate_rows < 1 or tuple(gate.shape) != (-(-rows // gate_rows), dim):
-            raise KgeError(f"gate: {-(-rows // max(gate_rows, 1))} rows of {dim} (one for each gate_rows rows) of y's type are wanted, got {gate.dtype} "
-                           f"{tuple(gate.shape)} with gate_rows = {gate_rows}")
-        s.gate_rows = gate_rows
-    elif gate_rows is not None and gate_rows < 1:
-        raise KgeError("gate_rows: one row at least")
-    return s
-
-
-def _on_norms(*norms):
-    return [t for n in norms if n is not None for t in (n.weight, n.bias)]
-
-
-def _like(t, rows: int, dim: int, dtype: int, what: str):
-    """(pointer, row stride) of an input matrix, or of none"""
+def _like(t, shape, dtype, what: str):
+    """(pointer, row stride) of a matrix of this shape and type, or of none."""
     if t is None:
         return None, 0
-    p, dt, ld = _matrix(t, what)
-    if tuple(t.shape) != (rows, dim) or dt != dtype:
-        raise KgeError(f"{what}: {(rows, dim)} of another type is wanted, got {t.dtype} {tuple(t.shape)}")
-    return p, ld
+    if t.dtype is not dtype or t.shape != shape:
+        raise KgeError(f"{what}: {dtype} {tuple(shape)} is wanted, got {t.dtype} {tuple(t.shape)}")
+    if t.is_contiguous():
+        return t.data_ptr(), shape[1]
+    if shape[1] > 1 and t.stride(1) != 1:
+        raise KgeError(f"{what}: contiguous rows are wanted")
+    return t.data_ptr(), (t.stride(0) if shape[0] > 1 else shape[1])
+
+
+def _result(out, like, shape, dtype, what: str):
+    """(out, pointer, row stride): the given matrix, or a new one.  (A call with a stream of its own allocates inside _allocating_for.)"""
+    if out is None:
+        out = torch.empty_like(like) if like is not None and like.dtype is dtype and like.is_contiguous() else torch.empty(shape, dtype=dtype, device="cuda")
+        return out, out.data_ptr(), shape[1]
+    return (out, *_like(out, shape, dtype, what))
+
+
+def _block(shape, stream_dtype, block_dtype, post, pre, scale, gate, gate_rows):
+    """kge_norm_block_t (of the tensors and norms given, which have to live as long)"""
+    rows, dim = shape
+    if stream_dtype not in _DTYPE or block_dtype not in _DTYPE:
+        raise KgeError(f"fp32 or bf16 is wanted, got {stream_dtype} and {block_dtype}")
+    for norm in (post, pre):
+        if norm is not None and norm.dim is not None and norm.dim != dim:
+            raise KgeError(f"a norm of {norm.dim} elements over rows of {dim}")
+    pg, ldg = None, 0
+    if gate is not None:
+        if gate_rows is None:
+            gate_rows = 1 if gate.shape[0] == rows else 0
+        if gate_rows < 1:
+            raise KgeError("gate_rows: rows that share a row of the gate, one at least")
+        pg, ldg = _like(gate, (-(-rows // gate_rows), dim), block_dtype, "gate (one row for each gate_rows rows)")
+    elif gate_rows is not None and gate_rows < 1:
+        raise KgeError("gate_rows: one row at least")
+    return KgeNormBlockT(dim, _DTYPE[stream_dtype], _DTYPE[block_dtype], 0, None if post is None else post.address, None if pre is None else pre.address,
+                         _vector(scale, dim, "scale"), pg, ldg, gate_rows or 0)
+
+
+def _on_norms(post, pre):
+    return (None if post is None else post.weight, None if post is None else post.bias, None if pre is None else pre.weight, None if pre is None else pre.bias)
+
+
+def _two(t, what: str):
+    if t.dim() != 2:
+        raise KgeError(f"{what}: a 2-D tensor is wanted, got {tuple(t.shape)}")
+    return t.shape
 
 
 def norm_block(x, y=None, post: Norm | None = None, pre: Norm | None = None, scale=None, gate=None, gate_rows: int | None = None, dtype=None,
@@ -907,32 +923,35 @@ def norm_block(x, y=None, post: Norm | None = None, pre: Norm | None = None, sca
     if some is None:
         raise KgeError("kge_norm_block: x or y is wanted")
     dev = _here(x, y, scale, gate, out_h, out_z, *_on_norms(post, pre))
-    rows, dim = some.shape
-    sdt = _matrix(x if x is not None else y, "x")[1]
-    bdt = _matrix(y, "y")[1] if y is not None else _DTYPE.get(dtype or x.dtype)
-    if bdt is None or (y is not None and dtype is not None and dtype != y.dtype):
-        raise KgeError(f"dtype: y's, or fp32 or bf16 without y, got {dtype}")
-    blk = _block(dim, sdt, bdt, post, pre, scale, gate, gate_rows, rows)
-    px, ldx = _like(x, rows, dim, sdt, "x")
-    py, ldy = _like(y, rows, dim, bdt, "y")
+    shape = _two(some, "y" if y is not None else "x")
+    sdt = some.dtype if x is None else x.dtype
+    bdt = y.dtype if y is not None else dtype or x.dtype
+    if dtype is not None and dtype is not bdt:
+        raise KgeError(f"dtype: z has y's, {bdt}, got {dtype}")
+    blk = _block(shape, sdt, bdt, post, pre, scale, gate, gate_rows)
+    px, ldx = _like(x, shape, sdt, "x")
+    py, ldy = _like(y, shape, bdt, "y")
     h, ph, ldh, z, pz, ldz = (x if y is None else None), None, 0, None, None, 0
-    if y is not None and (want_h or pre is None):
-        h, ph, dt, ldh = _new(out_h, rows, dim, some.dtype if x is None else x.dtype, "kge_norm_block", stream)
-        if dt != sdt:
-            raise KgeError("out_h has another type than x")
-    elif out_h is not None:
-        raise KgeError("out_h: there is no h to write")
-    if pre is not None:
-        z, pz, dt, ldz = _new(out_z, rows, dim, y.dtype if y is not None else dtype or x.dtype, "kge_norm_block", stream)
-        if dt != bdt:
-            raise KgeError("out_z has another type than wanted")
-    elif out_z is not None:
-        raise KgeError("out_z: there is no norm behind h")
-    _check(load().kge_norm_block(C.byref(blk), px, ldx, py, ldy, rows, ph, ldh, pz, ldz, _queue(dev, stream)), "kge_norm_block")
+    with _allocating_for(stream):
+        if y is not None and (want_h or pre is None):
+            h, ph, ldh = _result(out_h, some if x is None else x, shape, sdt, "out_h")
+        elif out_h is not None:
+            raise KgeError("out_h: there is no h to write")
+        if pre is not None:
+            z, pz, ldz = _result(out_z, some, shape, bdt, "out_z")
+        elif out_z is not None:
+            raise KgeError("out_z: there is no norm behind h")
+    _check(load().kge_norm_block(C.byref(blk), px, ldx, py, ldy, shape[0], ph, ldh, pz, ldz, _queue(dev, stream)), "kge_norm_block")
     return h, z
 
 
-_BLOCK_GRADS = ("post_weight", "post_bias", "pre_weight", "pre_bias", "scale")
+_BLOCK_GRADS = ("scale", "post_weight", "post_bias", "pre_weight", "pre_bias")
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_block_bytes(rows: int, dim: int, gate_rows: int) -> int:
+    blk = KgeNormBlockT(dim, 0, 0, 0, None, None, None, 16 if gate_rows else None, dim, gate_rows)        # (an address that nothing looks at)
+    return int(load().kge_norm_block_bwd_workspace_bytes(C.byref(blk), rows))
 
 
 def norm_block_bwd(h, y=None, dh=None, dz=None, post: Norm | None = None, pre: Norm | None = None, scale=None, gate=None,
@@ -940,64 +959,74 @@ def norm_block_bwd(h, y=None, dh=None, dz=None, post: Norm | None = None, pre: N
     """kge_norm_block_bwd: a dict of gradients, "x", "y", "gate", "scale", "post_weight", "post_bias", "pre_weight", "pre_bias", of what the block has; want: the
     names wanted of these (all unless given).  h: the forward pass's (without y: its x; may be None without pre).  out: a dict of tensors to write
     to, "x" may be dh; accumulate: the vectors' gradients are added to those in `out`."""
-    out = dict(out or {})
+    out = {} if out is None else dict(out)
     first = h if h is not None else dh
     if first is None:
         raise KgeError("kge_norm_block_bwd: h or dh is wanted")
-    dev = _here(h, y, dh, dz, scale, gate, *_on_norms(post, pre), *out.values())
-    rows, dim = first.shape
-    sdt = _matrix(first, "h")[1]
-    block = y if y is not None else dz if dz is not None else first
-    bdt = _matrix(block, "y")[1]
-    blk = _block(dim, sdt, bdt, post, pre, scale, gate, gate_rows, rows)
-    there = {"x": True, "y": y is not None, "gate": gate is not None, "scale": scale is not None}
-    for name, norm in (("post", post), ("pre", pre)):
-        there[name + "_weight"], there[name + "_bias"] = (norm is not None and norm.weight is not None), (norm is not None and norm.bias is not None)
-    names = [k for k, t in there.items() if t] if want is None else list(want)
-    for k in (*names, *out):
-        if not there.get(k) or k not in names:
-            raise KgeError(f"{k!r}: no gradient of the block that is wanted")
-    if accumulate and any(k in names and k not in out for k in _BLOCK_GRADS):
-        raise KgeError("accumulate needs the gradients to add to")
-    args = [a for t, dt, what in ((h, sdt, "h"), (y, bdt, "y"), (dh, sdt, "dh"), (dz, bdt, "dz")) for a in _like(t, rows, dim, dt, what)]
-    grads, to = KgeNormBlockGradsT(), [None, 0, None, 0]
-    for i, (k, like, dt) in enumerate((("x", first, sdt), ("y", block, bdt), ("gate", gate, bdt))):
-        if k not in names:
-            continue
-        out[k], p, got, ld = _new(out.get(k), rows if k != "gate" else gate.shape[0], dim, like.dtype, "kge_norm_block_bwd", stream)
-        if got != dt:
-            raise KgeError(f"out[{k!r}] has another type than wanted")
-        if k == "gate":
-            grads.gate, grads.gate_ld = p, ld
-        else:
-            to[2 * i], to[2 * i + 1] = p, ld
+    norms = _on_norms(post, pre)
+    dev = _here(h, y, dh, dz, scale, gate, *norms, *out.values())
+    shape = _two(first, "h")
+    dim = shape[1]
+    sdt, block = first.dtype, y if y is not None else dz if dz is not None else first
+    bdt = block.dtype
+    blk = _block(shape, sdt, bdt, post, pre, scale, gate, gate_rows)
+    there = ["x"]
+    if y is not None:
+        there.append("y")
+    if gate is not None:
+        there.append("gate")
+    there += [k for k, t in zip(_BLOCK_GRADS, (scale, *norms)) if t is not None]
+    names = there if want is None else list(want)
+    if want is not None or out:
+        for k in (*names, *out):
+            if k not in there or k not in names:
+                raise KgeError(f"{k!r}: no gradient of the block that is wanted")
     sums = [k for k in _BLOCK_GRADS if k in names]
-    if any(k not in out for k in sums):
-        with _allocating_for(stream):
-            for k in sums:
-                if k not in out:
-                    out[k] = torch.empty(dim, dtype=torch.float32, device="cuda")
-    for k in sums:
-        setattr(grads, k, _vector(out[k], dim, f"out[{k!r}]"))
-    grads.accumulate = 1 if accumulate else 0
-    buf = None
-    if sums or (gate is not None and "gate" in names and blk.gate_rows > 1):
-        buf = _scratch(ws, int(load().kge_norm_block_bwd_workspace_bytes(C.byref(blk), rows)), stream)
-    _check(load().kge_norm_block_bwd(C.byref(blk), *args, rows, *to, C.byref(grads), _ptr(buf), 0 if buf is None else buf.numel(), _queue(dev, stream)),
-           "kge_norm_block_bwd")
-    return {k: out[k] for k in names}
+    if accumulate and any(k not in out for k in sums):
+        raise KgeError("accumulate needs the gradients to add to")
+    ph, ldh = _like(h, shape, sdt, "h")
+    py, ldy = _like(y, shape, bdt, "y")
+    pdh, lddh = _like(dh, shape, sdt, "dh")
+    pdz, lddz = _like(dz, shape, bdt, "dz")
+    px = pdy = pg = buf = None
+    ldx = lddy = ldg = 0
+    with _allocating_for(stream):
+        if "x" in names:
+            out["x"], px, ldx = _result(out.get("x"), first, shape, sdt, "out['x']")
+        if "y" in names:
+            out["y"], pdy, lddy = _result(out.get("y"), block, shape, bdt, "out['y']")
+        if "gate" in names:
+            out["gate"], pg, ldg = _result(out.get("gate"), gate, gate.shape, bdt, "out['gate']")
+        at = {k: _vector(out[k], dim, k) for k in sums if k in out} if out else {}
+        new = [k for k in sums if k not in at]
+        if new:
+            fresh = torch.empty((len(new), dim), dtype=torch.float32, device="cuda")
+            p, step = fresh.data_ptr(), 4 * dim
+            for k, t in zip(new, fresh.unbind(0)):
+                out[k], at[k] = t, p
+                p += step
+    grads = KgeNormBlockGradsT(at.get("post_weight"), at.get("post_bias"), at.get("pre_weight"), at.get("pre_bias"), at.get("scale"), pg, ldg,
+                               1 if accumulate else 0, 0)
+    if sums or (pg is not None and blk.gate_rows > 1):
+        buf = _scratch(ws, _norm_block_bytes(shape[0], dim, blk.gate_rows), stream)
+    _check(load().kge_norm_block_bwd(C.byref(blk), ph, ldh, py, ldy, pdh, lddh, pdz, lddz, shape[0], px, ldx, pdy, lddy, C.byref(grads),
+                                     _ptr(buf), 0 if buf is None else buf.numel(), _queue(dev, stream)), "kge_norm_block_bwd")
+    return out if want is None else {k: out[k] for k in names}
 
 
 class Rowwise:
     """kge_rowwise_t: a matrix [rows, cols] in 8-bit integers (int8 [rows, 128 ceil(cols / 128)], zeros behind a row's end) with a scale per row (fp32)."""
 
     def __init__(self, codes, scales, cols: int):
-        if codes.dtype != torch.int8 or codes.dim() != 2 or codes.shape[1] < -(-cols // 128) * 128 or (codes.shape[0] > 0 and cols > 0 and codes.stride(1) != 1):
-            raise KgeError(f"codes: contiguous int8 rows of {-(-cols // 128) * 128} (padded to a multiple of 128) are wanted, got {codes.dtype} {tuple(codes.shape)}")
-        rows = codes.shape[0]
+        wide = (cols + 127) // 128 * 128
+        if codes.dtype is not torch.int8 or codes.dim() != 2:
+            raise KgeError(f"codes: int8 rows are wanted, got {codes.dtype} {tuple(codes.shape)}")
+        rows, ld = codes.shape
+        if ld < wide or (rows > 0 and cols > 0 and codes.stride(1) != 1):
+            raise KgeError(f"codes: contiguous rows of {wide} (padded to a multiple of 128) are wanted, got {tuple(codes.shape)}")
         if scales.get_device() != codes.get_device():
             raise KgeError("codes and scales are on different devices")
-        ld = codes.stride(0) if rows > 1 and cols > 0 else -(-cols // 128) * 128      # (else torch gives strides of its own choice)
+        ld = codes.stride(0) if rows > 1 and cols > 0 else wide                       # (else torch gives strides of its own choice)
         self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
         self.struct = KgeRowwiseT(rows, cols, codes.data_ptr(), ld, _vector(scales, rows, "scales"))
         self.ref = C.byref(self.struct)

@@ -90,7 +90,7 @@ __device__ __forceinline__ kge_f32x4 scales4(const MatmulArgs &p, int64_t col) {
 // (16,384 x 4,096 x 4,096: 268 us).  The copies are issued over half a stage, as fast as the address unit takes them.
 //
 // FAR: a copy's lanes have 64-bit addresses; else (codes of less than 4 GiB) a base and 32-bit offsets.
-template <int WM, int WN, int NJ, int NI, int OCC, bool FAR>
+template <int WM, int WN, int NJ, int NI, int OCC, bool FAR, bool GATHERED>
 __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 void matmul_tiles_kernel(const MatmulArgs p) {
     constexpr int NW = WM * WN, TM = 32 * NJ * WM, TN = 32 * NI * WN, ROWS = TM + TN, CP = ROWS / 8 / NW;      // copies of a wave per stage
@@ -112,7 +112,7 @@ void matmul_tiles_kernel(const MatmulArgs p) {
     // Row r of the stage: B's tile first, then A's.  Copy j of this wave takes rows 8 (CP wave + j) .. + 7
     auto b_row = [&](int r) { const int64_t s = n0 + r; return s < p.n ? s : 0; };
     auto a_row = [&](int r) -> int64_t {
-        const int64_t s = m0 + r, t = s < p.m ? source(p, s) : 0;
+        const int64_t s = m0 + r, t = s < p.m ? (GATHERED ? source(p, s) : s) : 0;
         return t < 0 ? 0 : t;
     };
     auto swizzle = [](int r) { return (r >> 1) & 7; };
@@ -164,8 +164,8 @@ void matmul_tiles_kernel(const MatmulArgs p) {
     };
     // products of a stage: in whose shadow the last step's fragments are read; between two copies; copies in front of the second half
     constexpr int FREE = SLOTS, GAP = SLOTS >= CP ? 2 : 1, ISSUED = SLOTS / GAP < CP ? SLOTS / GAP : CP;
-    constexpr int READS = 3 * FRAGS <= 2 * SLOTS ? 1 : 2;                         // reads behind a product
-    static_assert(READS * SLOTS >= FRAGS && READS * 2 * SLOTS >= 3 * FRAGS && FREE + GAP * (CP - 1) < 4 * SLOTS, "slots");
+    constexpr int READS = (2 * FRAGS + SLOTS - 1) / SLOTS;                        // reads behind a product
+    static_assert(READS * SLOTS >= 2 * FRAGS && FREE + GAP * (CP - 1) < 4 * SLOTS, "slots");
     // What stands behind each product keeps its place (the compiler would put all reads in front of all products).
     auto stage = [&](int P) {
 #pragma unroll
@@ -187,9 +187,10 @@ void matmul_tiles_kernel(const MatmulArgs p) {
                     if (t >= FREE && (t - FREE) % GAP == 0 && (t - FREE) / GAP < CP) copy(P, (t - FREE) / GAP);
 #pragma unroll
                     for (int u = 0; u < READS; ++u) {
-                        const int r = READS * (t - 2 * SLOTS) + u, last = READS * t + u;
-                        if (t >= 2 * SLOTS && r < 3 * FRAGS) read(P ^ 1, r);      // (step r / FRAGS is over: the first two were before, the third in the shadow of the fourth)
-                        if (t < SLOTS && last < FRAGS) read(P, 3 * FRAGS + last);
+                        const int r = READS * (t % SLOTS) + u;
+                        if (st == 0 && r < FRAGS) read(P, 3 * FRAGS + r);
+                        if (st == 2 && r < 2 * FRAGS) read(P ^ 1, r);             // (the fragments of steps that are over)
+                        if (st == 3 && r < FRAGS) read(P ^ 1, 2 * FRAGS + r);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -211,64 +212,99 @@ void matmul_tiles_kernel(const MatmulArgs p) {
         kge_wait_vmcnt<0>();                                                      // no copy may be in flight when the LDS is released
     }
 
-    // Accumulator layout: lane holds row lr of A's block; element e is B's row 8 (e / 4) + 4 g + e % 4.  Stored from there a row gets sixteen bytes at a
-    // time; so 32 rows of the wave at a time go through the LDS, and rows leave in whole lines.  (Row stride one piece more than
-    // the row: writes and reads of sixteen lanes fall into different banks.)
-    // The scales of the wave's rows stand beside them: read for each row from memory, every row's store would be waited for.
-    constexpr int LD = 32 * NI + 4, MINE = 32 * LD + 64 * NJ;
-    static_assert(NW * MINE * 4 <= NST * STAGE, "the waves' rows fit the ring");
-    int32_t *mine = (int32_t *)lds + wave * MINE;
-    float *scale = (float *)(mine + 32 * LD);                                     // [row], then whether there is such a row of A
+    // Accumulator layout: lane holds row lr of A's block; element e is B's row 8 (e / 4) + 4 g + e % 4.  Stored from there a row gets eight or sixteen bytes at a
+    // time; so 32 rows of the wave at a time go through the LDS, with their scales applied and rounded where nothing is added to them, and rows leave in whole
+    // lines.  (Row stride one piece more than the row: writes and reads of sixteen lanes fall into different banks.)
     const int64_t col0 = n0 + wn;
-    __syncthreads();                                                              // everyone is done with the ring
-    if (!p.part) {
+    float sa[NJ];
+    bool there[NJ];
+    kge_f32x4 sb[NI][4];
 #pragma unroll
-        for (int j = 0; j < NJ; j += 2) {
-            const int64_t row = m0 + wm + 32 * j + lane, from = row < p.m ? source(p, row) : -1;
-            scale[32 * j + lane] = from < 0 ? 0.f : p.as[from];
-            mine[32 * LD + 32 * NJ + 32 * j + lane] = from >= 0;
-        }
+    for (int j = 0; j < NJ; ++j) {
+        const int64_t row = m0 + wm + 32 * j + lr, from = row < p.m && !p.part ? (GATHERED ? source(p, row) : row) : -1;
+        there[j] = from >= 0;
+        sa[j] = from < 0 ? 0.f : p.as[from];
     }
-    auto store = [&](auto wide) {                                                 // wide: eight columns per lane, else four
-        constexpr int C = decltype(wide)::value ? 8 : 4, LPR = 32 * NI / C, RPI = 64 / LPR;         // lanes per row, rows at a time
-        const int c = C * (lane % LPR);
-        kge_f32x4 sb[C / 4];
 #pragma unroll
-        for (int e = 0; e < C / 4; ++e) sb[e] = scales4(p, col0 + c + 4 * e);
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sb[i][q] = scales4(p, col0 + 32 * i + 8 * q + 4 * g);
+    auto scaled = [&](int i, int j, int q) {
+        kge_f32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = (float)acc[i][j][4 * q + e] * sa[j] * sb[i][q][e];
+            if (GATHERED) v[e] = there[j] ? v[e] : 0.f;
+        }
+        return v;
+    };
+    constexpr int LD = 32 * NI + 4;                                               // in words; of 16-bit results half of it and a piece
+    static_assert(NW * 32 * LD * 4 <= NST * STAGE, "the waves' rows fit the ring");
+    uint32_t *mine = (uint32_t *)lds + wave * (32 * LD);
+    __syncthreads();                                                              // everyone is done with the ring
+    if (p.out16 && !p.part && !p.accumulate) {
+        typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf2;
+        constexpr int LPR = 4 * NI, RPI = 64 / LPR, LD16 = 16 * NI + 4;           // lanes per row, rows at a time
+        const int c = 8 * (lane % LPR);
+        const int n = (int)(p.n - col0 - c < 8 ? p.n - col0 - c : 8);
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
 #pragma unroll
             for (int i = 0; i < NI; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    *(mi_i32x4 *)(mine + lr * LD + 32 * i + 8 * q + 4 * g) = mi_i32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                for (int q = 0; q < 4; ++q) {
+                    const kge_f32x4 v = scaled(i, j, q);
+                    *(kge_u32x2 *)(mine + lr * LD16 + 16 * i + 4 * q + 2 * g) =
+                        kge_u32x2{__builtin_bit_cast(uint32_t, bf2{(__bf16)v[0], (__bf16)v[1]}), __builtin_bit_cast(uint32_t, bf2{(__bf16)v[2], (__bf16)v[3]})};
+                }
             __builtin_amdgcn_wave_barrier();
-            const int64_t row0 = m0 + wm + 32 * j;
-#pragma unroll 4
+#pragma unroll
             for (int r0 = 0; r0 < 32; r0 += RPI) {
                 const int r = r0 + lane / LPR;
-                const int64_t row = row0 + r;
-                mi_i32x4 x[C / 4];
+                const int64_t row = m0 + wm + 32 * j + r;
+                const kge_u32x4 x = *(const kge_u32x4 *)(mine + r * LD16 + c / 2);
+                if (row >= p.m || n <= 0) continue;
+                uint16_t *q = (uint16_t *)p.out + row * p.out_ld + col0 + c;
+                if (n == 8) *(kge_u32x4_a2 *)q = x;
+                else {
 #pragma unroll
-                for (int e = 0; e < C / 4; ++e) x[e] = *(const mi_i32x4 *)(mine + r * LD + c + 4 * e);
-                if constexpr (C == 4)
-                    if (p.part) {
-                        if (row < p.m && col0 + c < p.part_ld) *(mi_i32x4 *)(p.part + ((int64_t)split * p.m + row) * p.part_ld + col0 + c) = x[0];
-                        continue;
-                    }
-                const float sa = scale[32 * j + r];
-                const bool there = mine[32 * LD + 32 * NJ + 32 * j + r];
-                if (row >= p.m) continue;
-                float v[C];
-#pragma unroll
-                for (int e = 0; e < C; ++e) v[e] = there ? (float)x[e >> 2][e & 3] * sa * sb[e >> 2][e & 3] : 0.f;
-                put<C>(p, row, col0 + c, v);
+                    for (int e = 0; e < 7; ++e)
+                        if (e < n) q[e] = (uint16_t)(x[e >> 1] >> (16 * (e & 1)));
+                }
             }
             __builtin_amdgcn_wave_barrier();
         }
-    };
-    if (p.part || !p.out16) store(std::false_type());
-    else store(std::true_type());
+        return;
+    }
+    constexpr int LPR = 8 * NI, RPI = 64 / LPR;
+    const int c = 4 * (lane % LPR);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                mi_i32x4 x = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                if (!p.part) x = __builtin_bit_cast(mi_i32x4, scaled(i, j, q));
+                *(mi_i32x4 *)(mine + lr * LD + 32 * i + 8 * q + 4 * g) = x;
+            }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 4
+        for (int r0 = 0; r0 < 32; r0 += RPI) {
+            const int r = r0 + lane / LPR;
+            const int64_t row = m0 + wm + 32 * j + r;
+            const mi_i32x4 x = *(const mi_i32x4 *)(mine + r * LD + c);
+            if (row >= p.m) continue;
+            if (p.part) {
+                if (col0 + c < p.part_ld) *(mi_i32x4 *)(p.part + ((int64_t)split * p.m + row) * p.part_ld + col0 + c) = x;
+                continue;
+            }
+            const kge_f32x4 y = __builtin_bit_cast(kge_f32x4, x);
+            float v[4] = {y[0], y[1], y[2], y[3]};
+            put<4>(p, row, col0 + c, v);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
 // Sums the splits' partial results.
@@ -345,10 +381,7 @@ constexpr int64_t MAX_TILES = 1 << 22;                         // of a launch: a
 
 // Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B; waves per SIMD; whether matrices may be 4 GiB and more
 struct Tile { int wm, wn, nj, ni, occ; bool far; };
-#ifndef BIGT
-#define BIGT {2, 2, 4, 4, 1, false}
-#endif
-constexpr Tile BIG = BIGT, MID = {2, 2, 2, 2, 2, true};
+constexpr Tile BIG = {2, 4, 4, 2, 2, false}, MID = {2, 2, 2, 2, 2, true};
 constexpr int tile_m(const Tile &t) { return 32 * t.wm * t.nj; }
 constexpr int tile_n(const Tile &t) { return 32 * t.wn * t.ni; }
 
@@ -394,8 +427,11 @@ void launch(const MatmulArgs &p, const Plan &q, hipStream_t st) {
         return;
     }
     const dim3 grid((unsigned)((p.tiles_m * p.tiles_n * p.splits + 7) / 8 * 8));
-    if (q.big) hipLaunchKernelGGL((matmul_tiles_kernel<BIG.wm, BIG.wn, BIG.nj, BIG.ni, BIG.occ, BIG.far>), grid, dim3(64 * BIG.wm * BIG.wn), 0, st, p);
-    else hipLaunchKernelGGL((matmul_tiles_kernel<MID.wm, MID.wn, MID.nj, MID.ni, MID.occ, MID.far>), grid, dim3(64 * MID.wm * MID.wn), 0, st, p);
+#define KGE_TILES(T, GATHERED) \
+    hipLaunchKernelGGL((matmul_tiles_kernel<T.wm, T.wn, T.nj, T.ni, T.occ, T.far, GATHERED>), grid, dim3(64 * T.wm * T.wn), 0, st, p)
+    if (q.big) { if (p.rows) KGE_TILES(BIG, true); else KGE_TILES(BIG, false); }
+    else { if (p.rows) KGE_TILES(MID, true); else KGE_TILES(MID, false); }
+#undef KGE_TILES
     if (p.part) {
         const int64_t blocks = (p.m * (p.part_ld / 4) + 255) / 256;
         hipLaunchKernelGGL(matmul_join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, st, p);

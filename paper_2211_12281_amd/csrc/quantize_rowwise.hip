@@ -10,7 +10,7 @@
 
 namespace {
 
-constexpr int NT = 256, BLOCK = 128;
+constexpr int NT = 256, BLOCK = 128, MAX_RUNS = 64;
 constexpr uint32_t INF32 = 0x7f800000u;
 constexpr int64_t MAX_COLS = 131071, MAX_GROUPS = 1 << 21;       // (workgroups of a launch: a grid has fewer than 2^32 threads)
 
@@ -130,6 +130,7 @@ template <bool B16> __global__ __launch_bounds__(NT) void column_max_kernel(cons
 template <bool B16> __global__ __launch_bounds__(NT) void columns_kernel(const Args a) {
     __shared__ uint32_t tile[BLOCK][BLOCK / 4 + 1];                // (one word more per column: a wave's words fall into different banks)
     __shared__ float inv[BLOCK];
+    __shared__ __attribute__((aligned(16))) uint32_t top[8][BLOCK];
     const int64_t nb = (a.cols + BLOCK - 1) / BLOCK, tr = blockIdx.x / (uint32_t)nb, tc = blockIdx.x - tr * nb;
     const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;
     const int64_t row0 = tr * BLOCK, col0 = tc * BLOCK;
@@ -140,9 +141,22 @@ template <bool B16> __global__ __launch_bounds__(NT) void columns_kernel(const A
         const int d = 4 * rg + 64 * (i >> 2) + (i & 3);
         kge_load8<B16>((const char *)a.x + (row0 + (d < rows ? d : 0)) * a.ld * (B16 ? 2 : 4), col0 + 8 * cg, d < rows ? (n > 8 ? 8 : n) : 0, v[i]);
     }
+    {                                                              // a thread's four columns in every eighth run
+        const int c = 4 * (threadIdx.x & 31), r0 = threadIdx.x >> 5;
+        kge_u32x4 m = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < MAX_RUNS / 8; ++i) {
+            const int r = r0 + 8 * i;
+            const kge_u32x4 x = *(const kge_u32x4 *)(a.part + (r < a.runs ? r : 0) * a.part_ld + col0 + c);
+            m = __builtin_elementwise_max(m, x);
+        }
+        *(kge_u32x4 *)&top[r0][c] = m;
+    }
+    __syncthreads();
     if (threadIdx.x < BLOCK) {
         uint32_t m = 0;
-        for (int r = 0; r < a.runs; ++r) m = max(m, a.part[r * a.part_ld + col0 + threadIdx.x]);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) m = max(m, top[r][threadIdx.x]);
         const Scale s = scale_of(m);
         inv[threadIdx.x] = s.inv;
         if (tr == 0 && (int)threadIdx.x < cols) a.cs[col0 + threadIdx.x] = s.scale;
@@ -170,7 +184,7 @@ constexpr int64_t WANTED = 1024, MIN_RUN = 32;
 void runs_of(int64_t rows, int64_t cols, Args &a) {
     const int64_t across = (cols + 255) / 256;
     int64_t runs = (WANTED + across - 1) / across;
-    if (runs > 64) runs = 64;
+    if (runs > MAX_RUNS) runs = MAX_RUNS;
     if (runs > (rows + MIN_RUN - 1) / MIN_RUN) runs = (rows + MIN_RUN - 1) / MIN_RUN;
     if (runs < 1) runs = 1;
     a.run = (rows + runs - 1) / runs; a.runs = (int)runs; a.part_ld = across * 256;
