@@ -10,7 +10,7 @@
 
 namespace {
 
-constexpr int NT = 256, BLOCK = 128, MAX_RUNS = 64;
+constexpr int NT = 256, BLOCK = 128, MAX_RUNS = 128;
 constexpr uint32_t INF32 = 0x7f800000u;
 constexpr int64_t MAX_COLS = 131071, MAX_GROUPS = 1 << 21;       // (workgroups of a launch: a grid has fewer than 2^32 threads)
 
@@ -101,16 +101,16 @@ __global__ __launch_bounds__(WAVES == 1 ? NT : 64 * WAVES) void rows_kernel(cons
     }
 }
 
-// Largest magnitudes of the columns in a run of rows: a thread takes eight columns of every eighth row.
+// Largest magnitudes of 128 columns in a run of rows: a thread takes eight columns of every sixteenth row.
 template <bool B16> __global__ __launch_bounds__(NT) void column_max_kernel(const Args a) {
-    __shared__ uint32_t top[8][32][9];
-    const int cg = threadIdx.x & 31, rg = threadIdx.x >> 5;
-    const int64_t col = (int64_t)blockIdx.x * 256 + 8 * cg, left = a.cols - col;
+    __shared__ uint32_t top[16][16][9];
+    const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;
+    const int64_t col = (int64_t)blockIdx.x * BLOCK + 8 * cg, left = a.cols - col;
     const int64_t r0 = (int64_t)blockIdx.y * a.run, r1 = min(r0 + a.run, a.rows);
     uint32_t m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (left > 0)
-#pragma unroll 4
-        for (int64_t r = r0 + rg; r < r1; r += 8) {
+#pragma unroll 8
+        for (int64_t r = r0 + rg; r < r1; r += 16) {
             float v[8];
             kge_load8<B16>((const char *)a.x + r * a.ld * (B16 ? 2 : 4), col, left > 8 ? 8 : (int)left, v);
 #pragma unroll
@@ -119,10 +119,11 @@ template <bool B16> __global__ __launch_bounds__(NT) void column_max_kernel(cons
 #pragma unroll
     for (int e = 0; e < 8; ++e) top[rg][cg][e] = m[e];
     __syncthreads();
+    if (threadIdx.x >= BLOCK) return;
     uint32_t t = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t = max(t, top[i][threadIdx.x >> 3][threadIdx.x & 7]);
-    a.part[blockIdx.y * a.part_ld + (int64_t)blockIdx.x * 256 + threadIdx.x] = t;
+    for (int i = 0; i < 16; ++i) t = max(t, top[i][threadIdx.x >> 3][threadIdx.x & 7]);
+    a.part[blockIdx.y * a.part_ld + (int64_t)blockIdx.x * BLOCK + threadIdx.x] = t;
 }
 
 // Tiles of 128 x 128 turned in the LDS.  Thread (rg, cg) holds rows 4 rg .. + 3 and 64 + 4 rg .. + 3 of columns 8 cg .. + 7: four rows of a column make one
@@ -182,12 +183,12 @@ template <bool B16> __global__ __launch_bounds__(NT) void columns_kernel(const A
 // Runs of rows of the search for the columns' largest magnitudes: about 1,024 workgroups, of 32 rows at least
 constexpr int64_t WANTED = 1024, MIN_RUN = 32;
 void runs_of(int64_t rows, int64_t cols, Args &a) {
-    const int64_t across = (cols + 255) / 256;
+    const int64_t across = (cols + BLOCK - 1) / BLOCK;
     int64_t runs = (WANTED + across - 1) / across;
     if (runs > MAX_RUNS) runs = MAX_RUNS;
     if (runs > (rows + MIN_RUN - 1) / MIN_RUN) runs = (rows + MIN_RUN - 1) / MIN_RUN;
     if (runs < 1) runs = 1;
-    a.run = (rows + runs - 1) / runs; a.runs = (int)runs; a.part_ld = across * 256;
+    a.run = (rows + runs - 1) / runs; a.runs = (int)runs; a.part_ld = across * BLOCK;
 }
 
 template <bool B16, int NG, int WAVES, bool LONG> void launch_rows(const Args &a, hipStream_t st) {
@@ -205,7 +206,7 @@ template <bool B16> void launch(const Args &a, hipStream_t st) {
         else launch_rows<B16, 4, 16, true>(a, st);
     }
     if (a.cc) {
-        hipLaunchKernelGGL((column_max_kernel<B16>), dim3((unsigned)(a.part_ld / 256), (unsigned)a.runs), dim3(NT), 0, st, a);
+        hipLaunchKernelGGL((column_max_kernel<B16>), dim3((unsigned)(a.part_ld / BLOCK), (unsigned)a.runs), dim3(NT), 0, st, a);
         hipLaunchKernelGGL((columns_kernel<B16>), dim3((unsigned)(((a.cols + BLOCK - 1) / BLOCK) * ((a.rows + BLOCK - 1) / BLOCK))), dim3(NT), 0, st, a);
     }
 }
