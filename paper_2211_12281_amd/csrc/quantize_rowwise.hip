@@ -5,7 +5,7 @@
 //
 // Memory bounds it.  By rows a row of up to 32,768 elements stays in its threads' registers between the search for the largest magnitude and the
 // codes, so x is read once.  By columns the largest magnitudes come first (partial ones for each run of rows, in the workspace), then tiles of 128 x 128 are
-// turned in the LDS: x is read twice.
+// turned in the LDS: x is read twice.  For both layouts (up to 4,096 columns) the search finds the rows' magnitudes too, and a tile writes both.
 #include "text_ops.hpp"
 
 namespace {
@@ -54,6 +54,8 @@ struct Args {
     int8_t *rc; float *rs; int64_t rc_ld;                         // by rows
     int8_t *cc; float *cs; int64_t cc_ld;                         // by columns
     uint32_t *part; int64_t part_ld, run; int runs;               // largest magnitudes of the columns in runs of rows: [run][part_ld]
+    uint32_t *row_part; int64_t row_ld;                           // and of the rows in blocks of 128 columns: [block][row_ld]
+    float *col_inv, *row_inv;                                     // inverses of the scales
 };
 
 // A row per team of waves (one wave: four rows per workgroup), NG groups of eight columns per thread; longer rows (LONG) are read twice.
@@ -101,20 +103,35 @@ __global__ __launch_bounds__(WAVES == 1 ? NT : 64 * WAVES) void rows_kernel(cons
     }
 }
 
-// Largest magnitudes of 128 columns in a run of rows: a thread takes eight columns of every sixteenth row.
-template <bool B16> __global__ __launch_bounds__(NT) void column_max_kernel(const Args a) {
+// largest of sixteen neighbouring lanes
+__device__ __forceinline__ uint32_t max_of_16(uint32_t m) {
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xf, 0xf, true));      // lane ^ 1
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xf, 0xf, true));      // lane ^ 2
+    m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x141, 0xf, 0xf, true));     // 7 - lane
+    return max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x140, 0xf, 0xf, true));  // 15 - lane
+}
+// Largest magnitudes of 128 columns in a run of rows: a thread takes eight columns of every sixteenth row.  BOTH: those of the rows' 128 columns too.
+template <bool B16, bool BOTH> __global__ __launch_bounds__(NT) void column_max_kernel(const Args a) {
     __shared__ uint32_t top[16][16][9];
     const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;
     const int64_t col = (int64_t)blockIdx.x * BLOCK + 8 * cg, left = a.cols - col;
     const int64_t r0 = (int64_t)blockIdx.y * a.run, r1 = min(r0 + a.run, a.rows);
     uint32_t m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (left > 0)
+    if (BOTH || left > 0)                                         // (the lanes of a row go round together)
 #pragma unroll 8
         for (int64_t r = r0 + rg; r < r1; r += 16) {
             float v[8];
             kge_load8<B16>((const char *)a.x + r * a.ld * (B16 ? 2 : 4), col, left > 8 ? 8 : (int)left, v);
+            uint32_t row = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m[e] = max(m[e], mag(v[e]));
+            for (int e = 0; e < 8; ++e) {
+                m[e] = max(m[e], mag(v[e]));
+                if (BOTH) row = max(row, mag(v[e]));
+            }
+            if constexpr (BOTH) {
+                row = max_of_16(row);
+                if (cg == 0) a.row_part[(int64_t)blockIdx.x * a.row_ld + r] = row;
+            }
         }
 #pragma unroll
     for (int e = 0; e < 8; ++e) top[rg][cg][e] = m[e];
@@ -126,12 +143,47 @@ template <bool B16> __global__ __launch_bounds__(NT) void column_max_kernel(cons
     a.part[blockIdx.y * a.part_ld + (int64_t)blockIdx.x * BLOCK + threadIdx.x] = t;
 }
 
+// Scales of the columns (128 of them per workgroup, 32 slices of the runs) and, behind those workgroups, of the rows (one per thread), and their inverses, which the
+// tiles take: from the partial magnitudes every tile would read 64 KB, twice its own share of x in bf16.
+__global__ __launch_bounds__(1024) void scales_kernel(const Args a) {
+    const int64_t blocks = a.part_ld / BLOCK;
+    if (blockIdx.x >= blocks) {
+        const int64_t row = (int64_t)(blockIdx.x - blocks) * 1024 + threadIdx.x;
+        if (row >= a.rows) return;
+        uint32_t m = 0;
+#pragma unroll 8
+        for (int b = 0; b < (int)blocks; ++b) m = max(m, a.row_part[b * a.row_ld + row]);
+        const Scale s = scale_of(m);
+        a.rs[row] = s.scale;
+        a.row_inv[row] = s.inv;
+        return;
+    }
+    __shared__ __attribute__((aligned(16))) uint32_t top[32][BLOCK];
+    const int c = 4 * (threadIdx.x & 31), r0 = threadIdx.x >> 5;
+    kge_u32x4 m = {0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < MAX_RUNS / 32; ++i) {
+        const int r = r0 + 32 * i;
+        m = __builtin_elementwise_max(m, *(const kge_u32x4 *)(a.part + (r < a.runs ? r : 0) * a.part_ld + (int64_t)blockIdx.x * BLOCK + c));
+    }
+    *(kge_u32x4 *)&top[r0][c] = m;
+    __syncthreads();
+    const int64_t col = (int64_t)blockIdx.x * BLOCK + threadIdx.x;
+    if (threadIdx.x >= BLOCK || col >= a.cols) return;
+    uint32_t t = 0;
+#pragma unroll
+    for (int r = 0; r < 32; ++r) t = max(t, top[r][threadIdx.x]);
+    const Scale s = scale_of(t);
+    a.cs[col] = s.scale;
+    a.col_inv[col] = s.inv;
+}
+
 // Tiles of 128 x 128 turned in the LDS.  Thread (rg, cg) holds rows 4 rg .. + 3 and 64 + 4 rg .. + 3 of columns 8 cg .. + 7: four rows of a column make one
 // word of the transposed tile.
-template <bool B16> __global__ __launch_bounds__(NT) void columns_kernel(const Args a) {
+template <bool B16, bool BOTH> __global__ __launch_bounds__(NT) void columns_kernel(const Args a) {
     __shared__ uint32_t tile[BLOCK][BLOCK / 4 + 1];                // (one word more per column: a wave's words fall into different banks)
     __shared__ float inv[BLOCK];
-    __shared__ __attribute__((aligned(16))) uint32_t top[8][BLOCK];
+    __shared__ float row_inv[BOTH ? BLOCK : 1];
     const int64_t nb = (a.cols + BLOCK - 1) / BLOCK, tr = blockIdx.x / (uint32_t)nb, tc = blockIdx.x - tr * nb;
     const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4;
     const int64_t row0 = tr * BLOCK, col0 = tc * BLOCK;
@@ -142,27 +194,16 @@ template <bool B16> __global__ __launch_bounds__(NT) void columns_kernel(const A
         const int d = 4 * rg + 64 * (i >> 2) + (i & 3);
         kge_load8<B16>((const char *)a.x + (row0 + (d < rows ? d : 0)) * a.ld * (B16 ? 2 : 4), col0 + 8 * cg, d < rows ? (n > 8 ? 8 : n) : 0, v[i]);
     }
-    {                                                              // a thread's four columns in every eighth run
-        const int c = 4 * (threadIdx.x & 31), r0 = threadIdx.x >> 5;
-        kge_u32x4 m = {0u, 0u, 0u, 0u};
+    if (threadIdx.x < BLOCK) inv[threadIdx.x] = (int)threadIdx.x < cols ? a.col_inv[col0 + threadIdx.x] : 0.f;
+    else if (BOTH) row_inv[threadIdx.x - BLOCK] = (int)threadIdx.x - BLOCK < rows ? a.row_inv[row0 + threadIdx.x - BLOCK] : 0.f;
+    __syncthreads();
+    if constexpr (BOTH) {
 #pragma unroll
-        for (int i = 0; i < MAX_RUNS / 8; ++i) {
-            const int r = r0 + 8 * i;
-            const kge_u32x4 x = *(const kge_u32x4 *)(a.part + (r < a.runs ? r : 0) * a.part_ld + col0 + c);
-            m = __builtin_elementwise_max(m, x);
+        for (int i = 0; i < 8; ++i) {
+            const int d = 4 * rg + 64 * (i >> 2) + (i & 3);
+            if (d < rows) *(kge_u32x2 *)(a.rc + (row0 + d) * a.rc_ld + col0 + 8 * cg) = codes8(v[i], row_inv[d]);
         }
-        *(kge_u32x4 *)&top[r0][c] = m;
     }
-    __syncthreads();
-    if (threadIdx.x < BLOCK) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int r = 0; r < 8; ++r) m = max(m, top[r][threadIdx.x]);
-        const Scale s = scale_of(m);
-        inv[threadIdx.x] = s.inv;
-        if (tr == 0 && (int)threadIdx.x < cols) a.cs[col0 + threadIdx.x] = s.scale;
-    }
-    __syncthreads();
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int c = 8 * cg + e;
@@ -188,15 +229,19 @@ void runs_of(int64_t rows, int64_t cols, Args &a) {
     if (runs > MAX_RUNS) runs = MAX_RUNS;
     if (runs > (rows + MIN_RUN - 1) / MIN_RUN) runs = (rows + MIN_RUN - 1) / MIN_RUN;
     if (runs < 1) runs = 1;
-    a.run = (rows + runs - 1) / runs; a.runs = (int)runs; a.part_ld = across * BLOCK;
+    a.run = (rows + runs - 1) / runs; a.runs = (int)runs; a.part_ld = across * BLOCK; a.row_ld = (rows + BLOCK - 1) / BLOCK * BLOCK;
 }
+// words of the workspace; in both layouts at once (24,576 x 768 bf16: 28 us, one after the other 36) where a row has few blocks
+constexpr int64_t MOST_BLOCKS = 32;
+bool at_once(int64_t cols) { return cols <= MOST_BLOCKS * BLOCK; }
+int64_t words_of(const Args &a, bool both) { return (a.runs + 1) * a.part_ld + (both ? (a.part_ld / BLOCK + 1) * a.row_ld : 0); }
 
 template <bool B16, int NG, int WAVES, bool LONG> void launch_rows(const Args &a, hipStream_t st) {
     const int64_t teams = WAVES == 1 ? NT / 64 : 1, groups = (a.rows + teams - 1) / teams;
     hipLaunchKernelGGL((rows_kernel<B16, NG, WAVES, LONG>), dim3((unsigned)(groups < MAX_GROUPS ? groups : MAX_GROUPS)), dim3(WAVES == 1 ? NT : 64 * WAVES), 0, st, a);
 }
 template <bool B16> void launch(const Args &a, hipStream_t st) {
-    if (a.rc) {
+    if (a.rc && !a.row_part) {
         if (a.cols <= 512) launch_rows<B16, 1, 1, false>(a, st);
         else if (a.cols <= 1024) launch_rows<B16, 2, 1, false>(a, st);
         else if (a.cols <= 2048) launch_rows<B16, 1, 4, false>(a, st);
@@ -206,8 +251,16 @@ template <bool B16> void launch(const Args &a, hipStream_t st) {
         else launch_rows<B16, 4, 16, true>(a, st);
     }
     if (a.cc) {
-        hipLaunchKernelGGL((column_max_kernel<B16>), dim3((unsigned)(a.part_ld / BLOCK), (unsigned)a.runs), dim3(NT), 0, st, a);
-        hipLaunchKernelGGL((columns_kernel<B16>), dim3((unsigned)(((a.cols + BLOCK - 1) / BLOCK) * ((a.rows + BLOCK - 1) / BLOCK))), dim3(NT), 0, st, a);
+        const dim3 runs((unsigned)(a.part_ld / BLOCK), (unsigned)a.runs), tiles((unsigned)(((a.cols + BLOCK - 1) / BLOCK) * ((a.rows + BLOCK - 1) / BLOCK)));
+        if (a.row_part) {
+            hipLaunchKernelGGL((column_max_kernel<B16, true>), runs, dim3(NT), 0, st, a);
+            hipLaunchKernelGGL(scales_kernel, dim3((unsigned)(a.part_ld / BLOCK + (a.rows + 1023) / 1024)), dim3(1024), 0, st, a);
+            hipLaunchKernelGGL((columns_kernel<B16, true>), tiles, dim3(NT), 0, st, a);
+        } else {
+            hipLaunchKernelGGL((column_max_kernel<B16, false>), runs, dim3(NT), 0, st, a);
+            hipLaunchKernelGGL(scales_kernel, dim3((unsigned)(a.part_ld / BLOCK)), dim3(1024), 0, st, a);
+            hipLaunchKernelGGL((columns_kernel<B16, false>), tiles, dim3(NT), 0, st, a);
+        }
     }
 }
 
@@ -221,7 +274,7 @@ size_t kge_quantize_rowwise_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 0 || rows >= (1ll << 31) || cols >= (1ll << 31)) return 0;
     Args a = {};
     runs_of(rows, cols, a);
-    return (size_t)a.runs * a.part_ld * sizeof(uint32_t) + 256;
+    return (size_t)words_of(a, at_once(cols)) * sizeof(uint32_t) + 256;
 }
 
 int kge_quantize_rowwise(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, const kge_rowwise_t *by_row, const kge_rowwise_t *by_col,
@@ -245,8 +298,14 @@ int kge_quantize_rowwise(const void *x, int32_t dtype, int64_t rows, int64_t col
         a.cc = by_col->codes; a.cs = by_col->scales; a.cc_ld = by_col->ld;
         runs_of(rows, cols, a);
         const size_t lost = ws ? (256 - ((uintptr_t)ws & 255)) & 255 : 0;
-        if (!ws || ws_bytes < lost + (size_t)a.runs * a.part_ld * sizeof(uint32_t)) return KGE_E_WORKSPACE_TOO_SMALL;
+        const bool both = by_row && at_once(cols);
+        if (!ws || ws_bytes < lost + (size_t)words_of(a, both) * sizeof(uint32_t)) return KGE_E_WORKSPACE_TOO_SMALL;
         a.part = (uint32_t *)((char *)ws + lost);
+        a.col_inv = (float *)(a.part + a.runs * a.part_ld);
+        if (both && rows > 0) {
+            a.row_inv = a.col_inv + a.part_ld;
+            a.row_part = (uint32_t *)a.row_inv + a.row_ld;
+        }
     }
     hipStream_t st = (hipStream_t)hip_stream;
     if (rows == 0 || cols == 0) {                                 // rows of no elements have a scale all the same
