@@ -95,13 +95,15 @@ def _moments(m, v, g):
 
 
 def _check_params(got, p, m, v, wd, step):
-    """Parameters from the new moments (fp32 values): decay, bias corrections, root, quotient and their products, seven fp32 roundings of the update, two of the sum."""
+    """Parameters from the new moments (fp32 values).  The update is c1 m lr / (sqrt(c2 v) + eps): c1, m c1, lr, the quotient and eps's sum a rounding each, c2 and v c2
+    half of one behind the root, the root one; with 8-bit moments root and reciprocal are good to an ulp, two roundings each, and there is a product more: ten.
+    Two roundings of the decay and one of the sum, relative to what is added."""
     p, m, v = (t.astype(np.float64) for t in (p, m, v))
     b1, b2, lr, eps = (float(CFG[k]) for k in ("b1", "b2", "lr", "eps"))
     with np.errstate(invalid="ignore"):
         upd = lr * (m / (1 - b1 ** step)) / (np.sqrt(v / (1 - b2 ** step)) + eps)
     want = p * (1 - lr * float(F(wd))) - upd
-    tol = 9 * U * np.abs(upd) + 3 * U * (np.abs(p) + np.abs(want))
+    tol = 10 * U * np.abs(upd) + 3 * U * (np.abs(p) + np.abs(want))
     fine = np.isfinite(want)
     assert np.array_equal(np.isfinite(got), fine)
     assert (np.abs(got.astype(np.float64) - want) <= tol)[fine].all()
