@@ -1066,7 +1066,8 @@ def quantize_rowwise(x, by: str = "row", out=None, ws: Workspace | None = None, 
         for q in (qr, qc):
             if q is not None:
                 _here(q.codes, q.scales)
-    buf = _scratch(ws, _rowwise_bytes(rows, cols), stream) if qc is not None else None
+    need = _rowwise_bytes(rows, cols) if qc is not None else 0
+    buf = _scratch(ws, need, stream) if need > 256 else None                   # (256: nothing is written there)
     _check(load().kge_quantize_rowwise(px, dt, rows, cols, ld, qr.ref if qr else None, qc.ref if qc else None, _ptr(buf),
                                        0 if buf is None else buf.numel(), _queue(dev, stream)), "kge_quantize_rowwise")
     return (qr, qc) if by == "both" else qr or qc

@@ -218,7 +218,7 @@ template <bool B16> __global__ __launch_bounds__(JT) void norm_join_kernel(const
 // ---------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------
-constexpr int64_t FWD_GROUPS = 2048;
+constexpr int64_t FWD_GROUPS = 2048, FEW = 2;
 constexpr int64_t MANY_PARTS = 16;                              // runs of a group from which on its sums are a launch of their own
 
 bool bad_norm(const kge_norm_t *n) {
@@ -246,6 +246,7 @@ Runs runs_of(const kge_norm_block_t *b, int64_t rows) {
     const int64_t wanted = bwd_runs_of(b->dim), teams = bwd_teams_of(b->dim);
     int64_t run = (rows + wanted - 1) / wanted;
     if (run < teams) run = teams;
+    if (rows <= FEW * teams && (!b->gate || b->gate_rows == 1 || b->gate_rows >= rows)) run = rows;     // (a launch costs more than the longer run; several groups go one by one)
     Runs q = {run, (rows + run - 1) / run, 0};
     if (b->gate && b->gate_rows > 1) {
         const int64_t len = b->gate_rows < rows ? b->gate_rows : rows;
@@ -254,7 +255,7 @@ Runs runs_of(const kge_norm_block_t *b, int64_t rows) {
             q.run = (len + q.parts - 1) / q.parts;
             q.runs = (rows + len - 1) / len * q.parts;
         } else {
-            q.run = run / len * len;
+            q.run = (run >= rows ? rows + len - 1 : run) / len * len;
             q.runs = (rows + q.run - 1) / q.run;
         }
     }
@@ -362,12 +363,12 @@ int kge_norm_block_bwd(const kge_norm_block_t *blk, const void *h, int64_t h_ld,
     if (w.post_bias || (bias && (w.scale || of_group))) a.want |= 1u << SUM_B;
     if (w.pre_weight) a.want |= 1u << SUM_C;
     if (w.pre_bias) a.want |= 1u << SUM_D;
-    if (a.want) {
+    if (a.want && q.runs != 1) {
         const size_t lost = ws ? (256 - ((uintptr_t)ws & 255)) & 255 : 0, need = (size_t)q.runs * 4 * a.part_ld * sizeof(float);
         if (need && (!ws || ws_bytes < lost + need)) return KGE_E_WORKSPACE_TOO_SMALL;
         a.part = (float *)((char *)ws + lost);
     }
-    const bool folded = q.parts > MANY_PARTS && (a.want & 3);
+    const bool folded = q.parts > MANY_PARTS && q.runs > 1 && (a.want & 3);
     hipStream_t st = (hipStream_t)hip_stream;
     if (rows > 0) {
         if (s16) rows_bwd16(a, b16, st);
@@ -379,7 +380,7 @@ int kge_norm_block_bwd(const kge_norm_block_t *blk, const void *h, int64_t h_ld,
         }
     }
     const bool vectors = w.scale || w.post_weight || w.post_bias || w.pre_weight || w.pre_bias;
-    if (vectors || (of_group && !folded && rows > 0)) {
+    if (q.runs != 1 && (vectors || (of_group && !folded && rows > 0))) {
         const dim3 grid((unsigned)(a.part_ld / JC), a.want >> 2 ? 2 : 1);
         if (b16) hipLaunchKernelGGL(norm_join_kernel<true>, grid, dim3(JT), 0, st, a, folded);
         else hipLaunchKernelGGL(norm_join_kernel<false>, grid, dim3(JT), 0, st, a, folded);

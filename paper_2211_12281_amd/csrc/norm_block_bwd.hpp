@@ -193,7 +193,40 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
         }
         g0 = g1;
     } while (g0 < r1);
-    // the run's sums
+    // The only run has everything: the vectors' gradients, and that of the only group's gate, without another launch.
+    if (a.runs == 1) {
+        auto put = [&](float *q, int i, kge_f32x4 x) {
+            if (!q) return;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e < a.dim) q[i + e] = a.accumulate ? q[i + e] + x[e] : x[e];
+        };
+        if (a.y.p) {
+            if (!GROUPS) __syncthreads();                         // (everyone has read the factors, whose place takes B)
+            of_columns(B, [&](int i, kge_f32x4 x) { *(kge_f32x4 *)(vec + VEC_F * wide + i) = GROUPS ? *(const kge_f32x4 *)(vec + VEC_B * wide + i) : x; });
+            of_columns(A, [&](int i, kge_f32x4 x) {
+                kge_f32x4 s = GROUPS ? *(const kge_f32x4 *)(vec + VEC_A * wide + i) : x, d = *(const kge_f32x4 *)(vec + VEC_F * wide + i);
+                const kge_f32x4 sc = vector4(a.scale, i, a.dim, 1.f), w = vector4(a.post.w, i, a.dim, 1.f), b = vector4(a.post.b, i, a.dim, 0.f);
+                if (a.parts > 0) {                                // the gate of the one group
+                    const kge_f32x4 v = sc * fma4(w, s, b * d);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (i + e < a.dim) {
+                            const float g = load1<B16>(a.gate.p, i + e);
+                            if (a.g_gate.p) store1<B16>(a.g_gate.p, i + e, v[e]);
+                            s[e] *= g; d[e] *= g;
+                        }
+                }
+                put(a.g_scale, i, fma4(w, s, b * d));
+                put(a.g_postw, i, sc * s);
+                put(a.g_postb, i, sc * d);
+            });
+        }
+        of_columns(C, [&](int i, kge_f32x4 x) { put(a.g_prew, i, x); });
+        of_columns(D, [&](int i, kge_f32x4 x) { put(a.g_preb, i, x); });
+        return;
+    }
+    // the run's sums, for the join
     auto keep = [&](const kge_f32x4 (&s)[NG], int which, int folded) {
         if (!(a.want >> which & 1)) return;
         float *p = a.part + ((int64_t)which * a.runs + run) * a.part_ld;

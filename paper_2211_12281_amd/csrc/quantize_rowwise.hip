@@ -221,6 +221,53 @@ template <bool B16, bool BOTH> __global__ __launch_bounds__(NT) void columns_ker
     }
 }
 
+// A matrix of few rows, by columns in one launch: a workgroup takes 32 columns and all rows (512 at most), which stay in registers between the search and the codes.
+// Thread (rg, cg) holds rows 4 rg .. + 3 and 256 + 4 rg .. + 3 of columns 8 cg .. + 7: four rows of a column make one word of the transposed strip.
+constexpr int STRIP = 32, STRIP_ROWS = 512;
+bool in_strips(int64_t rows, int64_t cols) { return rows <= STRIP_ROWS && cols < 1ll << 28; }                  // (a grid has fewer than 2^32 threads)
+template <bool B16> __global__ __launch_bounds__(NT) void strips_kernel(const Args a) {
+    __shared__ uint32_t tile[STRIP][STRIP_ROWS / 4 + 1];
+    __shared__ uint32_t top[NT / 64][4][9];
+    const int cg = threadIdx.x & 3, rg = threadIdx.x >> 2, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int rows = (int)a.rows, halves = rows > STRIP_ROWS / 2 ? 2 : 1;
+    const int64_t col0 = (int64_t)blockIdx.x * STRIP;
+    const int cols = (int)min((int64_t)STRIP, a.cols - col0), n = cols - 8 * cg;
+    float v[8][8];
+    uint32_t m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int d = 4 * rg + 256 * (i >> 2) + (i & 3);
+        kge_load8<B16>((const char *)a.x + (int64_t)(d < rows ? d : 0) * a.ld * (B16 ? 2 : 4), col0 + 8 * cg, d < rows ? (n > 8 ? 8 : n) : 0, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m[e] = max(m[e], mag(v[i][e]));
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+#pragma unroll
+        for (int s = 4; s < 64; s *= 2) m[e] = max(m[e], (uint32_t)__shfl_xor((int)m[e], s));
+        if (lane < 4) top[wave][cg][e] = m[e];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int c = 8 * cg + e;
+        const Scale s = scale_of(max(max(top[0][cg][e], top[1][cg][e]), max(top[2][cg][e], top[3][cg][e])));
+        if (rg == 0 && c < cols) a.cs[col0 + c] = s.scale;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            tile[c][64 * h + rg] = code(v[4 * h][e], s.inv) | code(v[4 * h + 1][e], s.inv) << 8 | code(v[4 * h + 2][e], s.inv) << 16 | code(v[4 * h + 3][e], s.inv) << 24;
+    }
+    __syncthreads();
+    const int pieces = (int)(padded(rows) / 16);                  // of a column
+    for (int q = threadIdx.x; q < STRIP * 16 * halves; q += NT) {
+        const int c = q / (16 * halves), w = q % (16 * halves);
+        if (c < cols && w < pieces)
+            *(kge_u32x4 *)(a.cc + (col0 + c) * a.cc_ld + 16 * w) = kge_u32x4{tile[c][4 * w], tile[c][4 * w + 1], tile[c][4 * w + 2], tile[c][4 * w + 3]};
+    }
+}
+
 // Runs of rows of the search for the columns' largest magnitudes: about 1,024 workgroups, of 32 rows at least
 constexpr int64_t WANTED = 1024, MIN_RUN = 32;
 void runs_of(int64_t rows, int64_t cols, Args &a) {
@@ -252,7 +299,10 @@ template <bool B16> void launch(const Args &a, hipStream_t st) {
     }
     if (a.cc) {
         const dim3 runs((unsigned)(a.part_ld / BLOCK), (unsigned)a.runs), tiles((unsigned)(((a.cols + BLOCK - 1) / BLOCK) * ((a.rows + BLOCK - 1) / BLOCK)));
-        if (a.row_part) {
+        if (in_strips(a.rows, a.cols)) {
+            const int64_t strips = (a.cols + STRIP - 1) / STRIP;
+            hipLaunchKernelGGL((strips_kernel<B16>), dim3((unsigned)strips), dim3(NT), 0, st, a);
+        } else if (a.row_part) {
             hipLaunchKernelGGL((column_max_kernel<B16, true>), runs, dim3(NT), 0, st, a);
             hipLaunchKernelGGL(scales_kernel, dim3((unsigned)(a.part_ld / BLOCK + (a.rows + 1023) / 1024)), dim3(1024), 0, st, a);
             hipLaunchKernelGGL((columns_kernel<B16, true>), tiles, dim3(NT), 0, st, a);
@@ -274,7 +324,7 @@ size_t kge_quantize_rowwise_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 0 || rows >= (1ll << 31) || cols >= (1ll << 31)) return 0;
     Args a = {};
     runs_of(rows, cols, a);
-    return (size_t)words_of(a, at_once(cols)) * sizeof(uint32_t) + 256;
+    return !in_strips(rows, cols) ? (size_t)words_of(a, at_once(cols)) * sizeof(uint32_t) + 256 : 256;
 }
 
 int kge_quantize_rowwise(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, const kge_rowwise_t *by_row, const kge_rowwise_t *by_col,
@@ -298,9 +348,9 @@ int kge_quantize_rowwise(const void *x, int32_t dtype, int64_t rows, int64_t col
         a.cc = by_col->codes; a.cs = by_col->scales; a.cc_ld = by_col->ld;
         runs_of(rows, cols, a);
         const size_t lost = ws ? (256 - ((uintptr_t)ws & 255)) & 255 : 0;
-        const bool both = by_row && at_once(cols);
-        if (!ws || ws_bytes < lost + (size_t)words_of(a, both) * sizeof(uint32_t)) return KGE_E_WORKSPACE_TOO_SMALL;
-        a.part = (uint32_t *)((char *)ws + lost);
+        const bool both = by_row && at_once(cols) && !in_strips(rows, cols);
+        if (!in_strips(rows, cols) && (!ws || ws_bytes < lost + (size_t)words_of(a, both) * sizeof(uint32_t))) return KGE_E_WORKSPACE_TOO_SMALL;
+        a.part = (uint32_t *)((char *)ws + lost);                  // (few rows: nothing is written there)
         a.col_inv = (float *)(a.part + a.runs * a.part_ld);
         if (both && rows > 0) {
             a.row_inv = a.col_inv + a.part_ld;

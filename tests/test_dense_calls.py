@@ -108,8 +108,10 @@ def test_quantize_rowwise_refuses(lib):
         x, dt, rows, cols, ld, C.byref(r) if r else None, C.byref(c) if c else None, ws, wsb, None)
     for bad in [dict(x=None), dict(dt=2), dict(rows=255), dict(cols=299), dict(ld=299), dict(r=None), dict(x=OK + 2), dict(c=good), dict(rows=-1), dict(ld=1 << 31)]:
         assert call(**bad) == INVALID, bad
-    need = lib.kge_quantize_rowwise_workspace_bytes(256, 300)
-    assert need > 300 * 4 and call(c=col) == SMALL and call(c=col, ws=OK + 8, wsb=need - 256) == SMALL
+    need = lib.kge_quantize_rowwise_workspace_bytes(600, 300)
+    tall = dict(rows=600, r=_q(600), c=_q(300, 600))
+    assert need > 300 * 4 and call(**tall) == SMALL and call(**tall, ws=OK + 8, wsb=need - 256) == SMALL
+    assert lib.kge_quantize_rowwise_workspace_bytes(512, 300) == 256 and col.rows == 300
     assert call(rows=131_072, cols=2, ld=2, r=None, c=_q(2, 131_072), ws=OK, wsb=1 << 30) == UNSUPPORTED
     assert call(cols=131_072, rows=2, ld=131_072, r=_q(2, 131_072)) == UNSUPPORTED
     assert call(rows=0, cols=300, r=_q(0), x=None) == 0

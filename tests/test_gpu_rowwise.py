@@ -54,7 +54,7 @@ def _same(q, x):
 
 @pytest.mark.parametrize("dt", [F32, BF16])
 @pytest.mark.parametrize("rows,cols,pad", [(1, 1, 0), (3, 7, 1), (5, 128, 0), (130, 129, 3), (257, 300, 1), (2, 513, 0), (7, 1025, 1), (3, 2049, 0), (2, 4097, 1), (3, 8193, 0),
-                                           (2, 32_769, 1), (1, 131_071, 0), (700, 64, 0), (128, 128, 0)])
+                                           (2, 32_769, 1), (1, 131_071, 0), (700, 64, 0), (128, 128, 0), (256, 31, 1), (511, 33, 0), (512, 200, 1), (513, 200, 0)])
 @pytest.mark.parametrize("by", ["row", "col", "both"])
 def test_quantize(dt, rows, cols, pad, by):
     x = _values((rows, cols), dt, 1, rows, cols) * torch.from_numpy(_rng(2, rows).uniform(1e-3, 1e3, size=(rows, 1))).to(dt)
@@ -297,5 +297,5 @@ def test_the_binding_refuses():
             bad()
     with pytest.raises(kge.KgeError):
         with torch.cuda.graph(torch.cuda.CUDAGraph()):
-            kge.quantize_rowwise(x, by="col")
+            kge.quantize_rowwise(torch.zeros((600, 8), device="cuda"), by="col")
     torch.cuda.synchronize()
