@@ -19,14 +19,14 @@ using namespace kge_norm;
 // ---------------------------------------------------------------------------------------------
 // A team takes a row at a time; the vectors stand in the LDS (rows of more than 4,096 columns: in memory).
 enum { VEC_POST = 0, VEC_POST_BIAS = 1, VEC_SCALE = 2, VEC_PRE = 3, VEC_PRE_BIAS = 4, VECTORS = 5 };
-template <bool S16, bool B16, int NG, int LAST, int NT, int OCC>
+template <bool S16, bool B16, int NG, int NT, int OCC>
 __global__ __launch_bounds__(NT, OCC) void norm_fwd_kernel(const FwdArgs a) {
     constexpr bool LDS = NT == 256;
     __shared__ float red[2][NT / 64][1];
     extern __shared__ __attribute__((aligned(16))) float vec[];
     const Team t(a.waves);
     Reduce<1, NT> reduce(red, t);
-    const Columns<NG, LAST> c(a.dim, t.lane, t.size);
+    const Columns<NG> c(a.dim, t.lane, t.size);
     const float inv_dim = 1.f / (float)a.dim;
     const int wide = 4 * t.size * NG;
     const float *const from[VECTORS] = {a.post.w, a.post.b, a.scale, a.pre.w, a.pre.b};
@@ -239,33 +239,36 @@ bool bad_matrix(const void *p, int32_t dtype, int64_t ld, int64_t cols) { return
 Norm norm_of(const kge_norm_t *n) {
     return n ? Norm{true, n->kind == KGE_NORM_LAYER, n->eps, n->weight, n->bias} : Norm{false, false, 1.f, nullptr, nullptr};
 }
-// Runs of rows of the backward pass: as many as the chip holds at once, of a row for each team at least; of parts of one group of rows, where a group is as long as
-// a run, else of whole groups.
+// Runs of rows of the backward pass: as many as the chip holds at once, of a row for each team at least.  Groups of rows with a gate: whole ones, where every second
+// team can have one to itself; else a group is a run or several, so many that the chip's rounds take least.
 struct Runs { int64_t run, runs, parts; };
 Runs runs_of(const kge_norm_block_t *b, int64_t rows) {
     const int64_t wanted = bwd_runs_of(b->dim), teams = bwd_teams_of(b->dim);
     int64_t run = (rows + wanted - 1) / wanted;
     if (run < teams) run = teams;
-    if (rows <= FEW * teams && (!b->gate || b->gate_rows == 1 || b->gate_rows >= rows)) run = rows;     // (a launch costs more than the longer run; several groups go one by one)
-    Runs q = {run, (rows + run - 1) / run, 0};
     if (b->gate && b->gate_rows > 1) {
-        const int64_t len = b->gate_rows < rows ? b->gate_rows : rows;
-        if (len >= run) {
-            q.parts = (len + run - 1) / run;
-            q.run = (len + q.parts - 1) / q.parts;
-            q.runs = (rows + len - 1) / len * q.parts;
-        } else {
-            q.run = (run >= rows ? rows + len - 1 : run) / len * len;
-            q.runs = (rows + q.run - 1) / q.run;
+        const int64_t len = b->gate_rows < rows ? b->gate_rows : rows, groups = (rows + len - 1) / len;
+        if (2 * groups >= wanted * teams) {
+            run = (run + len * teams - 1) / (len * teams) * (len * teams);
+            return {run, (rows + run - 1) / run, 0};
         }
+        int64_t parts = 1, least = 0;
+        for (int64_t p = wanted / groups > 1 ? wanted / groups : 1, k = 0; k < 3; ++k, ++p) {
+            if (k > 0 && (len + p - 1) / p < teams) break;
+            const int64_t cost = (groups * p + wanted - 1) / wanted * ((len + p * teams - 1) / (p * teams) + 2);     // rows of a team and what a run costs besides
+            if (k == 0 || cost < least) { least = cost; parts = p; }
+        }
+        if (parts > (len + teams - 1) / teams) parts = (len + teams - 1) / teams;
+        return {(len + parts - 1) / parts, groups * parts, parts};
     }
-    return q;
+    if (rows <= FEW * teams) run = rows;                          // (a launch costs more than the longer run)
+    return {run, (rows + run - 1) / run, 0};
 }
-// No call of up to so many rows has more runs.  With r rows in a run before the groups' ends are looked at: groups of len >= r rows are
-// ceil(rows / len) ceil(len / r) < rows / r + rows / len + len / r + 1 runs, shorter ones less than 2 rows / r + 1.
+// No call of up to so many rows has more runs: without gates and with whole groups at most `wanted`; else there are fewer than wanted teams / 2 groups, and groups parts runs, parts at
+// most wanted / groups + 2 (3 where there are more groups than that): fewer than wanted + 3 wanted teams / 2; and as a run of a whole group has a row, fewer than 2 rows.
 int64_t most_runs(const kge_norm_block_t *b, int64_t rows) {
-    const int64_t few = 3 * (rows / bwd_teams_of(b->dim) + 1) + 1, all = 3 * bwd_runs_of(b->dim) + 1;
-    return rows == 0 ? 0 : few < all ? few : all;
+    const int64_t all = bwd_runs_of(b->dim) * (2 * bwd_teams_of(b->dim) + 3);
+    return 2 * rows < all ? 2 * rows : all;
 }
 int64_t part_ld_of(int dim) { return (dim + JC - 1) / JC * JC; }
 
@@ -275,19 +278,22 @@ template <bool S16, bool B16> void launch_fwd(const FwdArgs &a, hipStream_t st) 
     if (groups > FWD_GROUPS) groups = FWD_GROUPS;
     const dim3 grid((unsigned)groups), blk(64 * a.waves * teams);
     const int lds = a.waves <= 4 ? VECTORS * 256 * a.waves * ng * (int)sizeof(float) : 0;                   // 80 KB at most
-#define KGE_FWD(NG, LAST, NT, OCC)                                                                                              \
+#define KGE_FWD(NG, NT, OCC)                                                                                                    \
     do {                                                                                                                        \
         static KgeLdsLimit limit;                                                                                               \
-        const auto kern = norm_fwd_kernel<S16, B16, NG, LAST, NT, OCC>;                                                         \
+        const auto kern = norm_fwd_kernel<S16, B16, NG, NT, OCC>;                                                               \
         if (lds > 48 * 1024 && limit.set((const void *)kern, 80 * 1024) != KGE_OK) return;                                      \
         hipLaunchKernelGGL(kern, grid, blk, lds, st, a);                                                                        \
     } while (0)
-    if (a.waves == 8) KGE_FWD(4, 2, 512, 2);
-    else switch (ng) {
-    case 1: KGE_FWD(1, 1, 256, 8); break;
-    case 2: KGE_FWD(2, 1, 256, 6); break;
-    case 3: KGE_FWD(3, 1, 256, 5); break;
-    default: KGE_FWD(4, 1, 256, 4);
+    if (a.waves == 8) {
+        if (ng == 2) KGE_FWD(2, 512, 4);
+        else if (ng == 3) KGE_FWD(3, 512, 4);
+        else KGE_FWD(4, 512, 2);
+    } else switch (ng) {
+    case 1: KGE_FWD(1, 256, 8); break;
+    case 2: KGE_FWD(2, 256, 6); break;
+    case 3: KGE_FWD(3, 256, 5); break;
+    default: KGE_FWD(4, 256, 4);
     }
 #undef KGE_FWD
 }

@@ -29,23 +29,21 @@ __device__ __forceinline__ kge_f32x4 vector4(const float *p, int i, int dim, flo
     return r;
 }
 
-// A thread's share of a row: NG groups of four columns, the team's lanes side by side.  Only the last LAST groups may reach past the row's end; `mask` is 1 on
-// their columns that are inside and 0 on the others, whose values are kept zero: a mean is subtracted as fma(-mean, mask, x).
-template <int NG, int LAST> struct Columns {
+// A thread's share of a row: NG groups of four columns, the team's lanes side by side.  Only the last group may reach past the row's end; `mask` is 1 on
+// its columns that are inside and 0 on the others, whose values are kept zero: a mean is subtracted as fma(-mean, mask, x).
+template <int NG> struct Columns {
     int dim, lane, size;
-    kge_f32x4 mask[LAST];
+    kge_f32x4 mask;
     __device__ __forceinline__ Columns(int d, int l, int s) : dim(d), lane(l), size(s) {
 #pragma unroll
-        for (int k = 0; k < LAST; ++k)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mask[k][e] = col(NG - LAST + k) + e < d ? 1.f : 0.f;
+        for (int e = 0; e < 4; ++e) mask[e] = col(NG - 1) + e < d ? 1.f : 0.f;
     }
     __device__ __forceinline__ int col(int k) const { return 4 * (lane + size * k); }
     __device__ __forceinline__ int left(int k) const { return dim - col(k); }
-    __device__ __forceinline__ bool inside(int k) const { return k < NG - LAST || left(k) > 0; }
+    __device__ __forceinline__ bool inside(int k) const { return k < NG - 1 || left(k) > 0; }
     // x - m on the columns that are inside
     __device__ __forceinline__ kge_f32x4 minus(int k, kge_f32x4 x, float m) const {
-        return k < NG - LAST ? x - splat(m) : fma4(splat(-m), mask[k - (NG - LAST)], x);
+        return k < NG - 1 ? x - splat(m) : fma4(splat(-m), mask, x);
     }
 };
 
@@ -53,9 +51,9 @@ template <int NG, int LAST> struct Columns {
 // than four elements take them one by one).
 template <bool B16> struct Raw {
     kge_u32x4 w;                                                  // (bf16: two words)
-    template <int NG, int LAST> __device__ __forceinline__ void load(const char *row, const Columns<NG, LAST> &c, int k, bool in) {
+    template <int NG> __device__ __forceinline__ void load(const char *row, const Columns<NG> &c, int k, bool in) {
         w = kge_u32x4{0u, 0u, 0u, 0u};
-        const bool whole = k < NG - LAST;
+        const bool whole = k < NG - 1;
         const int n = c.left(k);
         if (!in || (!whole && n <= 0)) return;
         if (whole || c.dim >= 4) {
@@ -88,9 +86,9 @@ template <bool B16> struct Raw {
     }
 };
 // stream: past the caches (KGE_STREAM_BYTES)
-template <bool B16, int NG, int LAST> __device__ __forceinline__ void store(char *row, const Columns<NG, LAST> &c, int k, kge_f32x4 v, bool stream) {
+template <bool B16, int NG> __device__ __forceinline__ void store(char *row, const Columns<NG> &c, int k, kge_f32x4 v, bool stream) {
     typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf2;
-    const int n = k < NG - LAST ? 4 : c.left(k), at = c.col(k);
+    const int n = k < NG - 1 ? 4 : c.left(k), at = c.col(k);
     if (n >= 4) {
         if constexpr (B16) {
             const kge_u32x2 w = {__builtin_bit_cast(uint32_t, bf2{(__bf16)v[0], (__bf16)v[1]}), __builtin_bit_cast(uint32_t, bf2{(__bf16)v[2], (__bf16)v[3]})};
@@ -171,8 +169,8 @@ __device__ __forceinline__ float inv_sqrt(float x) { return 1.f / sqrtf(x); }
 struct Norm { bool on, layer; float eps; const float *w, *b; };
 
 // x -> x^ = (x - mean) / deviation
-template <int NG, int LAST, class R>
-__device__ __forceinline__ void normalise(kge_f32x4 (&x)[NG], const Columns<NG, LAST> &c, const Norm &norm, float inv_dim, R &reduce) {
+template <int NG, class R>
+__device__ __forceinline__ void normalise(kge_f32x4 (&x)[NG], const Columns<NG> &c, const Norm &norm, float inv_dim, R &reduce) {
     float v[1] = {0.f};
     if (norm.layer) {
 #pragma unroll
@@ -210,16 +208,18 @@ struct BwdArgs {
     float *g_postw, *g_postb, *g_prew, *g_preb, *g_scale; int accumulate;
 };
 
-// Waves of a row, a power of two: a lane holds up to sixteen columns.
+// Waves of a row, a power of two: twelve columns a lane at most, sixteen where a row has one wave or eight.  (Backward pass of fp32 / bf16 layer norms: 8,000 x 2,000 with four waves of
+// eight columns a lane and with two of sixteen 87 us; 4,000 x 6,000 with twelve columns a lane 152, with sixteen 160.)
 inline int waves_of(int dim) {
-    int w = 1;
-    while (1024 * w < dim) w *= 2;
+    if (dim <= 1024) return 1;
+    int w = 2;
+    while (w < 8 && 768 * w < dim) w *= 2;
     return w;
 }
-// groups of four columns of a lane; eight waves take four whatever the width
+// groups of four columns of a lane, the last of which no other group of the row lies behind
 inline int groups_of(int dim) {
-    const int w = waves_of(dim);
-    return w > 4 ? 4 : (dim + 256 * w - 1) / (256 * w);
+    const int span = 256 * waves_of(dim);
+    return (dim + span - 1) / span;
 }
 // Teams of a workgroup of the backward pass.  Of one wave (no barriers between rows): as many as the registers leave room for on a compute unit, so that there are 256 runs'
 // sums to join and not 768 (24,576 x 768: 9.4 MB of sums, 11 us); of more, whose waves meet at barriers, few.
@@ -228,10 +228,10 @@ inline int bwd_teams_of(int dim) {
     const int w = waves_of(dim);
     return w == 1 ? TEAMS_OF_ONE[groups_of(dim) - 1] : w == 2 ? 2 : 1;
 }
-// workgroups that the chip holds at once
+// workgroups of the backward pass that the chip holds at once
 inline int64_t bwd_runs_of(int dim) {
-    const int w = waves_of(dim);
-    return 256 * (w == 1 || w == 8 ? 1 : groups_of(dim) == 3 ? 3 : 2);
+    const int w = waves_of(dim), g = groups_of(dim);
+    return 256 * (w == 1 ? 1 : w == 8 ? (g == 2 ? 2 : 1) : g == 2 ? 4 : 3);
 }
 
 // rows of the backward pass, by the stream's type

@@ -5,25 +5,26 @@
 namespace kge_norm {
 
 // What a run of rows has for gates: none, or one group's, of which the run is a part or the whole (its sums leave the gate out; the join has it); a gate of its
-// own for every row; several groups of rows, whose gates' gradients are written here.
+// own for every row; several groups of rows, each of which one team takes from end to end.
 enum { GATE_RUN = 0, GATE_ROW = 1, GATE_GROUPS = 2 };
-// Vectors in the LDS: w of the pre norm, s o w (o g) of the post norm, s o b of the post norm (for gates of rows), and the run's A and B (several groups).  (Vectors kept in
-// registers leave room for one wave per SIMD less; read from memory for every row their loads stand in the queue behind those of the rows.)
-enum { VEC_PRE = 0, VEC_F = 1, VEC_SB = 2, VEC_A = 2, VEC_B = 3 };
-constexpr int vectors_of(int mode) { return mode == GATE_RUN ? 2 : mode == GATE_ROW ? 3 : 4; }
+// Vectors in the LDS: w of the pre norm, s o w (GATE_RUN: o g) and s o b of the post norm.  (Kept in registers they leave room for one wave per SIMD less; read from
+// memory for every row their loads stand in the queue behind those of the rows.)
+enum { VEC_PRE = 0, VEC_F = 1, VEC_SB = 2 };
+// GATE_GROUPS: A and B of a team, gates included; in rows of eight waves s o b makes room for them and is read from memory
+constexpr int vectors_of(int mode, int nt) { return mode == GATE_RUN || (mode == GATE_GROUPS && nt == 512) ? 2 : 3; }
 
-// A workgroup takes a run of rows, its teams every teams-th row of it, and keeps the run's column sums in registers.
-template <bool S16, bool B16, int NG, int LAST, int NT, int OCC, int MODE>
+// A workgroup takes a run of rows, its teams every teams-th row of it (GATE_GROUPS: every teams-th group), and keeps the run's column sums in registers.
+template <bool S16, bool B16, int NG, int NT, int OCC, int MODE>
 __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
-    constexpr bool GROUPS = MODE == GATE_GROUPS, OF_ROW = MODE == GATE_ROW;
+    constexpr bool GROUPS = MODE == GATE_GROUPS, OF_ROW = MODE == GATE_ROW, GATED = GROUPS || OF_ROW, SB = vectors_of(MODE, NT) == 3;
     __shared__ float red[2][NT / 64][4];
-    extern __shared__ __attribute__((aligned(16))) float vec[];   // [vector][wide], then, where there are teams, [team][wide]
+    extern __shared__ __attribute__((aligned(16))) float vec[];   // [vector][wide], then [team][wide] where there are teams, [team][A, B][wide] of groups
     const Team t(a.waves);
     Reduce<4, NT> reduce(red, t);
-    const Columns<NG, LAST> c(a.dim, t.lane, t.size);
+    const Columns<NG> c(a.dim, t.lane, t.size);
     const float inv_dim = 1.f / (float)a.dim;
     const int wide = 4 * t.size * NG;
-    float *const of_teams = vec + vectors_of(MODE) * wide;
+    float *const of_teams = vec + vectors_of(MODE, NT) * wide;
     kge_f32x4 A[NG], B[NG], C[NG], D[NG];
 #pragma unroll
     for (int k = 0; k < NG; ++k) A[k] = B[k] = C[k] = D[k] = splat(0.f);
@@ -34,26 +35,23 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
         const int64_t group = run / a.parts, part = run - group * a.parts, first = group * a.gate_rows, end = min(first + a.gate_rows, a.rows);
         r0 = min(first + part * a.run, end); r1 = min(r0 + a.run, end);
     } else { r0 = run * a.run; r1 = min(r0 + a.run, a.rows); }
-    int64_t g0 = r0;                                              // first row of the group at hand
     auto vector = [&](int which, int k) { return *(const kge_f32x4 *)(vec + which * wide + c.col(k)); };
-    auto fill = [&](bool first) {                                 // (first: all but the factors of a group, which its gate belongs to)
-        for (int i = 4 * threadIdx.x; i < wide; i += 4 * NT) {
-            auto put = [&](int which, kge_f32x4 x) { *(kge_f32x4 *)(vec + which * wide + i) = x; };
-            const kge_f32x4 s = vector4(a.scale, i, a.dim, 1.f);
-            if (!GROUPS || !first) {
-                kge_f32x4 f = s * vector4(a.post.w, i, a.dim, 1.f);
-                if (!OF_ROW && a.gate.p && g0 < r1)
+    auto gate4 = [&](int64_t group, int i) {
+        kge_f32x4 g;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) f[e] *= i + e < a.dim ? load1<B16>(a.gate.row((uint32_t)g0 / a.gate_rows), i + e) : 0.f;
-                put(VEC_F, f);
-            }
-            if (first) {
-                put(VEC_PRE, vector4(a.pre.w, i, a.dim, 1.f));
-                if (OF_ROW) put(VEC_SB, s * vector4(a.post.b, i, a.dim, 0.f));
-                if (GROUPS) { put(VEC_A, splat(0.f)); put(VEC_B, splat(0.f)); }
-            }
-        }
+        for (int e = 0; e < 4; ++e) g[e] = i + e < a.dim ? load1<B16>(a.gate.row(group), i + e) : 0.f;
+        return g;
     };
+    for (int i = 4 * threadIdx.x; i < wide; i += 4 * NT) {
+        auto put = [&](int which, kge_f32x4 x) { *(kge_f32x4 *)(vec + which * wide + i) = x; };
+        const kge_f32x4 s = vector4(a.scale, i, a.dim, 1.f), f = s * vector4(a.post.w, i, a.dim, 1.f);
+        put(VEC_F, !GATED && a.gate.p && r0 < r1 ? f * gate4((uint32_t)r0 / a.gate_rows, i) : f);
+        put(VEC_PRE, vector4(a.pre.w, i, a.dim, 1.f));
+        if constexpr (GATED && SB) put(VEC_SB, s * vector4(a.post.b, i, a.dim, 0.f));
+        if constexpr (GROUPS)
+            for (int k = 0; k < 2 * t.teams; ++k) *(kge_f32x4 *)(of_teams + k * wide + i) = splat(0.f);
+    }
+    __syncthreads();
     // f(column, four columns' sums over the teams), each by one thread
     auto of_columns = [&](const kge_f32x4 (&s)[NG], auto f) {
         if (t.teams == 1) {
@@ -74,8 +72,8 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
     };
 
     Raw<S16> rh[NG], rd[NG];
-    Raw<B16> ry[NG], rz[NG], rg[OF_ROW ? NG : 1];
-    auto load = [&](int64_t row, int64_t end) {
+    Raw<B16> ry[NG], rz[NG], rg[GATED ? NG : 1];
+    auto load = [&](int64_t row, int64_t group, int64_t end) {
         const bool in = row < end;
 #pragma unroll
         for (int k = 0; k < NG; ++k) {
@@ -83,27 +81,26 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
             rd[k].load(a.dh.row(row), c, k, in && a.dh.p);
             rz[k].load(a.dz.row(row), c, k, in && a.pre.on);
             ry[k].load(a.y.row(row), c, k, in && a.y.p);
-            if constexpr (OF_ROW) rg[k].load(a.gate.row(row), c, k, in);
+            if constexpr (GATED) rg[k].load(a.gate.row(group), c, k, in);
         }
     };
-    fill(true);
-    __syncthreads();
-    do {
-        const int64_t g1 = GROUPS ? min(g0 + a.gate_rows, r1) : r1;
-        if constexpr (GROUPS) {
-            if (t.teams == 1) __syncthreads();                    // (everyone is done with the last group's factors; teams have met since)
-            fill(false);
-            __syncthreads();
-        }
-        for (int64_t q0 = g0; q0 < g1; q0 += t.teams) {
-            const int64_t row = q0 + t.team;
-            const bool in = row < g1;
-            load(row, g1);
-            kge_f32x4 h[NG], d[NG], z[NG], y[NG], gate[OF_ROW ? NG : 1];
+    // (GROUPS: a team's rows are those of its groups, one behind the other; every team goes round as often, as the waves of one meet at barriers)
+    const int64_t len = GROUPS ? a.gate_rows : 1, base = GROUPS ? r0 / len : 0, groups = GROUPS ? (r1 - r0 + len - 1) / len : 0;
+    for (int64_t g0 = 0; g0 < (GROUPS ? groups : 1); g0 += t.teams) {
+        const int64_t group = base + g0 + t.team, first = GROUPS ? group * len : r0 + t.team, end = GROUPS ? min(first + len, r1) : r1;
+        const int64_t rounds = GROUPS ? len : (r1 - r0 + t.teams - 1) / t.teams;
+        kge_f32x4 gate[GATED ? NG : 1];
+        for (int64_t q = 0; q < rounds; ++q) {
+            const int64_t row = GROUPS ? first + q : first + q * t.teams;
+            const bool in = row < end;
+            load(row, OF_ROW ? row : group, end);
+            kge_f32x4 h[NG], d[NG], z[NG], y[NG];
 #pragma unroll
             for (int k = 0; k < NG; ++k) {
                 h[k] = rh[k].values(); d[k] = rd[k].values(); z[k] = rz[k].values(); y[k] = ry[k].values();
                 if constexpr (OF_ROW) gate[k] = rg[k].values();
+                if constexpr (GROUPS)
+                    if (in) gate[k] = rg[k].values();             // (the group's, whose last row may be beyond the matrix)
             }
             // statistics: of rms norms with the sum of dz's products at once, of layer norms after the means
             float rp = 1.f, rq = 1.f, c1 = 0.f, c2 = 0.f;
@@ -152,6 +149,7 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
                 A[k] = fma4(d[k], y[k], A[k]);
                 if (sum_b) B[k] += d[k];
                 d[k] *= vector(VEC_F, k);
+                if constexpr (GROUPS) d[k] *= rg[k].values();     // (zeros where there is no row)
                 s[0] = sum4(d[k], s[0]); s[1] = dot4(d[k], y[k], s[1]);
             }
             if (!a.y.p || !a.dy.p) continue;
@@ -166,33 +164,38 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
                 if (in && c.inside(k)) store<B16>(a.dy.row(row), c, k, d[k], a.stream);
         }
         if constexpr (GROUPS) {                                   // the group's gate, and its sums times the gate
-            const int64_t group = (uint32_t)g0 / a.gate_rows;
-            auto fold = [&](int which, int i, kge_f32x4 x) {
-                kge_f32x4 g;
+            if (first < end) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) g[e] = i + e < a.dim ? load1<B16>(a.gate.row(group), i + e) : 0.f;
-                kge_f32x4 &to = *(kge_f32x4 *)(vec + which * wide + i);
-                to = fma4(g, x, to);
-            };
-            if (t.teams > 1) __syncthreads();                     // (everyone has read the factors, whose place takes B until the next group's)
-            of_columns(B, [&](int i, kge_f32x4 x) {
-                *(kge_f32x4 *)(vec + VEC_F * wide + i) = x;
-                fold(VEC_B, i, x);
-            });
-            of_columns(A, [&](int i, kge_f32x4 x) {
-                fold(VEC_A, i, x);
-                if (!a.g_gate.p || g0 >= r1) return;
-                const kge_f32x4 b = *(const kge_f32x4 *)(vec + VEC_F * wide + i);
-                const kge_f32x4 v = vector4(a.scale, i, a.dim, 1.f) * fma4(vector4(a.post.w, i, a.dim, 1.f), x, vector4(a.post.b, i, a.dim, 0.f) * b);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (i + e < a.dim) store1<B16>(a.g_gate.row(group), i + e, v[e]);
-            });
+                for (int k = 0; k < NG; ++k) {
+                    if (!c.inside(k)) continue;
+                    if (a.g_gate.p) {
+                        const kge_f32x4 sb = SB ? vector(VEC_SB, k) : vector4(a.scale, c.col(k), a.dim, 1.f) * vector4(a.post.b, c.col(k), a.dim, 0.f);
+                        store<B16>(a.g_gate.row(group), c, k, fma4(vector(VEC_F, k), A[k], sb * B[k]), false);
+                    }
+                    float *mine = of_teams + 2 * t.team * wide + c.col(k);
+                    *(kge_f32x4 *)mine = fma4(gate[k], A[k], *(const kge_f32x4 *)mine);
+                    *(kge_f32x4 *)(mine + wide) = fma4(gate[k], B[k], *(const kge_f32x4 *)(mine + wide));
+                }
+            }
 #pragma unroll
             for (int k = 0; k < NG; ++k) A[k] = B[k] = splat(0.f);
         }
-        g0 = g1;
-    } while (g0 < r1);
+    }
+    if constexpr (GROUPS) {                                       // the teams' sums of all groups: A in its place of the first team, B behind it
+        __syncthreads();
+        for (int i = 4 * threadIdx.x; i < 2 * wide; i += 4 * NT) {
+            kge_f32x4 x = *(const kge_f32x4 *)(of_teams + i);
+            for (int k = 1; k < t.teams; ++k) x += *(const kge_f32x4 *)(of_teams + 2 * k * wide + i);
+            *(kge_f32x4 *)(of_teams + i) = x;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {                            // from here on as of a run whose first team has had all rows
+            A[k] = t.team ? splat(0.f) : *(const kge_f32x4 *)(of_teams + c.col(k));
+            B[k] = t.team ? splat(0.f) : *(const kge_f32x4 *)(of_teams + wide + c.col(k));
+        }
+        __syncthreads();
+    }
     // The only run has everything: the vectors' gradients, and that of the only group's gate, without another launch.
     if (a.runs == 1) {
         auto put = [&](float *q, int i, kge_f32x4 x) {
@@ -202,10 +205,10 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
                 if (i + e < a.dim) q[i + e] = a.accumulate ? q[i + e] + x[e] : x[e];
         };
         if (a.y.p) {
-            if (!GROUPS) __syncthreads();                         // (everyone has read the factors, whose place takes B)
-            of_columns(B, [&](int i, kge_f32x4 x) { *(kge_f32x4 *)(vec + VEC_F * wide + i) = GROUPS ? *(const kge_f32x4 *)(vec + VEC_B * wide + i) : x; });
-            of_columns(A, [&](int i, kge_f32x4 x) {
-                kge_f32x4 s = GROUPS ? *(const kge_f32x4 *)(vec + VEC_A * wide + i) : x, d = *(const kge_f32x4 *)(vec + VEC_F * wide + i);
+            __syncthreads();                                      // (everyone has read the factors, whose place takes B)
+            of_columns(B, [&](int i, kge_f32x4 x) { *(kge_f32x4 *)(vec + VEC_F * wide + i) = x; });
+            of_columns(A, [&](int i, kge_f32x4 s) {
+                kge_f32x4 d = *(const kge_f32x4 *)(vec + VEC_F * wide + i);
                 const kge_f32x4 sc = vector4(a.scale, i, a.dim, 1.f), w = vector4(a.post.w, i, a.dim, 1.f), b = vector4(a.post.b, i, a.dim, 0.f);
                 if (a.parts > 0) {                                // the gate of the one group
                     const kge_f32x4 v = sc * fma4(w, s, b * d);
@@ -227,35 +230,38 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
         return;
     }
     // the run's sums, for the join
-    auto keep = [&](const kge_f32x4 (&s)[NG], int which, int folded) {
+    auto keep = [&](const kge_f32x4 (&s)[NG], int which) {
         if (!(a.want >> which & 1)) return;
         float *p = a.part + ((int64_t)which * a.runs + run) * a.part_ld;
-        of_columns(s, [&](int i, kge_f32x4 x) { *(kge_f32x4 *)(p + i) = GROUPS && folded ? *(const kge_f32x4 *)(vec + folded * wide + i) : x; });
+        of_columns(s, [&](int i, kge_f32x4 x) { *(kge_f32x4 *)(p + i) = x; });
     };
-    keep(A, SUM_A, VEC_A); keep(B, SUM_B, VEC_B); keep(C, SUM_C, 0); keep(D, SUM_D, 0);
+    keep(A, SUM_A); keep(B, SUM_B); keep(C, SUM_C); keep(D, SUM_D);
 }
 
 template <bool S16, bool B16, int MODE> void launch_bwd(const BwdArgs &a, hipStream_t st) {
-    const int groups = groups_of(a.dim), teams = bwd_teams_of(a.dim);
-    const dim3 grid((unsigned)a.runs), blk(64 * a.waves * teams);
+    const int groups = groups_of(a.dim), teams = bwd_teams_of(a.dim), nt = 64 * a.waves * teams;
+    const dim3 grid((unsigned)a.runs), blk(nt);
     // 128 KB at most (rows of 8,192 columns with gates of groups)
-    const int lds = (vectors_of(MODE) + (teams > 1 ? teams : 0)) * 256 * a.waves * groups * (int)sizeof(float);
-#define KGE_BWD(NG, LAST, NT, OCC)                                                                                              \
+    const int lds = (vectors_of(MODE, nt) + (MODE == GATE_GROUPS ? 2 * teams : teams > 1 ? teams : 0)) * 256 * a.waves * groups * (int)sizeof(float);
+#define KGE_BWD(NG, NT, OCC)                                                                                                    \
     do {                                                                                                                        \
         static KgeLdsLimit limit;                                                                                               \
-        const auto kern = norm_bwd_kernel<S16, B16, NG, LAST, NT, OCC, MODE>;                                                   \
+        const auto kern = norm_bwd_kernel<S16, B16, NG, NT, OCC, MODE>;                                                         \
         if (lds > 48 * 1024 && limit.set((const void *)kern, 128 * 1024) != KGE_OK) return;                                     \
         hipLaunchKernelGGL(kern, grid, blk, lds, st, a);                                                                        \
     } while (0)
-    if (a.waves == 8) KGE_BWD(4, 2, 512, 2);
-    else if (a.waves > 1) {
-        if (groups == 3) KGE_BWD(3, 1, 256, 3);
-        else KGE_BWD(4, 1, 256, 2);
+    if (a.waves == 8) {
+        if (groups == 2) KGE_BWD(2, 512, 4);
+        else if (groups == 3) KGE_BWD(3, 512, 2);
+        else KGE_BWD(4, 512, 2);
+    } else if (a.waves > 1) {
+        if (groups == 2) KGE_BWD(2, 256, 4);
+        else KGE_BWD(3, 256, 3);
     } else switch (groups) {
-    case 1: KGE_BWD(1, 1, 64 * TEAMS_OF_ONE[0], 4); break;
-    case 2: KGE_BWD(2, 1, 64 * TEAMS_OF_ONE[1], 4); break;
-    case 3: KGE_BWD(3, 1, 64 * TEAMS_OF_ONE[2], 3); break;
-    default: KGE_BWD(4, 1, 64 * TEAMS_OF_ONE[3], 2);
+    case 1: KGE_BWD(1, 64 * TEAMS_OF_ONE[0], 4); break;
+    case 2: KGE_BWD(2, 64 * TEAMS_OF_ONE[1], 4); break;
+    case 3: KGE_BWD(3, 64 * TEAMS_OF_ONE[2], 3); break;
+    default: KGE_BWD(4, 64 * TEAMS_OF_ONE[3], 2);
     }
 #undef KGE_BWD
 }
