@@ -4,6 +4,10 @@
 //
 // The sums are exact: 8-bit matrix instructions with 32-bit integer accumulators (k <= 131,071 keeps them below 2^31), partial sums of a split contraction too, so the
 // result does not depend on tiles or splits.  The scales are applied once, as the sums leave the accumulators.
+//
+// What bounds it: large products the matrix pipe under the clock that operands which toggle bits leave it (16,384 x 4,096 x 4,096 243 us, 2.26 PFLOP/s; on zeros 200; 4,096 more of k 220 and 162);
+// products of a few hundred tiles the trips to memory of a tile's start and end (24,576 gathered rows x 256 x 768, fp32 output: 18.5 us, of which its bytes are 9); a split contraction the
+// reads from the L2 (768 x 1,024 x 24,576 in five parts: 32.4 us, of them 5 for the launch that adds the parts); one token the weights' bytes or the launch (1 x 4,096 x 1,024 3.4 us).
 #include "lds_copy.hpp"
 #include "text_ops.hpp"
 #include <type_traits>
@@ -373,10 +377,19 @@ template <int MF> __global__ __launch_bounds__(64 * SKINNY_WAVES) void matmul_sk
 }
 
 // ---------------------------------------------------------------------------------------------
-constexpr int SKINNY_GROUPS = 512, SKINNY_WORK = 12, SKINNY_LONG = 4;
+// Which kernel (bf16 output, replayed from a graph, us):
+// sixteen rows of B against 16, 32 or 64 of A per workgroup where there are few such pairs (SKINNY_GROUPS) and each has little to do (SKINNY_WORK: blocks of k per wave times sixteens of rows):
+//   64 x 4,096 x 4,096 12.5 against 14.9 in split tiles and 18.5 in whole ones, 1 x 4,096 x 16,384 16.4 / 23.1 / 54.3, 300 x 300 x 3,000 9.8 / 11.6 / 13.5; more work per pair loses
+//   (64 x 4,096 x 8,192 21.7 / 16.8, 32 x 1,024 x 16,384 23.5 / 16.7); and at up to 16 rows with a short k for any number of pairs (1 x 50,000 x 768 10.2 and 10.9 in tiles; 16 rows 12.6 and 11.7);
+// tiles of 256 x 256 from BIG_TILES of them on: 196 52.9 and 66.2 in tiles of 128 x 128, 121 47.7 and 43.4 (3,584 and 2,816 squared x 4,096).  Eight waves of 128 x 64 each; four of 128 x 128,
+//   which read a quarter less from the LDS, take k = 1,024 105 and not 91, 4,096 254 and not 243, 8,192 449 and not 445 (16,384 x 4,096);
+// tiles of 128 x 128 otherwise, split along k into as many workgroups as there are compute units: 768 x 1,024 x 24,576 32.4 in 5 parts, 51.5 in 2, 34.8 in 10, two per compute unit; 1,000 x 1,000 x 32,768
+//   45.3 in 4, 46.5 in 8.  A split takes blocks of k off a workgroup (0.42 us each) and costs a launch (SPLIT_LAUNCH blocks) and its parts' bytes (SPLIT_MB blocks per MB): 200 x 4,096 x 4,096 20.8
+//   against 18.9 whole, x 6,144 22.2 / 25.9, 300 x 256 x 4,096 11.6 / 15.3, 1,000 x 1,000 x 4,096 21.5 / 19.4.
+constexpr int SKINNY_GROUPS = 512, SKINNY_WORK = 16, SKINNY_LONG = 4;
 constexpr int BIG_TILES = 192;
-constexpr int64_t WANTED = 512;
-constexpr int SPLIT_BLOCKS = 8;
+constexpr int64_t WANTED = 256;
+constexpr int SPLIT_BLOCKS = 8, SPLIT_LAUNCH = 12, SPLIT_MB = 1;
 constexpr int64_t MAX_TILES = 1 << 22;                         // of a launch: a grid has fewer than 2^32 threads
 
 // Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B; waves per SIMD; whether matrices may be 4 GiB and more
@@ -404,12 +417,12 @@ Plan make_plan(int64_t m, int64_t n, int64_t k, size_t room, bool far = false) {
     if (!q.big) tiles = tiles_of(MID, tm, tn);
     q.tiles_m = (int)tm; q.tiles_n = (int)tn;
     q.part_ld = (n + 3) / 4 * 4;
-    if (!q.big && tiles * 4 <= WANTED && kb >= 2 * SPLIT_BLOCKS) {
+    if (!q.big && tiles * 2 <= WANTED && kb >= 2 * SPLIT_BLOCKS) {
         int64_t s = WANTED / tiles;
         if (s > kb / SPLIT_BLOCKS) s = kb / SPLIT_BLOCKS;
         const int64_t one = m * q.part_ld * 4;
         if (s * one > (int64_t)room) s = (int64_t)room / one;
-        if (s > 1) {
+        if (s > 1 && kb - kb / s > SPLIT_LAUNCH + SPLIT_MB * s * one / 1000000) {
             q.kb_per = (int)((kb + s - 1) / s);
             q.splits = (int)((kb + q.kb_per - 1) / q.kb_per);
             q.part_bytes = q.splits * one;

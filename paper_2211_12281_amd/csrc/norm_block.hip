@@ -8,6 +8,11 @@
 //
 // So the backward pass has four column sums at most, whatever is asked for.  A row's statistics are computed again from h and y, which it has to read
 // anyway: nothing is stored between the passes.
+//
+// Memory bounds both: a row is read once, held in registers by one wave (up to 1,024 columns) or several, and its sums stay there for the run of rows that a
+// workgroup takes.  24,576 x 768, layer norms, fp32 stream, bf16 block, gates of 96 rows: forward 42 us (227 MB, 5.4 TB/s), backward 76 (340 MB, 4.5 TB/s) and 10 for the launch
+// that joins the runs' sums, most of it the wait for what the rows' launch has written (behind small calls it takes 4); one row 3.7 us, a launch and three trips to memory.
+// No row is fetched ahead: the registers that it takes are a wave per SIMD (backward with 82, without 77 us; forward 58 and 42).
 #include "norm_block.hpp"
 
 namespace {

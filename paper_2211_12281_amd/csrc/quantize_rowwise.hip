@@ -6,6 +6,8 @@
 // Memory bounds it.  By rows a row of up to 32,768 elements stays in its threads' registers between the search for the largest magnitude and the
 // codes, so x is read once.  By columns the largest magnitudes come first (partial ones for each run of rows, in the workspace), then tiles of 128 x 128 are
 // turned in the LDS: x is read twice.  For both layouts (up to 4,096 columns) the search finds the rows' magnitudes too, and a tile writes both.
+// Up to 512 rows a strip of columns stays in registers and one launch does it.  Measured: by rows 65,536 x 1,024 bf16 35.3 us (201 MB, 5.7 TB/s); by columns 30,000 x 2,048 bf16 63
+// (search 24, scales 4.6, tiles 34); both, 9,999 x 1,001 fp32 24 (27 under the profiler: 9.9, 3.4, 13.4); 30 x 768 by columns 7.5, a launch and the chain from load to store.
 #include "text_ops.hpp"
 
 namespace {
