@@ -385,11 +385,12 @@ template <int MF> __global__ __launch_bounds__(64 * SKINNY_WAVES) void matmul_sk
 //   which read a quarter less from the LDS, take k = 1,024 105 and not 91, 4,096 254 and not 243, 8,192 449 and not 445 (16,384 x 4,096);
 // tiles of 128 x 128 otherwise, split along k into as many workgroups as there are compute units: 768 x 1,024 x 24,576 32.4 in 5 parts, 51.5 in 2, 34.8 in 10, two per compute unit; 1,000 x 1,000 x 32,768
 //   45.3 in 4, 46.5 in 8.  A split takes blocks of k off a workgroup (0.42 us each) and costs a launch (SPLIT_LAUNCH blocks) and its parts' bytes (SPLIT_MB blocks per MB): 200 x 4,096 x 4,096 20.8
-//   against 18.9 whole, x 6,144 22.2 / 25.9, 300 x 256 x 4,096 11.6 / 15.3, 1,000 x 1,000 x 4,096 21.5 / 19.4.
+//   against 18.9 whole, x 6,144 22.2 / 25.9, 300 x 256 x 4,096 11.6 / 15.3, 1,000 x 1,000 x 4,096 21.5 / 19.4.  The launch that adds the parts reads
+//   them one behind the other, so of few tiles a long k has at most sqrt(1.4 k / BLOCK) parts: 100 x 300 x 65,536 24.5 in 24 or 32, 27.5 in 48, 31.8 in 64; 256 x 256 x 24,576 18.5 in 16, 20.4 in 24.
 constexpr int SKINNY_GROUPS = 512, SKINNY_WORK = 16, SKINNY_LONG = 4;
 constexpr int BIG_TILES = 192;
 constexpr int64_t WANTED = 256;
-constexpr int SPLIT_BLOCKS = 8, SPLIT_LAUNCH = 12, SPLIT_MB = 1;
+constexpr int SPLIT_LAUNCH = 12, SPLIT_MB = 1;
 constexpr int64_t MAX_TILES = 1 << 22;                         // of a launch: a grid has fewer than 2^32 threads
 
 // Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B; waves per SIMD; whether matrices may be 4 GiB and more
@@ -417,9 +418,9 @@ Plan make_plan(int64_t m, int64_t n, int64_t k, size_t room, bool far = false) {
     if (!q.big) tiles = tiles_of(MID, tm, tn);
     q.tiles_m = (int)tm; q.tiles_n = (int)tn;
     q.part_ld = (n + 3) / 4 * 4;
-    if (!q.big && tiles * 2 <= WANTED && kb >= 2 * SPLIT_BLOCKS) {
+    if (!q.big && tiles * 2 <= WANTED) {
         int64_t s = WANTED / tiles;
-        if (s > kb / SPLIT_BLOCKS) s = kb / SPLIT_BLOCKS;
+        while (5 * s * s > 7 * kb) s--;
         const int64_t one = m * q.part_ld * 4;
         if (s * one > (int64_t)room) s = (int64_t)room / one;
         if (s > 1 && kb - kb / s > SPLIT_LAUNCH + SPLIT_MB * s * one / 1000000) {
