@@ -5,6 +5,7 @@ stream.  There is no CPU fallback: if the library is missing or a call fails, an
 """
 from __future__ import annotations
 
+import collections
 import contextlib
 import ctypes as C
 import functools
@@ -861,6 +862,15 @@ class Norm:
         self.struct = KgeNormT(code, eps, _vector(weight, self.dim, "weight"), _vector(bias, self.dim, "bias"))
         self.address = C.addressof(self.struct)
 
+    def at(self) -> int:
+        """Address of the struct, with the vectors where they are now (a parameter's storage may have been replaced)."""
+        s, w, b = self.struct, self.weight, self.bias
+        if w is not None and w.data_ptr() != s.weight:
+            s.weight = _vector(w, self.dim, "weight")
+        if b is not None and b.data_ptr() != s.bias:
+            s.bias = _vector(b, self.dim, "bias")
+        return self.address
+
 
 def _like(t, shape, dtype, what: str):
     """(pointer, row stride) of a matrix of this shape and type, or of none."""
@@ -900,7 +910,7 @@ def _block(shape, stream_dtype, block_dtype, post, pre, scale, gate, gate_rows):
         pg, ldg = _like(gate, (-(-rows // gate_rows), dim), block_dtype, "gate (one row for each gate_rows rows)")
     elif gate_rows is not None and gate_rows < 1:
         raise KgeError("gate_rows: one row at least")
-    return KgeNormBlockT(dim, _DTYPE[stream_dtype], _DTYPE[block_dtype], 0, None if post is None else post.address, None if pre is None else pre.address,
+    return KgeNormBlockT(dim, _DTYPE[stream_dtype], _DTYPE[block_dtype], 0, None if post is None else post.at(), None if pre is None else pre.at(),
                          _vector(scale, dim, "scale"), pg, ldg, gate_rows or 0)
 
 
@@ -1087,15 +1097,19 @@ def matmul_rowwise(a: Rowwise, b: Rowwise, rows=None, dtype=torch.bfloat16, out=
     return out
 
 
-class AdamWState:
+class AdamWState(collections.namedtuple("AdamWState", "m v m_scales v_scales")):
     """The moments of one tensor of kge_adamw: fp32 (m, v), or 8-bit codes (uint8, e4m3 and e5m2, padded to a multiple of 128) with a scale byte per 128
-    elements (uint8, padded to a multiple of four)."""
+    elements (uint8, padded to a multiple of four).  They stay the same tensors: what is restored is copied into them."""
+    __slots__ = ()
 
-    def __init__(self, m, v, m_scales=None, v_scales=None):
-        self.m, self.v, self.m_scales, self.v_scales = m, v, m_scales, v_scales
-        self.bits = 32 if m_scales is None else 8
+    def __new__(cls, m, v, m_scales=None, v_scales=None):
         if (m_scales is None) != (v_scales is None):
             raise KgeError("scales: of both moments or of none")
+        return super().__new__(cls, m, v, m_scales, v_scales)
+
+    @property
+    def bits(self) -> int:
+        return 32 if self.m_scales is None else 8
 
     @staticmethod
     def zeros(n: int, bits: int = 32, device="cuda"):
@@ -1113,31 +1127,41 @@ class AdamW:
     moments (another tag for each AdamW of a program)."""
 
     def __init__(self, params, states=None, shadows=None, bits=32, weight_decay=0.01, seed: int = 0, tag: int = 0):
-        self.params = list(params)
+        self.params = tuple(params)
         k = len(self.params)
         each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * k       # noqa: E731
-        self.states = [AdamWState.zeros(p.numel(), b, p.device) for p, b in zip(self.params, each(bits), strict=True)] if states is None else list(states)
-        self.shadows = [None] * k if shadows is None else list(shadows)
-        decays = each(weight_decay)
-        if not len(self.states) == len(self.shadows) == len(decays) == k:
+        self.states = tuple(AdamWState.zeros(p.numel(), b, p.device) for p, b in zip(self.params, each(bits), strict=True)) if states is None else tuple(states)
+        self.shadows = (None,) * k if shadows is None else tuple(shadows)
+        self.decays = each(weight_decay)
+        if not len(self.states) == len(self.shadows) == len(self.decays) == k:
             raise KgeError("states, shadows and weight_decay: one for each tensor")
         if not 0 <= seed < 1 << 64 or not 0 <= tag < 1 << 32:
             raise KgeError("seed: 64 bits, tag: 32 bits")
-        self.seed, self.tag, self.sizes, self.dev = seed, tag, [p.numel() for p in self.params], None
-        self.structs = (KgeAdamwTensorT * max(k, 1))()
-        for s, p, st, sh, wd, n in zip(self.structs, self.params, self.states, self.shadows, decays, self.sizes):
+        self.seed, self.tag, self.sizes = seed, tag, [p.numel() for p in self.params]
+        self.dev = self.params[0].get_device() if k else None
+        self.moving = [*self.params, *(s for s in self.shadows if s is not None)]
+        self._lay_out()
+
+    def _lay_out(self):
+        """The structs of all tensors, where they are now."""
+        self.structs = (KgeAdamwTensorT * max(len(self.params), 1))()
+        written = []
+        for s, p, st, sh, wd, n in zip(self.structs, self.params, self.states, self.shadows, self.decays, self.sizes):
             nb = -(-n // 128)
             want = (n, n, torch.float32) if st.bits == 32 else (128 * nb, -(-nb // 4) * 4, torch.uint8)
-            dev = p.get_device()
-            if p.dtype != torch.float32 or not p.is_contiguous() or dev < 0 or (self.dev is not None and dev != self.dev):
+            if p.dtype != torch.float32 or p.numel() != n or not p.is_contiguous() or p.get_device() != self.dev or self.dev < 0:
                 raise KgeError(f"params: contiguous fp32 tensors of one GPU are wanted, got {p.dtype} {tuple(p.shape)} on {p.device}")
-            self.dev = dev
             for t, size, dt in ((st.m, want[0], want[2]), (st.v, want[0], want[2]), (st.m_scales, want[1], torch.uint8), (st.v_scales, want[1], torch.uint8),
                                 (sh, n, torch.bfloat16)):
-                if t is not None and (t.dtype != dt or t.numel() != size or not t.is_contiguous() or t.get_device() != dev):
+                if t is not None and (t.dtype != dt or t.numel() != size or not t.is_contiguous() or t.get_device() != self.dev):
                     raise KgeError(f"moments and shadows: {size} contiguous {dt} on {p.device} are wanted, got {t.dtype} {tuple(t.shape)} on {t.device}")
             s.param_f32, s.param_bf16, s.state_bits, s.n, s.weight_decay = p.data_ptr(), _ptr(sh), st.bits, n, wd
             s.m, s.v, s.m_scales, s.v_scales = st.m.data_ptr(), st.v.data_ptr(), _ptr(st.m_scales), _ptr(st.v_scales)
+            written += [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in (p, *st, sh) if t is not None and t.numel() > 0]
+        written.sort()
+        if any(a[1] > b[0] for a, b in zip(written, written[1:])):
+            raise KgeError("params, moments and shadows overlap: a tensor that several names share is given once")
+        self.where = [t.data_ptr() for t in self.moving]
 
     def step(self, grads, lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale=None, step_counter=None,
              stream=None):
@@ -1152,6 +1176,8 @@ class AdamW:
             raise KgeError(f"the tensors are on cuda:{self.dev}, the current device is cuda:{dev}")
         if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
             raise KgeError("grad_scale: one fp32 number on the GPU")
+        if [t.data_ptr() for t in self.moving] != self.where:                     # (a parameter's storage has been replaced)
+            self._lay_out()
         arr = (KgeAdamwTensorT * len(grads)).from_buffer_copy(self.structs)       # (of this call: two may run at once)
         for s, g, n in zip(arr, grads, self.sizes):
             dt = _DTYPE.get(g.dtype)

@@ -227,8 +227,8 @@ __global__ __launch_bounds__(NT) void adamw_kernel(const Args a) {
         }
         moments(a, g[k], m[k], v[k]);
         // With 8-bit moments the vector pipe is nearly as busy as memory: root and reciprocal from one instruction each, 2^-23 of themselves off (89M elements
-        // 339 -> 301 us).  (The root of a subnormal number is 0 there: only beside an eps that does not mind.)
-        if (state8 && a.eps >= 1e-15f) {
+        // 339 -> 301 us).  (The root of a subnormal number, below 1.1e-19, is 0 there: only beside an eps that it does not change.)
+        if (state8 && a.eps >= 1e-12f) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 p[k][e] = p[k][e] * t.keep - a.lr * (m[k][e] * c1) * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[k][e] * c2) + a.eps);

@@ -295,3 +295,31 @@ def test_the_binding_refuses():
         with pytest.raises(kge.KgeError):
             bad()
     kge.AdamW([]).step([], 1e-3, 1)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_replaced_storage_is_found(bits):
+    """A parameter whose storage has been replaced (p.data = ...) is updated where it is now, and its old storage left alone."""
+    first = torch.linspace(-1, 1, 300, device="cuda")
+    grad = torch.linspace(1, 2, 300, device="cuda")
+    got, want = first.clone(), first.clone()
+    shadow = [torch.zeros(300, dtype=BF16, device="cuda") for _ in range(2)]
+    moved, still = kge.AdamW([got], bits=bits, shadows=shadow[:1]), kge.AdamW([want], bits=bits, shadows=shadow[1:])
+    for step in (1, 2, 3):
+        old = got.data
+        kept = old.clone()
+        got.data, shadow[0].data = old.clone(), torch.zeros_like(shadow[0])
+        moved.step([grad], 1e-2, step)
+        still.step([grad], 1e-2, step)
+        assert torch.equal(got, want) and torch.equal(old, kept) and torch.equal(*shadow) and not torch.equal(got, kept)
+
+
+def test_shared_tensors_are_refused():
+    p = torch.zeros(1000, device="cuda")
+    st = kge.AdamWState.zeros(1000)
+    for bad in [lambda: kge.AdamW([p, p]), lambda: kge.AdamW([p[:600], p[500:]]), lambda: kge.AdamW([p, p.clone()], [st, st]), lambda: kge.AdamW([p], [kge.AdamWState(st.m, st.m)]),
+                lambda: kge.AdamW([p], [kge.AdamWState(p, st.v)]), lambda: kge.AdamW([p], shadows=[p[:500].view(BF16)])]:
+        with pytest.raises(kge.KgeError, match="overlap"):
+            bad()
+    kge.AdamW([p[:500], p[500:], torch.zeros(0, device="cuda"), torch.zeros(0, device="cuda")]).step([p[:500] + 1, p[500:] + 1, p[:0], p[:0]], 1e-3, 1)
+    assert bool((p < 0).all())

@@ -407,3 +407,18 @@ def test_the_binding_refuses():
         kge.Norm("batch")
     with pytest.raises(kge.KgeError):
         kge.norm_block(torch.zeros((1, 8193), device="cuda"), pre=kge.Norm())
+
+
+def test_replaced_storage_is_found():
+    """A norm's weight and bias are read where they are at the call (weight.data = ... replaces the storage)."""
+    x, w, b = torch.randn(40, 96, device="cuda"), torch.randn(96, device="cuda"), torch.randn(96, device="cuda")
+    n = kge.Norm("layer", w, b)
+    kge.norm_block(x, pre=n)
+    w.data, b.data = torch.randn(96, device="cuda"), torch.randn(96, device="cuda")
+    fresh = kge.Norm("layer", w.clone(), b.clone())
+    assert torch.equal(kge.norm_block(x, pre=n)[1], kge.norm_block(x, pre=fresh)[1])
+    g, f = (kge.norm_block_bwd(x, dz=x, pre=k) for k in (n, fresh))
+    assert all(torch.equal(g[k], f[k]) for k in ("x", "pre_weight", "pre_bias"))
+    w.data = torch.randn(95, device="cuda")
+    with pytest.raises(kge.KgeError):
+        kge.norm_block(x, pre=n)
