@@ -94,12 +94,12 @@ __device__ __forceinline__ kge_f32x4 scales4(const MatmulArgs &p, int64_t col) {
 // (16,384 x 4,096 x 4,096: 268 us).  The copies are issued over half a stage, as fast as the address unit takes them.
 //
 // FAR: a copy's lanes have 64-bit addresses; else (codes of less than 4 GiB) a base and 32-bit offsets.
-template <int WM, int WN, int NJ, int NI, int OCC, bool FAR, bool GATHERED>
+template <int WM, int WN, int NJ, int NI, int NST, int OCC, bool FAR, bool GATHERED>
 __global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(OCC, OCC)))
 void matmul_tiles_kernel(const MatmulArgs p) {
     constexpr int NW = WM * WN, TM = 32 * NJ * WM, TN = 32 * NI * WN, ROWS = TM + TN, CP = ROWS / 8 / NW;      // copies of a wave per stage
-    constexpr int NST = 2, STAGE = ROWS * BLOCK, SLOTS = NI * NJ, FRAGS = NI + NJ;
-    static_assert(ROWS % (8 * NW) == 0 && CP < 64 && NST * STAGE <= 160 * 1024, "tile");
+    constexpr int STAGE = ROWS * BLOCK, SLOTS = NI * NJ, FRAGS = NI + NJ;
+    static_assert(ROWS % (8 * NW) == 0 && NST * CP < 64 && (NST & (NST - 1)) == 0 && NST * STAGE <= 160 * 1024, "tile");
     __shared__ __attribute__((aligned(16))) char lds[NST * STAGE];
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 31, g = lane >> 5;
@@ -172,6 +172,7 @@ void matmul_tiles_kernel(const MatmulArgs p) {
     static_assert(READS * SLOTS >= 2 * FRAGS && FREE + GAP * (CP - 1) < 4 * SLOTS, "slots");
     // What stands behind each product keeps its place (the compiler would put all reads in front of all products).
     auto stage = [&](int P) {
+        const int Q = (P + 1) & (NST - 1);
 #pragma unroll
         for (int st = 0; st < 4; ++st)
 #pragma unroll
@@ -184,7 +185,7 @@ void matmul_tiles_kernel(const MatmulArgs p) {
                         __syncthreads();                                          // everyone has this stage's fragments: its place takes the stage after the next
                     }
                     if (t == 2 * SLOTS) {
-                        kge_wait_vmcnt<ISSUED>();
+                        kge_wait_vmcnt<ISSUED + (NST - 2) * CP>();
                         __syncthreads();                                          // the next stage has landed for everyone
                     }
                     acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f[set][i], f[set][NI + j], acc[i][j], 0, 0, 0);
@@ -193,8 +194,8 @@ void matmul_tiles_kernel(const MatmulArgs p) {
                     for (int u = 0; u < READS; ++u) {
                         const int r = READS * (t % SLOTS) + u;
                         if (st == 0 && r < FRAGS) read(P, 3 * FRAGS + r);
-                        if (st == 2 && r < 2 * FRAGS) read(P ^ 1, r);             // (the fragments of steps that are over)
-                        if (st == 3 && r < FRAGS) read(P ^ 1, 2 * FRAGS + r);
+                        if (st == 2 && r < 2 * FRAGS) read(Q, r);                 // (the fragments of steps that are over)
+                        if (st == 3 && r < FRAGS) read(Q, 2 * FRAGS + r);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -208,11 +209,11 @@ void matmul_tiles_kernel(const MatmulArgs p) {
             for (int c = 0; c < CP; ++c) copy(s, c);
             advance();
         }
-        kge_wait_vmcnt<CP>();
+        kge_wait_vmcnt<(NST - 1) * CP>();
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < 3 * FRAGS; ++r) read(0, r);
-        for (int kb = kb0; kb < kb1; ++kb) stage((kb - kb0) & 1);
+        for (int kb = kb0; kb < kb1; ++kb) stage((kb - kb0) & (NST - 1));
         kge_wait_vmcnt<0>();                                                      // no copy may be in flight when the LDS is released
     }
 
@@ -387,15 +388,18 @@ template <int MF> __global__ __launch_bounds__(64 * SKINNY_WAVES) void matmul_sk
 //   45.3 in 4, 46.5 in 8.  A split takes blocks of k off a workgroup (0.42 us each) and costs a launch (SPLIT_LAUNCH blocks) and its parts' bytes (SPLIT_MB blocks per MB): 200 x 4,096 x 4,096 20.8
 //   against 18.9 whole, x 6,144 22.2 / 25.9, 300 x 256 x 4,096 11.6 / 15.3, 1,000 x 1,000 x 4,096 21.5 / 19.4.  The launch that adds the parts reads
 //   them one behind the other, so of few tiles a long k has at most sqrt(1.4 k / BLOCK) parts: 100 x 300 x 65,536 24.5 in 24 or 32, 27.5 in 48, 31.8 in 64; 256 x 256 x 24,576 18.5 in 16, 20.4 in 24.
+// A workgroup that has its compute unit to itself takes a ring of four stages from DEEP_BLOCKS blocks on: 1,500 x 1,500 x 16,384 53.4 against 61.1 with two, 1,000 x 1,000 x 4,096 17.3 / 19.4, 768 x 1,024 x 24,576
+//   33.1 / 33.5 (a workgroup per compute unit reads 12 TB/s from the L2s by then); 100 x 1,000 x 6,000 in eight blocks each 13.7 / 13.4, 2,000 x 2,000 x 256 7.5 / 7.0.
 constexpr int SKINNY_GROUPS = 512, SKINNY_WORK = 16, SKINNY_LONG = 4;
 constexpr int BIG_TILES = 192;
-constexpr int64_t WANTED = 256;
+constexpr int64_t CUS = 256;
 constexpr int SPLIT_LAUNCH = 12, SPLIT_MB = 1;
+constexpr int DEEP_BLOCKS = 16;
 constexpr int64_t MAX_TILES = 1 << 22;                         // of a launch: a grid has fewer than 2^32 threads
 
 // Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B; waves per SIMD; whether matrices may be 4 GiB and more
-struct Tile { int wm, wn, nj, ni, occ; bool far; };
-constexpr Tile BIG = {2, 4, 4, 2, 2, false}, MID = {2, 2, 2, 2, 2, true};
+struct Tile { int wm, wn, nj, ni, stages, occ; bool far; };
+constexpr Tile BIG = {2, 4, 4, 2, 2, 2, false}, MID = {2, 2, 2, 2, 2, 2, true}, DEEP = {2, 2, 2, 2, 4, 1, true};
 constexpr int tile_m(const Tile &t) { return 32 * t.wm * t.nj; }
 constexpr int tile_n(const Tile &t) { return 32 * t.wn * t.ni; }
 
@@ -418,8 +422,8 @@ Plan make_plan(int64_t m, int64_t n, int64_t k, size_t room, bool far = false) {
     if (!q.big) tiles = tiles_of(MID, tm, tn);
     q.tiles_m = (int)tm; q.tiles_n = (int)tn;
     q.part_ld = (n + 3) / 4 * 4;
-    if (!q.big && tiles * 2 <= WANTED) {
-        int64_t s = WANTED / tiles;
+    if (!q.big && tiles * 2 <= CUS) {
+        int64_t s = CUS / tiles;
         while (5 * s * s > 7 * kb) s--;
         const int64_t one = m * q.part_ld * 4;
         if (s * one > (int64_t)room) s = (int64_t)room / one;
@@ -442,8 +446,9 @@ void launch(const MatmulArgs &p, const Plan &q, hipStream_t st) {
     }
     const dim3 grid((unsigned)((p.tiles_m * p.tiles_n * p.splits + 7) / 8 * 8));
 #define KGE_TILES(T, GATHERED) \
-    hipLaunchKernelGGL((matmul_tiles_kernel<T.wm, T.wn, T.nj, T.ni, T.occ, T.far, GATHERED>), grid, dim3(64 * T.wm * T.wn), 0, st, p)
+    hipLaunchKernelGGL((matmul_tiles_kernel<T.wm, T.wn, T.nj, T.ni, T.stages, T.occ, T.far, GATHERED>), grid, dim3(64 * T.wm * T.wn), 0, st, p)
     if (q.big) { if (p.rows) KGE_TILES(BIG, true); else KGE_TILES(BIG, false); }
+    else if (p.tiles_m * p.tiles_n * p.splits <= CUS && p.kb_per >= DEEP_BLOCKS) { if (p.rows) KGE_TILES(DEEP, true); else KGE_TILES(DEEP, false); }
     else { if (p.rows) KGE_TILES(MID, true); else KGE_TILES(MID, false); }
 #undef KGE_TILES
     if (p.part) {

@@ -194,6 +194,23 @@ def test_matmul_gathered_accumulated_strided(dt, m, n, k, pad):
     _equal(kge.matmul_rowwise(a, _cuda(b, k), rows=rows.cuda(), dtype=dt), _product(table, b, rows).to(dt))
 
 
+@pytest.mark.parametrize("k", [1921, 2048, 2100, 2300, 2432, 2433, 3900, 4096, 6200, 20_001])
+def test_matmul_of_a_workgroup_per_compute_unit(k):
+    """Tiles that have a compute unit each, contractions of every length in blocks modulo the ring, whole and split; gathered rows too."""
+    m, n = 700, 900
+    a, b = _matrix(m, k, 16), _matrix(n, k, 17)
+    rows = torch.from_numpy(_rng(18, k).integers(-1, m + 1, size=1300).astype(np.int32))
+    qa, qb = _cuda(a, k), _cuda(b, k)
+    sums = a[0].cuda().double() @ b[0].cuda().double().t()
+    want = (sums.float() * a[1].cuda().unsqueeze(1) * b[1].cuda()).cpu()
+    got = kge.matmul_rowwise(qa, qb, dtype=F32)
+    _equal(got, want)
+    _equal(kge.matmul_rowwise(qa, qb, dtype=BF16), want.to(BF16))
+    live = (rows >= 0) & (rows < m)
+    taken = torch.where(live.unsqueeze(1), want[rows.clamp(0, m - 1).long()], torch.zeros(()))
+    _equal(kge.matmul_rowwise(qa, qb, rows=rows.cuda(), dtype=F32), taken)
+
+
 @pytest.mark.parametrize("m,n", [(3, 20), (200, 130), (2100, 2000)])
 def test_sums_reach_the_end_of_32_bits(m, n):
     """The longest contraction of the largest codes."""
