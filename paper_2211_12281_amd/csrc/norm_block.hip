@@ -24,13 +24,13 @@ using namespace kge_norm;
 // ---------------------------------------------------------------------------------------------
 // A team takes a row at a time; the vectors stand in the LDS (rows of more than 4,096 columns: in memory).
 enum { VEC_POST = 0, VEC_POST_BIAS = 1, VEC_SCALE = 2, VEC_PRE = 3, VEC_PRE_BIAS = 4, VECTORS = 5 };
-template <bool S16, bool B16, int NG, int NT, int OCC>
+template <bool S16, bool B16, int NG, int SUB, int NT, int OCC>
 __global__ __launch_bounds__(NT, OCC) void norm_fwd_kernel(const FwdArgs a) {
     constexpr bool LDS = NT == 256;
     __shared__ float red[2][NT / 64][1];
     extern __shared__ __attribute__((aligned(16))) float vec[];
-    const Team t(a.waves);
-    Reduce<1, NT> reduce(red, t);
+    const Team<SUB> t(a.waves);
+    Reduce<1, NT, SUB> reduce(red, t);
     const Columns<NG> c(a.dim, t.lane, t.size);
     const float inv_dim = 1.f / (float)a.dim;
     const int wide = 4 * t.size * NG;
@@ -272,33 +272,36 @@ Runs runs_of(const kge_norm_block_t *b, int64_t rows) {
 // No call of up to so many rows has more runs: without gates and with whole groups at most `wanted`; else there are fewer than wanted teams / 2 groups, and groups parts runs, parts at
 // most wanted / groups + 2 (3 where there are more groups than that): fewer than wanted + 3 wanted teams / 2; and as a run of a whole group has a row, fewer than 2 rows.
 int64_t most_runs(const kge_norm_block_t *b, int64_t rows) {
-    const int64_t all = bwd_runs_of(b->dim) * (2 * bwd_teams_of(b->dim) + 3);
+    const int64_t all = bwd_runs_of(b->dim) * (b->gate && b->gate_rows > 1 ? 2 * bwd_teams_of(b->dim) + 3 : 1);
     return 2 * rows < all ? 2 * rows : all;
 }
 int64_t part_ld_of(int dim) { return (dim + JC - 1) / JC * JC; }
 
 template <bool S16, bool B16> void launch_fwd(const FwdArgs &a, hipStream_t st) {
-    const int teams = a.waves < 4 ? 4 / a.waves : 1, ng = groups_of(a.dim);
+    const int lanes = fwd_lanes_of(a.dim), teams = lanes < 256 ? 256 / lanes : 1, ng = groups_of(a.dim, lanes);
     int64_t groups = (a.rows + teams - 1) / teams;
     if (groups > FWD_GROUPS) groups = FWD_GROUPS;
-    const dim3 grid((unsigned)groups), blk(64 * a.waves * teams);
-    const int lds = a.waves <= 4 ? VECTORS * 256 * a.waves * ng * (int)sizeof(float) : 0;                   // 80 KB at most
-#define KGE_FWD(NG, NT, OCC)                                                                                                    \
+    const dim3 grid((unsigned)groups), blk(lanes * teams);
+    const int lds = a.waves <= 4 ? VECTORS * 4 * lanes * ng * (int)sizeof(float) : 0;                   // 80 KB at most
+#define KGE_FWD(NG, SUB, NT, OCC)                                                                                                    \
     do {                                                                                                                        \
         static KgeLdsLimit limit;                                                                                               \
-        const auto kern = norm_fwd_kernel<S16, B16, NG, NT, OCC>;                                                               \
+        const auto kern = norm_fwd_kernel<S16, B16, NG, SUB, NT, OCC>;                                                               \
         if (lds > 48 * 1024 && limit.set((const void *)kern, 80 * 1024) != KGE_OK) return;                                      \
         hipLaunchKernelGGL(kern, grid, blk, lds, st, a);                                                                        \
     } while (0)
     if (a.waves == 8) {
-        if (ng == 2) KGE_FWD(2, 512, 4);
-        else if (ng == 3) KGE_FWD(3, 512, 4);
-        else KGE_FWD(4, 512, 2);
+        if (ng == 2) KGE_FWD(2, 64, 512, 4);
+        else if (ng == 3) KGE_FWD(3, 64, 512, 4);
+        else KGE_FWD(4, 64, 512, 2);
+    } else if (lanes == 16) {
+        if (ng == 1) KGE_FWD(1, 16, 256, 8);
+        else KGE_FWD(2, 16, 256, 8);
     } else switch (ng) {
-    case 1: KGE_FWD(1, 256, 8); break;
-    case 2: KGE_FWD(2, 256, 6); break;
-    case 3: KGE_FWD(3, 256, 5); break;
-    default: KGE_FWD(4, 256, 4);
+    case 1: KGE_FWD(1, 64, 256, 8); break;
+    case 2: KGE_FWD(2, 64, 256, 6); break;
+    case 3: KGE_FWD(3, 64, 256, 5); break;
+    default: KGE_FWD(4, 64, 256, 4);
     }
 #undef KGE_FWD
 }

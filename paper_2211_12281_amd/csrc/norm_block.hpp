@@ -113,21 +113,38 @@ template <bool B16> __device__ __forceinline__ void store1(void *row, int64_t co
     else ((float *)row)[col] = v;
 }
 
-// A workgroup's waves in teams of `waves`, each of which holds a row
-struct Team {
+// A workgroup's threads in teams, each of which holds a row: of `waves` waves, or (SUB < 64) of SUB lanes of a wave
+template <int SUB> struct Team {
     int waves, size, teams, team, lane;
     __device__ __forceinline__ explicit Team(int w) {
+        if constexpr (SUB < 64) {
+            waves = 1; size = SUB; teams = (int)blockDim.x / SUB;
+            team = (int)threadIdx.x / SUB; lane = (int)threadIdx.x % SUB;
+            return;
+        }
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         waves = w; size = 64 * w; teams = max(1, (int)(blockDim.x >> 6) / w);
         team = wave / w; lane = (int)threadIdx.x - team * size;
     }
 };
 
-__device__ __forceinline__ float wave_sum(float x) {
+// x of the lanes 16 (32) further on, or back, added: rows 0 and 1, 2 and 3 of sixteen lanes (halves of the wave) change places
+__device__ __forceinline__ float add_16(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float add_32(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// sum over the SUB lanes of a team (64: over the wave), for all of them
+template <int SUB> __device__ __forceinline__ float wave_sum(float x) {
     x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0xB1, 0xf, 0xf, true));      // lane ^ 1
     x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x4E, 0xf, 0xf, true));      // lane ^ 2
     x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x141, 0xf, 0xf, true));     // 7 - lane
     x += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x140, 0xf, 0xf, true));     // 15 - lane
+    if constexpr (SUB == 16) return x;
+    if constexpr (SUB == 32) return add_16(x);
     const int b = (int)__float_as_uint(x);
     const float s0 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(b, 0)), s1 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(b, 16));
     const float s2 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(b, 32)), s3 = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(b, 48));
@@ -136,16 +153,16 @@ __device__ __forceinline__ float wave_sum(float x) {
 
 // Sums of N values over the threads of a team, for all of them.  Two places in turn: who writes to one again has passed the barrier of the sums in
 // between, behind which nobody reads it any more.  (Teams of one wave need no barrier, and go round as they like.)
-template <int K, int NT> struct Reduce {
+template <int K, int NT, int SUB> struct Reduce {
     float (&lds)[2][NT / 64][K];
-    const Team &t;
+    const Team<SUB> &t;
     int place = 0;
-    __device__ __forceinline__ Reduce(float (&l)[2][NT / 64][K], const Team &team) : lds(l), t(team) {}
+    __device__ __forceinline__ Reduce(float (&l)[2][NT / 64][K], const Team<SUB> &team) : lds(l), t(team) {}
     template <int N> __device__ __forceinline__ void operator()(float (&v)[N]) {
         static_assert(N <= K, "sums at once");
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
-        if (t.waves == 1) return;
+        for (int i = 0; i < N; ++i) v[i] = wave_sum<SUB>(v[i]);
+        if (SUB < 64 || t.waves == 1) return;
         const int wave = (int)threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0) {
 #pragma unroll
@@ -216,22 +233,24 @@ inline int waves_of(int dim) {
     while (w < 8 && 768 * w < dim) w *= 2;
     return w;
 }
+// Lanes of a row: narrow ones share a wave, whose sums over lanes then serve two or four of them.  Layer norms, fp32 / bf16, 25.6M elements, shared and one row per
+// wave: forward 64 columns 62 and 167 us, 128 64 and 93 (256 68 and 62: not shared); backward 64 104 and 315, 128 82 and 181, 256 84 and 112.
+inline int bwd_lanes_of(int dim) { return dim <= 128 ? 16 : dim <= 256 ? 32 : 64 * waves_of(dim); }
+inline int fwd_lanes_of(int dim) { return dim <= 128 ? 16 : 64 * waves_of(dim); }
 // groups of four columns of a lane, the last of which no other group of the row lies behind
-inline int groups_of(int dim) {
-    const int span = 256 * waves_of(dim);
-    return (dim + span - 1) / span;
-}
+inline int groups_of(int dim, int lanes) { return (dim + 4 * lanes - 1) / (4 * lanes); }
 // Teams of a workgroup of the backward pass.  Of one wave (no barriers between rows): as many as the registers leave room for on a compute unit, so that there are 256 runs'
 // sums to join and not 768 (24,576 x 768: 9.4 MB of sums, 11 us); of more, whose waves meet at barriers, few.
-constexpr int TEAMS_OF_ONE[4] = {16, 16, 12, 8};
+// (Narrow rows have short sums: four workgroups per compute unit.)
+constexpr int TEAMS_OF_ONE[3] = {16, 12, 8}, NARROW_THREADS = 256;    // (of two, three, four groups)
 inline int bwd_teams_of(int dim) {
-    const int w = waves_of(dim);
-    return w == 1 ? TEAMS_OF_ONE[groups_of(dim) - 1] : w == 2 ? 2 : 1;
+    const int w = waves_of(dim), lanes = bwd_lanes_of(dim);
+    return lanes < 64 ? NARROW_THREADS / lanes : w == 1 ? TEAMS_OF_ONE[groups_of(dim, lanes) - 2] : w == 2 ? 2 : 1;
 }
 // workgroups of the backward pass that the chip holds at once
 inline int64_t bwd_runs_of(int dim) {
-    const int w = waves_of(dim), g = groups_of(dim);
-    return 256 * (w == 1 ? 1 : w == 8 ? (g == 2 ? 2 : 1) : g == 2 ? 4 : 3);
+    const int w = waves_of(dim), lanes = bwd_lanes_of(dim), g = groups_of(dim, lanes);
+    return 256 * (lanes < 64 ? 4 : w == 1 ? 1 : w == 8 ? (g == 2 ? 2 : 1) : g == 2 ? 4 : 3);
 }
 
 // rows of the backward pass, by the stream's type

@@ -14,13 +14,13 @@ enum { VEC_PRE = 0, VEC_F = 1, VEC_SB = 2 };
 constexpr int vectors_of(int mode, int nt) { return mode == GATE_RUN || (mode == GATE_GROUPS && nt == 512) ? 2 : 3; }
 
 // A workgroup takes a run of rows, its teams every teams-th row of it (GATE_GROUPS: every teams-th group), and keeps the run's column sums in registers.
-template <bool S16, bool B16, int NG, int NT, int OCC, int MODE>
+template <bool S16, bool B16, int NG, int SUB, int NT, int OCC, int MODE>
 __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
     constexpr bool GROUPS = MODE == GATE_GROUPS, OF_ROW = MODE == GATE_ROW, GATED = GROUPS || OF_ROW, SB = vectors_of(MODE, NT) == 3;
     __shared__ float red[2][NT / 64][4];
     extern __shared__ __attribute__((aligned(16))) float vec[];   // [vector][wide], then [team][wide] where there are teams, [team][A, B][wide] of groups
-    const Team t(a.waves);
-    Reduce<4, NT> reduce(red, t);
+    const Team<SUB> t(a.waves);
+    Reduce<4, NT, SUB> reduce(red, t);
     const Columns<NG> c(a.dim, t.lane, t.size);
     const float inv_dim = 1.f / (float)a.dim;
     const int wide = 4 * t.size * NG;
@@ -48,24 +48,34 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
         put(VEC_F, !GATED && a.gate.p && r0 < r1 ? f * gate4((uint32_t)r0 / a.gate_rows, i) : f);
         put(VEC_PRE, vector4(a.pre.w, i, a.dim, 1.f));
         if constexpr (GATED && SB) put(VEC_SB, s * vector4(a.post.b, i, a.dim, 0.f));
-        if constexpr (GROUPS)
-            for (int k = 0; k < 2 * t.teams; ++k) *(kge_f32x4 *)(of_teams + k * wide + i) = splat(0.f);
     }
+    if constexpr (GROUPS)
+        for (int i = 4 * threadIdx.x; i < 2 * t.teams * wide; i += 4 * NT) *(kge_f32x4 *)(of_teams + i) = splat(0.f);
     __syncthreads();
     // f(column, four columns' sums over the teams), each by one thread
-    auto of_columns = [&](const kge_f32x4 (&s)[NG], auto f) {
-        if (t.teams == 1) {
+    auto of_columns = [&](kge_f32x4 (&s)[NG], auto f) {
+        if (SUB == 64 && t.teams == 1) {
 #pragma unroll
             for (int k = 0; k < NG; ++k)
                 if (c.inside(k)) f(c.col(k), s[k]);
             return;
         }
+        int teams = t.teams, team = t.team;
+        if constexpr (SUB < 64) {                                 // those of a wave first
 #pragma unroll
-        for (int k = 0; k < NG; ++k) *(kge_f32x4 *)(of_teams + t.team * wide + c.col(k)) = s[k];
+            for (int k = 0; k < NG; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[k][e] = add_32(SUB == 16 ? add_16(s[k][e]) : s[k][e]);
+            teams = NT / 64; team = threadIdx.x / 64;
+        }
+        if (SUB == 64 || (threadIdx.x & 63) < SUB) {
+#pragma unroll
+            for (int k = 0; k < NG; ++k) *(kge_f32x4 *)(of_teams + team * wide + c.col(k)) = s[k];
+        }
         __syncthreads();
         for (int i = 4 * threadIdx.x; i < a.dim; i += 4 * NT) {
             kge_f32x4 x = *(const kge_f32x4 *)(of_teams + i);
-            for (int k = 1; k < t.teams; ++k) x += *(const kge_f32x4 *)(of_teams + k * wide + i);
+            for (int k = 1; k < teams; ++k) x += *(const kge_f32x4 *)(of_teams + k * wide + i);
             f(i, x);
         }
         __syncthreads();
@@ -230,7 +240,7 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
         return;
     }
     // the run's sums, for the join
-    auto keep = [&](const kge_f32x4 (&s)[NG], int which) {
+    auto keep = [&](kge_f32x4 (&s)[NG], int which) {
         if (!(a.want >> which & 1)) return;
         float *p = a.part + ((int64_t)which * a.runs + run) * a.part_ld;
         of_columns(s, [&](int i, kge_f32x4 x) { *(kge_f32x4 *)(p + i) = x; });
@@ -239,29 +249,32 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
 }
 
 template <bool S16, bool B16, int MODE> void launch_bwd(const BwdArgs &a, hipStream_t st) {
-    const int groups = groups_of(a.dim), teams = bwd_teams_of(a.dim), nt = 64 * a.waves * teams;
+    const int lanes = bwd_lanes_of(a.dim), groups = groups_of(a.dim, lanes), teams = bwd_teams_of(a.dim), nt = lanes * teams;
     const dim3 grid((unsigned)a.runs), blk(nt);
     // 128 KB at most (rows of 8,192 columns with gates of groups)
-    const int lds = (vectors_of(MODE, nt) + (MODE == GATE_GROUPS ? 2 * teams : teams > 1 ? teams : 0)) * 256 * a.waves * groups * (int)sizeof(float);
-#define KGE_BWD(NG, NT, OCC)                                                                                                    \
+    const int lds = (vectors_of(MODE, nt) + (MODE == GATE_GROUPS ? 2 * teams : teams > 1 ? teams : 0)) * 4 * lanes * groups * (int)sizeof(float);
+#define KGE_BWD(NG, SUB, NT, OCC)                                                                                                    \
     do {                                                                                                                        \
         static KgeLdsLimit limit;                                                                                               \
-        const auto kern = norm_bwd_kernel<S16, B16, NG, NT, OCC, MODE>;                                                         \
+        const auto kern = norm_bwd_kernel<S16, B16, NG, SUB, NT, OCC, MODE>;                                                         \
         if (lds > 48 * 1024 && limit.set((const void *)kern, 128 * 1024) != KGE_OK) return;                                     \
         hipLaunchKernelGGL(kern, grid, blk, lds, st, a);                                                                        \
     } while (0)
     if (a.waves == 8) {
-        if (groups == 2) KGE_BWD(2, 512, 4);
-        else if (groups == 3) KGE_BWD(3, 512, 2);
-        else KGE_BWD(4, 512, 2);
+        if (groups == 2) KGE_BWD(2, 64, 512, 4);
+        else if (groups == 3) KGE_BWD(3, 64, 512, 2);
+        else KGE_BWD(4, 64, 512, 2);
     } else if (a.waves > 1) {
-        if (groups == 2) KGE_BWD(2, 256, 4);
-        else KGE_BWD(3, 256, 3);
-    } else switch (groups) {
-    case 1: KGE_BWD(1, 64 * TEAMS_OF_ONE[0], 4); break;
-    case 2: KGE_BWD(2, 64 * TEAMS_OF_ONE[1], 4); break;
-    case 3: KGE_BWD(3, 64 * TEAMS_OF_ONE[2], 3); break;
-    default: KGE_BWD(4, 64 * TEAMS_OF_ONE[3], 2);
+        if (groups == 2) KGE_BWD(2, 64, 256, 4);
+        else KGE_BWD(3, 64, 256, 3);
+    } else if (lanes == 16) {
+        if (groups == 1) KGE_BWD(1, 16, NARROW_THREADS, 4);
+        else KGE_BWD(2, 16, NARROW_THREADS, 4);
+    } else if (lanes == 32) KGE_BWD(2, 32, NARROW_THREADS, 4);
+    else switch (groups) {
+    case 2: KGE_BWD(2, 64, 64 * TEAMS_OF_ONE[0], 4); break;
+    case 3: KGE_BWD(3, 64, 64 * TEAMS_OF_ONE[1], 3); break;
+    default: KGE_BWD(4, 64, 64 * TEAMS_OF_ONE[2], 2);
     }
 #undef KGE_BWD
 }

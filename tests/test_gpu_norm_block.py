@@ -225,6 +225,16 @@ def test_gates_of_groups(rows, dim, kind, gate_rows):
 
 
 @pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("s,b", TYPES)
+@pytest.mark.parametrize("rows,dim", [(9_000, 128), (2_000, 65), (8_501, 250), (900, 256), (3_000, 257), (35_000, 60)])
+@pytest.mark.parametrize("gate_rows", [0, 1, 2, 150])
+def test_narrow_rows_share_a_wave(rows, dim, gate_rows, s, b, kind):
+    c = Case(rows, dim, kind, s, b, gate_rows=gate_rows, key=4)
+    _check_forward(c, 1)
+    _check_backward(c, 1)
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
 @pytest.mark.parametrize("parts", [dict(y=False), dict(pre=False), dict(post=False), dict(post=False, pre=False), dict(scale=False), dict(post=False, scale=False),
                                    dict(bias=False), dict(weight=False), dict(weight=False, bias=False, scale=False)])
 @pytest.mark.parametrize("gate_rows", [0, 1, 9])
