@@ -6,7 +6,7 @@
 // result does not depend on tiles or splits.  The scales are applied once, as the sums leave the accumulators.
 //
 // What bounds it: large products the matrix pipe under the clock that operands which toggle bits leave it (16,384 x 4,096 x 4,096 243 us, 2.26 PFLOP/s; on zeros 200; 4,096 more of k 220 and 162);
-// products of a few hundred tiles the trips to memory of a tile's start and end (24,576 gathered rows x 256 x 768, fp32 output: 18.5 us, of which its bytes are 9); a split contraction the
+// products of a few hundred tiles the trips to memory of a tile's start and end (24,576 gathered rows x 256 x 768, fp32 output: 18.0 us, of which its bytes are 9); a split contraction the
 // reads from the L2 (768 x 1,024 x 24,576 in five parts: 32.4 us, of them 5 for the launch that adds the parts); one token the weights' bytes or the launch (1 x 4,096 x 1,024 3.4 us).
 #include "lds_copy.hpp"
 #include "text_ops.hpp"
@@ -384,6 +384,8 @@ template <int MF> __global__ __launch_bounds__(64 * SKINNY_WAVES) void matmul_sk
 //   (64 x 4,096 x 8,192 21.7 / 16.8, 32 x 1,024 x 16,384 23.5 / 16.7); and at up to 16 rows with a short k for any number of pairs (1 x 50,000 x 768 10.2 and 10.9 in tiles; 16 rows 12.6 and 11.7);
 // tiles of 256 x 256 from BIG_TILES of them on: 196 52.9 and 66.2 in tiles of 128 x 128, 121 47.7 and 43.4 (3,584 and 2,816 squared x 4,096).  Eight waves of 128 x 64 each; four of 128 x 128,
 //   which read a quarter less from the LDS, take k = 1,024 105 and not 91, 4,096 254 and not 243, 8,192 449 and not 445 (16,384 x 4,096);
+// tiles of 128 x 256, one per compute unit, where those of 128 x 128 would be more than one: 2,200 x 2,200 x 4,096 29.7 and 33.1, 20,000 x 256 x 768 11.4 and 13.2, 8,200 x 512 x 2,048 17.7 and 19.5,
+//   2,816 x 2,816 x 4,096 39.5 and 40.0; where both are at most one they lose (1,800 x 1,800 x 4,096 26.4 and 21.8, 16,000 x 256 x 768 10.9 and 9.8);
 // tiles of 128 x 128 otherwise, split along k into as many workgroups as there are compute units: 768 x 1,024 x 24,576 32.4 in 5 parts, 51.5 in 2, 34.8 in 10, two per compute unit; 1,000 x 1,000 x 32,768
 //   45.3 in 4, 46.5 in 8.  A split takes blocks of k off a workgroup (0.42 us each) and costs a launch (SPLIT_LAUNCH blocks) and its parts' bytes (SPLIT_MB blocks per MB): 200 x 4,096 x 4,096 20.8
 //   against 18.9 whole, x 6,144 22.2 / 25.9, 300 x 256 x 4,096 11.6 / 15.3, 1,000 x 1,000 x 4,096 21.5 / 19.4.  The launch that adds the parts reads
@@ -399,12 +401,13 @@ constexpr int64_t MAX_TILES = 1 << 22;                         // of a launch: a
 
 // Tiles of a workgroup: waves and blocks of a wave, in rows of A and of B; waves per SIMD; whether matrices may be 4 GiB and more
 struct Tile { int wm, wn, nj, ni, stages, occ; bool far; };
-constexpr Tile BIG = {2, 4, 4, 2, 2, 2, false}, MID = {2, 2, 2, 2, 2, 2, true}, DEEP = {2, 2, 2, 2, 4, 1, true};
+constexpr Tile BIG = {2, 4, 4, 2, 2, 2, false}, WIDE = {2, 4, 2, 2, 2, 2, true}, MID = {2, 2, 2, 2, 2, 2, true}, DEEP = {2, 2, 2, 2, 4, 1, true};
 constexpr int tile_m(const Tile &t) { return 32 * t.wm * t.nj; }
 constexpr int tile_n(const Tile &t) { return 32 * t.wn * t.ni; }
 
 // skinny: sixteens of rows of A that a workgroup of matmul_skinny_kernel takes, 0 for tiles
-struct Plan { int skinny, big, tiles_m, tiles_n, splits, kb_per; int64_t part_ld, part_bytes; };
+enum { TILES_MID, TILES_WIDE, TILES_BIG };
+struct Plan { int skinny, kind, tiles_m, tiles_n, splits, kb_per; int64_t part_ld, part_bytes; };
 
 Plan make_plan(int64_t m, int64_t n, int64_t k, size_t room, bool far = false) {
     Plan q = {};
@@ -417,12 +420,13 @@ Plan make_plan(int64_t m, int64_t n, int64_t k, size_t room, bool far = false) {
         return q;
     }
     const auto tiles_of = [&](const Tile &t, int64_t &tm, int64_t &tn) { tm = (m + tile_m(t) - 1) / tile_m(t); tn = (n + tile_n(t) - 1) / tile_n(t); return tm * tn; };
-    int64_t tm, tn, tiles = tiles_of(BIG, tm, tn);
-    q.big = tiles >= BIG_TILES && m > tile_m(MID) && n > tile_n(MID) && !far;
-    if (!q.big) tiles = tiles_of(MID, tm, tn);
+    int64_t tm, tn;
+    if (tiles_of(BIG, tm, tn) >= BIG_TILES && m > tile_m(MID) && n > tile_n(MID) && !far) q.kind = TILES_BIG;
+    else if (tiles_of(MID, tm, tn) > CUS && tiles_of(WIDE, tm, tn) <= CUS) q.kind = TILES_WIDE;
+    const int64_t tiles = tiles_of(q.kind == TILES_BIG ? BIG : q.kind == TILES_WIDE ? WIDE : MID, tm, tn);
     q.tiles_m = (int)tm; q.tiles_n = (int)tn;
     q.part_ld = (n + 3) / 4 * 4;
-    if (!q.big && tiles * 2 <= CUS) {
+    if (q.kind == TILES_MID && tiles * 2 <= CUS) {
         int64_t s = CUS / tiles;
         while (5 * s * s > 7 * kb) s--;
         const int64_t one = m * q.part_ld * 4;
@@ -447,7 +451,8 @@ void launch(const MatmulArgs &p, const Plan &q, hipStream_t st) {
     const dim3 grid((unsigned)((p.tiles_m * p.tiles_n * p.splits + 7) / 8 * 8));
 #define KGE_TILES(T, GATHERED) \
     hipLaunchKernelGGL((matmul_tiles_kernel<T.wm, T.wn, T.nj, T.ni, T.stages, T.occ, T.far, GATHERED>), grid, dim3(64 * T.wm * T.wn), 0, st, p)
-    if (q.big) { if (p.rows) KGE_TILES(BIG, true); else KGE_TILES(BIG, false); }
+    if (q.kind == TILES_BIG) { if (p.rows) KGE_TILES(BIG, true); else KGE_TILES(BIG, false); }
+    else if (q.kind == TILES_WIDE) { if (p.rows) KGE_TILES(WIDE, true); else KGE_TILES(WIDE, false); }
     else if (p.tiles_m * p.tiles_n * p.splits <= CUS && p.kb_per >= DEEP_BLOCKS) { if (p.rows) KGE_TILES(DEEP, true); else KGE_TILES(DEEP, false); }
     else { if (p.rows) KGE_TILES(MID, true); else KGE_TILES(MID, false); }
 #undef KGE_TILES

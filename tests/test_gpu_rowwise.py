@@ -194,6 +194,25 @@ def test_matmul_gathered_accumulated_strided(dt, m, n, k, pad):
     _equal(kge.matmul_rowwise(a, _cuda(b, k), rows=rows.cuda(), dtype=dt), _product(table, b, rows).to(dt))
 
 
+@pytest.mark.parametrize("m,n,k", [(2100, 2101, 100), (2250, 2000, 1000), (8200, 500, 640), (20_000, 256, 129), (9000, 511, 260)])
+def test_matmul_of_wide_tiles(m, n, k):
+    """Tiles of 128 x 256: more than a compute unit has of 128 x 128; gathered rows, and added to what is there."""
+    a, b = _matrix(m, k, 19), _matrix(n, k, 20)
+    rows = torch.from_numpy(_rng(21, k).integers(-1, m + 1, size=m).astype(np.int32)).cuda()
+    qa, qb = _cuda(a, k), _cuda(b, k)
+    want = (a[0].cuda().double() @ b[0].cuda().double().t()).float() * a[1].cuda().unsqueeze(1) * b[1].cuda()
+    for dt in (F32, BF16):
+        got = kge.matmul_rowwise(qa, qb, dtype=dt)
+        assert torch.equal(got, want.to(dt)), (got != want.to(dt)).nonzero()[:3]
+    live = (rows >= 0) & (rows < m)
+    taken = torch.where(live.unsqueeze(1), want[rows.clamp(0, m - 1).long()], torch.zeros((), device="cuda"))
+    got = kge.matmul_rowwise(qa, qb, rows=rows, dtype=BF16)
+    assert torch.equal(got, taken.to(BF16))
+    out = torch.full((m, n), 0.0, device="cuda")
+    kge.matmul_rowwise(qa, qb, rows=rows, dtype=F32, out=out, accumulate=True)
+    assert torch.equal(out, taken)
+
+
 @pytest.mark.parametrize("k", [1921, 2048, 2100, 2300, 2432, 2433, 3900, 4096, 6200, 20_001])
 def test_matmul_of_a_workgroup_per_compute_unit(k):
     """Tiles that have a compute unit each, contractions of every length in blocks modulo the ring, whole and split; gathered rows too."""
