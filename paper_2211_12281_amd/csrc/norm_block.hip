@@ -277,7 +277,7 @@ int64_t most_runs(const kge_norm_block_t *b, int64_t rows) {
 }
 int64_t part_ld_of(int dim) { return (dim + JC - 1) / JC * JC; }
 
-template <bool S16, bool B16> void launch_fwd(const FwdArgs &a, hipStream_t st) {
+template <bool S16, bool B16> int launch_fwd(const FwdArgs &a, hipStream_t st) {
     const int lanes = fwd_lanes_of(a.dim), teams = lanes < 256 ? 256 / lanes : 1, ng = groups_of(a.dim, lanes);
     int64_t groups = (a.rows + teams - 1) / teams;
     if (groups > FWD_GROUPS) groups = FWD_GROUPS;
@@ -287,7 +287,7 @@ template <bool S16, bool B16> void launch_fwd(const FwdArgs &a, hipStream_t st) 
     do {                                                                                                                        \
         static KgeLdsLimit limit;                                                                                               \
         const auto kern = norm_fwd_kernel<S16, B16, NG, SUB, NT, OCC>;                                                               \
-        if (lds > 48 * 1024 && limit.set((const void *)kern, 80 * 1024) != KGE_OK) return;                                      \
+        if (lds > 48 * 1024 && limit.set((const void *)kern, 80 * 1024) != KGE_OK) return KGE_E_HIP;                                     \
         hipLaunchKernelGGL(kern, grid, blk, lds, st, a);                                                                        \
     } while (0)
     if (a.waves == 8) {
@@ -304,6 +304,7 @@ template <bool S16, bool B16> void launch_fwd(const FwdArgs &a, hipStream_t st) 
     default: KGE_FWD(4, 64, 256, 4);
     }
 #undef KGE_FWD
+    return kge_launch_status();
 }
 
 }  // namespace
@@ -329,9 +330,8 @@ int kge_norm_block(const kge_norm_block_t *blk, const void *x, int64_t x_ld, con
     a.x = matrix((void *)x, x_ld, s16); a.y = matrix((void *)y, y_ld, b16); a.h = matrix(h, h_ld, s16); a.z = matrix(z, z_ld, b16);
     a.stream = rows * blk->dim * ((h ? (s16 ? 2 : 4) : 0) + (z ? (b16 ? 2 : 4) : 0)) >= KGE_STREAM_BYTES;
     hipStream_t st = (hipStream_t)hip_stream;
-    if (s16) b16 ? launch_fwd<true, true>(a, st) : launch_fwd<true, false>(a, st);
-    else b16 ? launch_fwd<false, true>(a, st) : launch_fwd<false, false>(a, st);
-    return kge_launch_status();
+    if (s16) return b16 ? launch_fwd<true, true>(a, st) : launch_fwd<true, false>(a, st);
+    return b16 ? launch_fwd<false, true>(a, st) : launch_fwd<false, false>(a, st);
 }
 
 size_t kge_norm_block_bwd_workspace_bytes(const kge_norm_block_t *blk, int64_t rows) {
@@ -385,8 +385,7 @@ int kge_norm_block_bwd(const kge_norm_block_t *blk, const void *h, int64_t h_ld,
     const bool folded = q.parts > MANY_PARTS && q.runs > 1 && (a.want & 3);
     hipStream_t st = (hipStream_t)hip_stream;
     if (rows > 0) {
-        if (s16) rows_bwd16(a, b16, st);
-        else rows_bwd32(a, b16, st);
+        if (const int e = s16 ? rows_bwd16(a, b16, st) : rows_bwd32(a, b16, st)) return e;
         if (folded) {
             const dim3 grid((unsigned)(q.runs / q.parts * ((a.part_ld + 255) / 256)));
             if (b16) hipLaunchKernelGGL((norm_groups_kernel<true>), grid, dim3(64 * GROUP_SLICES), 0, st, a);

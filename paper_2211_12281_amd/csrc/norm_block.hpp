@@ -254,7 +254,7 @@ inline int64_t bwd_runs_of(int dim) {
 }
 
 // rows of the backward pass, by the stream's type
-void rows_bwd16(const BwdArgs &a, bool b16, hipStream_t st);
-void rows_bwd32(const BwdArgs &a, bool b16, hipStream_t st);
+int rows_bwd16(const BwdArgs &a, bool b16, hipStream_t st);
+int rows_bwd32(const BwdArgs &a, bool b16, hipStream_t st);
 
 }  // namespace kge_norm

@@ -248,7 +248,7 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
     keep(A, SUM_A); keep(B, SUM_B); keep(C, SUM_C); keep(D, SUM_D);
 }
 
-template <bool S16, bool B16, int MODE> void launch_bwd(const BwdArgs &a, hipStream_t st) {
+template <bool S16, bool B16, int MODE> int launch_bwd(const BwdArgs &a, hipStream_t st) {
     const int lanes = bwd_lanes_of(a.dim), groups = groups_of(a.dim, lanes), teams = bwd_teams_of(a.dim), nt = lanes * teams;
     const dim3 grid((unsigned)a.runs), blk(nt);
     // 128 KB at most (rows of 8,192 columns with gates of groups)
@@ -257,7 +257,7 @@ template <bool S16, bool B16, int MODE> void launch_bwd(const BwdArgs &a, hipStr
     do {                                                                                                                        \
         static KgeLdsLimit limit;                                                                                               \
         const auto kern = norm_bwd_kernel<S16, B16, NG, SUB, NT, OCC, MODE>;                                                         \
-        if (lds > 48 * 1024 && limit.set((const void *)kern, 128 * 1024) != KGE_OK) return;                                     \
+        if (lds > 48 * 1024 && limit.set((const void *)kern, 128 * 1024) != KGE_OK) return KGE_E_HIP;                                    \
         hipLaunchKernelGGL(kern, grid, blk, lds, st, a);                                                                        \
     } while (0)
     if (a.waves == 8) {
@@ -277,11 +277,12 @@ template <bool S16, bool B16, int MODE> void launch_bwd(const BwdArgs &a, hipStr
     default: KGE_BWD(4, 64, 64 * TEAMS_OF_ONE[2], 2);
     }
 #undef KGE_BWD
+    return KGE_OK;
 }
-template <bool S16> void launch_bwd(const BwdArgs &a, bool b16, hipStream_t st) {
+template <bool S16> int launch_bwd(const BwdArgs &a, bool b16, hipStream_t st) {
     const int mode = !a.gate.p || a.parts > 0 ? GATE_RUN : a.gate_rows == 1 ? GATE_ROW : GATE_GROUPS;
-    if (b16) mode == GATE_RUN ? launch_bwd<S16, true, GATE_RUN>(a, st) : mode == GATE_ROW ? launch_bwd<S16, true, GATE_ROW>(a, st) : launch_bwd<S16, true, GATE_GROUPS>(a, st);
-    else mode == GATE_RUN ? launch_bwd<S16, false, GATE_RUN>(a, st) : mode == GATE_ROW ? launch_bwd<S16, false, GATE_ROW>(a, st) : launch_bwd<S16, false, GATE_GROUPS>(a, st);
+    if (b16) return mode == GATE_RUN ? launch_bwd<S16, true, GATE_RUN>(a, st) : mode == GATE_ROW ? launch_bwd<S16, true, GATE_ROW>(a, st) : launch_bwd<S16, true, GATE_GROUPS>(a, st);
+    return mode == GATE_RUN ? launch_bwd<S16, false, GATE_RUN>(a, st) : mode == GATE_ROW ? launch_bwd<S16, false, GATE_ROW>(a, st) : launch_bwd<S16, false, GATE_GROUPS>(a, st);
 }
 
 }  // namespace kge_norm
