@@ -9,7 +9,7 @@
 // So the backward pass has four column sums at most, whatever is asked for.  A row's statistics are computed again from h and y, which it has to read
 // anyway: nothing is stored between the passes.
 //
-// Memory bounds both: a row is read once, held in registers by one wave (up to 1,024 columns) or several, and its sums stay there for the run of rows that a
+// Memory bounds both: a row is read once, held in registers by part of a wave (norm_block.hpp), one wave (up to 1,024 columns) or several, and its sums stay there for the run of rows that a
 // workgroup takes.  24,576 x 768, layer norms, fp32 stream, bf16 block, gates of 96 rows: forward 42 us (227 MB, 5.4 TB/s), backward 76 (340 MB, 4.5 TB/s) and 10 for the launch
 // that joins the runs' sums, most of it the wait for what the rows' launch has written (behind small calls it takes 4); one row 3.7 us, a launch and three trips to memory.
 // No row is fetched ahead: the registers that it takes are a wave per SIMD (backward with 82, without 77 us; forward 58 and 42).
@@ -22,7 +22,7 @@ using namespace kge_norm;
 // ---------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------
-// A team takes a row at a time; the vectors stand in the LDS (rows of more than 4,096 columns: in memory).
+// A team takes a row at a time; the vectors stand in the LDS (rows of eight waves: in memory).
 enum { VEC_POST = 0, VEC_POST_BIAS = 1, VEC_SCALE = 2, VEC_PRE = 3, VEC_PRE_BIAS = 4, VECTORS = 5 };
 template <bool S16, bool B16, int NG, int SUB, int NT, int OCC>
 __global__ __launch_bounds__(NT, OCC) void norm_fwd_kernel(const FwdArgs a) {
@@ -282,12 +282,12 @@ template <bool S16, bool B16> int launch_fwd(const FwdArgs &a, hipStream_t st) {
     int64_t groups = (a.rows + teams - 1) / teams;
     if (groups > FWD_GROUPS) groups = FWD_GROUPS;
     const dim3 grid((unsigned)groups), blk(lanes * teams);
-    const int lds = a.waves <= 4 ? VECTORS * 4 * lanes * ng * (int)sizeof(float) : 0;                   // 80 KB at most
+    const int lds = a.waves <= 2 ? VECTORS * 4 * lanes * ng * (int)sizeof(float) : 0;                   // 60 KB at most
 #define KGE_FWD(NG, SUB, NT, OCC)                                                                                                    \
     do {                                                                                                                        \
         static KgeLdsLimit limit;                                                                                               \
         const auto kern = norm_fwd_kernel<S16, B16, NG, SUB, NT, OCC>;                                                               \
-        if (lds > 48 * 1024 && limit.set((const void *)kern, 80 * 1024) != KGE_OK) return KGE_E_HIP;                                     \
+        if (lds > 48 * 1024 && limit.set((const void *)kern, 60 * 1024) != KGE_OK) return KGE_E_HIP;                                     \
         hipLaunchKernelGGL(kern, grid, blk, lds, st, a);                                                                        \
     } while (0)
     if (a.waves == 8) {
@@ -301,7 +301,9 @@ template <bool S16, bool B16> int launch_fwd(const FwdArgs &a, hipStream_t st) {
     case 1: KGE_FWD(1, 64, 256, 8); break;
     case 2: KGE_FWD(2, 64, 256, 6); break;
     case 3: KGE_FWD(3, 64, 256, 5); break;
-    default: KGE_FWD(4, 64, 256, 4);
+    case 4: KGE_FWD(4, 64, 256, 4); break;
+    case 5: KGE_FWD(5, 64, 256, 2); break;
+    default: KGE_FWD(6, 64, 256, 2);
     }
 #undef KGE_FWD
     return kge_launch_status();
@@ -324,7 +326,7 @@ int kge_norm_block(const kge_norm_block_t *blk, const void *x, int64_t x_ld, con
     if (rc != KGE_OK) return rc;
     const bool s16 = blk->stream_dtype == KGE_BF16, b16 = blk->block_dtype == KGE_BF16;
     FwdArgs a = {};
-    a.dim = blk->dim; a.waves = waves_of(blk->dim); a.rows = rows;
+    a.dim = blk->dim; a.waves = fwd_waves_of(blk->dim); a.rows = rows;
     a.post = norm_of(blk->post); a.pre = norm_of(blk->pre); a.scale = blk->scale;
     a.gate = matrix((void *)blk->gate, blk->gate_ld, b16); a.gate_rows = (uint32_t)(blk->gate_rows < rows ? blk->gate_rows : rows);
     a.x = matrix((void *)x, x_ld, s16); a.y = matrix((void *)y, y_ld, b16); a.h = matrix(h, h_ld, s16); a.z = matrix(z, z_ld, b16);

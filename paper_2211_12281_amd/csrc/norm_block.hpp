@@ -233,10 +233,13 @@ inline int waves_of(int dim) {
     while (w < 8 && 768 * w < dim) w *= 2;
     return w;
 }
+// Forward: two waves hold up to six groups a lane.  (Four waves, whose vectors leave the LDS room for fewer rows at once: 10,000 x 2,048 79 against 61 us, 6,000 x 3,000 76 against 64.  With
+// eight groups in two waves 5,000 x 4,000 takes 100 us, with two in eight 81.)
+inline int fwd_waves_of(int dim) { return dim <= 1024 ? 1 : dim <= 512 * 6 ? 2 : 8; }
 // Lanes of a row: narrow ones share a wave, whose sums over lanes then serve two or four of them.  Layer norms, fp32 / bf16, 25.6M elements, shared and one row per
 // wave: forward 64 columns 62 and 167 us, 128 64 and 93 (256 68 and 62: not shared); backward 64 104 and 315, 128 82 and 181, 256 84 and 112.
 inline int bwd_lanes_of(int dim) { return dim <= 128 ? 16 : dim <= 256 ? 32 : 64 * waves_of(dim); }
-inline int fwd_lanes_of(int dim) { return dim <= 128 ? 16 : 64 * waves_of(dim); }
+inline int fwd_lanes_of(int dim) { return dim <= 128 ? 16 : 64 * fwd_waves_of(dim); }
 // groups of four columns of a lane, the last of which no other group of the row lies behind
 inline int groups_of(int dim, int lanes) { return (dim + 4 * lanes - 1) / (4 * lanes); }
 // Teams of a workgroup of the backward pass.  Of one wave (no barriers between rows): as many as the registers leave room for on a compute unit, so that there are 256 runs'

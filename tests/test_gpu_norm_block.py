@@ -235,6 +235,13 @@ def test_narrow_rows_share_a_wave(rows, dim, gate_rows, s, b, kind):
 
 
 @pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("s,b", TYPES)
+@pytest.mark.parametrize("rows,dim", [(5, 1025), (300, 1537), (31, 2000), (77, 2048), (12, 2560), (9000, 2561), (64, 2900), (7, 3333)])
+def test_rows_of_two_waves(rows, dim, s, b, kind):
+    _check_forward(Case(rows, dim, kind, s, b, gate_rows=[0, 1, 3, rows][rows % 4], key=5), 1)
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
 @pytest.mark.parametrize("parts", [dict(y=False), dict(pre=False), dict(post=False), dict(post=False, pre=False), dict(scale=False), dict(post=False, scale=False),
                                    dict(bias=False), dict(weight=False), dict(weight=False, bias=False, scale=False)])
 @pytest.mark.parametrize("gate_rows", [0, 1, 9])
