@@ -379,9 +379,10 @@ template <int MF> __global__ __launch_bounds__(64 * SKINNY_WAVES) void matmul_sk
 
 // ---------------------------------------------------------------------------------------------
 // Which kernel (bf16 output, replayed from a graph, us):
-// sixteen rows of B against 16, 32 or 64 of A per workgroup where there are few such pairs (SKINNY_GROUPS) and each has little to do (SKINNY_WORK: blocks of k per wave times sixteens of rows):
-//   64 x 4,096 x 4,096 12.5 against 14.9 in split tiles and 18.5 in whole ones, 1 x 4,096 x 16,384 16.4 / 23.1 / 54.3, 300 x 300 x 3,000 9.8 / 11.6 / 13.5; more work per pair loses
-//   (64 x 4,096 x 8,192 21.7 / 16.8, 32 x 1,024 x 16,384 23.5 / 16.7); and at up to 16 rows with a short k for any number of pairs (1 x 50,000 x 768 10.2 and 10.9 in tiles; 16 rows 12.6 and 11.7);
+// sixteen rows of B against 16 of A per workgroup, 32 or 64 if those would be more workgroups than compute units (300 x 300 x 3,000 6.9 us with 32 and 9.8 with 64, 64 x 1,024 x 4,096 5.8 with 16 and 11.0 with 64,
+//   but 64 x 4,096 x 4,096 15.3 with 16), where there are few such pairs (SKINNY_GROUPS) and each has little to do (SKINNY_WORK: blocks of k per wave times sixteens of rows):
+//   64 x 4,096 x 4,096 12.5 against 15.2 in split tiles and 18.5 in whole ones, 1 x 4,096 x 16,384 16.4 / 23.1 / 54.3, 100 x 1,000 x 6,000 10.7 / 13.5 / 23.8; more work per pair loses
+//   (64 x 4,096 x 8,192 21.6 / 16.8, 100 x 1,000 x 12,000 18.1 / 16.8, 1 x 1,000 x 32,768 26.8 / 19.0); and at up to 16 rows with a short k for any number of pairs (1 x 50,000 x 768 10.2 and 10.9 in tiles; 16 rows 12.6 and 11.7);
 // tiles of 256 x 256 from BIG_TILES of them on: 196 52.9 and 66.2 in tiles of 128 x 128, 121 47.7 and 43.4 (3,584 and 2,816 squared x 4,096).  Eight waves of 128 x 64 each; four of 128 x 128,
 //   which read a quarter less from the LDS, take k = 1,024 105 and not 91, 4,096 254 and not 243, 8,192 449 and not 445 (16,384 x 4,096);
 // tiles of 128 x 256, one per compute unit, where those of 128 x 128 would be more than one: 2,200 x 2,200 x 4,096 29.7 and 33.1, 20,000 x 256 x 768 11.4 and 13.2, 8,200 x 512 x 2,048 17.7 and 19.5,
@@ -413,8 +414,10 @@ Plan make_plan(int64_t m, int64_t n, int64_t k, size_t room, bool far = false) {
     Plan q = {};
     const int64_t kb = (k + BLOCK - 1) / BLOCK;
     q.splits = 1; q.kb_per = (int)kb;
-    const int mf = m <= 16 ? 1 : m <= 32 ? 2 : 4;
-    const int64_t gm = (m + 16 * mf - 1) / (16 * mf), gn = (n + 15) / 16, rounds = (kb + SKINNY_WAVES - 1) / SKINNY_WAVES;
+    const int64_t gn = (n + 15) / 16;
+    int mf = 1;
+    while (mf < 4 && 16 * mf < m && (m + 16 * mf - 1) / (16 * mf) * gn > CUS) mf *= 2;
+    const int64_t gm = (m + 16 * mf - 1) / (16 * mf), rounds = (kb + SKINNY_WAVES - 1) / SKINNY_WAVES;
     if (gm * gn <= SKINNY_GROUPS ? rounds * mf <= SKINNY_WORK : m <= 16 && gn <= MAX_TILES && rounds <= SKINNY_LONG) {
         q.skinny = mf; q.tiles_m = (int)gm; q.tiles_n = (int)gn;
         return q;

@@ -264,7 +264,7 @@ def test_matmul_gathers_nothing_from_an_empty_table():
 
 
 def test_splits_do_not_change_the_result():
-    m, n, k = 200, 96, 6000
+    m, n, k = 200, 700, 9000                                      # (a product that is split)
     a, b = _matrix(m, k, 16), _matrix(n, k, 17)
     want = _product(a, b)
     lib, da, db = kge.load(), _cuda(a, k), _cuda(b, k)
