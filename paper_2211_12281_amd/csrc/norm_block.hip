@@ -10,7 +10,7 @@
 // anyway: nothing is stored between the passes.
 //
 // Memory bounds both: a row is read once, held in registers by part of a wave (norm_block.hpp), one wave (up to 1,024 columns) or several, and its sums stay there for the run of rows that a
-// workgroup takes.  24,576 x 768, layer norms, fp32 stream, bf16 block, gates of 96 rows: forward 42 us (227 MB, 5.4 TB/s), backward 76 (340 MB, 4.5 TB/s) and 10 for the launch
+// workgroup takes.  24,576 x 768, layer norms, fp32 stream, bf16 block, gates of 96 rows: forward 42-43 us (227 MB, 5.3 TB/s), backward 76 (340 MB, 4.5 TB/s) and 10 for the launch
 // that joins the runs' sums, most of it the wait for what the rows' launch has written (behind small calls it takes 4); one row 3.7 us, a launch and three trips to memory.
 // No row is fetched ahead: the registers that it takes are a wave per SIMD (backward with 82, without 77 us; forward 58 and 42).
 #include "norm_block.hpp"
@@ -22,15 +22,17 @@ using namespace kge_norm;
 // ---------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------
-// A team takes a row at a time; the vectors stand in the LDS (rows of eight waves: in memory).
+// A team takes R rows at a time; the vectors stand in the LDS (rows of eight waves: in memory, from where they are read for every turn, more bytes than a row has of its own, so that
+// two rows share them and the barriers of their sums: 7,256 x 3,304 86 us and not 114, 5,000 x 4,000 65 and 81, 3,000 x 8,192 88 and 102; with three groups a lane two rows lose,
+// 4,000 x 6,000 98 and 82, and where every row has a workgroup they take longer, 10 x 4,096 7.5 and 6.0).
 enum { VEC_POST = 0, VEC_POST_BIAS = 1, VEC_SCALE = 2, VEC_PRE = 3, VEC_PRE_BIAS = 4, VECTORS = 5 };
-template <bool S16, bool B16, int NG, int SUB, int NT, int OCC>
+template <bool S16, bool B16, int NG, int SUB, int NT, int OCC, int R>
 __global__ __launch_bounds__(NT, OCC) void norm_fwd_kernel(const FwdArgs a) {
     constexpr bool LDS = NT == 256;
-    __shared__ float red[2][NT / 64][1];
+    __shared__ float red[2][NT / 64][R];
     extern __shared__ __attribute__((aligned(16))) float vec[];
     const Team<SUB> t(a.waves);
-    Reduce<1, NT, SUB> reduce(red, t);
+    Reduce<R, NT, SUB> reduce(red, t);
     const Columns<NG> c(a.dim, t.lane, t.size);
     const float inv_dim = 1.f / (float)a.dim;
     const int wide = 4 * t.size * NG;
@@ -38,19 +40,23 @@ __global__ __launch_bounds__(NT, OCC) void norm_fwd_kernel(const FwdArgs a) {
     auto vector = [&](int which, int k) {
         return LDS ? *(const kge_f32x4 *)(vec + which * wide + c.col(k)) : vector4(from[which], c.col(k), a.dim, which == VEC_POST_BIAS || which == VEC_PRE_BIAS ? 0.f : 1.f);
     };
-    const int64_t step = (int64_t)gridDim.x * t.teams, first = (int64_t)blockIdx.x * t.teams;
-    Raw<S16> x[NG];
-    Raw<B16> y[NG], g[NG];
-    auto load = [&](int64_t row) {
-        const bool in = row < a.rows;
+    const int64_t step = (int64_t)gridDim.x * t.teams * R, first = (int64_t)blockIdx.x * t.teams * R;
+    Raw<S16> x[R][NG];
+    Raw<B16> y[R][NG], g[R][NG];
+    auto load = [&](int64_t row0) {
 #pragma unroll
-        for (int k = 0; k < NG; ++k) {
-            x[k].load(a.x.row(row), c, k, in && a.x.p);
-            y[k].load(a.y.row(row), c, k, in && a.y.p);
-            g[k].load(a.gate.row(a.gate.p && in ? (uint32_t)row / a.gate_rows : 0), c, k, in && a.gate.p);
+        for (int r = 0; r < R; ++r) {
+            const int64_t row = row0 + r;
+            const bool in = row < a.rows;
+#pragma unroll
+            for (int k = 0; k < NG; ++k) {
+                x[r][k].load(a.x.row(row), c, k, in && a.x.p);
+                y[r][k].load(a.y.row(row), c, k, in && a.y.p);
+                g[r][k].load(a.gate.row(a.gate.p && in ? (uint32_t)row / a.gate_rows : 0), c, k, in && a.gate.p);
+            }
         }
     };
-    load(first + t.team);                                         // (under the loads of the vectors; later rows' wait for nobody but their own wave)
+    load(first + t.team * R);                                     // (under the loads of the vectors; later rows' wait for nobody but their own wave)
     if constexpr (LDS) {
         for (int i = 4 * threadIdx.x; i < wide; i += 4 * NT)
 #pragma unroll
@@ -59,31 +65,51 @@ __global__ __launch_bounds__(NT, OCC) void norm_fwd_kernel(const FwdArgs a) {
         __syncthreads();
     }
     for (int64_t r0 = first; r0 < a.rows; r0 += step) {           // (every team goes round equally often: the waves of one meet at barriers)
-        if constexpr (!LDS) asm volatile("" ::: "memory");        // (the vectors are read for every row: no registers for them in between)
-        const int64_t row = r0 + t.team;
-        const bool in = row < a.rows;
-        if (r0 > first) load(row);
-        kge_f32x4 h[NG], u[NG], f[NG];
+        if constexpr (!LDS) asm volatile("" ::: "memory");        // (the vectors are read for every turn: no registers for them in between)
+        const int64_t row0 = r0 + t.team * R;
+        bool in[R];
 #pragma unroll
-        for (int k = 0; k < NG; ++k) { h[k] = x[k].values(); u[k] = y[k].values(); f[k] = g[k].values(); }
+        for (int r = 0; r < R; ++r) in[r] = row0 + r < a.rows;
+        if (r0 > first) load(row0);
+        kge_f32x4 h[R][NG], u[R][NG], f[R][NG];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int k = 0; k < NG; ++k) { h[r][k] = x[r][k].values(); u[r][k] = y[r][k].values(); f[r][k] = g[r][k].values(); }
         if (a.y.p) {
             if (a.post.on) {
                 normalise(u, c, a.post, inv_dim, reduce);
 #pragma unroll
-                for (int k = 0; k < NG; ++k) u[k] = fma4(u[k], vector(VEC_POST, k), vector(VEC_POST_BIAS, k));
+                for (int k = 0; k < NG; ++k) {
+                    const kge_f32x4 w = vector(VEC_POST, k), b = vector(VEC_POST_BIAS, k);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) u[r][k] = fma4(u[r][k], w, b);
+                }
             }
 #pragma unroll
             for (int k = 0; k < NG; ++k) {
-                if (a.scale) u[k] *= vector(VEC_SCALE, k);
-                h[k] = a.gate.p ? fma4(u[k], f[k], h[k]) : u[k] + h[k];
-                if (a.h.p && in && c.inside(k)) store<S16>(a.h.row(row), c, k, h[k], a.stream);
+                if (a.scale) {
+                    const kge_f32x4 s = vector(VEC_SCALE, k);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) u[r][k] *= s;
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    h[r][k] = a.gate.p ? fma4(u[r][k], f[r][k], h[r][k]) : u[r][k] + h[r][k];
+                    if (a.h.p && in[r] && c.inside(k)) store<S16>(a.h.row(row0 + r), c, k, h[r][k], a.stream);
+                }
             }
         }
         if (a.pre.on) {
             normalise(h, c, a.pre, inv_dim, reduce);
 #pragma unroll
-            for (int k = 0; k < NG; ++k)
-                if (in && c.inside(k)) store<B16>(a.z.row(row), c, k, fma4(h[k], vector(VEC_PRE, k), vector(VEC_PRE_BIAS, k)), a.stream);
+            for (int k = 0; k < NG; ++k) {
+                if (!in[0] || !c.inside(k)) continue;
+                const kge_f32x4 w = vector(VEC_PRE, k), b = vector(VEC_PRE_BIAS, k);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+                    if (in[r]) store<B16>(a.z.row(row0 + r), c, k, fma4(h[r][k], w, b), a.stream);
+            }
         }
     }
 }
@@ -223,7 +249,7 @@ template <bool B16> __global__ __launch_bounds__(JT) void norm_join_kernel(const
 // ---------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------
-constexpr int64_t FWD_GROUPS = 2048, FEW = 2;
+constexpr int64_t FWD_GROUPS = 2048, PAIRS_FROM = 512, FEW = 2;
 constexpr int64_t MANY_PARTS = 16;                              // runs of a group from which on its sums are a launch of their own
 
 bool bad_norm(const kge_norm_t *n) {
@@ -279,31 +305,33 @@ int64_t part_ld_of(int dim) { return (dim + JC - 1) / JC * JC; }
 
 template <bool S16, bool B16> int launch_fwd(const FwdArgs &a, hipStream_t st) {
     const int lanes = fwd_lanes_of(a.dim), teams = lanes < 256 ? 256 / lanes : 1, ng = groups_of(a.dim, lanes);
+    const bool pairs = a.waves == 8 && ng != 3 && a.rows > PAIRS_FROM;
     int64_t groups = (a.rows + teams - 1) / teams;
     if (groups > FWD_GROUPS) groups = FWD_GROUPS;
     const dim3 grid((unsigned)groups), blk(lanes * teams);
     const int lds = a.waves <= 2 ? VECTORS * 4 * lanes * ng * (int)sizeof(float) : 0;                   // 60 KB at most
-#define KGE_FWD(NG, SUB, NT, OCC)                                                                                                    \
+#define KGE_FWD(NG, SUB, NT, OCC, R)                                                                                                    \
     do {                                                                                                                        \
         static KgeLdsLimit limit;                                                                                               \
-        const auto kern = norm_fwd_kernel<S16, B16, NG, SUB, NT, OCC>;                                                               \
+        const auto kern = norm_fwd_kernel<S16, B16, NG, SUB, NT, OCC, R>;                                                               \
         if (lds > 48 * 1024 && limit.set((const void *)kern, 60 * 1024) != KGE_OK) return KGE_E_HIP;                                     \
         hipLaunchKernelGGL(kern, grid, blk, lds, st, a);                                                                        \
     } while (0)
     if (a.waves == 8) {
-        if (ng == 2) KGE_FWD(2, 64, 512, 4);
-        else if (ng == 3) KGE_FWD(3, 64, 512, 4);
-        else KGE_FWD(4, 64, 512, 2);
+        if (ng == 3) KGE_FWD(3, 64, 512, 4, 1);
+        else if (ng == 2) { if (pairs) KGE_FWD(2, 64, 512, 4, 2); else KGE_FWD(2, 64, 512, 4, 1); }
+        else if (pairs) KGE_FWD(4, 64, 512, 2, 2);
+        else KGE_FWD(4, 64, 512, 2, 1);
     } else if (lanes == 16) {
-        if (ng == 1) KGE_FWD(1, 16, 256, 8);
-        else KGE_FWD(2, 16, 256, 8);
+        if (ng == 1) KGE_FWD(1, 16, 256, 8, 1);
+        else KGE_FWD(2, 16, 256, 8, 1);
     } else switch (ng) {
-    case 1: KGE_FWD(1, 64, 256, 8); break;
-    case 2: KGE_FWD(2, 64, 256, 6); break;
-    case 3: KGE_FWD(3, 64, 256, 5); break;
-    case 4: KGE_FWD(4, 64, 256, 4); break;
-    case 5: KGE_FWD(5, 64, 256, 2); break;
-    default: KGE_FWD(6, 64, 256, 2);
+    case 1: KGE_FWD(1, 64, 256, 8, 1); break;
+    case 2: KGE_FWD(2, 64, 256, 6, 1); break;
+    case 3: KGE_FWD(3, 64, 256, 4, 1); break;
+    case 4: KGE_FWD(4, 64, 256, 4, 1); break;
+    case 5: KGE_FWD(5, 64, 256, 2, 1); break;
+    default: KGE_FWD(6, 64, 256, 2, 1);
     }
 #undef KGE_FWD
     return kge_launch_status();

@@ -185,25 +185,37 @@ __device__ __forceinline__ float inv_sqrt(float x) { return 1.f / sqrtf(x); }
 
 struct Norm { bool on, layer; float eps; const float *w, *b; };
 
-// x -> x^ = (x - mean) / deviation
-template <int NG, class R>
-__device__ __forceinline__ void normalise(kge_f32x4 (&x)[NG], const Columns<NG> &c, const Norm &norm, float inv_dim, R &reduce) {
-    float v[1] = {0.f};
+// x -> x^ = (x - mean) / deviation, of R rows at once
+template <int NG, int R, class Sums>
+__device__ __forceinline__ void normalise(kge_f32x4 (&x)[R][NG], const Columns<NG> &c, const Norm &norm, float inv_dim, Sums &reduce) {
+    float v[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = 0.f;
     if (norm.layer) {
 #pragma unroll
-        for (int k = 0; k < NG; ++k) v[0] = sum4(x[k], v[0]);
-        reduce(v);
-        const float mean = v[0] * inv_dim;
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int k = 0; k < NG; ++k) x[k] = c.minus(k, x[k], mean);
-        v[0] = 0.f;
+            for (int k = 0; k < NG; ++k) v[r] = sum4(x[r][k], v[r]);
+        reduce(v);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float mean = v[r] * inv_dim;
+#pragma unroll
+            for (int k = 0; k < NG; ++k) x[r][k] = c.minus(k, x[r][k], mean);
+            v[r] = 0.f;
+        }
     }
 #pragma unroll
-    for (int k = 0; k < NG; ++k) v[0] = dot4(x[k], x[k], v[0]);
-    reduce(v);
-    const float r = inv_sqrt(fmaf(v[0], inv_dim, norm.eps));
+    for (int r = 0; r < R; ++r)
 #pragma unroll
-    for (int k = 0; k < NG; ++k) x[k] *= splat(r);
+        for (int k = 0; k < NG; ++k) v[r] = dot4(x[r][k], x[r][k], v[r]);
+    reduce(v);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const float s = inv_sqrt(fmaf(v[r], inv_dim, norm.eps));
+#pragma unroll
+        for (int k = 0; k < NG; ++k) x[r][k] *= splat(s);
+    }
 }
 
 struct FwdArgs {

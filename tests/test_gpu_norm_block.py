@@ -242,6 +242,13 @@ def test_rows_of_two_waves(rows, dim, s, b, kind):
 
 
 @pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("s,b", TYPES)
+@pytest.mark.parametrize("rows,dim", [(513, 3400), (1111, 4096), (701, 8001), (515, 5000), (512, 4000)])
+def test_pairs_of_wide_rows(rows, dim, s, b, kind):
+    _check_forward(Case(rows, dim, kind, s, b, gate_rows=[0, 1, 3, rows][rows % 4], key=6), 1)
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
 @pytest.mark.parametrize("parts", [dict(y=False), dict(pre=False), dict(post=False), dict(post=False, pre=False), dict(scale=False), dict(post=False, scale=False),
                                    dict(bias=False), dict(weight=False), dict(weight=False, bias=False, scale=False)])
 @pytest.mark.parametrize("gate_rows", [0, 1, 9])
