@@ -270,14 +270,13 @@ template <bool B16> __global__ __launch_bounds__(NT) void strips_kernel(const Ar
     }
 }
 
-// Runs of rows of the search for the columns' largest magnitudes: about 1,024 workgroups, of 32 rows at least
+// Runs of rows of the search for the columns' largest magnitudes, of a matrix that has any: about 1,024 workgroups, of 32 rows at least
 constexpr int64_t WANTED = 1024, MIN_RUN = 32;
 void runs_of(int64_t rows, int64_t cols, Args &a) {
     const int64_t across = (cols + BLOCK - 1) / BLOCK;
     int64_t runs = (WANTED + across - 1) / across;
     if (runs > MAX_RUNS) runs = MAX_RUNS;
     if (runs > (rows + MIN_RUN - 1) / MIN_RUN) runs = (rows + MIN_RUN - 1) / MIN_RUN;
-    if (runs < 1) runs = 1;
     a.run = (rows + runs - 1) / runs; a.runs = (int)runs; a.part_ld = across * BLOCK; a.row_ld = (rows + BLOCK - 1) / BLOCK * BLOCK;
 }
 // words of the workspace; in both layouts at once (24,576 x 768 bf16: 28 us, one after the other 36) where a row has few blocks
@@ -324,6 +323,7 @@ extern "C" {
 
 size_t kge_quantize_rowwise_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 0 || rows >= (1ll << 31) || cols >= (1ll << 31)) return 0;
+    if (rows == 0 || cols == 0) return 256;                       // (nothing to search)
     Args a = {};
     runs_of(rows, cols, a);
     return !in_strips(rows, cols) ? (size_t)words_of(a, at_once(cols)) * sizeof(uint32_t) + 256 : 256;
@@ -343,6 +343,15 @@ int kge_quantize_rowwise(const void *x, int32_t dtype, int64_t rows, int64_t col
     if (rc != KGE_OK) return rc;
     if (rows > 0 && cols > 0 && kge_bad_rows(x, dtype, ld, cols)) return KGE_E_INVALID_ARG;
     if (by_col && ((rows + BLOCK - 1) / BLOCK) * ((cols + BLOCK - 1) / BLOCK) >= (1ll << 24)) return KGE_E_UNSUPPORTED;   // (a grid's limit)
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (rows == 0 || cols == 0) {                                 // rows of no elements have a scale all the same
+        Args e = {};
+        const kge_rowwise_t *q = rows ? by_row : by_col;
+        e.rows = rows ? rows : cols; e.rs = q ? q->scales : nullptr;
+        if (!e.rs || e.rows == 0) return KGE_OK;
+        launch_rows<false, 1, 1, false>(e, st);
+        return kge_launch_status();
+    }
     Args a = {};
     a.x = x; a.ld = ld; a.rows = rows; a.cols = cols;
     if (by_row) { a.rc = by_row->codes; a.rs = by_row->scales; a.rc_ld = by_row->ld; }
@@ -354,18 +363,10 @@ int kge_quantize_rowwise(const void *x, int32_t dtype, int64_t rows, int64_t col
         if (!in_strips(rows, cols) && (!ws || ws_bytes < lost + (size_t)words_of(a, both) * sizeof(uint32_t))) return KGE_E_WORKSPACE_TOO_SMALL;
         a.part = (uint32_t *)((char *)ws + lost);                  // (few rows: nothing is written there)
         a.col_inv = (float *)(a.part + a.runs * a.part_ld);
-        if (both && rows > 0) {
+        if (both) {
             a.row_inv = a.col_inv + a.part_ld;
             a.row_part = (uint32_t *)a.row_inv + a.row_ld;
         }
-    }
-    hipStream_t st = (hipStream_t)hip_stream;
-    if (rows == 0 || cols == 0) {                                 // rows of no elements have a scale all the same
-        Args e = {};
-        e.rows = rows ? rows : cols; e.rs = rows ? a.rs : a.cs;
-        if (!e.rs || e.rows == 0) return KGE_OK;
-        launch_rows<false, 1, 1, false>(e, st);
-        return kge_launch_status();
     }
     if (dtype == KGE_BF16) launch<true>(a, st);
     else launch<false>(a, st);

@@ -206,3 +206,23 @@ def test_a_given_workspace_is_used(monkeypatch, on_the_host, sizes, call):      
     ws = b.Workspace()
     ((p, n),) = _at_once(monkeypatch, [lambda: call(ws=ws)])
     assert (p, n) == (ws.buf.data_ptr(), ws.buf.numel())
+
+
+# Matrices without rows or columns
+@pytest.mark.parametrize("rows", [0, 5, 600, 1 << 20])
+def test_quantize_rowwise_of_no_columns(lib, rows):
+    size = lib.kge_quantize_rowwise_workspace_bytes
+    assert size(rows, 0) == size(0, rows) == 256
+    by_col = _q(0, min(rows, 131_071), codes=None, scales=None)
+    assert lib.kge_quantize_rowwise(None, 0, by_col.cols, 0, 0, None, C.byref(by_col), None, 0, None) == 0
+
+
+def test_quantize_rowwise_of_nothing_both_ways(lib):
+    nothing = [_q(0, 0, codes=None, scales=None, ld=0) for _ in range(2)]
+    assert lib.kge_quantize_rowwise(None, 1, 0, 0, 0, C.byref(nothing[0]), C.byref(nothing[1]), None, 0, None) == 0
+
+
+@pytest.mark.parametrize("rows", [0, 5, 600])
+def test_the_binding_quantizes_no_columns(on_the_host, rows):                                          # noqa: F811
+    q = b.quantize_rowwise(torch.zeros((rows, 0)), by="col")
+    assert (q.rows, q.cols, tuple(q.codes.shape), tuple(q.scales.shape)) == (0, rows, (0, -(-rows // 128) * 128), (0,))

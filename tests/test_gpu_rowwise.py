@@ -115,6 +115,16 @@ def test_quantize_of_nothing():
     assert not bool(kge.matmul_rowwise(q, q, dtype=F32).any())
 
 
+@pytest.mark.parametrize("rows", [0, 5, 600])
+def test_quantize_of_no_columns_both_ways(rows):
+    q, t = kge.quantize_rowwise(torch.empty((rows, 0), device="cuda"), by="both")
+    assert (q.rows, q.cols, t.rows, t.cols) == (rows, 0, 0, rows)
+    _same(q, torch.empty((rows, 0)))
+    y = kge.matmul_rowwise(q, q, dtype=F32)
+    assert y.shape == (rows, rows) and not bool(y.any())
+    assert kge.matmul_rowwise(t, t).shape == (0, 0)
+
+
 # ---------------------------------------------------------------------------------------------------------------
 # product
 # ---------------------------------------------------------------------------------------------------------------
