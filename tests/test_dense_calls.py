@@ -226,3 +226,21 @@ def test_quantize_rowwise_of_nothing_both_ways(lib):
 def test_the_binding_quantizes_no_columns(on_the_host, rows):                                          # noqa: F811
     q = b.quantize_rowwise(torch.zeros((rows, 0)), by="col")
     assert (q.rows, q.cols, tuple(q.codes.shape), tuple(q.scales.shape)) == (0, rows, (0, -(-rows // 128) * 128), (0,))
+
+
+# Products without rows
+@pytest.mark.parametrize("k", [0, 100, 16_384, 16_385, 20_000, 131_071])
+def test_matmul_rowwise_of_no_rows(lib, k):
+    size = lib.kge_matmul_rowwise_workspace_bytes
+    assert size(0, 100, k) == size(100, 0, k) == size(0, 0, k) == 256
+    a, nothing = _q(100, k), _q(0, k, codes=None, scales=None)
+    for m, x, y, rows in ((0, nothing, a, None), (0, a, a, OK), (100, a, nothing, None), (0, nothing, nothing, None)):
+        assert lib.kge_matmul_rowwise(C.byref(x), rows, m, C.byref(y), 0, None, 0, y.rows, None, 0, None) == 0
+
+
+@pytest.mark.parametrize("k", [100, 20_000])
+def test_the_binding_multiplies_no_rows(on_the_host, k):                                               # noqa: F811
+    wide = -(-k // 128) * 128
+    matrix = lambda rows: b.Rowwise(torch.zeros((rows, wide), dtype=torch.int8), torch.ones(rows), k)  # noqa: E731
+    assert b.matmul_rowwise(matrix(0), matrix(100)).shape == (0, 100)
+    assert b.matmul_rowwise(matrix(100), matrix(0)).shape == (100, 0)
