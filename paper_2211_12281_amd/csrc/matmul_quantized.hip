@@ -579,6 +579,7 @@ extern "C" {
 
 size_t kge_matmul_quantized_workspace_bytes(int64_t m, int64_t n, int64_t k) {
     if (m < 0 || n < 0 || k < 0 || m >= (1ll << 31) || n >= (1ll << 31) || k >= (1ll << 31)) return 0;
+    if (m == 0 || n == 0) return 256;                             // (nothing to do, which has no plan)
     return (size_t)make_plan(m, n, k, ~0ull >> 1).part_bytes + 256;
 }
 

@@ -148,3 +148,10 @@ def test_matmul_refuses_other_widths_and_takes_nothing(lib):
     size = lib.kge_matmul_quantized_workspace_bytes
     assert size(-1, 1, 1) == 0 and size(1, 1 << 31, 1) == 0 and size(1, 2048, 2048) >= 256
     assert size(1024, 768, 24576) >= 2 * 4 * 1024 * 768                                    # a long contraction over few tiles is split
+
+
+@pytest.mark.parametrize("k", [0, 100, 20_000, 1 << 20])
+def test_matmul_of_no_rows(lib, k):
+    size = lib.kge_matmul_quantized_workspace_bytes
+    assert size(0, 100, k) == size(100, 0, k) == size(0, 0, k) == 256
+    assert _mm(lib, a=_q(0, k), bb=_q(512, k), m=0) == 0 and _mm(lib, a=_q(256, k), bb=_q(0, k)) == 0
