@@ -515,7 +515,7 @@ int kge_quantize(const void *x, int32_t dtype, int64_t rows, int64_t cols, int64
                  const kge_quantized_t *by_col, void *hip_stream);
 
 /*
- * kge_matmul_quantized: out[i, j] = sum over k of a[rows[i], k] * b[j, k], i < m, j < b->rows; rows NULL: row i itself (m = a->rows); a row
+ * kge_matmul_quantized: out[i, j] = sum over k of a[rows[i], k] * b[j, k], i < m, j < b->rows; rows NULL: row i itself (m = a->rows, or 0); a row
  * number outside [0, a->rows) gives a row of zeros.  With accumulate = 1 the product is added to out.  A layer y = x W^t is (x by row, W by
  * row), its dx = dy W (dy by row, W by column), dW = dy^t x (dy by column, x by column).  With gathered rows x by column is quantised from the
  * slots' own fp32 or bf16 rows: no call makes it from a table's codes, whose blocks run along the other side.
@@ -607,7 +607,7 @@ typedef struct {
  * invalid arguments, 256 where nothing is written there).  KGE_E_UNSUPPORTED: by_col with 2^24 and more tiles of 128 x 128.
  *
  * kge_matmul_rowwise: out[i, j] = a.scales[rows[i]] * b.scales[j] * sum over k of a.codes[rows[i], k] * b.codes[j, k], i < m, j < b->rows; rows NULL: row i itself
- * (m = a->rows); a row number outside [0, a->rows) gives a row of zeros.  The sums are exact (8-bit matrix cores, 32-bit integers); then three
+ * (m = a->rows, or 0); a row number outside [0, a->rows) gives a row of zeros.  The sums are exact (8-bit matrix cores, 32-bit integers); then three
  * fp32 roundings ((float)sum * a's scale * b's, in this order: an intermediate result beyond fp32's range is infinite) and that of out_dtype.  accumulate = 1: added to out, in fp32.  The products
  * of a layer's backward pass are those of kge_matmul_quantized, each with a scale per row of its own operands.  Few rows over long contractions are
  * split along k into partial sums in the workspace (kge_matmul_rowwise_workspace_bytes, k = a->cols; 256 bytes where nothing is split); with less

@@ -586,7 +586,7 @@ size_t kge_matmul_quantized_workspace_bytes(int64_t m, int64_t n, int64_t k) {
 int kge_matmul_quantized(const kge_quantized_t *a, const int32_t *rows, int64_t m, const kge_quantized_t *b, int32_t accumulate, void *out,
                          int32_t out_dtype, int64_t out_ld, void *ws, size_t ws_bytes, void *hip_stream) {
     if (kge_check_quantized(a) != KGE_OK || kge_check_quantized(b) != KGE_OK || a->cols != b->cols || m < 0 || m >= (1ll << 31) ||
-        (!rows && m != a->rows) || ((uintptr_t)rows & 3) != 0 || (accumulate != 0 && accumulate != 1)) return KGE_E_INVALID_ARG;
+        (!rows && m != 0 && m != a->rows) || ((uintptr_t)rows & 3) != 0 || (accumulate != 0 && accumulate != 1)) return KGE_E_INVALID_ARG;
     const bool wide = out_dtype != KGE_BF16;
     if (out_dtype == (KGE_BF16 | KGE_FP32_SUMS)) out_dtype = KGE_BF16;
     if (out_dtype != KGE_F32 && out_dtype != KGE_BF16) return KGE_E_INVALID_ARG;

@@ -478,7 +478,7 @@ size_t kge_matmul_rowwise_workspace_bytes(int64_t m, int64_t n, int64_t k) {
 int kge_matmul_rowwise(const kge_rowwise_t *a, const int32_t *rows, int64_t m, const kge_rowwise_t *b, int32_t accumulate, void *out, int32_t out_dtype,
                        int64_t out_ld, void *ws, size_t ws_bytes, void *hip_stream) {
     const int ca = kge_check_rowwise(a), cb = kge_check_rowwise(b);
-    if (ca == KGE_E_INVALID_ARG || cb == KGE_E_INVALID_ARG || a->cols != b->cols || m < 0 || m >= (1ll << 31) || (!rows && m != a->rows) ||
+    if (ca == KGE_E_INVALID_ARG || cb == KGE_E_INVALID_ARG || a->cols != b->cols || m < 0 || m >= (1ll << 31) || (!rows && m != 0 && m != a->rows) ||
         ((uintptr_t)rows & 3) != 0 || (accumulate != 0 && accumulate != 1) || kge_bad_type(out_dtype)) return KGE_E_INVALID_ARG;
     if (m > 0 && b->rows > 0 && (kge_bad_rows(out, out_dtype, out_ld, b->rows) || out_ld >= KGE_MAX_LD)) return KGE_E_INVALID_ARG;
     if (ca != KGE_OK || cb != KGE_OK) return KGE_E_UNSUPPORTED;

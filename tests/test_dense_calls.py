@@ -244,3 +244,13 @@ def test_the_binding_multiplies_no_rows(on_the_host, k):                        
     matrix = lambda rows: b.Rowwise(torch.zeros((rows, wide), dtype=torch.int8), torch.ones(rows), k)  # noqa: E731
     assert b.matmul_rowwise(matrix(0), matrix(100)).shape == (0, 100)
     assert b.matmul_rowwise(matrix(100), matrix(0)).shape == (100, 0)
+
+
+@pytest.mark.parametrize("k", [100, 20_000])
+def test_no_rows_are_gathered(on_the_host, k):                                                         # noqa: F811
+    """An empty tensor of row numbers (whose address is NULL) over a table that has rows."""
+    wide, none = -(-k // 128) * 128, torch.zeros(0, dtype=torch.int32)
+    q = b.Rowwise(torch.zeros((100, wide), dtype=torch.int8), torch.ones(100), k)
+    assert b.matmul_rowwise(q, q, rows=none, dtype=torch.float32).shape == (0, 100)
+    q = b.Quantized(torch.zeros((100, wide), dtype=torch.uint8), torch.zeros((100, -(-wide // 512) * 4), dtype=torch.uint8), k)
+    assert b.matmul_quantized(q, q, rows=none).shape == (0, 100)
