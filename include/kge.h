@@ -603,8 +603,9 @@ typedef struct {
  * kge_quantize_rowwise: writes x [rows, cols] by rows (by_row: [rows, cols]) and / or the transposed matrix (by_col: [cols, rows], a scale for each column
  * of x), padding included.  With a the largest magnitude of the row, but 2^-100 at least: scale = a / 127, code = x * (127 / a) rounded to nearest even,
  * each operation rounded to fp32.  A row that holds a NaN or an infinity gets a NaN for its scale and codes of 0: 8-bit integers have neither, and a product of
- * that row is NaN.  The layouts overlap neither each other nor x.  by_col with more than 512 rows needs a workspace (kge_quantize_rowwise_workspace_bytes: 0 for
- * invalid arguments, 256 where nothing is written there).  KGE_E_UNSUPPORTED: by_col with 2^24 and more tiles of 128 x 128.
+ * that row is NaN.  The layouts overlap neither each other nor x.  by_col with more than 512 rows, or 2^28 columns and more, needs a workspace
+ * (kge_quantize_rowwise_workspace_bytes: 0 for invalid arguments, 256 where nothing is written there).  KGE_E_UNSUPPORTED: by_col with 2^24 and more tiles of
+ * 128 x 128, or 2^22 and more of them side by side.
  *
  * kge_matmul_rowwise: out[i, j] = a.scales[rows[i]] * b.scales[j] * sum over k of a.codes[rows[i], k] * b.codes[j, k], i < m, j < b->rows; rows NULL: row i itself
  * (m = a->rows, or 0); a row number outside [0, a->rows) gives a row of zeros.  The sums are exact (8-bit matrix cores, 32-bit integers); then three

@@ -342,7 +342,9 @@ int kge_quantize_rowwise(const void *x, int32_t dtype, int64_t rows, int64_t col
     if (by_row && by_row == by_col) return KGE_E_INVALID_ARG;
     if (rc != KGE_OK) return rc;
     if (rows > 0 && cols > 0 && kge_bad_rows(x, dtype, ld, cols)) return KGE_E_INVALID_ARG;
-    if (by_col && ((rows + BLOCK - 1) / BLOCK) * ((cols + BLOCK - 1) / BLOCK) >= (1ll << 24)) return KGE_E_UNSUPPORTED;   // (a grid's limit)
+    // (a grid has fewer than 2^32 threads: the tiles' of 256 each, the scales' of 1,024 for 128 columns)
+    const int64_t down = (rows + BLOCK - 1) / BLOCK, across = (cols + BLOCK - 1) / BLOCK;
+    if (by_col && (down * across >= (1ll << 24) || across >= (1ll << 22))) return KGE_E_UNSUPPORTED;
     hipStream_t st = (hipStream_t)hip_stream;
     if (rows == 0 || cols == 0) {                                 // rows of no elements have a scale all the same
         Args e = {};

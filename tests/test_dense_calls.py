@@ -254,3 +254,9 @@ def test_no_rows_are_gathered(on_the_host, k):                                  
     assert b.matmul_rowwise(q, q, rows=none, dtype=torch.float32).shape == (0, 100)
     q = b.Quantized(torch.zeros((100, wide), dtype=torch.uint8), torch.zeros((100, -(-wide // 512) * 4), dtype=torch.uint8), k)
     assert b.matmul_quantized(q, q, rows=none).shape == (0, 100)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, (1 << 29) - 127), (1, 1 << 29), (300, (1 << 29) + 5), (513, 1 << 29), (100_000, 1 << 22)])
+def test_more_columns_than_a_launch_holds(lib, rows, cols):
+    q = _q(cols, rows)
+    assert lib.kge_quantize_rowwise(OK, 1, rows, cols, cols, None, C.byref(q), OK, 1 << 60, None) == UNSUPPORTED
