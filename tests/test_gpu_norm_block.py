@@ -446,3 +446,34 @@ def test_replaced_storage_is_found():
     w.data = torch.randn(95, device="cuda")
     with pytest.raises(kge.KgeError):
         kge.norm_block(x, pre=n)
+
+
+# Rows by which every workgroup of the backward pass is full, its teams take a second row, and gates of two rows give each team groups of its own; a shape for each number of
+# waves and of groups of four columns that a lane of a row may have
+FULL = [(4_201, 300), (3_101, 700), (2_101, 1000), (1_601, 1100), (1_101, 1800), (1_101, 2048), (801, 2500), (601, 3500), (301, 4501), (301, 8191), (301, 8192)]
+
+
+def _backward_on_the_gpu(c):
+    for k, t in vars(c).items():
+        setattr(c, k, t.cuda() if torch.is_tensor(t) else [None if p is None else p.cuda() for p in t] if isinstance(t, list) else t)
+    with torch.device("cuda"):
+        want = _backward(c)
+    got = kge.norm_block_bwd(c.x, c.y, dh=c.dh, dz=c.dz, **c.args())
+    assert set(got) == set(want)
+    for k, (v, tol) in want.items():
+        _within(got[k], v.cpu(), tol.cpu(), k)
+
+
+@pytest.mark.parametrize("s,b", TYPES)
+@pytest.mark.parametrize("rows,dim", FULL)
+@pytest.mark.parametrize("gate_rows", [0, 1, 2, 150])
+def test_full_workgroups(rows, dim, gate_rows, s, b):
+    _backward_on_the_gpu(Case(rows, dim, "layer" if (rows + gate_rows + (s is b)) % 2 else "rms", s, b, gate_rows=gate_rows, key=12))
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("rows,dim", FULL)
+def test_full_workgroups_of_groups_with_an_odd_end(rows, dim, kind):
+    """Groups of three rows, the last of which has one or two."""
+    rows = rows * 8 // 5
+    _backward_on_the_gpu(Case(rows + (rows % 3 == 0), dim, kind, F32, BF16, gate_rows=3, key=13))
