@@ -190,7 +190,7 @@ template <bool B16> __global__ __launch_bounds__(64 * GROUP_SLICES) void norm_gr
         const float g = load1<B16>(a.gate.row(group), col + e);
         if (a.g_gate.p) {
             const float sc = a.scale ? a.scale[col + e] : 1.f, w = a.post.w ? a.post.w[col + e] : 1.f, b = a.post.b ? a.post.b[col + e] : 0.f;
-            store1<B16>(a.g_gate.row(group), col + e, sc * fmaf(w, s[0][e], b * s[1][e]));
+            store1<B16>(a.g_gate.row(group), col + e, sc * of_sums(w, s[0][e], b, s[1][e], a.post.b));
         }
 #pragma unroll
         for (int w = 0; w < 2; ++w)
@@ -220,7 +220,7 @@ template <bool B16> __global__ __launch_bounds__(JT) void norm_join_kernel(const
             for (int e = 0; e < 4; ++e) gate[e] = col + 4 * l + e < a.dim ? load1<B16>(a.gate.row(g), col + 4 * l + e) : 0.f;
             add_rows(p, s, g * a.parts, (g + 1) * a.parts, 1, a.part_ld);
             if (a.g_gate.p) {
-                const kge_f32x4 d = sc * fma4(w, s[0], b * s[1]);
+                const kge_f32x4 d = sc * of_sums(w, s[0], b, s[1], a.post.b);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (col + 4 * l + e < a.dim) store1<B16>(a.g_gate.row(g), col + 4 * l + e, d[e]);
@@ -241,7 +241,7 @@ template <bool B16> __global__ __launch_bounds__(JT) void norm_join_kernel(const
     };
     if (!branch) { put(a.g_prew, s[0]); put(a.g_preb, s[1]); return; }
     const float sc = a.scale ? a.scale[col + c] : 1.f, w = a.post.w ? a.post.w[col + c] : 1.f, b = a.post.b ? a.post.b[col + c] : 0.f;
-    put(a.g_scale, fmaf(w, s[0], b * s[1]));
+    put(a.g_scale, of_sums(w, s[0], b, s[1], a.post.b));
     put(a.g_postw, sc * s[0]);
     put(a.g_postb, sc * s[1]);
 }

@@ -185,6 +185,11 @@ __device__ __forceinline__ float inv_sqrt(float x) { return 1.f / sqrtf(x); }
 
 struct Norm { bool on, layer; float eps; const float *w, *b; };
 
+// w A + b B, the sum over rows of what a norm with weight w and bias b has made, from the sums A and B of its parts.  Without a bias B may be infinite, or another sum may stand
+// in its place: it does not count.
+__device__ __forceinline__ float of_sums(float w, float a, float b, float bias_sum, bool bias) { return bias ? fmaf(w, a, b * bias_sum) : w * a; }
+__device__ __forceinline__ kge_f32x4 of_sums(kge_f32x4 w, kge_f32x4 a, kge_f32x4 b, kge_f32x4 bias_sum, bool bias) { return bias ? fma4(w, a, b * bias_sum) : w * a; }
+
 // x -> x^ = (x - mean) / deviation, of R rows at once
 template <int NG, int R, class Sums>
 __device__ __forceinline__ void normalise(kge_f32x4 (&x)[R][NG], const Columns<NG> &c, const Norm &norm, float inv_dim, Sums &reduce) {

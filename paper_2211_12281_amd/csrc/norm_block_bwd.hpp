@@ -180,7 +180,7 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
                     if (!c.inside(k)) continue;
                     if (a.g_gate.p) {
                         const kge_f32x4 sb = SB ? vector(VEC_SB, k) : vector4(a.scale, c.col(k), a.dim, 1.f) * vector4(a.post.b, c.col(k), a.dim, 0.f);
-                        store<B16>(a.g_gate.row(group), c, k, fma4(vector(VEC_F, k), A[k], sb * B[k]), false);
+                        store<B16>(a.g_gate.row(group), c, k, of_sums(vector(VEC_F, k), A[k], sb, B[k], a.post.b), false);
                     }
                     float *mine = of_teams + 2 * t.team * wide + c.col(k);
                     *(kge_f32x4 *)mine = fma4(gate[k], A[k], *(const kge_f32x4 *)mine);
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
                 kge_f32x4 d = *(const kge_f32x4 *)(vec + VEC_F * wide + i);
                 const kge_f32x4 sc = vector4(a.scale, i, a.dim, 1.f), w = vector4(a.post.w, i, a.dim, 1.f), b = vector4(a.post.b, i, a.dim, 0.f);
                 if (a.parts > 0) {                                // the gate of the one group
-                    const kge_f32x4 v = sc * fma4(w, s, b * d);
+                    const kge_f32x4 v = sc * of_sums(w, s, b, d, a.post.b);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (i + e < a.dim) {
@@ -230,7 +230,7 @@ __global__ __launch_bounds__(NT, OCC) void norm_bwd_kernel(const BwdArgs a) {
                             s[e] *= g; d[e] *= g;
                         }
                 }
-                put(a.g_scale, i, fma4(w, s, b * d));
+                put(a.g_scale, i, of_sums(w, s, b, d, a.post.b));
                 put(a.g_postw, i, sc * s);
                 put(a.g_postb, i, sc * d);
             });

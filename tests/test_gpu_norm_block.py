@@ -477,3 +477,20 @@ def test_full_workgroups_of_groups_with_an_odd_end(rows, dim, kind):
     """Groups of three rows, the last of which has one or two."""
     rows = rows * 8 // 5
     _backward_on_the_gpu(Case(rows + (rows % 3 == 0), dim, kind, F32, BF16, gate_rows=3, key=13))
+
+
+@pytest.mark.parametrize("rows,dim,gate_rows", [(20, 72, 0), (20, 72, 20), (300, 100, 0), (300, 100, 1), (300, 100, 100), (2_000, 72, 2_000), (20_011, 16, 2), (3_101, 700, 2), (301, 8191, 2)])
+def test_an_infinite_gradient_without_a_bias(rows, dim, gate_rows):
+    """Sums that an infinity is in are infinite, whatever number of workgroups they come from: what a bias would be multiplied by does not count."""
+    c = Case(rows, dim, "rms", F32, F32, pre=False, bias=False, gate_rows=gate_rows, key=14)
+    r, k = 3, 5
+    c.dh[r, k] = float("inf")
+    got = kge.norm_block_bwd(None, c.y.cuda(), dh=c.dh.cuda(), want=["scale", "post_weight"] + (["gate"] if gate_rows else []), **c.args())
+    g = float(c.gate[r // gate_rows, k]) if gate_rows else 1.0
+    y, w, s = float(c.y[r, k]), float(c.post[0][k]), float(c.scale[k])
+    at = {"scale": (k, g * w * y), "post_weight": (k, g * s * y)} | ({"gate": ((r // gate_rows, k), s * w * y)} if gate_rows else {})
+    for name, (i, sign) in at.items():
+        t = got[name].cpu()
+        assert t[i] == np.copysign(np.inf, sign), (name, t[i])
+        t[i] = 0
+        assert bool(torch.isfinite(t).all()), name
