@@ -323,3 +323,63 @@ def test_shared_tensors_are_refused():
             bad()
     kge.AdamW([p[:500], p[500:], torch.zeros(0, device="cuda"), torch.zeros(0, device="cuda")]).step([p[:500] + 1, p[500:] + 1, p[:0], p[:0]], 1e-3, 1)
     assert bool((p < 0).all())
+
+
+def test_moments_on_the_grid_keep_their_codes():
+    """Moments that a step halves exactly: the scale of a block falls by one and no code changes, whatever the random number - of four million for each moment every value of
+    sixteen bits, 0 among them, comes up about 64 times - and whatever the block's scale."""
+    blocks = 1 << 15
+    n, g = 128 * blocks, _rng(95)
+    codes = {}
+    for k, top in (("m", 0x7e), ("v", 0x7b)):
+        c = g.integers(0, top + 1, size=(blocks, 128)).astype(np.uint8)
+        c[:, 0] = top                                             # (1.75 times the largest power of two: the block's scale follows from it)
+        if k == "m":
+            c[:, 1:] |= (g.integers(0, 2, size=(blocks, 127)) << 7).astype(np.uint8)
+            c[c == 0x80] = 0                                      # (no zeros with a sign)
+        codes[k] = torch.from_numpy(c.reshape(-1)).cuda()
+    ms, vs = (torch.from_numpy((2 + np.arange(blocks) * 7919 % span).astype(np.uint8)).cuda() for span in (245, 238))
+    st = kge.AdamWState(codes["m"].clone(), codes["v"].clone(), ms.clone(), vs.clone())
+    p = torch.zeros(n, device="cuda")
+    kge.AdamW([p], [st], weight_decay=0.0, seed=5).step([torch.zeros(n, device="cuda")], 0.0, 1, beta1=0.5, beta2=0.5)
+    assert torch.equal(st.m_scales, ms - 1) and torch.equal(st.v_scales, vs - 1)
+    assert torch.equal(st.m, codes["m"]), int((st.m != codes["m"]).sum())
+    assert torch.equal(st.v, codes["v"]), int((st.v != codes["v"]).sum())
+
+
+def _words(n, tensor, step, seed, tag):
+    """_philox on whole arrays."""
+    low, half = np.uint64(0xFFFFFFFF), np.uint64(32)
+    c = [np.arange(-(-n // 4), dtype=np.uint64)] + [np.full(-(-n // 4), w, dtype=np.uint64) for w in (tensor, step, tag)]
+    k = [seed & 0xFFFFFFFF, seed >> 32]
+    for _ in range(10):
+        p0, p1 = np.uint64(0xD2511F53) * c[0], np.uint64(0xCD9E8D57) * c[2]
+        c = [p1 >> half ^ c[1] ^ np.uint64(k[0]), p1 & low, p0 >> half ^ c[3] ^ np.uint64(k[1]), p0 & low]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return np.stack(c, axis=1).reshape(-1)[:n]
+
+
+def _codes(x, scales, fmt, u):
+    """Codes of finite fp32 values in blocks of these scale bytes: the value in units of the spacing at its place, q, exact; floor(q + u) of the sum rounded to fp32."""
+    bits, emin, top = (3, -6, 0x7e) if fmt == "e4m3" else (2, -14, 0x7b)
+    t = np.abs(x.astype(np.float64)) * 2.0 ** (127.0 - scales[np.arange(x.size) // 128])
+    e = np.maximum(np.frexp(t)[1] - 1, emin)
+    q = (t * 2.0 ** (bits - e)).astype(F)
+    code = np.minimum(((e - emin) << bits) + np.floor(q + u.astype(F)).astype(np.int64), top)
+    if fmt == "e5m2":
+        code = np.where((x > 0) & (code == 0), 1, code)
+    return code | np.signbit(x).astype(np.int64) << 7
+
+
+@pytest.mark.parametrize("gdt", [F32, BF16])
+@pytest.mark.parametrize("n", [1000, 70_001])
+def test_codes_bit_for_bit(n, gdt):
+    assert np.array_equal(_words(101, 2, 3, 0xABCDEF0123456789, 9), _philox(101, 2, 3, 0xABCDEF0123456789, 9))
+    ts, _ = _run([n, n], [8, 8], gdt, False, key=96)
+    for i, (_, grad, st, _, m, v) in enumerate(ts):
+        m, v = _moments(m, v, grad.float().cpu().numpy())
+        w = _words(n, i, 3, 0xABCDEF0123456789, 9)
+        for codes, scales, x, fmt, u in ((st.m, st.m_scales, m, "e4m3", w & np.uint64(0xFFFF)), (st.v, st.v_scales, v, "e5m2", w >> np.uint64(16))):
+            s = scales.cpu().numpy()
+            assert [int(b) for b in s[:-(-n // 128)]] == [_byte(x[at:at + 128], fmt) for at in range(0, n, 128)]
+            assert np.array_equal(codes.cpu().numpy()[:n], _codes(x, s.astype(np.float64), fmt, u.astype(np.float64) / 65536))
