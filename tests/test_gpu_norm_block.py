@@ -494,3 +494,26 @@ def test_an_infinite_gradient_without_a_bias(rows, dim, gate_rows):
         assert t[i] == np.copysign(np.inf, sign), (name, t[i])
         t[i] = 0
         assert bool(torch.isfinite(t).all()), name
+
+
+@pytest.mark.parametrize("s,b", [(BF16, BF16), (F32, BF16)])
+def test_rows_beyond_32_bits_in_all_tensors(s, b):
+    """The last rows of tensors of 4.3 GB (fp32: 8.6), forward and backward, each tensor its own; the rows before them are zeros and add nothing to the sums."""
+    c, rows, dim = Case(3, 1024, "layer", s, b, key=15), (1 << 21) + 40, 1024
+
+    def behind_zeros(t):
+        wide = torch.zeros((rows, dim), dtype=t.dtype, device="cuda")
+        wide[-3:] = t.cuda()
+        return wide
+    x, y = behind_zeros(c.x), behind_zeros(c.y)
+    h, z = kge.norm_block(x, y, **c.args())
+    for k, t in (("h", h), ("z", z)):
+        _within(t[-3:], *_forward(c)[k], k)
+    del h, z
+    dh = behind_zeros(c.dh)
+    got = kge.norm_block_bwd(x, y, dh=dh, dz=behind_zeros(c.dz), out={"x": dh}, **c.args())
+    for k, (v, tol) in _backward(c).items():
+        _within(got[k][-3:] if k in ("x", "y") else got[k], v, tol, k)
+    for k in ("x", "y"):
+        for at in (0, (1 << 20) - 2, (1 << 21) - 2, rows - 10):
+            assert not bool(got[k][at:at + 4].any()), (k, at)
