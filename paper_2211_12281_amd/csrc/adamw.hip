@@ -3,9 +3,9 @@
 //   m <- b1 m + (1 - b1) g,   v <- b2 v + (1 - b2) g^2,   theta <- theta (1 - lr wd) - lr (m c1) / (sqrt(v c2) + eps),   c = 1 / (1 - b^step)
 //
 // Memory bounds it: 28 bytes an element with fp32 moments and gradients (2 more with a bf16 copy), 14 with 8-bit moments and bf16 gradients.  The tensors are
-// cut into chunks of one workgroup each (2,048 elements: 301 us for the tower below, 4,096: 336), which finds its tensor among the launch's by its chunk number; the descriptors are kernel arguments,
-// so that nothing has to be copied to the device first and a captured call keeps them.  Measured: 89M elements in 181 tensors with 8-bit moments, bf16 gradients and copies 299 us
-// (1.43 GB, 4.8 TB/s; without the generator's rounds 292: the vector pipe is nearly as busy as memory); 25M with fp32 moments 143 (712 MB, 5.0 TB/s); the encoder's two projections 5.4.
+// cut into chunks of one workgroup each (2,048 elements: 291 us for the tower below, 4,096: 324), which finds its tensor among the launch's by its chunk number; the descriptors are kernel arguments,
+// so that nothing has to be copied to the device first and a captured call keeps them.  Measured: 89M elements in 181 tensors with 8-bit moments, bf16 gradients and copies 291 us
+// (1.43 GB, 4.9 TB/s; without the generator's rounds 289); 25M with fp32 moments 143 (712 MB, 5.0 TB/s); the encoder's two projections 5.4.
 //
 // 8-bit moments: e4m3 (m) and e5m2 (v) codes with a power of two per 128 elements.  The scale is a power of two, so an element whose value and block stay as they
 // are keeps its code exactly, and stochastic rounding adds noise only in proportion to what a step changes.
@@ -208,7 +208,7 @@ __global__ __launch_bounds__(NT) void adamw_kernel(const Args a) {
         }
         moments(a, g[k], m[k], v[k]);
         // With 8-bit moments the vector pipe is nearly as busy as memory: root and reciprocal from one instruction each, 2^-23 of themselves off (89M elements
-        // 310 -> 292 us), beside a v whose codes carry 0.3 of noise.  (The root of a subnormal number, below 1.1e-19, is 0 there: only beside an eps that it does not change.)
+        // 310 -> 291 us), beside a v whose codes carry 0.3 of noise.  (The root of a subnormal number, below 1.1e-19, is 0 there: only beside an eps that it does not change.)
         if (state8 && a.eps >= 1e-12f) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
