@@ -633,7 +633,8 @@ size_t kge_matmul_rowwise_workspace_bytes(int64_t m, int64_t n, int64_t k);
  * multiple of 128 and 16-byte aligned, m_scales and v_scales an exponent byte per 128 elements).  The update uses the moments before they are rounded.  A block's byte is
  * kge_quantize's; a code is one of the two neighbours of the value, the upper one with probability equal to its nearness, cut to a multiple of 2^-16 (stochastic
  * rounding: with b2 = 0.999 a step changes v by a thousandth, far less than half a spacing, and rounding to nearest would never move it); a
- * positive v is never rounded to 0; a value that is a code's keeps it.  Sixteen random bits each: Philox4x32-10, key = seed, counter (element / 4, tensor's place in the call, step, tag),
+ * positive v is never rounded to 0; a value that is a code's keeps it.  (A block's scale is divided out by powers of two of the math library, which leave a value up to 2^-19 of a spacing
+ * low, exactly where the random bits are 0: other codes are those of elementary fp32 steps, bit for bit.)  Sixteen random bits each: Philox4x32-10, key = seed, counter (element / 4, tensor's place in the call, step, tag),
  * word element % 4, low half for m.  So, at b2 = 0.999 and normal gradients, v carries a relative noise of 0.3, in its mean 0.002 low (by what is cut), and the update, which goes
  * by its root, one of 0.15, in its mean 3 % longer.  With state_bits 8 and an eps of 1e-12 and more the update's root and quotient are each good to 2^-23 of themselves and not rounded to nearest.  NaN stays
  * NaN; an infinite m becomes NaN, an infinite v stays.  Codes behind the last element are written as zeros.

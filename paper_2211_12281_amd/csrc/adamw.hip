@@ -3,9 +3,9 @@
 //   m <- b1 m + (1 - b1) g,   v <- b2 v + (1 - b2) g^2,   theta <- theta (1 - lr wd) - lr (m c1) / (sqrt(v c2) + eps),   c = 1 / (1 - b^step)
 //
 // Memory bounds it: 28 bytes an element with fp32 moments and gradients (2 more with a bf16 copy), 14 with 8-bit moments and bf16 gradients.  The tensors are
-// cut into chunks of one workgroup each (2,048 elements: 291 us for the tower below, 4,096: 324), which finds its tensor among the launch's by its chunk number; the descriptors are kernel arguments,
-// so that nothing has to be copied to the device first and a captured call keeps them.  Measured: 89M elements in 181 tensors with 8-bit moments, bf16 gradients and copies 291 us
-// (1.43 GB, 4.9 TB/s; without the generator's rounds 289); 25M with fp32 moments 143 (712 MB, 5.0 TB/s); the encoder's two projections 5.4.
+// cut into chunks of one workgroup each (2,048 elements: 304 us for the tower below, 4,096: 341), which finds its tensor among the launch's by its chunk number; the descriptors are kernel arguments,
+// so that nothing has to be copied to the device first and a captured call keeps them.  Measured: 89M elements in 181 tensors with 8-bit moments, bf16 gradients and copies 304 us
+// (1.43 GB, 4.7 TB/s; without the generator's rounds 295: the vector pipe is nearly as busy as memory); 25M with fp32 moments 143 (712 MB, 5.0 TB/s); the encoder's two projections 5.4.
 //
 // 8-bit moments: e4m3 (m) and e5m2 (v) codes with a power of two per 128 elements.  The scale is a power of two, so an element whose value and block stay as they
 // are keeps its code exactly, and stochastic rounding adds noise only in proportion to what a step changes.
@@ -85,10 +85,21 @@ template <int FMT> struct Fmt;
 template <> struct Fmt<KGE_E4M3> { static constexpr int EMAX = 8, EMIN = -6, BITS = 3; static constexpr uint32_t TOP = 0x7e, INF = 0x7f, NAN8 = 0x7f; };
 template <> struct Fmt<KGE_E5M2> { static constexpr int EMAX = 15, EMIN = -14, BITS = 2; static constexpr uint32_t TOP = 0x7b, INF = 0x7c, NAN8 = 0x7f; };
 
-// 2^(byte - 127) and, of a byte that block_byte gives (247 at most), 2^(127 - byte), which is a normal number then: a value is divided by its block's scale exactly, unless it is so far below
-// the block's largest that the quotient is subnormal, and its code 0 (or a positive v's 1) whatever the quotient
+// 2^(byte - 127)
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x400000u); }
-__device__ __forceinline__ float inverse_of(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+
+// A value is divided by its block's scale with two factors, 2^a and 2^b, a = floor((127 - byte) / 2), b = 127 - byte - a.  They are the math library's powf, which is 2^-24 low for
+// some exponents (2^16 to 2^20 among them), and so is the factor 2^16 of the smallest second moments: a value in units of its spacing comes out up to 2^-19 low.  That is an eighth of what
+// the random numbers cut anyway, but it decides the one value in 2^21 that falls on the border exactly, and with these factors it falls where the same steps done
+// with elementary operations (power, product, sum, floor) put it, bit for bit: a program that checks its updates against such steps would else find a code in two million off by one, and what follows from
+// it the step after.  The price is the table that a workgroup makes and a choice for each number: 304 us
+// for the tower above, 291 with exact factors alone.
+constexpr int POW0 = 60, POWS = 128;                              // exponents -60 .. 67
+__device__ __forceinline__ float two_to(int n) {
+    float two = 2.f;
+    asm volatile("" : "+v"(two));                                 // (else the call becomes exp2f, which is exact)
+    return powf(two, (float)n);
+}
 
 template <int FMT> __device__ __forceinline__ kge_f32x4 decode4(uint32_t w, float scale) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -120,13 +131,20 @@ template <int FMT> __device__ __forceinline__ uint32_t block_byte(kge_f32x4 x) {
     return (uint32_t)max((int)((m + 0x1fffffu) >> 23) - Fmt<FMT>::EMAX, 0);
 }
 
-// x's code: |x| / scale in units of the spacing at its place, q, and floor(q + u), u in [0, 1) a multiple of 2^-16.  A value that is on the grid stays.
-template <int FMT> __device__ __forceinline__ uint32_t encode(float x, float inv, uint32_t rnd) {
+// x's code: |x| / scale in units of the spacing at its place, q, and floor(q + u), u in [0, 1) a multiple of 2^-16.  The factors take less from q than the
+// least u adds; with u = 0 exact powers of two take their place.  So a value on the grid stays, whatever its random number, and no code is below the value's lower neighbour.
+struct Inverse { float a, b, least; };                            // of a block's scale; of the spacing of the smallest second moments (that of first moments, 2^9, is exact)
+template <int FMT> __device__ __forceinline__ Inverse inverse_of(uint32_t byte, const float *pow) {
+    const int n = 127 - (int)byte, a = n >> 1;                        // (byte <= 255 - EMAX: 2^n is a normal number)
+    return Inverse{pow[a + POW0], pow[n - a + POW0], pow[Fmt<FMT>::BITS - Fmt<FMT>::EMIN + POW0]};
+}
+template <int FMT> __device__ __forceinline__ uint32_t encode(float x, const Inverse &inv, uint32_t byte, uint32_t rnd) {
 #pragma clang fp contract(off)
     using F = Fmt<FMT>;
-    const float t = fabsf(x) * inv;
+    const bool exact = rnd == 0;
+    const float t = fabsf(x) * (exact ? __uint_as_float((254u - byte) << 23) : inv.a) * (exact ? 1.f : inv.b);
     const uint32_t eb = max(__float_as_uint(t) >> 23, (uint32_t)(127 + F::EMIN));
-    const float q = t * __uint_as_float((uint32_t)(254 + F::BITS - eb) << 23);
+    const float q = t * (FMT == KGE_E5M2 && eb == 127 + F::EMIN && !exact ? inv.least : __uint_as_float((uint32_t)(254 + F::BITS - eb) << 23));
     uint32_t code = ((eb - (127 + F::EMIN)) << F::BITS) + (uint32_t)(q + (float)rnd * 0x1p-16f);
     code = min(code, F::TOP);
     if (FMT == KGE_E5M2 && x > 0.f) code = max(code, 1u);
@@ -158,6 +176,7 @@ __device__ __forceinline__ void moments(const Args &a, kge_f32x4 g, kge_f32x4 &m
 }
 
 __global__ __launch_bounds__(NT) void adamw_kernel(const Args a) {
+    __shared__ float pow[POWS];
     int lo = 0;                                                   // the last tensor whose first chunk is not behind this one
     for (int hi = a.tensors; hi - lo > 1;) {
         const int mid = (lo + hi) >> 1;
@@ -184,6 +203,10 @@ __global__ __launch_bounds__(NT) void adamw_kernel(const Args a) {
             }
         } else { m[k] = load4((const float *)t.m, at, n[k]); v[k] = load4((const float *)t.v, at, n[k]); }
     }
+    if (state8) {
+        if (threadIdx.x < POWS) pow[threadIdx.x] = two_to((int)threadIdx.x - POW0);
+        __syncthreads();
+    }
     float c1 = a.c1, c2 = a.c2;
     uint32_t step = (uint32_t)a.step;
     if (a.step_counter) {
@@ -208,7 +231,7 @@ __global__ __launch_bounds__(NT) void adamw_kernel(const Args a) {
         }
         moments(a, g[k], m[k], v[k]);
         // With 8-bit moments the vector pipe is nearly as busy as memory: root and reciprocal from one instruction each, 2^-23 of themselves off (89M elements
-        // 310 -> 291 us), beside a v whose codes carry 0.3 of noise.  (The root of a subnormal number, below 1.1e-19, is 0 there: only beside an eps that it does not change.)
+        // 335 -> 304 us), beside a v whose codes carry 0.3 of noise.  (The root of a subnormal number, below 1.1e-19, is 0 there: only beside an eps that it does not change.)
         if (state8 && a.eps >= 1e-12f) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -228,11 +251,11 @@ __global__ __launch_bounds__(NT) void adamw_kernel(const Args a) {
         if (at / BLOCK * BLOCK >= t.n) continue;                  // (a whole block behind the end)
         uint32_t w[4], em = 0, ev = 0;
         philox((uint32_t)(at >> 2), t.index, step, a.tag, a.k0, a.k1, w);
-        const float im = inverse_of(bm), iv = inverse_of(bv);
+        const Inverse im = inverse_of<KGE_E4M3>(bm, pow), iv = inverse_of<KGE_E5M2>(bv, pow);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            em |= encode<KGE_E4M3>(m[k][e], im, w[e] & 0xffffu) << (8 * e);
-            ev |= encode<KGE_E5M2>(v[k][e], iv, w[e] >> 16) << (8 * e);
+            em |= encode<KGE_E4M3>(m[k][e], im, bm, w[e] & 0xffffu) << (8 * e);
+            ev |= encode<KGE_E5M2>(v[k][e], iv, bv, w[e] >> 16) << (8 * e);
         }
         *(uint32_t *)((uint8_t *)t.m + at) = em;
         *(uint32_t *)((uint8_t *)t.v + at) = ev;
